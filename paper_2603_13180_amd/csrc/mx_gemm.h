@@ -1,8 +1,8 @@
 // mx_gemm.h -- what the MX product kernels share: argument block, tile order,
-// LDS DMA, fragment reads, output stores.  mx_gemm.hip holds the entry point,
-// the choice of kernel and the 256 x 256 kernel; mx_gemm_ring.h smaller tiles
-// with a deeper ring of K steps; mx_gemm_ksplit.h few small tiles, their K
-// steps dealt to the waves.
+// LDS DMA, fragment reads, output stores.  mx_gemm_256.h holds the 256 x 256
+// kernel; mx_gemm_ring.h smaller tiles with a deeper ring of K steps;
+// mx_gemm_ksplit.h few small tiles, their K steps dealt to the waves;
+// mx_gemm_plan.h the choice between them; mx_gemm.hip the entry point.
 #pragma once
 
 #include <hip/hip_runtime.h>
