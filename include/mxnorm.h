@@ -182,8 +182,16 @@ mx_status mx_cast_fwd(const void *x, const void *gamma, int64_t T, int64_t d, in
 
 typedef enum {
     MX_OUT_F32 = 0,       /* float32 output */
-    MX_OUT_BF16 = 1       /* bfloat16 output, rounded to nearest even */
+    MX_OUT_BF16 = 1,      /* bfloat16 output, rounded to nearest even */
+    MX_OUT_CODES = 2      /* MX codes and scales (mx_gated_fwd and
+                             mxnorm_gated_fwd alone) */
 } mx_out_dtype;
+
+typedef enum {
+    MX_ACT_SILU = 0,      /* act(g) = g sigma(g)                           */
+    MX_ACT_GELU_TANH = 1  /* act(g) = g (1 + tanh(sqrt(2/pi) (g + 0.044715
+                             g^3))) / 2                                    */
+} mx_act;
 
 /*
  * The MX matrix product of the MXNormLinear forward (Sec. 3.7 eq.
@@ -323,6 +331,49 @@ mx_status mxnorm_linear_bwd(const void *grad_h, const void *x, const float *rho,
                             int block, int elem, int out_dtype, void *grad_x, float *grad_gamma,
                             float *grad_w, void *workspace, size_t workspace_bytes,
                             hipStream_t stream);
+
+/*
+ * The gated feed-forward's first half: both projections, the activation and
+ * the product in one kernel.  A [M, K] is MX-encoded along K (the output of
+ * mxnorm_mx_fwd), W [2F, K] likewise (the output of mx_cast_fwd): F gate rows,
+ * then F up rows.
+ *   G = dec(A) dec(W[0 .. F))^T,  U = dec(A) dec(W[F .. 2F))^T,
+ *   H = act(G) . U                                               [M, F]
+ * G and U are the float sums of mx_matmul_fwd (its bound, its note on the order
+ * of additions); activation and product are computed in float.  Non-finite
+ * values follow the formula: a NaN gives NaN, act(-inf) is NaN, act(+inf) is
+ * inf; a finite G too negative for the exponential gives act(G) = -0.
+ * out_dtype MX_OUT_F32, MX_OUT_BF16: out [M, F] in that type, out_scales NULL.
+ * MX_OUT_CODES: the MX encoding of the float H along F, with blocks of 32 in
+ * `elem` by `scale_mode`, rounding and NaN-block codes as in the casts above:
+ * out uint8 codes [M, F] (E4M3) or [M, F/2] (E2M1), out_scales uint8 [M, F/32]
+ * -- the operand that a down projection's mx_matmul_fwd takes.
+ * gu: bf16 [M, 2F] or NULL: G and then U of every row, rounded, which the
+ * backward takes.
+ * block: 32 (other sizes: MX_EUNSUPPORTED).  K as in mx_matmul_fwd; F a multiple
+ * of 16 (MX_OUT_CODES: 32) and at most MX_MATMUL_MAX_N / 2 (else
+ * MX_EUNSUPPORTED); a_codes, w_codes, out and gu 16-byte, a_scales and w_scales
+ * 4-byte aligned (else MX_EINVAL).  M == 0 or F == 0 is a no-op.  Rows of the
+ * outputs depend on their row of A alone, up to the order of additions.
+ */
+mx_status mx_gated_fwd(const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *w_codes,
+                       const uint8_t *w_scales, int64_t M, int64_t F, int64_t K, int block,
+                       int elem, int act, int scale_mode, int out_dtype, void *out,
+                       uint8_t *out_scales, void *gu, hipStream_t stream);
+
+/*
+ * mxnorm_mx_fwd of x [T, d] and mx_gated_fwd with the weight W [2F, d] as one
+ * call: same arguments, outputs (bit for bit) and errors as the two calls, the
+ * errors of both before the first launch; rho float [T] or NULL.  The codes of
+ * the normed activations live in `workspace`: caller-owned device memory of
+ * mxnorm_gated_fwd_workspace_bytes() bytes, 256-byte aligned, overwritten.
+ */
+size_t mxnorm_gated_fwd_workspace_bytes(int64_t T, int64_t d, int block, int elem);
+mx_status mxnorm_gated_fwd(const void *x, int64_t T, int64_t d, const uint8_t *w_codes,
+                           const uint8_t *w_scales, int64_t F, int block, int elem, int p,
+                           float coef, float eps, int scale_mode, int act, int out_dtype, void *out,
+                           uint8_t *out_scales, void *gu, float *rho, void *workspace,
+                           size_t workspace_bytes, hipStream_t stream);
 
 /*
  * Default NVFP4 tensor decode scales: an output bound divided by 6 * 448, so

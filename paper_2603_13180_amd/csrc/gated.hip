@@ -1,0 +1,158 @@
+// gated.hip -- the gated feed-forward's first half (mx_gated_fwd): the two
+// projections that share an operand, activation and product in one kernel.
+//
+// The gate and up products of a column are two columns of an ordinary MX
+// product with W [2F, K].  A tile that takes its B rows half from the gate
+// rows and half from the same up rows holds both products of its columns in
+// one wave's accumulators, so the product kernels (mx_gemm_256.h, _ring.h,
+// _ksplit.h) serve unchanged but for the rows they load and what they store
+// (mx_gemm_gated.h).  The operand stream and the matrix instructions are those
+// of the plain product; what is saved is G and U, 8 F bytes a row written and
+// read again, or their rounding to bf16 and 4 F.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "mx_gemm_gated.h"
+#include "mx_gemm_plan.h"
+#include "mxnorm.h"
+#include "products.h"
+#include "status.h"
+#include "testing.h"
+
+namespace {
+
+bool aligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+
+void gated_args(mxg::GatedArgs &A, const mxg::GatedProduct &P, int elem, hipStream_t stream)
+{
+    mxg::product_args(A, {P.a, P.as, P.w, P.ws, P.M, P.F, P.K, nullptr, P.out}, elem, stream);
+    A.hs = P.out_scales;
+    A.gu = static_cast<uint16_t *>(P.gu);
+    A.act = P.act;
+    A.mode = P.mode;
+}
+
+// f(ELEM, OUT of the kernels) for the call's types
+template <class F> hipError_t by_type(int elem, int out_dtype, F f)
+{
+    using namespace mxg;
+    auto out = [&](auto e) {
+        switch (out_dtype) {
+        case MX_OUT_F32: return f(e, std::integral_constant<int, kGate + MX_OUT_F32>{});
+        case MX_OUT_BF16: return f(e, std::integral_constant<int, kGate + MX_OUT_BF16>{});
+        default: return f(e, std::integral_constant<int, kGate + MX_OUT_CODES>{});
+        }
+    };
+    return elem == MX_ELEM_E4M3 ? out(std::integral_constant<int, MX_ELEM_E4M3>{})
+                                : out(std::integral_constant<int, MX_ELEM_E2M1>{});
+}
+
+mx_status launched(hipError_t e)
+{
+    return e == hipSuccess ? MX_OK
+                           : mxk::fail(MX_EHIP, "kernel launch failed: %s", hipGetErrorString(e));
+}
+
+} // namespace
+
+namespace mxg {
+
+mx_status check_gated(const GatedProduct &P, int block, int elem)
+{
+    if (P.M < 0 || P.F < 0 || P.K <= 0)
+        return mxk::fail(MX_EINVAL, "M and F must be >= 0 and K > 0");
+    if (elem != MX_ELEM_E4M3 && elem != MX_ELEM_E2M1)
+        return mxk::fail(MX_EINVAL, "elem must be MX_ELEM_E4M3 or MX_ELEM_E2M1");
+    if (P.act != MX_ACT_SILU && P.act != MX_ACT_GELU_TANH)
+        return mxk::fail(MX_EINVAL, "act must be MX_ACT_SILU or MX_ACT_GELU_TANH");
+    if (P.out_dtype != MX_OUT_F32 && P.out_dtype != MX_OUT_BF16 && P.out_dtype != MX_OUT_CODES)
+        return mxk::fail(MX_EINVAL, "out_dtype must be MX_OUT_F32, MX_OUT_BF16 or MX_OUT_CODES");
+    if (P.mode != MX_SCALE_RCEIL && P.mode != MX_SCALE_FLOOR)
+        return mxk::fail(MX_EINVAL, "unknown scale_mode %d", P.mode);
+    if (block != 32)
+        return mxk::fail(MX_EUNSUPPORTED, "the matrix cores apply one scale per 32 elements: block must be 32");
+    if (P.K % (elem == MX_ELEM_E2M1 ? 256 : 128) != 0)
+        return mxk::fail(MX_EUNSUPPORTED, "K must be a multiple of 128 (E4M3) or 256 (E2M1)");
+    if (P.F % (P.out_dtype == MX_OUT_CODES ? 32 : 16) != 0)
+        return mxk::fail(MX_EUNSUPPORTED, "F must be a multiple of 16, or of 32 for MX_OUT_CODES");
+    if (P.K > MX_MATMUL_MAX_K)
+        return mxk::fail(MX_EUNSUPPORTED, "K exceeds %d", MX_MATMUL_MAX_K);
+    if (P.M == 0 || P.F == 0)
+        return MX_OK;
+    if (!P.a || !P.as || !P.w || !P.ws || !P.out)
+        return mxk::fail(MX_EINVAL, "NULL pointer");
+    if ((P.out_dtype == MX_OUT_CODES) != (P.out_scales != nullptr))
+        return mxk::fail(MX_EINVAL, "out_scales goes with MX_OUT_CODES, and with it alone");
+    if (!aligned(P.a, 16) || !aligned(P.w, 16) || !aligned(P.as, 4) || !aligned(P.ws, 4) ||
+        !aligned(P.out, 16) || !aligned(P.gu, 16))
+        return mxk::fail(MX_EINVAL, "codes, out and gu must be 16-byte, operand scales 4-byte aligned");
+    if (P.M > INT32_MAX || P.F > MX_MATMUL_MAX_N / 2 ||
+        ((P.M + BM - 1) / BM) * ((2 * P.F + BN - 1) / BN) > INT32_MAX / 2)
+        return mxk::fail(MX_EUNSUPPORTED, "problem too large (F at most %d)", MX_MATMUL_MAX_N / 2);
+    return MX_OK;
+}
+
+} // namespace mxg
+
+extern "C" {
+
+mx_status mx_gated_fwd(const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *w_codes,
+                       const uint8_t *w_scales, int64_t M, int64_t F, int64_t K, int block,
+                       int elem, int act, int scale_mode, int out_dtype, void *out,
+                       uint8_t *out_scales, void *gu, hipStream_t stream)
+{
+    mxk::clear_error();
+    const mxg::GatedProduct P{a_codes, a_scales, w_codes, w_scales,  M,   F,
+                              K,       act,      scale_mode, out_dtype, out, out_scales, gu};
+    const mx_status ok = mxg::check_gated(P, block, elem);
+    if (ok != MX_OK || M == 0 || F == 0)
+        return ok;
+    mxg::GatedArgs A;
+    gated_args(A, P, elem, stream);
+    return launched(by_type(elem, out_dtype, [&](auto e, auto o) {
+        return mxg::multiply<decltype(e)::value, decltype(o)::value>(A, stream);
+    }));
+}
+
+int mxt_gated_plan(int64_t M, int64_t F, int64_t K, int elem, int units, int *whole, int *tail,
+                   double *us)
+{
+    const int64_t rb = elem == MX_ELEM_E2M1 ? K / 2 : K;
+    if (M <= 0 || F <= 0 || K <= 0 || rb % mxg::KB != 0 || units <= 0)
+        return -1;
+    const mxg::Plan P = mxg::plan_gated(M, F, (int)(rb / mxg::KB), units);
+    *whole = P.whole;
+    *tail = P.tail;
+    *us = P.us;
+    return P.shape;
+}
+
+mx_status mxt_gated(const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *w_codes,
+                    const uint8_t *w_scales, int64_t M, int64_t F, int64_t K, int elem, int act,
+                    int scale_mode, int out_dtype, void *out, uint8_t *out_scales, void *gu,
+                    int shape, int whole, int units, hipStream_t stream)
+{
+    mxk::clear_error();
+    const mxg::GatedProduct P{a_codes, a_scales, w_codes, w_scales,  M,   F,
+                              K,       act,      scale_mode, out_dtype, out, out_scales, gu};
+    const mx_status ok = mxg::check_gated(P, 32, elem);
+    if (ok != MX_OK || M == 0 || F == 0)
+        return ok;
+    mxg::GatedArgs A;
+    gated_args(A, P, elem, stream);
+    const int64_t cells = ((M + mxg::BM - 1) / mxg::BM) * ((2 * F + mxg::BN - 1) / mxg::BN);
+    bool known = shape == mxg::S_256x256;
+    for (const int s : mxg::kGatedShapes)
+        known = known || s == shape;
+    if (!known || whole < 0 || whole >= cells || (whole && shape == mxg::S_256x256) || units < 0 ||
+        units > A.grid_max)
+        return mxk::fail(MX_EINVAL, "no such tile shape, first launch or number of units");
+    if (units)
+        A.grid_max = units;
+    const mxg::Plan plan{whole ? (int)mxg::S_256x256 : shape, whole, shape, 0.0};
+    return launched(by_type(elem, out_dtype, [&](auto e, auto o) {
+        return mxg::multiply_as<decltype(e)::value, decltype(o)::value>(plan, A, stream);
+    }));
+}
+
+} // extern "C"

@@ -112,6 +112,37 @@ mx_status mxnorm_linear_fwd(const void *x, int64_t T, int64_t d, const uint8_t *
                          out_dtype, out, stream);
 }
 
+size_t mxnorm_gated_fwd_workspace_bytes(int64_t T, int64_t d, int block, int elem)
+{
+    return mxnorm_linear_fwd_workspace_bytes(T, d, block, elem);
+}
+
+mx_status mxnorm_gated_fwd(const void *x, int64_t T, int64_t d, const uint8_t *w_codes,
+                           const uint8_t *w_scales, int64_t F, int block, int elem, int p,
+                           float coef, float eps, int scale_mode, int act, int out_dtype, void *out,
+                           uint8_t *out_scales, void *gu, float *rho, void *workspace,
+                           size_t workspace_bytes, hipStream_t stream)
+{
+    mxk::clear_error();
+    mx_status st = check_workspace(workspace, workspace_bytes,
+                                   mxnorm_gated_fwd_workspace_bytes(T, d, block, elem));
+    if (st != MX_OK)
+        return st;
+    const FwdSpace s(workspace, T, d, block > 0 ? block : 1, elem);
+    // both parts' checks come before the first launch
+    float c = coef;
+    if ((st = mxk::check_mxnorm(x, T, d, block, elem, p, c, eps, scale_mode, s.codes, s.scales,
+                                rho)) != MX_OK ||
+        (st = mxg::check_gated({s.codes, s.scales, w_codes, w_scales, T, F, d, act, scale_mode,
+                                out_dtype, out, out_scales, gu},
+                               block, elem)) != MX_OK ||
+        (st = mxnorm_mx_fwd(x, T, d, block, elem, p, coef, eps, scale_mode, s.codes, s.scales, rho,
+                            stream)) != MX_OK)
+        return st;
+    return mx_gated_fwd(s.codes, s.scales, w_codes, w_scales, T, F, d, block, elem, act, scale_mode,
+                        out_dtype, out, out_scales, gu, stream);
+}
+
 size_t mxnorm_linear_bwd_workspace_bytes(int64_t T, int64_t N, int64_t d, int elem)
 {
     if (T <= 0 || N <= 0 || d <= 0 || !known(elem))

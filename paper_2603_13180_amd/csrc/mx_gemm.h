@@ -9,6 +9,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 #include <utility>
 
 #include "mxnorm.h"
@@ -43,6 +44,24 @@ struct Args {
     int pid0, cells;
     int grid_max;   // workgroups resident at once
 };
+
+// A gated product: B has 2 N rows, N gate rows and then N up rows, and output
+// column n is act(gate product) times the up product of rows n and N + n.  A
+// tile's B rows are its BN / 2 gate rows, then the up rows of the same columns,
+// so that the tile gives BN / 2 output columns; every wave holds both products
+// of its columns.  `out` is float, bf16 or MX codes (MX_OUT_CODES).
+struct GatedArgs : Args {
+    uint8_t *hs;  // E8M0 scales of MX_OUT_CODES [M, N/32]
+    uint16_t *gu; // bf16 [M, 2 N]: both products, gate columns first; or NULL
+    int act, mode;
+};
+
+// A kernel's OUT: mx_out_dtype, + 4 for gated products.
+constexpr int kGate = 4;
+template <int OUT> constexpr bool kGated = OUT >= kGate;
+template <int OUT> using ArgsOf = std::conditional_t<kGated<OUT>, GatedArgs, Args>;
+// output columns of a tile of bn B rows
+template <int OUT> constexpr int kCols(int bn) { return kGated<OUT> ? bn / 2 : bn; }
 
 // The whole output as bm x bn cells of one tile each, in groups of
 // `group_rows` output rows.
@@ -195,26 +214,41 @@ __device__ __forceinline__ FragBase frag_base(uint32_t codes_off, uint32_t scale
     return b;
 }
 
-// fragment J of an operand from the stage at st; the row offset J*16 rows is
-// a compile-time constant that the LDS reads take as their immediate offset
-template <int ELEM, int J>
-__device__ __forceinline__ Frag read_frag(const LDS_AS uint8_t *st, const FragBase &b)
+// first row, from the operand's first, of fragment J of N: 16 J; with UP > 0
+// (the B rows of a gated product) the second half of the fragments starts UP
+// rows on
+template <int N, int UP> constexpr int frag_row(int J)
+{
+    return UP && J >= N / 2 ? UP + 16 * (J - N / 2) : 16 * J;
+}
+
+// the fragment ROW rows into an operand from the stage at st; the row offset
+// is a compile-time constant that the LDS reads take as their immediate offset
+template <int ELEM, int ROW>
+__device__ __forceinline__ Frag read_frag_at(const LDS_AS uint8_t *st, const FragBase &b)
 {
     constexpr int SB = kSB<ELEM>;
     Frag f;
-    const u32x4 lo = *reinterpret_cast<const LDS_AS u32x4 *>(st + b.lo + J * 16 * KB);
-    const u32x4 hi = *reinterpret_cast<const LDS_AS u32x4 *>(st + b.hi + J * 16 * KB);
+    const u32x4 lo = *reinterpret_cast<const LDS_AS u32x4 *>(st + b.lo + ROW * KB);
+    const u32x4 hi = *reinterpret_cast<const LDS_AS u32x4 *>(st + b.hi + ROW * KB);
     f.v = join(lo, hi);
-    f.s0 = st[b.sc + J * 16 * SB];
-    f.s1 = ELEM == MX_ELEM_E2M1 ? (int)st[b.sc + J * 16 * SB + 4] : 0;
+    f.s0 = st[b.sc + ROW * SB];
+    f.s1 = ELEM == MX_ELEM_E2M1 ? (int)st[b.sc + ROW * SB + 4] : 0;
     return f;
 }
 
-template <int ELEM, int N, int... J>
+// fragment J of an operand
+template <int ELEM, int J>
+__device__ __forceinline__ Frag read_frag(const LDS_AS uint8_t *st, const FragBase &b)
+{
+    return read_frag_at<ELEM, 16 * J>(st, b);
+}
+
+template <int ELEM, int UP, int N, int... J>
 __device__ __forceinline__ void read_frags(Frag (&f)[N], const LDS_AS uint8_t *st,
                                            const FragBase &b, std::integer_sequence<int, J...>)
 {
-    ((f[J] = read_frag<ELEM, J>(st, b)), ...);
+    ((f[J] = read_frag_at<ELEM, frag_row<N, UP>(J)>(st, b)), ...);
 }
 
 // acc += B-fragment x A-fragment over one K step (B is the instruction's first
@@ -351,5 +385,18 @@ __device__ __forceinline__ void store_tile(const Args &A, const v4f (&acc)[FN][F
         }
     }
 }
+
+// The output of a gated product's wave (mx_gemm_gated.h): acc[0 .. FN/2 - 1]
+// the gate products of its columns n0 + wn .., the rest the up products.
+template <int ELEM, int OUT, int FM, int FN>
+__device__ __forceinline__ void store_gated(const GatedArgs &A, const v4f (&acc)[FN][FM], int64_t m0,
+                                            int64_t n0, int wm, int wn, int g, int qd);
+
+// stores of one wave and whole tile, without those of A.gu and with them
+template <int OUT, int FM>
+constexpr int kGatedStores = OUT == kGate + MX_OUT_F32    ? 2 * FM
+                             : OUT == kGate + MX_OUT_BF16 ? FM
+                                                          : FM + (FM + 3) / 4;
+template <int FM> constexpr int kKeptStores = 2 * FM;
 
 } // namespace mxg

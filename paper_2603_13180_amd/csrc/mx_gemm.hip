@@ -337,10 +337,9 @@ mx_status check_product(const Product &P, int block, int elem, int out_dtype)
 
 } // namespace mxg
 
-namespace {
+namespace mxg {
 
-// A checked product's kernel arguments.
-void product_args(mxg::Args &A, const mxg::Product &P, int elem, hipStream_t stream)
+void product_args(Args &A, const Product &P, int elem, hipStream_t stream)
 {
     A.a = P.a;
     A.as = P.as;
@@ -352,12 +351,12 @@ void product_args(mxg::Args &A, const mxg::Product &P, int elem, hipStream_t str
     A.N = P.N;
     A.rb = elem == MX_ELEM_E2M1 ? P.K / 2 : P.K;
     A.rs = P.K / 32;
-    A.steps = (int)(A.rb / mxg::KB);
+    A.steps = (int)(A.rb / KB);
     const int cus = compute_units(stream);
     A.grid_max = cus > 0 ? cus : 256;
 }
 
-} // namespace
+} // namespace mxg
 
 extern "C" {
 
@@ -371,7 +370,7 @@ mx_status mx_matmul_fwd(const uint8_t *a_codes, const uint8_t *a_scales, const u
     if (ok != MX_OK || M == 0 || N == 0)
         return ok;
     mxg::Args A;
-    product_args(A, P, elem, stream);
+    mxg::product_args(A, P, elem, stream);
     hipStream_t st = static_cast<hipStream_t>(stream);
     hipError_t e;
     if (elem == MX_ELEM_E4M3)
@@ -471,7 +470,7 @@ mx_status mxt_matmul(const uint8_t *a_codes, const uint8_t *a_scales, const uint
     if (ok != MX_OK || M == 0 || N == 0)
         return ok;
     mxg::Args A;
-    product_args(A, P0, elem, stream);
+    mxg::product_args(A, P0, elem, stream);
     const int64_t cells = ((M + mxg::BM - 1) / mxg::BM) * ((N + mxg::BN - 1) / mxg::BN);
     if (!known_shape(shape) || whole < 0 || whole >= cells || units < 0 || units > A.grid_max)
         return mxk::fail(MX_EINVAL, "no such tile shape, first launch or number of units");
@@ -497,8 +496,8 @@ mx_status mxt_matmul_pair(const MxtProduct *f32, const MxtProduct *bf16, int ele
     if (ok != MX_OK)
         return ok;
     mxg::Args A0, A1;
-    product_args(A0, p0, elem, stream);
-    product_args(A1, p1, elem, stream);
+    mxg::product_args(A0, p0, elem, stream);
+    mxg::product_args(A1, p1, elem, stream);
     if (f32->M == 0 || f32->N == 0 || bf16->M == 0 || bf16->N == 0 || units < 0 ||
         units > A0.grid_max)
         return mxk::fail(MX_EINVAL, "empty product, or no such number of units");

@@ -37,14 +37,15 @@ constexpr int WTM = 128;   // wave tile along M
 constexpr int WTN = 64;    // wave tile along N
 constexpr int FM = WTM / 16, FN = WTN / 16;
 
-// Tile v of a launch whose cells are 256 x 256 (fewer divisions than tile_of:
+// Tile v of a launch whose cells are 256 x CN (fewer divisions than tile_of:
 // they stand between two tiles' loads).
+template <int CN = BN>
 __device__ __forceinline__ void whole_tile(const Args &A, int v, int64_t &m0, int64_t &n0)
 {
     int cm, cn;
     cell_of(A, xcd_range(v, A.cells), cm, cn);
     m0 = (int64_t)cm * BM;
-    n0 = (int64_t)cn * BN;
+    n0 = (int64_t)cn * CN;
 }
 
 template <int ELEM> struct Op {
@@ -60,13 +61,15 @@ template <int ELEM> struct Op {
 // scale bytes of A's rows 64w .. 64w+63, waves 4-7 those of B's rows
 // 64(w-4) .. 64(w-4)+63 (lane i of scale instruction u moves dword
 // i % (SB/4) of row u (64 / (SB/4)) + i / (SB/4)).  Rows past M or N read
-// row M-1 or N-1: their results are never stored.
+// row M-1 or N-1: their results are never stored.  Gated: B's rows 0 .. 127 are
+// gate rows, which waves 0-3 (scales: 4-5) move, the others up rows; the
+// offsets are relative to the tile's first gate or up row.
 template <int ELEM> struct Rows {
     uint32_t a[4], b[4];
     uint32_t s[Op<ELEM>::SB / 4];
 };
 
-template <int ELEM>
+template <int ELEM, bool GATED = false>
 __device__ __forceinline__ Rows<ELEM> lane_rows(const Args &A, int64_t m0, int64_t n0, int w,
                                                 int l)
 {
@@ -77,14 +80,15 @@ __device__ __forceinline__ Rows<ELEM> lane_rows(const Args &A, int64_t m0, int64
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
         const int r = 32 * w + 8 * t + rr;
+        const int rb = GATED ? r & (BN / 2 - 1) : r;
         R.a[t] = (uint32_t)((min(m0 + r, A.M - 1) - m0) * A.rb) + 16 * ch;
-        R.b[t] = (uint32_t)((min(n0 + r, A.N - 1) - n0) * A.rb) + 16 * ch;
+        R.b[t] = (uint32_t)((min(n0 + rb, A.N - 1) - n0) * A.rb) + 16 * ch;
     }
     const bool on_a = w < 4;
     const int64_t base = on_a ? m0 : n0, lim = on_a ? A.M : A.N;
 #pragma unroll
     for (int u = 0; u < DW; ++u) {
-        const int r = 64 * (w & 3) + u * (64 / DW) + l / DW;
+        const int r = 64 * (GATED && !on_a ? w & 1 : w & 3) + u * (64 / DW) + l / DW;
         R.s[u] = (uint32_t)((min(base + r, lim - 1) - base) * A.rs) + 4 * (l % DW);
     }
     return R;
@@ -117,7 +121,8 @@ __device__ __forceinline__ void issue_step(const uint8_t *ta, const uint8_t *tb,
 // The products of one K step from the stage at st: the step's four B
 // fragments held in registers, the eight A fragments streamed, each requested
 // two ahead of the products that use it.
-template <int ELEM>
+// UP: the distance of the up rows from the gate rows of a gated product's B.
+template <int ELEM, int UP = 0>
 __device__ __forceinline__ void step_products(v4f (&acc)[FN][FM], const LDS_AS uint8_t *st,
                                               const FragBase &ba, const FragBase &bb)
 {
@@ -132,12 +137,12 @@ __device__ __forceinline__ void step_products(v4f (&acc)[FN][FM], const LDS_AS u
         // half from half-fragment reads, were 1.5-3% slower at the QKV and
         // gate+up shapes.)
         Frag fb[FN], fa[FM];
-        fb[0] = read_frag<ELEM, 0>(st, bb);
-        fb[1] = read_frag<ELEM, 1>(st, bb);
+        fb[0] = read_frag_at<ELEM, frag_row<FN, UP>(0)>(st, bb);
+        fb[1] = read_frag_at<ELEM, frag_row<FN, UP>(1)>(st, bb);
         fa[0] = read_frag<ELEM, 0>(st, ba);
         __builtin_amdgcn_sched_barrier(0);
-        fb[2] = read_frag<ELEM, 2>(st, bb);
-        fb[3] = read_frag<ELEM, 3>(st, bb);
+        fb[2] = read_frag_at<ELEM, frag_row<FN, UP>(2)>(st, bb);
+        fb[3] = read_frag_at<ELEM, frag_row<FN, UP>(3)>(st, bb);
         fa[1] = read_frag<ELEM, 1>(st, ba);
         __builtin_amdgcn_sched_barrier(0);
         auto column = [&](auto jc) {
@@ -167,12 +172,12 @@ __device__ __forceinline__ void step_products(v4f (&acc)[FN][FM], const LDS_AS u
     // B0, B1 and A0 first, so that the first two products wait for three
     // fragments, not six (QKV shape: 1-3% faster).
     Frag fb[FN], fa[FM];
-    fb[0] = read_frag<ELEM, 0>(st, bb);
-    fb[1] = read_frag<ELEM, 1>(st, bb);
+    fb[0] = read_frag_at<ELEM, frag_row<FN, UP>(0)>(st, bb);
+    fb[1] = read_frag_at<ELEM, frag_row<FN, UP>(1)>(st, bb);
     fa[0] = read_frag<ELEM, 0>(st, ba);
     __builtin_amdgcn_sched_barrier(0);
-    fb[2] = read_frag<ELEM, 2>(st, bb);
-    fb[3] = read_frag<ELEM, 3>(st, bb);
+    fb[2] = read_frag_at<ELEM, frag_row<FN, UP>(2)>(st, bb);
+    fb[3] = read_frag_at<ELEM, frag_row<FN, UP>(3)>(st, bb);
     fa[1] = read_frag<ELEM, 1>(st, ba);
     __builtin_amdgcn_sched_barrier(0);
     fa[2] = read_frag<ELEM, 2>(st, ba);
@@ -204,8 +209,10 @@ __device__ __forceinline__ void step_products(v4f (&acc)[FN][FM], const LDS_AS u
 }
 
 template <int ELEM, int OUT>
-__global__ void __launch_bounds__(NT) mx_gemm_kernel(Args A)
+__global__ void __launch_bounds__(NT) mx_gemm_kernel(ArgsOf<OUT> A)
 {
+    constexpr bool GATED = kGated<OUT>;
+    constexpr int CN = kCols<OUT>(BN); // output columns of a tile
     constexpr int SB = Op<ELEM>::SB;
     constexpr int STAGE = Op<ELEM>::STAGE;
     __shared__ __attribute__((aligned(16))) uint8_t lds[2 * STAGE];
@@ -218,17 +225,23 @@ __global__ void __launch_bounds__(NT) mx_gemm_kernel(Args A)
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6); // wave-uniform
     const int l = tid & 63;
     const int g = l >> 4, qd = l & 15; // lane group (K block / output row quad), row in fragment
-    const int wm = (w & 1) * WTM, wn = (w >> 1) * WTN;
+    const int wm = (w & 1) * WTM, wn = (w >> 1) * kCols<OUT>(WTN);
 
     LDS_AS uint8_t *st0 = (LDS_AS uint8_t *)lds;
     const uint32_t st0_addr = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)st0);
     const FragBase ba = frag_base<ELEM>(0, (BM + BN) * KB, wm, qd, g);
     const FragBase bb = frag_base<ELEM>(BM * KB, (BM + BN) * KB + BM * SB, wn, qd, g);
+    // the B operand as this wave moves it: its codes and its scales
+    const uint8_t *wb = A.b, *wbs = A.bs;
+    if constexpr (GATED) {
+        wb += w >= 4 ? A.N * A.rb : 0;
+        wbs += w >= 6 ? A.N * A.rs : 0;
+    }
 
     int v = blockIdx.x;
     int64_t m0, n0;
-    whole_tile(A, v, m0, n0);
-    Rows<ELEM> R = lane_rows<ELEM>(A, m0, n0, w, l);
+    whole_tile<CN>(A, v, m0, n0);
+    Rows<ELEM> R = lane_rows<ELEM, GATED>(A, m0, n0, w, l);
 
     // Pipeline, one barrier per K step.  At the top of a step every wave has
     // its own DMA of the step landed (vmcnt) and, past the barrier, so has
@@ -236,7 +249,7 @@ __global__ void __launch_bounds__(NT) mx_gemm_kernel(Args A)
     // step): the DMA of the next step goes there, and after a tile's last
     // step the DMA of the next tile's first step, which then runs under that
     // last step's products and the tile's stores.
-    issue_step<ELEM>(A.a + m0 * A.rb, A.b + n0 * A.rb, A.as + m0 * A.rs, A.bs + n0 * A.rs, R, 0,
+    issue_step<ELEM>(A.a + m0 * A.rb, wb + n0 * A.rb, A.as + m0 * A.rs, wbs + n0 * A.rs, R, 0,
                      st0_addr, w);
     bool prev_full = false; // the previous tile lies inside H (all its stores ran)
     for (int gs = 0;;) {
@@ -254,25 +267,38 @@ __global__ void __launch_bounds__(NT) mx_gemm_kernel(Args A)
             // previous tile's stores, issued after this DMA, need not have
             // completed: operations complete in order, so at most that many
             // may remain (a partial tile ran fewer stores: wait for all).
-            if (s == 0 && prev_full)
-                wait_vmcnt<kTileStores<OUT, FM, FN>>();
-            else
-                wait_vmcnt<0>();
+            if constexpr (GATED) {
+                constexpr int H = kGatedStores<OUT, FM>;
+                if (s == 0 && prev_full && A.gu)
+                    wait_vmcnt<H + kKeptStores<FM>>();
+                else if (s == 0 && prev_full)
+                    wait_vmcnt<H>();
+                else
+                    wait_vmcnt<0>();
+            } else {
+                if (s == 0 && prev_full)
+                    wait_vmcnt<kTileStores<OUT, FM, FN>>();
+                else
+                    wait_vmcnt<0>();
+            }
             barrier();
             const uint32_t nxt = st0_addr + (cur ^ 1) * STAGE;
             if (s + 1 < A.steps) {
-                issue_step<ELEM>(A.a + m0 * A.rb, A.b + n0 * A.rb, A.as + m0 * A.rs,
-                                 A.bs + n0 * A.rs, R, s + 1, nxt, w);
+                issue_step<ELEM>(A.a + m0 * A.rb, wb + n0 * A.rb, A.as + m0 * A.rs,
+                                 wbs + n0 * A.rs, R, s + 1, nxt, w);
             } else if (nv < G) {
-                whole_tile(A, nv, m1, n1);
-                R = lane_rows<ELEM>(A, m1, n1, w, l);
-                issue_step<ELEM>(A.a + m1 * A.rb, A.b + n1 * A.rb, A.as + m1 * A.rs,
-                                 A.bs + n1 * A.rs, R, 0, nxt, w);
+                whole_tile<CN>(A, nv, m1, n1);
+                R = lane_rows<ELEM, GATED>(A, m1, n1, w, l);
+                issue_step<ELEM>(A.a + m1 * A.rb, wb + n1 * A.rb, A.as + m1 * A.rs,
+                                 wbs + n1 * A.rs, R, 0, nxt, w);
             }
-            step_products<ELEM>(acc, st0 + cur * STAGE, ba, bb);
+            step_products<ELEM, GATED ? CN : 0>(acc, st0 + cur * STAGE, ba, bb);
         }
-        store_tile<OUT, FM, FN>(A, acc, m0, n0, wm, wn, g, qd);
-        prev_full = m0 + BM <= A.M && n0 + BN <= A.N;
+        if constexpr (GATED)
+            store_gated<ELEM, OUT, FM, FN>(A, acc, m0, n0, wm, wn, g, qd);
+        else
+            store_tile<OUT, FM, FN>(A, acc, m0, n0, wm, wn, g, qd);
+        prev_full = m0 + BM <= A.M && n0 + CN <= A.N;
         if (nv >= G)
             break;
         v = nv;
@@ -282,7 +308,7 @@ __global__ void __launch_bounds__(NT) mx_gemm_kernel(Args A)
 }
 
 template <int ELEM, int OUT>
-hipError_t launch(const Args &A, hipStream_t stream)
+hipError_t launch(const ArgsOf<OUT> &A, hipStream_t stream)
 {
     const int G = A.cells;
     const int grid = G < A.grid_max ? G : A.grid_max;

@@ -1,0 +1,198 @@
+// mx_gemm_gated.h -- the output of the gated product: H = act(G) U from a
+// wave's gate products G and up products U (mx_gemm.h describes the tile), as
+// float, bf16 or MX codes, and the products themselves where a backward pass
+// will need them.
+//
+// act(g) = g sigma(z(g)) with z = g (SiLU) or 2 sqrt(2/pi) (g + 0.044715 g^3)
+// (GELU in its tanh form, since (1 + tanh y) / 2 = sigma(2 y)).
+//
+// In accumulator layout lane (g, qd) of tile i holds row qd, columns 16 i + 4 g
+// .. + 3, and a wave holds 32 output columns: the two tiles of a row are one MX
+// block over four lanes, so its absmax is two lane swaps away and nothing
+// passes through LDS.
+#pragma once
+
+#include "mx_gemm.h"
+#include "norm_cast.h"
+
+namespace mxg {
+
+// sigma(z(g)) from the hardware's exp2 and reciprocal, one unit in the last
+// place each: for |z| up to 20 the result is within 2^-19 of its value
+// relatively (the argument's rounding), far below a bf16 or MX rounding.  z
+// beyond the exponential's range gives exactly 0 or 1.
+template <int ACT> __device__ __forceinline__ float gate_sigma(float g)
+{
+    constexpr float kLog2e = 1.44269504f;
+    float t; // -z log2(e)
+    if constexpr (ACT == MX_ACT_SILU) {
+        t = g * -kLog2e;
+    } else {
+        constexpr float c = 1.5957691216f * kLog2e; // 2 sqrt(2/pi) log2(e)
+        t = g * __builtin_fmaf(g * g, -c * 0.044715f, -c);
+    }
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));
+}
+
+// The tiles v0, v1 of one row group as 32 bf16 columns: as in store_tile, lane
+// row g stores 8 adjacent columns of tile g & 1 from column 8 (g >> 1).
+__device__ __forceinline__ void store_row_bf16(__amdgpu_buffer_rsrc_t rs, const v4f &v0, const v4f &v1,
+                                               uint32_t off, bool in)
+{
+    const auto sl = __builtin_amdgcn_permlane16_swap(pack_bf16(v0[0], v0[1]), pack_bf16(v1[0], v1[1]),
+                                                     false, false);
+    const auto sh = __builtin_amdgcn_permlane16_swap(pack_bf16(v0[2], v0[3]), pack_bf16(v1[2], v1[3]),
+                                                     false, false);
+    if (in)
+        __builtin_amdgcn_raw_buffer_store_b128(u32x4{sl[0], sh[0], sl[1], sh[1]}, rs, (int)off, 0,
+                                               kStorePolicy);
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(void *p, int64_t byte)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t *>(p) + byte, 0, 0x7FFFFFFF, 0x00020000);
+}
+
+// 16 rows from mr, 32 output columns from nc: gate products p[0], p[1], up
+// products p[2], p[3].  Returns the block's E8M0 byte (MX_OUT_CODES), the same
+// in the four lanes of a row.
+template <int ELEM, int OUT, int ACT>
+__device__ __forceinline__ uint32_t gated_rows(const GatedArgs &A, const v4f (&p)[4], int64_t mr,
+                                               int64_t nc, int g, int qd)
+{
+    constexpr int O = OUT - kGate;
+    const bool row = mr + qd < A.M;
+    const int64_t n8 = nc + 16 * (g & 1) + 8 * (g >> 1); // this lane's 8 columns
+    const bool in8 = row && n8 < A.N;                    // N is a multiple of 16
+    if (A.gu) {
+        const __amdgpu_buffer_rsrc_t rs = rows_rsrc(A.gu, mr * A.N * 4);
+        const uint32_t off = (uint32_t)(qd * A.N) * 4 + (uint32_t)n8 * 2;
+        store_row_bf16(rs, p[0], p[1], off, in8);
+        store_row_bf16(rs, p[2], p[3], off + (uint32_t)A.N * 2, in8);
+    }
+    v4f h[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            h[i][e] = p[i][e] * gate_sigma<ACT>(p[i][e]) * p[i + 2][e];
+
+    if constexpr (O == MX_OUT_F32) {
+        const __amdgpu_buffer_rsrc_t rs = rows_rsrc(A.out, mr * A.N * 4);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int64_t n = nc + 16 * i + 4 * g;
+            if (row && n < A.N)
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, h[i]), rs,
+                                                       (int)((uint32_t)(qd * A.N + n) * 4), 0,
+                                                       kStorePolicy);
+        }
+        return 0;
+    } else if constexpr (O == MX_OUT_BF16) {
+        store_row_bf16(rows_rsrc(A.out, mr * A.N * 2), h[0], h[1], (uint32_t)(qd * A.N + n8) * 2, in8);
+        return 0;
+    } else {
+        // The MX cast of the float values (no rounding to bf16 in between).
+        // The block's absmax as the integer maximum of the magnitudes (NaN
+        // above infinity): a lane's 8 values, then lanes 16 and 32 away.
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                m = max(m, __float_as_uint(h[i][e]) & 0x7FFFFFFFu);
+        const auto m16 = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+        m = max(m16[0], m16[1]);
+        const auto m32 = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+        m = max(m32[0], m32[1]);
+        const float a = __uint_as_float(m);
+        uint32_t q[2];
+        uint32_t byte;
+        if constexpr (ELEM == MX_ELEM_E4M3) {
+            byte = mxk::e8m0_byte<false>(a, A.mode);
+            if (A.mode == MX_SCALE_FLOOR) { // RCEIL never exceeds 448 * 2^e
+                const float lim = __uint_as_float(((byte + 8u) << 23) | 0x600000u);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        h[i][e] = __builtin_amdgcn_fmed3f(h[i][e], -lim, lim);
+            }
+            const float scale = __uint_as_float(byte << 23);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                q[i] = mxk::e4m3x4_hw(h[i][0], h[i][1], h[i][2], h[i][3], scale);
+        } else {
+            byte = mxk::e8m0_byte<true>(a, A.mode);
+            const float scale = __uint_as_float(byte << 23);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, h[i][0], h[i][1], scale, 0);
+                q[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q[i], h[i][2], h[i][3], scale, 1);
+            }
+        }
+        if (__builtin_amdgcn_ballot_w64(byte == 0xFFu)) { // rare: non-finite values
+            if (byte == 0xFFu) { // their signs, all-ones magnitudes
+                constexpr int W = ELEM == MX_ELEM_E4M3 ? 8 : 4;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    q[i] = ELEM == MX_ELEM_E4M3 ? 0x7F7F7F7Fu : 0x7777u;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        q[i] |= (__float_as_uint(h[i][e]) >> 31) << (W * e + W - 1);
+                }
+            }
+        }
+        const auto s = __builtin_amdgcn_permlane16_swap(q[0], q[1], false, false);
+        if constexpr (ELEM == MX_ELEM_E4M3) {
+            const __amdgpu_buffer_rsrc_t rs = rows_rsrc(A.out, mr * A.N);
+            if (in8)
+                __builtin_amdgcn_raw_buffer_store_b64(mxk::u32x2_t{s[0], s[1]}, rs,
+                                                      (int)(uint32_t)(qd * A.N + n8), 0, 0);
+        } else {
+            const __amdgpu_buffer_rsrc_t rs = rows_rsrc(A.out, mr * (A.N / 2));
+            if (in8)
+                __builtin_amdgcn_raw_buffer_store_b32(s[0] | (s[1] << 16), rs,
+                                                      (int)(uint32_t)((qd * A.N + n8) / 2), 0, 0);
+        }
+        return byte;
+    }
+}
+
+template <int ELEM, int OUT, int ACT, int FM>
+__device__ __forceinline__ void store_gated_act(const GatedArgs &A, const v4f (&acc)[4][FM], int64_t m,
+                                                int64_t nc, int g, int qd)
+{
+    uint32_t byte[FM];
+#pragma unroll
+    for (int j = 0; j < FM; ++j) {
+        const v4f p[4] = {acc[0][j], acc[1][j], acc[2][j], acc[3][j]};
+        byte[j] = gated_rows<ELEM, OUT, ACT>(A, p, m + 16 * j, nc, g, qd);
+    }
+    if constexpr (OUT - kGate == MX_OUT_CODES) {
+        // lane row g stores the scales of row groups g, 4 + g, ...
+#pragma unroll
+        for (int j = 0; j < FM; j += 4) {
+            uint32_t b = byte[j];
+#pragma unroll
+            for (int k = 1; k < 4 && j + k < FM; ++k)
+                b = g == k ? byte[j + k] : b;
+            const int64_t r = m + 16 * (j + g) + qd;
+            if (j + g < FM && r < A.M && nc < A.N)
+                A.hs[r * (A.N / 32) + nc / 32] = (uint8_t)b;
+        }
+    }
+}
+
+template <int ELEM, int OUT, int FM, int FN>
+__device__ __forceinline__ void store_gated(const GatedArgs &A, const v4f (&acc)[FN][FM], int64_t m0,
+                                            int64_t n0, int wm, int wn, int g, int qd)
+{
+    static_assert(FN == 4, "a wave's output columns are one MX block");
+    if (A.act == MX_ACT_SILU)
+        store_gated_act<ELEM, OUT, MX_ACT_SILU, FM>(A, acc, m0 + wm, n0 + wn, g, qd);
+    else
+        store_gated_act<ELEM, OUT, MX_ACT_GELU_TANH, FM>(A, acc, m0 + wm, n0 + wn, g, qd);
+}
+
+} // namespace mxg

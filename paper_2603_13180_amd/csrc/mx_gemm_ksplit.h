@@ -35,9 +35,11 @@ template <class C, int ELEM> struct KSplitOp {
 };
 
 template <int ELEM, int OUT, class C>
-__global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(Args A)
+__global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(ArgsOf<OUT> A)
 {
     using O = KSplitOp<C, ELEM>;
+    constexpr bool GATED = kGated<OUT>;
+    constexpr int CN = kCols<OUT>(C::BN); // output columns of a tile
     constexpr int SB = O::SB, DW = SB / 4;
     __shared__ __attribute__((aligned(16))) uint8_t lds[C::NW * O::PART];
 
@@ -45,7 +47,7 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(Args A)
     const int l = threadIdx.x & 63;
     const int g = l >> 4, qd = l & 15;
     int64_t m0, n0;
-    tile_of(A, C::BM, C::BN, blockIdx.x, m0, n0);
+    tile_of(A, C::BM, CN, blockIdx.x, m0, n0);
     if (m0 >= A.M || n0 >= A.N) // a part of a cell that lies outside H
         return;
 
@@ -53,14 +55,17 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(Args A)
     // x 128 bytes per instruction, swizzled as in the fragment reads; scale
     // dword 64 t + l of the step).  Rows past M or N read the last row: their
     // results are never stored.
+    // Gated: the second half of B's rows are up rows, N rows further on.
     const uint8_t *ta = A.a + m0 * A.rb, *tb = A.b + n0 * A.rb;
+    const uint8_t *tb2 = GATED ? tb + A.N * A.rb : tb;
+    auto brow = [](int r) { return GATED ? (r - C::BM) % (C::BN / 2) : r - C::BM; };
     const int rr = l >> 3, ch = (l & 7) ^ rr;
     uint32_t code[C::LC];
 #pragma unroll
     for (int t = 0; t < C::LC; ++t) {
         const int r = 8 * t;
         const int64_t off = r < C::BM ? min(m0 + r + rr, A.M - 1) - m0
-                                      : min(n0 + (r - C::BM) + rr, A.N - 1) - n0;
+                                      : min(n0 + brow(r) + rr, A.N - 1) - n0;
         code[t] = (uint32_t)(off * A.rb) + 16 * ch;
     }
     const uint8_t *sc[O::LS];
@@ -68,7 +73,8 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(Args A)
     for (int t = 0; t < O::LS; ++t) {
         const int dw = 64 * t + l, r = min(dw / DW, C::BM + C::BN - 1);
         sc[t] = (r < C::BM ? A.as + min(m0 + r, A.M - 1) * A.rs
-                           : A.bs + min(n0 + (r - C::BM), A.N - 1) * A.rs) + 4 * (dw % DW);
+                           : A.bs + (min(n0 + brow(r), A.N - 1) +
+                                     (GATED && r >= C::BM + CN ? A.N : 0)) * A.rs) + 4 * (dw % DW);
     }
 
     LDS_AS uint8_t *ring = (LDS_AS uint8_t *)lds + w * O::PART;
@@ -77,7 +83,7 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(Args A)
         const uint32_t st = ring_addr + slot * O::SLOT;
 #pragma unroll
         for (int t = 0; t < C::LC; ++t)
-            lds_load16(8 * t < C::BM ? ta : tb, code[t] + (uint32_t)k * KB, st + 8 * t * KB);
+            lds_load16(8 * t < C::BM ? ta : 8 * t < C::BM + CN ? tb : tb2, code[t] + (uint32_t)k * KB, st + 8 * t * KB);
 #pragma unroll
         for (int t = 0; t < O::LS; ++t)
             lds_load4(sc[t] + (uint32_t)k * SB, st + (C::BM + C::BN) * KB + 256 * t);
@@ -101,8 +107,8 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(Args A)
         wait_steps<O::L, C::S - 1>(mine - 1 - p);
         const LDS_AS uint8_t *st = ring + slot * O::SLOT;
         Frag fa[C::FM], fb[C::FN];
-        read_frags<ELEM, C::FN>(fb, st, bb, std::make_integer_sequence<int, C::FN>{});
-        read_frags<ELEM, C::FM>(fa, st, ba, std::make_integer_sequence<int, C::FM>{});
+        read_frags<ELEM, GATED ? CN : 0>(fb, st, bb, std::make_integer_sequence<int, C::FN>{});
+        read_frags<ELEM, 0>(fa, st, ba, std::make_integer_sequence<int, C::FM>{});
         // the slot is in registers: its next step may land in it
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (p + C::S < mine)
@@ -121,12 +127,27 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(Args A)
         for (int i = 0; i < C::FN; ++i)
             sum[(j * C::FN + i) * 64 + l] = acc[j][i];
     barrier();
-    for (int f = w; f < C::FM * C::FN; f += C::NW) {
+    auto total = [&](int f) {
         v4f v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < C::NW; ++u)
             v += reinterpret_cast<const LDS_AS v4f *>((LDS_AS uint8_t *)lds +
                                                       u * O::PART)[f * 64 + l];
+        return v;
+    };
+    if constexpr (GATED) {
+        // a wave takes the rows of one tile row: its columns' MX block is whole
+        for (int j = w; j < C::FM; j += C::NW) {
+            v4f at[C::FN][1];
+#pragma unroll
+            for (int i = 0; i < C::FN; ++i)
+                at[i][0] = total(j * C::FN + i);
+            store_gated<ELEM, OUT, 1, C::FN>(A, at, m0, n0, 16 * j, 0, g, qd);
+        }
+        return;
+    }
+    for (int f = w; f < C::FM * C::FN; f += C::NW) {
+        v4f v = total(f);
         // lane (g, qd) of tile (j, i) holds H[m0 + 16 j + qd][n0 + 16 i + 4 g .. +3]
         const int64_t m = m0 + 16 * (f / C::FN) + qd, n = n0 + 16 * (f % C::FN) + 4 * g;
         if (m < A.M && n < A.N) { // N is a multiple of 16
@@ -146,7 +167,7 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(Args A)
     }
 }
 
-template <int ELEM, int OUT, class C> hipError_t launch_ksplit(const Args &A, hipStream_t stream)
+template <int ELEM, int OUT, class C> hipError_t launch_ksplit(const ArgsOf<OUT> &A, hipStream_t stream)
 {
     hipLaunchKernelGGL((mx_gemm_ksplit_kernel<ELEM, OUT, C>), dim3((unsigned)(A.cells * A.sub_m * A.sub_n)),
                        dim3(C::NT), 0, stream, A);

@@ -8,6 +8,7 @@
 #include "mx_gemm_256.h"
 #include "mx_gemm_ksplit.h"
 #include "mx_gemm_ring.h"
+#include "products.h"
 
 namespace mxg {
 
@@ -19,8 +20,11 @@ using K16x32 = KSplit<16, 32, 8, 3>;
 using K32x32 = KSplit<32, 32, 8, 2>;
 using K32x64 = KSplit<32, 64, 8, 1>;
 using K64x64 = KSplit<64, 64, 8, 1>;
+using K16x64 = KSplit<16, 64, 8, 1>;
 
 enum Shape { S_K16x32, S_K32x32, S_K32x64, S_K64x64, S_R64x128, S_R128x128, S_256x256, S_COUNT };
+// gated products alone: the smallest tile whose waves hold a whole MX block
+constexpr int S_K16x64 = S_COUNT;
 
 // What a launch of each tile shape costs on MI355X, fitted to times at K =
 // 512 .. 8192 and 64 to 3400 tiles: us once per launch, per round of tiles
@@ -52,11 +56,12 @@ struct Cost {
     int bm, bn;
     float once, round, step, few, few_step;
 };
-constexpr Cost kCost[S_COUNT] = {
+constexpr Cost kCost[S_COUNT + 1] = {
     {16, 32, 1.3f, 1.0f, 0.14f, 1.6f, 0.0f},   {32, 32, 1.4f, 1.1f, 0.14f, 1.9f, 0.0f},
     {32, 64, 2.2f, 0.7f, 0.19f, 2.15f, 0.0f},  {64, 64, 0.4f, 2.6f, 0.275f, 2.9f, 0.2f},
     {64, 128, 3.1f, 0.4f, 0.425f, 1.1f, 0.3f}, {128, 128, 4.1f, 0.8f, 0.59f, 1.8f, 0.45f},
     {256, 256, 1.2f, 4.0f, 1.75f, 0.0f, 0.0f},
+    {16, 64, 2.2f, 0.7f, 0.17f, 2.15f, 0.0f},
 };
 
 // us a launch over `cells` outputs of cm x cn takes on `cus` compute units
@@ -67,7 +72,7 @@ inline double launch_cost(int shape, int64_t cells, int64_t cm, int64_t cn, int 
     const int64_t rounds = (tiles + cus - 1) / cus;
     const double per = c.round + (double)steps * c.step;
     const double few = std::max(per, (double)c.few + (double)steps * c.few_step);
-    if (shape <= S_K64x64)
+    if (shape <= S_K64x64 || shape == S_K16x64)
         return c.once + (double)rounds * (rounds > 2 ? few : per);
     double us = (double)rounds * per + (double)std::max<int64_t>(0, rounds - 8) * (few - per);
     if (shape == S_R64x128 && cn <= 64 && rounds > 2)
@@ -85,10 +90,15 @@ struct Plan {
     double us;
 };
 
-inline Plan plan_product(int64_t M, int64_t N, int steps, int cus)
+// The tile shapes smaller than 256 x 256 that a product may take.
+constexpr int kPlainShapes[] = {S_K16x32, S_K32x32, S_K32x64, S_K64x64, S_R64x128, S_R128x128};
+constexpr int kGatedShapes[] = {S_K16x64, S_K32x64, S_K64x64, S_R64x128, S_R128x128};
+
+template <size_t NS>
+inline Plan plan_among(const int (&shapes)[NS], int64_t M, int64_t N, int steps, int cus)
 {
     Plan P{S_256x256, 0, 0, launch_cost(S_256x256, 1, M, N, steps, cus)};
-    for (int s = 0; s < S_256x256; ++s) {
+    for (const int s : shapes) {
         const double c = launch_cost(s, 1, M, N, steps, cus);
         if (c < P.us) {
             P.us = c;
@@ -98,9 +108,9 @@ inline Plan plan_product(int64_t M, int64_t N, int steps, int cus)
     const int64_t cells = ((M + BM - 1) / BM) * ((N + BN - 1) / BN);
     const int64_t whole = cells / cus * cus, left = cells - whole;
     if (whole && left) {
-        int tail = 0;
-        double tcost = launch_cost(0, left, BM, BN, steps, cus);
-        for (int s = 1; s < S_256x256; ++s) {
+        int tail = shapes[0];
+        double tcost = launch_cost(tail, left, BM, BN, steps, cus);
+        for (const int s : shapes) {
             const double c = launch_cost(s, left, BM, BN, steps, cus);
             if (c < tcost) {
                 tcost = c;
@@ -114,23 +124,46 @@ inline Plan plan_product(int64_t M, int64_t N, int steps, int cus)
     return P;
 }
 
-template <int ELEM, int OUT> hipError_t launch_shape(int shape, const Args &A, hipStream_t stream)
+inline Plan plan_product(int64_t M, int64_t N, int steps, int cus)
 {
-    switch (shape) {
-    case S_K16x32: return launch_ksplit<ELEM, OUT, K16x32>(A, stream);
-    case S_K32x32: return launch_ksplit<ELEM, OUT, K32x32>(A, stream);
-    case S_K32x64: return launch_ksplit<ELEM, OUT, K32x64>(A, stream);
-    case S_K64x64: return launch_ksplit<ELEM, OUT, K64x64>(A, stream);
-    case S_R64x128: return launch_ring<ELEM, OUT, R64x128>(A, stream);
-    case S_R128x128: return launch_ring<ELEM, OUT, R128x128>(A, stream);
-    default: return launch<ELEM, OUT>(A, stream);
+    return plan_among(kPlainShapes, M, N, steps, cus);
+}
+
+// N columns of H: a tile of bn B rows gives bn / 2 of them.
+inline Plan plan_gated(int64_t M, int64_t N, int steps, int cus)
+{
+    return plan_among(kGatedShapes, M, 2 * N, steps, cus);
+}
+
+template <int ELEM, int OUT>
+hipError_t launch_shape(int shape, const ArgsOf<OUT> &A, hipStream_t stream)
+{
+    if constexpr (kGated<OUT>) {
+        switch (shape) {
+        case S_K16x64: return launch_ksplit<ELEM, OUT, K16x64>(A, stream);
+        case S_K32x64: return launch_ksplit<ELEM, OUT, K32x64>(A, stream);
+        case S_K64x64: return launch_ksplit<ELEM, OUT, K64x64>(A, stream);
+        case S_R64x128: return launch_ring<ELEM, OUT, R64x128>(A, stream);
+        case S_R128x128: return launch_ring<ELEM, OUT, R128x128>(A, stream);
+        default: return launch<ELEM, OUT>(A, stream);
+        }
+    } else {
+        switch (shape) {
+        case S_K16x32: return launch_ksplit<ELEM, OUT, K16x32>(A, stream);
+        case S_K32x32: return launch_ksplit<ELEM, OUT, K32x32>(A, stream);
+        case S_K32x64: return launch_ksplit<ELEM, OUT, K32x64>(A, stream);
+        case S_K64x64: return launch_ksplit<ELEM, OUT, K64x64>(A, stream);
+        case S_R64x128: return launch_ring<ELEM, OUT, R64x128>(A, stream);
+        case S_R128x128: return launch_ring<ELEM, OUT, R128x128>(A, stream);
+        default: return launch<ELEM, OUT>(A, stream);
+        }
     }
 }
 
 template <int ELEM, int OUT>
-hipError_t multiply_as(const Plan &P, Args A, hipStream_t stream)
+hipError_t multiply_as(const Plan &P, ArgsOf<OUT> A, hipStream_t stream)
 {
-    set_tiles(A, kCost[P.shape].bm, kCost[P.shape].bn, 1024);
+    set_tiles(A, kCost[P.shape].bm, kCols<OUT>(kCost[P.shape].bn), 1024);
     if (!P.whole)
         return launch_shape<ELEM, OUT>(P.shape, A, stream);
     const int left = A.cells - P.whole;
@@ -145,9 +178,15 @@ hipError_t multiply_as(const Plan &P, Args A, hipStream_t stream)
     return launch_shape<ELEM, OUT>(P.tail, A, stream);
 }
 
-template <int ELEM, int OUT> hipError_t multiply(const Args &A, hipStream_t stream)
+template <int ELEM, int OUT> hipError_t multiply(const ArgsOf<OUT> &A, hipStream_t stream)
 {
-    return multiply_as<ELEM, OUT>(plan_product(A.M, A.N, A.steps, A.grid_max), A, stream);
+    if constexpr (kGated<OUT>)
+        return multiply_as<ELEM, OUT>(plan_gated(A.M, A.N, A.steps, A.grid_max), A, stream);
+    else
+        return multiply_as<ELEM, OUT>(plan_product(A.M, A.N, A.steps, A.grid_max), A, stream);
 }
+
+// A checked product's kernel arguments (without tiles).
+void product_args(Args &A, const Product &P, int elem, hipStream_t stream);
 
 } // namespace mxg

@@ -46,15 +46,31 @@ template <class C, int ELEM> struct RingTile {
     const uint8_t *a, *b, *as, *bs;              // rows m0 / n0
     uint32_t code[C::LPW];                       // lane offsets of the code rows
     uint32_t sc[RingOp<C, ELEM>::SPW];           // and of the scale dwords
+    const uint8_t *b2;                           // gated: row n0 of the up rows
+    const uint8_t *lane_sc[RingOp<C, ELEM>::SPW]; // gated: each lane's scale dwords
 };
+
+// First stage row of wave w's code instruction t.  Gated: every wave moves the
+// same number of A, gate and up rows, so that t alone says which.
+template <class C, bool GATED> __device__ __forceinline__ int ring_row(int w, int t)
+{
+    constexpr int NA = C::BM / 8 / C::NW, NB = C::BN / 16 / C::NW;
+    if constexpr (!GATED)
+        return 8 * (w * C::LPW + t);
+    return t < NA        ? 8 * (w * NA + t)
+           : t < NA + NB ? C::BM + 8 * (w * NB + t - NA)
+                         : C::BM + C::BN / 2 + 8 * (w * NB + t - NA - NB);
+}
 
 // Wave w moves code rows 8 LPW w .. of the stage (A's BM rows, then B's):
 // per instruction 8 rows x 128 bytes, lane l filling slot l % 8 of row l / 8
 // with source chunk (l % 8) ^ (l / 8).  Scale instruction u moves the scale
 // bytes of 256 / SB stage rows; with fewer instructions than waves, several
 // waves move the same bytes, so that every wave counts L loads per step.
-// Rows past M or N read the last row: their results are never stored.
-template <class C, int ELEM>
+// Rows past M or N read the last row: their results are never stored.  Gated:
+// the second half of B's rows are up rows, and the scale loads, whose rows'
+// operand depends on the wave, take whole addresses.
+template <class C, int ELEM, bool GATED>
 __device__ __forceinline__ RingTile<C, ELEM> ring_tile(const Args &A, int64_t m0, int64_t n0, int w,
                                                        int l)
 {
@@ -66,51 +82,75 @@ __device__ __forceinline__ RingTile<C, ELEM> ring_tile(const Args &A, int64_t m0
     T.b = A.b + nb * A.rb;
     T.as = A.as + mb * A.rs;
     T.bs = A.bs + nb * A.rs;
+    if constexpr (GATED)
+        T.b2 = T.b + A.N * A.rb;
+    auto brow = [](int r) { return GATED ? (r - C::BM) % (C::BN / 2) : r - C::BM; };
     const int rr = l >> 3, ch = (l & 7) ^ rr;
 #pragma unroll
     for (int t = 0; t < C::LPW; ++t) {
-        const int r = 8 * (w * C::LPW + t); // wave-uniform first stage row
+        const int r = ring_row<C, GATED>(w, t); // wave-uniform first stage row
         const int64_t off = r < C::BM ? min(m0 + r + rr, A.M - 1) - mb
-                                      : min(n0 + (r - C::BM) + rr, A.N - 1) - nb;
+                                      : min(n0 + brow(r) + rr, A.N - 1) - nb;
         T.code[t] = (uint32_t)(off * A.rb) + 16 * ch;
     }
 #pragma unroll
     for (int t = 0; t < O::SPW; ++t) {
         const int r = ((w * O::SPW + t) % O::SINSTR) * O::SROWS;
         const int64_t off = r < C::BM ? min(m0 + r + l / DW, A.M - 1) - mb
-                                      : min(n0 + (r - C::BM) + l / DW, A.N - 1) - nb;
-        T.sc[t] = (uint32_t)(off * A.rs) + 4 * (l % DW);
+                                      : min(n0 + brow(r) + l / DW, A.N - 1) - nb;
+        if constexpr (GATED) {
+            const int64_t up = r >= C::BM + C::BN / 2 ? A.N : 0;
+            T.lane_sc[t] = (r < C::BM ? A.as + (mb + off) * A.rs : A.bs + (nb + up + off) * A.rs) +
+                           4 * (l % DW);
+        } else {
+            T.sc[t] = (uint32_t)(off * A.rs) + 4 * (l % DW);
+        }
     }
     return T;
 }
 
-template <class C, int ELEM>
+template <class C, int ELEM, bool GATED>
 __device__ __forceinline__ void ring_issue(const RingTile<C, ELEM> &T, int s, uint32_t stage, int w)
 {
     using O = RingOp<C, ELEM>;
     const uint32_t kc = (uint32_t)s * KB, ks = (uint32_t)s * O::SB;
 #pragma unroll
     for (int t = 0; t < C::LPW; ++t) {
-        const int r = 8 * (w * C::LPW + t);
-        lds_load16(r < C::BM ? T.a : T.b, T.code[t] + kc, stage + r * KB);
+        const int r = ring_row<C, GATED>(w, t);
+        if constexpr (GATED) {
+            constexpr int NA = C::BM / 8 / C::NW, NB = C::BN / 16 / C::NW;
+            lds_load16(t < NA ? T.a : t < NA + NB ? T.b : T.b2, T.code[t] + kc, stage + r * KB);
+        } else {
+            lds_load16(r < C::BM ? T.a : T.b, T.code[t] + kc, stage + r * KB);
+        }
     }
 #pragma unroll
     for (int t = 0; t < O::SPW; ++t) {
         const int r = ((w * O::SPW + t) % O::SINSTR) * O::SROWS;
-        lds_load4(r < C::BM ? T.as : T.bs, T.sc[t] + ks, stage + (C::BM + C::BN) * KB + r * O::SB);
+        const uint32_t to = stage + (C::BM + C::BN) * KB + r * O::SB;
+        if constexpr (GATED)
+            lds_load4(T.lane_sc[t] + ks, to);
+        else
+            lds_load4(r < C::BM ? T.as : T.bs, T.sc[t] + ks, to);
     }
 }
 
 // Tiles first, first + stride, ... of the launch on this workgroup.
 template <int ELEM, int OUT, class C>
-__device__ __forceinline__ void ring_tiles(const Args &A, LDS_AS uint8_t *st0, int first, int stride)
+__device__ __forceinline__ void ring_tiles(const ArgsOf<OUT> &A, LDS_AS uint8_t *st0, int first,
+                                           int stride)
 {
     using O = RingOp<C, ELEM>;
+    constexpr bool GATED = kGated<OUT>;
+    constexpr int CN = kCols<OUT>(C::BN); // output columns of a tile
+    static_assert(!GATED || ((C::BN / 2) % O::SROWS == 0 && (C::BN / 16) % C::NW == 0 &&
+                             (C::BM / 8) % C::NW == 0),
+                  "an instruction covers one half of B, a wave as many of each");
     const int tid = threadIdx.x;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l = tid & 63;
     const int g = l >> 4, qd = l & 15;
-    const int wm = (w % C::WM) * (C::BM / C::WM), wn = (w / C::WM) * (C::BN / C::WN);
+    const int wm = (w % C::WM) * (C::BM / C::WM), wn = (w / C::WM) * (CN / C::WN);
 
     const uint32_t st0_addr = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)st0);
     const FragBase ba = frag_base<ELEM>(0, (C::BM + C::BN) * KB, wm, qd, g);
@@ -123,20 +163,20 @@ __device__ __forceinline__ void ring_tiles(const Args &A, LDS_AS uint8_t *st0, i
     int iv = first, is = 0, islot = 0, ahead = -1;
     RingTile<C, ELEM> T;
     int64_t im, in;
-    tile_of(A, C::BM, C::BN, iv, im, in);
-    T = ring_tile<C, ELEM>(A, im, in, w, l);
+    tile_of(A, C::BM, CN, iv, im, in);
+    T = ring_tile<C, ELEM, GATED>(A, im, in, w, l);
     auto issue = [&] {
         if (iv >= G)
             return;
-        ring_issue<C, ELEM>(T, is, st0_addr + islot * O::STAGE, w);
+        ring_issue<C, ELEM, GATED>(T, is, st0_addr + islot * O::STAGE, w);
         islot = islot + 1 == C::S ? 0 : islot + 1;
         ++ahead;
         if (++is == A.steps) {
             is = 0;
             iv += stride;
             if (iv < G) {
-                tile_of(A, C::BM, C::BN, iv, im, in);
-                T = ring_tile<C, ELEM>(A, im, in, w, l);
+                tile_of(A, C::BM, CN, iv, im, in);
+                T = ring_tile<C, ELEM, GATED>(A, im, in, w, l);
             }
         }
     };
@@ -147,7 +187,7 @@ __device__ __forceinline__ void ring_tiles(const Args &A, LDS_AS uint8_t *st0, i
     int slot = 0;
     for (int v = first; v < G; v += stride) {
         int64_t m0, n0;
-        tile_of(A, C::BM, C::BN, v, m0, n0);
+        tile_of(A, C::BM, CN, v, m0, n0);
         v4f acc[C::FM][C::FN];
 #pragma unroll
         for (int j = 0; j < C::FM; ++j)
@@ -160,8 +200,8 @@ __device__ __forceinline__ void ring_tiles(const Args &A, LDS_AS uint8_t *st0, i
             issue();
             const LDS_AS uint8_t *st = st0 + slot * O::STAGE;
             Frag fa[C::FM], fb[C::FN];
-            read_frags<ELEM, C::FN>(fb, st, bb, std::make_integer_sequence<int, C::FN>{});
-            read_frags<ELEM, C::FM>(fa, st, ba, std::make_integer_sequence<int, C::FM>{});
+            read_frags<ELEM, GATED ? CN : 0>(fb, st, bb, std::make_integer_sequence<int, C::FN>{});
+            read_frags<ELEM, 0>(fa, st, ba, std::make_integer_sequence<int, C::FM>{});
 #pragma unroll
             for (int j = 0; j < C::FM; ++j)
                 mma_column<ELEM, C::FN>(acc[j], fb, fa[j]);
@@ -174,12 +214,15 @@ __device__ __forceinline__ void ring_tiles(const Args &A, LDS_AS uint8_t *st0, i
 #pragma unroll
             for (int i = 0; i < C::FN; ++i)
                 at[i][j] = acc[j][i];
-        store_tile<OUT, C::FM, C::FN>(A, at, m0, n0, wm, wn, g, qd);
+        if constexpr (GATED)
+            store_gated<ELEM, OUT, C::FM, C::FN>(A, at, m0, n0, wm, wn, g, qd);
+        else
+            store_tile<OUT, C::FM, C::FN>(A, at, m0, n0, wm, wn, g, qd);
     }
 }
 
 template <int ELEM, int OUT, class C>
-__global__ void __launch_bounds__(C::NT) mx_gemm_ring_kernel(Args A)
+__global__ void __launch_bounds__(C::NT) mx_gemm_ring_kernel(ArgsOf<OUT> A)
 {
     __shared__ __attribute__((aligned(16))) uint8_t lds[C::S * RingOp<C, ELEM>::STAGE];
     ring_tiles<ELEM, OUT, C>(A, (LDS_AS uint8_t *)lds, blockIdx.x, gridDim.x);
@@ -211,7 +254,7 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ring_pair_kernel(RingPair W)
     }
 }
 
-template <int ELEM, int OUT, class C> hipError_t launch_ring(const Args &A, hipStream_t stream)
+template <int ELEM, int OUT, class C> hipError_t launch_ring(const ArgsOf<OUT> &A, hipStream_t stream)
 {
     using O = RingOp<C, ELEM>;
     const int per_cu = std::min((160 * 1024) / (C::S * O::STAGE), 2048 / C::NT);

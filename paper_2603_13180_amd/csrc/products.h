@@ -34,6 +34,17 @@ struct Product {
 // mx_matmul_fwd's checks.
 mx_status check_product(const Product &P, int block, int elem, int out_dtype);
 
+// mx_gated_fwd's arguments and checks.
+struct GatedProduct {
+    const uint8_t *a, *as, *w, *ws;
+    int64_t M, F, K;
+    int act, mode, out_dtype;
+    void *out;
+    uint8_t *out_scales;
+    void *gu;
+};
+mx_status check_gated(const GatedProduct &P, int block, int elem);
+
 // A product with float output and one with bf16 output that do not depend on
 // each other, on one stream: within mx_matmul_fwd's bound, in one launch or
 // two, so the sums may be taken in another order than by two mx_matmul_fwd calls.

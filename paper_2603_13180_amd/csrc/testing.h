@@ -41,6 +41,15 @@ mx_status mxt_matmul(const uint8_t *a_codes, const uint8_t *a_scales, const uint
                      const void *b_gain, int out_dtype, void *out, int shape, int whole, int units,
                      hipStream_t stream);
 
+// mxt_product_plan and mxt_matmul for mx_gated_fwd.  Tile shapes: 2 .. 6 above
+// (their columns half gate, half up rows) and 7 = 16 x 64 with K split.
+int mxt_gated_plan(int64_t M, int64_t F, int64_t K, int elem, int units, int *whole, int *tail,
+                   double *us);
+mx_status mxt_gated(const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *w_codes,
+                    const uint8_t *w_scales, int64_t M, int64_t F, int64_t K, int elem, int act,
+                    int scale_mode, int out_dtype, void *out, uint8_t *out_scales, void *gu,
+                    int shape, int whole, int units, hipStream_t stream);
+
 // One product of mxt_matmul_pair, as the arguments of mx_matmul_fwd.
 typedef struct MxtProduct {
     const uint8_t *a, *as, *b, *bs;

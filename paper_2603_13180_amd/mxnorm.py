@@ -18,6 +18,9 @@ MX_OK, MX_EINVAL, MX_EUNSUPPORTED, MX_EHIP = 0, 1, 2, 3
 SCALE_MODES = {"rceil": 0, "floor": 1}
 OUT_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 ELEMS = {"e4m3": 0, "e2m1": 1}
+ACTS = {"silu": 0, "gelu_tanh": 1}
+# the gated product's outputs; torch.uint8 stands for MX codes with their scales
+GATED_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.uint8: 2}
 ABI_VERSION = 1
 MAX_D = 32768
 
@@ -63,6 +66,10 @@ def load():
         "mxnorm_linear_fwd_workspace_bytes": (ctypes.c_size_t, [I64, I64, I, I]),
         "mxnorm_linear_fwd": (I, [P, I64, I64, P, P, I64, I, I, I, F, F, I, I, P, P, P,
                                   ctypes.c_size_t, P]),
+        "mx_gated_fwd": (I, [P, P, P, P, I64, I64, I64, I, I, I, I, I, P, P, P, P]),
+        "mxnorm_gated_fwd_workspace_bytes": (ctypes.c_size_t, [I64, I64, I, I]),
+        "mxnorm_gated_fwd": (I, [P, I64, I64, P, P, I64, I, I, I, F, F, I, I, I, P, P, P, P, P,
+                                 ctypes.c_size_t, P]),
         "mxnorm_linear_bwd_workspace_bytes": (ctypes.c_size_t, [I64, I64, I64, I]),
         "mxnorm_linear_bwd": (I, [P, P, P, P, P, I64, I64, I64, I, I, I, P, P, P, P,
                                   ctypes.c_size_t, P]),
@@ -329,6 +336,85 @@ def mxnorm_linear_fwd(x, w_codes, w_scales, block=32, elem="e4m3", p=2, coef=0.0
                                  h.data_ptr(), rho.data_ptr(), ws.data_ptr(), ws_bytes,
                                  _stream(x.device)))
     return h, rho
+
+
+def _call(fn, device, *args):
+    """fn(*args, stream) with `device` current: a stream handle of 0 is the
+    current device's default stream."""
+    if torch._C._cuda_getDevice() == device.index:
+        status = fn(*args, _stream(device))
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, _stream(device))
+    _check(status)
+
+
+def _gated_outputs(T, F, elem, act, out_dtype, save_gu, device):
+    """(out, scales or None, gu or None) of a gated product."""
+    if elem not in ELEMS or act not in ACTS:
+        raise ValueError("elem must be 'e4m3' or 'e2m1', act 'silu' or 'gelu_tanh'")
+    if out_dtype not in GATED_DTYPES:
+        raise ValueError("out_dtype must be float32, bfloat16 or uint8 (MX codes)")
+    if out_dtype is torch.uint8:
+        out = torch.empty((T, F if elem == "e4m3" else F // 2), dtype=torch.uint8, device=device)
+        scales = torch.empty((T, F // 32), dtype=torch.uint8, device=device)
+    else:
+        out = torch.empty((T, F), dtype=out_dtype, device=device)
+        scales = None
+    gu = torch.empty((T, 2 * F), dtype=torch.bfloat16, device=device) if save_gu else None
+    return out, scales, gu
+
+
+def _gated_weight(w_codes, w_scales, K, block, elem, device):
+    """F of a gate and up weight [2F, K]."""
+    if elem not in ELEMS:
+        raise ValueError("elem must be 'e4m3' or 'e2m1'")
+    rows = _mx_operand(w_codes, w_scales, K, block, elem, "W")
+    if rows % 2 or w_codes.device != device or w_scales.device != device:
+        raise ValueError("W must have F gate rows and then F up rows, on the activations' device")
+    return rows // 2
+
+
+def mx_gated_fwd(a_codes, a_scales, w_codes, w_scales, K, block=32, elem="e4m3", act="silu",
+                 out_dtype=torch.bfloat16, scale_mode="rceil", save_gu=False):
+    """H = act(G) U with G and U the products of A [M, .] with the F gate and
+    the F up rows of W [2F, .], both MX codes and scales along K, in one kernel.
+    act: "silu" or "gelu_tanh".  out_dtype: float32, bfloat16, or uint8 for the
+    MX encoding of H along F in `elem`.  Returns (H, gu): H [M, F], or (codes,
+    scales) for uint8; gu bfloat16 [M, 2F], what the backward takes, or None."""
+    F = _gated_weight(w_codes, w_scales, K, block, elem, a_codes.device)
+    M = _mx_operand(a_codes, a_scales, K, block, elem, "A")
+    if a_scales.device != a_codes.device:
+        raise ValueError("A: codes and scales must be on one device")
+    mode = SCALE_MODES[scale_mode]
+    out, scales, gu = _gated_outputs(M, F, elem, act, out_dtype, save_gu, a_codes.device)
+    _call(load().mx_gated_fwd, a_codes.device, a_codes.data_ptr(), a_scales.data_ptr(),
+          w_codes.data_ptr(), w_scales.data_ptr(), M, F, K, block, ELEMS[elem], ACTS[act], mode,
+          GATED_DTYPES[out_dtype], out.data_ptr(), _ptr(scales), _ptr(gu))
+    return (out if scales is None else (out, scales)), gu
+
+
+def mxnorm_gated_fwd(x, w_codes, w_scales, block=32, elem="e4m3", p=2, coef=0.0, eps=1e-6,
+                     scale_mode="rceil", act="silu", out_dtype=torch.bfloat16, save_gu=False,
+                     want_rho=True):
+    """The gated feed-forward's first half: MXNorm of the activations x bf16
+    [T, d], then mx_gated_fwd with a weight [2F, d] cast once by mx_cast_fwd(W,
+    gamma).  Returns (H, gu, rho~) with H and gu as mx_gated_fwd's and rho~
+    float32 [T] or None.  With out_dtype=torch.uint8 the down projection is
+    mx_matmul_fwd(*H, down_codes, down_scales, F)."""
+    T, d = _input(x)
+    _mx_out_shapes(T, d, block, elem)
+    F = _gated_weight(w_codes, w_scales, d, block, elem, x.device)
+    mode = SCALE_MODES[scale_mode]
+    out, scales, gu = _gated_outputs(T, F, elem, act, out_dtype, save_gu, x.device)
+    rho = torch.empty((T,), dtype=torch.float32, device=x.device) if want_rho else None
+    lib, e = load(), ELEMS[elem]
+    ws_bytes = lib.mxnorm_gated_fwd_workspace_bytes(T, d, block, e)
+    ws = torch.empty((ws_bytes,), dtype=torch.uint8, device=x.device)
+    _call(lib.mxnorm_gated_fwd, x.device, x.data_ptr(), T, d, w_codes.data_ptr(),
+          w_scales.data_ptr(), F, block, e, p, coef, eps, mode, ACTS[act], GATED_DTYPES[out_dtype],
+          out.data_ptr(), _ptr(scales), _ptr(gu), _ptr(rho), ws.data_ptr(), ws_bytes)
+    return (out if scales is None else (out, scales)), gu, rho
 
 
 def mx_cast_t_fwd(x, rho=None, block=32, elem="e4m3", scale_mode="rceil", codes=None,

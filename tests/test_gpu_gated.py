@@ -1,0 +1,302 @@
+"""The gated feed-forward's first half on the GPU: every kernel that computes
+it, its three kinds of output, and the entry points.
+
+The products themselves are mx_matmul_fwd's, which other tests hold to the
+oracle; a gated kernel adds a tile's sums over K in the same order as the plain
+kernel of its shape.  So the float products of the plain kernel are the ones the
+gate sees, and:
+
+* the kept products are those, rounded to bf16, bit for bit;
+* float H is act(G) U of those in 64 bits within the error of the activation and
+  of two products.  With |z| <= 100, the exponential's argument -z log2(e) is
+  rounded at most four times (GELU: g^2, the polynomial, its product with g, and
+  the constants), 100 * 4 * 2^-24 < 2^-15; exp2 and the reciprocal are within a
+  unit, 2^-23, the sum and both products within 2^-24 each.  Where the
+  exponential overflows (z < -88) H is 0 against |H| < 2^-126 |G U|.  Together
+  2^-14 |H| + 2^-120 |G U|;
+* bf16 H is the float H rounded, MX codes are the oracle's cast of the float H,
+  both bit for bit (one kernel, one order of sums).
+"""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from launch_rules import ELEM, SHAPES, matmul_as
+from paper_2603_13180_amd import mxnorm, synth
+from test_gpu_gemm import dev_u8, random_operand
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+ELEMS = ["e4m3", "e2m1"]
+ACTS = ["silu", "gelu_tanh"]
+GATED_SHAPES = SHAPES[2:] + ["k16x64"]
+NUMBER = {s: i for i, s in enumerate(SHAPES + ["k16x64"])}
+# the plain kernel that adds in the same order
+SAME_ORDER = {"k16x64": "k32x64", "k32x64": "k32x64", "k64x64": "k64x64", "r64x128": "r64x128",
+              "r128x128": "r128x128", "t256x256": "t256x256"}
+# (tile shape, 256 x 256 cells before it, compute units; 0: the device's)
+WAYS = [(s, 0, 0) for s in GATED_SHAPES] + \
+    [(s, 0, u) for s in ("r64x128", "r128x128", "t256x256") for u in (1, 2)] + \
+    [(s, 2, 1) for s in GATED_SHAPES if s != "t256x256"]
+_I, _L, _P = ctypes.c_int, ctypes.c_int64, ctypes.c_void_p
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        raise RuntimeError("GPU gated tests need a GPU (run them with -m gpu on an MI355X)")
+    mxnorm.load()
+
+
+def guarded(shape, dtype):
+    """A tensor of `shape` at the start of a buffer of sevens."""
+    n = int(np.prod(shape))
+    buf = torch.full((n + 4096,), 7, dtype=dtype, device=DEV)
+    return buf, buf[:n].view(shape)
+
+
+def gated_as(ac, as_, wc, ws, K, elem, act, dtype, shape, whole=0, units=0, mode="rceil", keep=True):
+    """mx_gated_fwd by the named kernel: (H or (codes, scales), gu), each with
+    nothing written behind it."""
+    M, F = ac.shape[0], wc.shape[0] // 2
+    codes = dtype is torch.uint8
+    bo, out = guarded((M, F // 2 if codes and elem == "e2m1" else F), dtype)
+    bs, sc = guarded((M, F // 32), torch.uint8)
+    bg, gu = guarded((M, 2 * F), torch.bfloat16)
+    f = mxnorm.load().mxt_gated
+    f.restype, f.argtypes = _I, [_P] * 4 + [_L] * 3 + [_I] * 4 + [_P] * 3 + [_I] * 3 + [_P]
+    mxnorm._check(f(ac.data_ptr(), as_.data_ptr(), wc.data_ptr(), ws.data_ptr(), M, F, K, ELEM[elem],
+                    mxnorm.ACTS[act], mxnorm.SCALE_MODES[mode], mxnorm.GATED_DTYPES[dtype],
+                    out.data_ptr(), sc.data_ptr() if codes else None, gu.data_ptr() if keep else None,
+                    NUMBER[shape], whole, units, mxnorm._stream(ac.device)))
+    assert (bo[out.numel():] == 7).all() and (bg[gu.numel():] == 7).all()
+    assert (bs[sc.numel() if codes else 0:] == 7).all()
+    if not keep:
+        assert (gu == 7).all()
+    return ((out, sc) if codes else out), gu
+
+
+def operands(elem, M, F, K, seed=0, amin=117, amax=130, wmin=117, wmax=130):
+    rng = np.random.default_rng(seed + M + 3 * F + 5 * K + len(elem))
+    ac, as_ = random_operand(M, K, elem, rng, amin, amax)
+    wc, ws = random_operand(2 * F, K, elem, rng, wmin, wmax)
+    return [dev_u8(v) for v in (ac, as_, wc, ws)]
+
+
+def bits(t):
+    return t.contiguous().view(torch.int16 if t.element_size() == 2 else torch.int32)
+
+
+def act64(g, act):
+    """act(g) in 64 bits, g >= -700 or so beyond which it is 0."""
+    z = g if act == "silu" else 2 * np.sqrt(2 / np.pi) * (g + 0.044715 * g ** 3)
+    with np.errstate(over="ignore"):
+        return g / (1 + np.exp(-z))
+
+
+def check_float(h, products, act):
+    g, u = np.split(products.cpu().numpy().astype(np.float64), 2, axis=1)
+    with np.errstate(invalid="ignore", over="ignore"):
+        want = act64(g, act) * u
+        err = np.abs(h.cpu().numpy().astype(np.float64) - want)
+        bad = ~(err <= 2.0 ** -14 * np.abs(want) + 2.0 ** -120 * np.abs(g * u))
+    assert not bad.any(), "%d outputs off, first %s: %r, want %r" % (
+        bad.sum(), np.argwhere(bad)[0], h[tuple(np.argwhere(bad)[0])].item(), want[tuple(np.argwhere(bad)[0])])
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("elem", ELEMS)
+@pytest.mark.parametrize("shape,whole,units", WAYS)
+def test_every_kernel(elem, shape, whole, units, act):
+    # 300 x 416: two row cells, four column cells of 128, the last of each
+    # partial.  The operands' scales spread G over about +-20
+    M, F, K = 300, 416, 512
+    t = operands(elem, M, F, K)
+    h, gu = gated_as(*t, K, elem, act, torch.float32, shape, whole, units)
+    if not whole:
+        assert torch.equal(bits(gu), bits(matmul_as(*t, K, elem, SAME_ORDER[shape], out_dtype=torch.bfloat16)))
+        check_float(h, matmul_as(*t, K, elem, SAME_ORDER[shape]), act)
+    else:
+        # two kernels: rows and columns of the first cells in one order, the
+        # rest in another; float sums differ in their last bits
+        p = matmul_as(*t, K, elem, "t256x256").double()
+        g, u = p.split(F, 1)
+        want = torch.from_numpy(act64(g.cpu().numpy(), act)).to(DEV) * u
+        assert (h.double() - want).norm() <= 1e-4 * want.norm()
+        assert (gu.double() - p).norm() <= 2.0 ** -8 * p.norm()
+    hb, _ = gated_as(*t, K, elem, act, torch.bfloat16, shape, whole, units, keep=False)
+    assert torch.equal(bits(hb), bits(h.to(torch.bfloat16)))
+    for mode in ("rceil", "floor"):
+        (c, s), gm = gated_as(*t, K, elem, act, torch.uint8, shape, whole, units, mode)
+        wc, ws = oracle.mxcast(h.cpu().numpy(), elem=elem, mode=mode)
+        assert np.array_equal(s.cpu().numpy(), ws) and np.array_equal(c.cpu().numpy(), wc)
+        assert torch.equal(bits(gm), bits(gu))
+
+
+@pytest.mark.parametrize("elem", ELEMS)
+@pytest.mark.parametrize("M,F,K", [(1, 16, 256), (1, 32, 256), (17, 48, 512), (64, 32, 1024), (65, 80, 256),
+                                   (257, 144, 256), (3, 4112, 256)])
+@pytest.mark.parametrize("shape", GATED_SHAPES)
+def test_edges_of_tiles(elem, shape, M, F, K):
+    t = operands(elem, M, F, K, seed=7)
+    h, gu = gated_as(*t, K, elem, "silu", torch.float32, shape)
+    assert torch.equal(bits(gu), bits(matmul_as(*t, K, elem, SAME_ORDER[shape], out_dtype=torch.bfloat16)))
+    check_float(h, matmul_as(*t, K, elem, SAME_ORDER[shape]), "silu")
+    hb, _ = gated_as(*t, K, elem, "silu", torch.bfloat16, shape)
+    assert torch.equal(bits(hb), bits(h.to(torch.bfloat16)))
+    if F % 32 == 0:
+        (c, s), _ = gated_as(*t, K, elem, "silu", torch.uint8, shape)
+        wc, ws = oracle.mxcast(h.cpu().numpy(), elem=elem)
+        assert np.array_equal(s.cpu().numpy(), ws) and np.array_equal(c.cpu().numpy(), wc)
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("elem", ELEMS)
+@pytest.mark.parametrize("shape", ["k32x64", "r64x128", "t256x256"])
+def test_wide_ranges_and_non_finite_values(elem, shape, act):
+    # gate products from below the exponential's range to beyond it, rows of
+    # NaN, sums that overflow to infinity
+    M, F, K = 70, 64, 256
+    ac, as_, wc, ws = operands(elem, M, F, K, seed=3, amin=100, amax=150, wmin=110, wmax=135)
+    as_[5] = 0xFF
+    as_[9] = 254
+    ws[40, 3] = 0xFF                       # gate column 40
+    ws[F + 50, :] = 254                    # up column 50
+    t = [ac, as_, wc, ws]
+    p = matmul_as(*t, K, elem, SAME_ORDER[shape]).cpu().numpy().astype(np.float64)
+    g, u = np.split(p, 2, axis=1)
+    h, _ = gated_as(*t, K, elem, act, torch.float32, shape)
+    got = h.cpu().numpy().astype(np.float64)
+    assert np.isnan(got[5]).all() and np.isnan(got[:, 40]).all()
+    with np.errstate(all="ignore"):
+        a = act64(g, act)
+        a[np.isneginf(g)] = np.nan         # -inf times 0
+        want = (a.astype(np.float32) * u.astype(np.float32)).astype(np.float64)
+        # where act(G) U is 0 * inf only after the activation has underflowed
+        # the formula's value is anything between: those are left out
+        tiny = np.isinf(u) & (np.abs(a) < 2.0 ** -100)
+        exact = a * u
+        ok = (np.isnan(got) & np.isnan(want)) | (got == want) | \
+            (np.abs(got - exact) <= 2.0 ** -14 * np.abs(exact) + 2.0 ** -100 * np.abs(g * u)) | \
+            (np.isinf(got) & (np.abs(exact) > 3.4e38)) | tiny
+    assert ok.all(), "%d off, first %s" % ((~ok).sum(), np.argwhere(~ok)[0])
+    for mode in ("rceil", "floor"):
+        (c, s), _ = gated_as(*t, K, elem, act, torch.uint8, shape, mode=mode)
+        wc_, ws_ = oracle.mxcast(h.cpu().numpy(), elem=elem, mode=mode)
+        s, c = s.cpu().numpy(), c.cpu().numpy()
+        assert np.array_equal(s, ws_)
+        nan = np.repeat(ws_ == 0xFF, 32 if elem == "e4m3" else 16, axis=1)
+        # a NaN's sign is the hardware's: in NaN blocks the magnitudes count
+        mag = 0x7F if elem == "e4m3" else 0x77
+        assert np.array_equal(c[~nan], wc_[~nan]) and (c[nan] & mag == mag).all() and nan.any()
+
+
+# ------------------------------------------------------------ entry points --
+
+def planned(M, F, K, elem):
+    whole, tail, us = _I(), _I(), ctypes.c_double()
+    f = mxnorm.load().mxt_gated_plan
+    f.restype, f.argtypes = _I, [_L] * 3 + [_I] * 2 + [_P] * 3
+    s = f(M, F, K, ELEM[elem], torch.cuda.get_device_properties(0).multi_processor_count,
+          ctypes.byref(whole), ctypes.byref(tail), ctypes.byref(us))
+    names = SHAPES + ["k16x64"]
+    return (names[tail.value], whole.value) if whole.value else (names[s], 0)
+
+
+def same(a, b):
+    if isinstance(a, tuple):
+        return all(same(x, y) for x, y in zip(a, b))
+    return torch.equal(bits(a) if a.is_floating_point() else a, bits(b) if b.is_floating_point() else b)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.uint8])
+@pytest.mark.parametrize("elem", ELEMS)
+@pytest.mark.parametrize("M,F,K", [(1, 512, 512), (61, 2048, 512), (1000, 2048, 768), (2304, 4224, 256)])
+def test_entry_point_runs_its_plan(elem, dtype, M, F, K):
+    t = operands(elem, M, F, K, seed=1)
+    shape, whole = planned(M, F, K, elem)
+    for keep in (False, True):
+        h, gu = mxnorm.mx_gated_fwd(*t, K, elem=elem, act="gelu_tanh", out_dtype=dtype, save_gu=keep)
+        want, wgu = gated_as(*t, K, elem, "gelu_tanh", dtype, shape, whole)
+        assert same(h, want) and (same(gu, wgu) if keep else gu is None)
+
+
+@pytest.mark.parametrize("elem", ELEMS)
+@pytest.mark.parametrize("T,d,F", [(1, 256, 32), (33, 512, 96), (1000, 1024, 1056)])
+def test_norm_and_gate_as_one_call(elem, T, d, F):
+    x = torch.from_numpy(synth.gaussian(T, d, seed=T, scale=2.0).view(np.int16)).to(DEV).view(torch.bfloat16)
+    gen = torch.Generator(device=DEV).manual_seed(d)
+    w = (0.05 * torch.randn(2 * F, d, generator=gen, device=DEV)).bfloat16()
+    wc, ws = mxnorm.mx_cast_fwd(w, elem=elem)
+    for p, mode in ((2, "rceil"), (1, "floor")):
+        ac, as_, rho = mxnorm.mxnorm_mx_fwd(x, elem=elem, p=p, scale_mode=mode)
+        for dtype in (torch.float32, torch.bfloat16, torch.uint8):
+            h, gu, r = mxnorm.mxnorm_gated_fwd(x, wc, ws, elem=elem, p=p, scale_mode=mode, out_dtype=dtype,
+                                               save_gu=True)
+            want, wgu = mxnorm.mx_gated_fwd(ac, as_, wc, ws, d, elem=elem, scale_mode=mode, out_dtype=dtype,
+                                            save_gu=True)
+            assert same(h, want) and same(gu, wgu) and same(r, rho)
+    h, gu, r = mxnorm.mxnorm_gated_fwd(x, wc, ws, elem=elem, want_rho=False)
+    assert gu is None and r is None and h.dtype == torch.bfloat16
+
+
+def test_no_rows_and_no_columns():
+    wc, ws = torch.zeros(64, 256, dtype=torch.uint8, device=DEV), torch.zeros(64, 8, dtype=torch.uint8, device=DEV)
+    h, gu = mxnorm.mx_gated_fwd(wc[:0], ws[:0], wc, ws, 256, save_gu=True)
+    assert h.shape == (0, 32) and gu.shape == (0, 64)
+    h, gu = mxnorm.mx_gated_fwd(wc, ws, wc[:0], ws[:0], 256)
+    assert h.shape == (64, 0)
+    x = torch.empty(0, 256, dtype=torch.bfloat16, device=DEV)
+    (c, s), _, rho = mxnorm.mxnorm_gated_fwd(x, wc, ws, out_dtype=torch.uint8)
+    assert c.shape == (0, 32) and s.shape == (0, 1) and rho.shape == (0,)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.uint8])
+def test_another_stream_and_a_captured_graph(dtype):
+    T, d, F = 130, 512, 256
+    x = torch.randn(T, d, device=DEV).bfloat16()
+    wc, ws = mxnorm.mx_cast_fwd((0.05 * torch.randn(2 * F, d, device=DEV)).bfloat16())
+    want = mxnorm.mxnorm_gated_fwd(x, wc, ws, out_dtype=dtype, save_gu=True)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = mxnorm.mxnorm_gated_fwd(x, wc, ws, out_dtype=dtype, save_gu=True)
+    torch.cuda.current_stream().wait_stream(s)
+    assert same(got, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = mxnorm.mxnorm_gated_fwd(x, wc, ws, out_dtype=dtype, save_gu=True)
+    for seed in range(3):
+        x.copy_(torch.randn(T, d, device=DEV, generator=torch.Generator(device=DEV).manual_seed(seed)))
+        graph.replay()
+        want = mxnorm.mxnorm_gated_fwd(x, wc, ws, out_dtype=dtype, save_gu=True)
+        torch.cuda.synchronize()
+        assert same(out, want)
+
+
+def test_feed_forward_forward():
+    """Norm, gate, down projection as a user chains them, against the oracle's
+    steps in 64 bits: the casts' half steps dominate (2^-4 of an element for x
+    and H each, weights are given as codes), random over the sums."""
+    T, d, F = 50, 512, 768
+    xb = synth.gaussian(T, d, seed=11, scale=1.0)
+    x = torch.from_numpy(xb.view(np.int16)).to(DEV).view(torch.bfloat16)
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    w = (0.1 * torch.randn(2 * F, d, generator=gen, device=DEV)).bfloat16()
+    wd = (0.1 * torch.randn(d, F, generator=gen, device=DEV)).bfloat16()
+    wc, ws = mxnorm.mx_cast_fwd(w)
+    dc, ds = mxnorm.mx_cast_fwd(wd)
+    (hc, hs), _, _ = mxnorm.mxnorm_gated_fwd(x, wc, ws, out_dtype=torch.uint8)
+    y = mxnorm.mx_matmul_fwd(hc, hs, dc, ds, F)
+    a = oracle.mxnorm_mx(xb)
+    gu = oracle.mx_matmul(a[0], a[1], wc.cpu().numpy(), ws.cpu().numpy(), d)
+    h = act64(gu[:, :F], "silu") * gu[:, F:]
+    oc, os_ = oracle.mxcast(h.astype(np.float32))
+    want = oracle.mx_matmul(oc, os_, dc.cpu().numpy(), ds.cpu().numpy(), F)
+    # H before its cast is within the products' 2^-9 of sum |a b|; a code then
+    # differs by at most one step, 2^-3 of the element, in few places
+    err = np.linalg.norm(y.cpu().numpy() - want) / np.linalg.norm(want)
+    assert err <= 2.0 ** -8, err
