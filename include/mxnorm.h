@@ -376,6 +376,66 @@ mx_status mxnorm_gated_fwd(const void *x, int64_t T, int64_t d, const uint8_t *w
                            size_t workspace_bytes, hipStream_t stream);
 
 /*
+ * A tensor of heads [T, heads, D]: bf16, element (t, h, e) at data[t token_stride
+ * + h head_stride + e] (strides in elements, multiples of 8; a stride of a
+ * dimension of size 1 is not used), data 16-byte aligned.  So the queries and
+ * keys of a fused projection's output are read where they are.  Inputs may have
+ * strides of 0; the heads of an output must not share elements.
+ */
+typedef struct {
+    void *data;
+    int64_t heads, token_stride, head_stride;
+} mx_heads;
+
+/*
+ * RMSNorm of every query and key head, with a gain, and the rotation of its
+ * first R elements by its token's position, in one pass.  Per head x of D
+ * elements:
+ *   r = ((1/D) sum x^2 + eps)^(-1/2);   n = RN(RN(x r) gamma);
+ *   for the pairs i = 0 .. R/2 - 1 of n, (a, b) = (n_i, n_(i + R/2)), or
+ *   (n_2i, n_(2i+1)) if interleaved:  t = pos[token] inv_freq[i],
+ *   y_a = a cos t - b sin t,  y_b = b cos t + a sin t;
+ *   elements from R on: y = n.
+ * r comes from a double sum, is formed in double and rounded once to float (a
+ * zero or infinite radicand gives 0); the angle is formed in double turns and
+ * its fraction rounded to float, so far and negative positions keep their
+ * angles (to 2^-23 of a turn up to |pos inv_freq| of 2^29); the rest is float,
+ * rounded once to bf16.
+ * q_gamma, k_gamma: bf16 [D] or NULL (= 1), 16-byte aligned.  pos: int64 [T]
+ * or NULL (0, 1, ...).  inv_freq: float [R/2].  q and k may have different
+ * numbers of heads, or none; q_out and k_out have those of q and k, and may be
+ * q and k themselves (data and strides), but not overlap them otherwise.
+ * D a multiple of 8 (at most 512, else MX_EUNSUPPORTED), R a multiple of 16
+ * from 0 to D; at most 65536 heads each.  T == 0 is a no-op.
+ */
+mx_status qk_norm_rope_fwd(const mx_heads *q, const mx_heads *k, const void *q_gamma,
+                           const void *k_gamma, int64_t T, int64_t D, int64_t R,
+                           const int64_t *pos, const float *inv_freq, int interleaved, float eps,
+                           const mx_heads *q_out, const mx_heads *k_out, hipStream_t stream);
+
+/*
+ * Its gradients from those of q_out and k_out, q and k as the forward took
+ * them.  Per head, with m the gradient turned back by the angles and v = gamma
+ * m:  u = sum_e v_e x_e (in double);  grad_x = RN(RN(r v) - RN(c x)), c = r^3 u /
+ * D in double rounded to float;  grad_gamma_e = sum over the tokens and heads of
+ * RN(RN(x r) m), in float within a workgroup's heads (at most 1024 workgroups),
+ * then in double, in a fixed order: the same call gives the same bits.
+ * grad_q, grad_k: bf16; each may be the incoming gradient itself (data and
+ * strides).  grad_q_gamma, grad_k_gamma: float [D] or NULL (not computed); with
+ * no tokens or heads they are 0.  They need `workspace`, caller-owned device
+ * memory of qk_norm_rope_bwd_workspace_bytes(T, D) bytes, 16-byte aligned,
+ * overwritten.
+ */
+size_t qk_norm_rope_bwd_workspace_bytes(int64_t T, int64_t D);
+mx_status qk_norm_rope_bwd(const mx_heads *grad_q_out, const mx_heads *grad_k_out,
+                           const mx_heads *q, const mx_heads *k, const void *q_gamma,
+                           const void *k_gamma, int64_t T, int64_t D, int64_t R,
+                           const int64_t *pos, const float *inv_freq, int interleaved, float eps,
+                           const mx_heads *grad_q, const mx_heads *grad_k, float *grad_q_gamma,
+                           float *grad_k_gamma, void *workspace, size_t workspace_bytes,
+                           hipStream_t stream);
+
+/*
  * Default NVFP4 tensor decode scales: an output bound divided by 6 * 448, so
  * the bound maps to the largest E2M1 x E4M3 magnitude.  MXNorm: Lemma 2's
  * bound K^(1/p) / coef (K = d / block; coef <= 0 selects the table value);

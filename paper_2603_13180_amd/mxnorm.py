@@ -73,6 +73,10 @@ def load():
         "mxnorm_linear_bwd_workspace_bytes": (ctypes.c_size_t, [I64, I64, I64, I]),
         "mxnorm_linear_bwd": (I, [P, P, P, P, P, I64, I64, I64, I, I, I, P, P, P, P,
                                   ctypes.c_size_t, P]),
+        "qk_norm_rope_fwd": (I, [P, P, P, P, I64, I64, I64, P, P, I, F, P, P, P]),
+        "qk_norm_rope_bwd_workspace_bytes": (ctypes.c_size_t, [I64, I64]),
+        "qk_norm_rope_bwd": (I, [P, P, P, P, P, P, I64, I64, I64, P, P, I, F, P, P, P, P, P,
+                                 ctypes.c_size_t, P]),
         "mxnorm_default_global_scale": (F, [I64, I, I, F]),
         "rmsnorm_default_global_scale": (F, [I64, F]),
         "mxnorm_coef": (F, [I, I]),
@@ -539,6 +543,93 @@ def mxnorm_linear_bwd(grad_h, x, rho, gamma, w, block=32, elem="e4m3",
                                  grad_x.data_ptr(), grad_gamma.data_ptr(), grad_w.data_ptr(),
                                  ws.data_ptr(), ws_bytes, _stream(x.device)))
     return grad_x, grad_gamma, grad_w
+
+
+class _Heads(ctypes.Structure):
+    """mx_heads of include/mxnorm.h."""
+    _fields_ = [("data", ctypes.c_void_p), ("heads", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+def _heads(t, name, like=None):
+    """A tensor of heads [T, H, D] by its strides; shaped as `like` if given."""
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16 or t.dim() != 3:
+        raise TypeError("%s must be a 3-D torch.bfloat16 tensor [T, heads, D]" % name)
+    if not t.is_cuda:
+        raise RuntimeError("%s must be on the GPU: libmxnorm has no CPU path" % name)
+    if like is not None and (t.shape != like.shape or t.device != like.device):
+        raise ValueError("%s must have the shape and device of its input" % name)
+    st, sh, se = t.stride()
+    if se != 1 and t.shape[2] > 1:
+        raise ValueError("%s: the elements of a head must be contiguous" % name)
+    return _Heads(t.data_ptr(), t.shape[1], st, sh)
+
+
+def _rope_arguments(q, k, q_gamma, k_gamma, pos, inv_freq, rotary):
+    """(T, D, R) of a call on queries q and keys k, its vectors checked."""
+    T, _, D = q.shape
+    if k.shape[0] != T or k.shape[2] != D or k.device != q.device:
+        raise ValueError("q and k must have the same tokens, head size and device")
+    for g, name in ((q_gamma, "q_gamma"), (k_gamma, "k_gamma")):
+        if g is not None and (g.dtype != torch.bfloat16 or g.shape != (D,) or g.device != q.device
+                              or not g.is_contiguous()):
+            raise ValueError("%s must be a contiguous bfloat16 [D] tensor on q's device" % name)
+    R = D if rotary is None else rotary
+    if pos is not None and (pos.dtype != torch.int64 or pos.shape != (T,) or pos.device != q.device
+                            or not pos.is_contiguous()):
+        raise ValueError("pos must be a contiguous int64 [T] tensor on q's device")
+    if R and (inv_freq is None or inv_freq.dtype != torch.float32 or inv_freq.shape != (R // 2,)
+              or inv_freq.device != q.device or not inv_freq.is_contiguous()):
+        raise ValueError("inv_freq must be a contiguous float32 [rotary / 2] tensor on q's device")
+    return T, D, R
+
+
+def qk_norm_rope_fwd(q, k, q_gamma, k_gamma, pos, inv_freq, rotary=None, interleaved=False, eps=1e-6,
+                     q_out=None, k_out=None):
+    """RMSNorm of every head of q [T, Hq, D] and k [T, Hk, D] with its gain (bf16
+    [D] or None) and the rotation of its first `rotary` (None: all) elements by
+    pos [T] (int64; None: 0, 1, ...) times inv_freq [rotary / 2] (float32), pairs
+    (i, i + rotary / 2) or, interleaved, (2i, 2i + 1).  q and k may be views of
+    a fused projection's output; q_out and k_out views of any buffer, q and k
+    themselves among them.  Returns (q_out, k_out)."""
+    dq, dk = _heads(q, "q"), _heads(k, "k")
+    T, D, R = _rope_arguments(q, k, q_gamma, k_gamma, pos, inv_freq, rotary)
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    if k_out is None:
+        k_out = torch.empty(k.shape, dtype=torch.bfloat16, device=q.device)
+    oq, ok = _heads(q_out, "q_out", q), _heads(k_out, "k_out", k)
+    ref = ctypes.byref
+    _call(load().qk_norm_rope_fwd, q.device, ref(dq), ref(dk), _ptr(q_gamma), _ptr(k_gamma), T, D, R,
+          _ptr(pos), _ptr(inv_freq), int(bool(interleaved)), eps, ref(oq), ref(ok))
+    return q_out, k_out
+
+
+def qk_norm_rope_bwd(grad_q_out, grad_k_out, q, k, q_gamma, k_gamma, pos, inv_freq, rotary=None,
+                     interleaved=False, eps=1e-6, grad_q=None, grad_k=None, want_grad_gamma=True):
+    """The gradients of qk_norm_rope_fwd, q and k as it took them: (grad_q,
+    grad_k, grad_q_gamma, grad_k_gamma).  grad_q and grad_k may be views of the
+    fused projection's gradient, or the incoming gradients themselves; the gain
+    gradients are float32 [D], None without a gain or with want_grad_gamma =
+    False."""
+    dq, dk = _heads(q, "q"), _heads(k, "k")
+    T, D, R = _rope_arguments(q, k, q_gamma, k_gamma, pos, inv_freq, rotary)
+    gq, gk = _heads(grad_q_out, "grad_q_out", q), _heads(grad_k_out, "grad_k_out", k)
+    if grad_q is None:
+        grad_q = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    if grad_k is None:
+        grad_k = torch.empty(k.shape, dtype=torch.bfloat16, device=q.device)
+    oq, ok = _heads(grad_q, "grad_q", q), _heads(grad_k, "grad_k", k)
+    lib = load()
+    gg = [torch.empty((D,), dtype=torch.float32, device=q.device)
+          if want_grad_gamma and g is not None else None for g in (q_gamma, k_gamma)]
+    ws_bytes = lib.qk_norm_rope_bwd_workspace_bytes(T, D) if gg[0] is not None or gg[1] is not None else 0
+    ws = torch.empty((ws_bytes,), dtype=torch.uint8, device=q.device) if ws_bytes else None
+    ref = ctypes.byref
+    _call(lib.qk_norm_rope_bwd, q.device, ref(gq), ref(gk), ref(dq), ref(dk), _ptr(q_gamma),
+          _ptr(k_gamma), T, D, R, _ptr(pos), _ptr(inv_freq), int(bool(interleaved)), eps, ref(oq),
+          ref(ok), _ptr(gg[0]), _ptr(gg[1]), _ptr(ws), ws_bytes)
+    return grad_q, grad_k, gg[0], gg[1]
 
 
 def mxnorm_default_global_scale(d, block=16, p=2, coef=0.0):
