@@ -376,6 +376,42 @@ mx_status mxnorm_gated_fwd(const void *x, int64_t T, int64_t d, const uint8_t *w
                            size_t workspace_bytes, hipStream_t stream);
 
 /*
+ * The gradients of both projections of mx_gated_fwd from that of H: with g, u
+ * the kept products (gu, bf16 [T, 2F]) and grad_h bf16 [T, F],
+ *   grad_gu[:, :F] = RN16(grad_h u act'(g)),  grad_gu[:, F:] = RN16(grad_h act(g)),
+ * computed in float; act'(g) = sigma + g sigma (1 - sigma) z'(g) where act(g) = g
+ * sigma(z(g)).  grad_gu: bf16 [T, 2F]; it may be gu itself.  F a multiple of 8 and
+ * at most MX_MATMUL_MAX_N / 2; all three 16-byte aligned.  T == 0 or F == 0 is a
+ * no-op.
+ */
+mx_status mx_gated_bwd(const void *grad_h, const void *gu, int64_t T, int64_t F, int act,
+                       void *grad_gu, hipStream_t stream);
+
+/*
+ * The backward of mxnorm_gated_fwd as one call: the projections' gradient
+ * grad_P = grad_gu of mx_gated_bwd [T, 2F], then with W [2F, d]
+ *   grad_Z = MXCast(grad_P) MXCast_2F(W)                      (bf16)
+ *   grad_X, grad_gamma = mxnorm_ste_bwd(X, grad_Z, gamma, rho~)
+ *   grad_W = (MXCast(grad_P^T) MXCast(rho~ X)^T) . gamma
+ * grad_h: bf16 [T, F]; gu: bf16 [T, 2F] and rho: float [T] as the forward gave
+ * them; x: bf16 [T, d]; gamma: bf16 [d] or NULL; w: bf16 [2F, d], before its
+ * cast.  grad_x [T, d] in out_dtype; grad_gamma [d] (or NULL) and grad_w [2F, d]
+ * in grad_dtype.  Codes, scales and products as in mxnorm_linear_bwd; the casts
+ * along T are of T rows followed by zeros, so T is any number of tokens.
+ * block: 32; F a multiple of 64 (E4M3) or 128 (E2M1), d of 16 and at most
+ * MXNORM_MAX_D; T and 2F at most MX_MATMUL_MAX_K (else MX_EUNSUPPORTED).  T, F
+ * and d must be positive.  Alignment as in mxnorm_linear_bwd, all checks before
+ * the first launch.  `workspace`: caller-owned device memory of
+ * mxnorm_gated_bwd_workspace_bytes() bytes, 256-byte aligned, overwritten.
+ */
+size_t mxnorm_gated_bwd_workspace_bytes(int64_t T, int64_t F, int64_t d, int elem);
+mx_status mxnorm_gated_bwd(const void *grad_h, const void *gu, const void *x, const float *rho,
+                           const void *gamma, const void *w, int64_t T, int64_t F, int64_t d,
+                           int block, int elem, int act, int out_dtype, int grad_dtype,
+                           void *grad_x, void *grad_gamma, void *grad_w, void *workspace,
+                           size_t workspace_bytes, hipStream_t stream);
+
+/*
  * A tensor of heads [T, heads, D]: bf16, element (t, h, e) at data[t token_stride
  * + h head_stride + e] (strides in elements, multiples of 8; a stride of a
  * dimension of size 1 is not used), data 16-byte aligned.  So the queries and

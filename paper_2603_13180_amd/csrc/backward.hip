@@ -56,6 +56,7 @@ struct CastTArgs {
     uint8_t *codes;
     uint8_t *scales;
     int64_t R, C;
+    int64_t rows;    // rows that x has: the others, up to R, are zeros
     int64_t tile_r0; // row tile of blockIdx.y == 0 (launches of at most 65535 row tiles)
     int mode;
     int order;       // tile visiting order, see cast_t_kernel
@@ -186,7 +187,7 @@ __device__ __forceinline__ void fetch_tile(const CastTArgs &A, int64_t r0, int64
     const int ch = tid % S::CPR, rbase = tid / S::CPR;
     const uint32_t chunk_off = c0 + 8 * ch < A.C ? 16u * (uint32_t)ch : kOutside; // C % 8 == 0
     const uint32_t pitch = (uint32_t)A.C * 2u;
-    const uint32_t rows = (uint32_t)max((int64_t)0, min((int64_t)CT_ROWS, A.R - r0));
+    const uint32_t rows = (uint32_t)max((int64_t)0, min((int64_t)CT_ROWS, A.rows - r0));
     const __amdgpu_buffer_rsrc_t xr = buffer_rsrc(A.x + r0 * A.C + c0, rows * pitch);
 #pragma unroll
     for (int k = 0; k < S::NLD; ++k) {
@@ -323,6 +324,45 @@ __global__ void __launch_bounds__(NTH) cast_t_kernel(CastTArgs A)
 // lanes one row's 256 or 128.  The four blocks of 16 lanes gather their scale
 // bytes by two rotations and store them as one dword.  RCEIL scales (no clamp
 // is needed before the conversion); C a multiple of 128.
+template <bool FP4>
+__device__ __forceinline__ void cast_row_chunk(uint8_t *codes, uint8_t *scales, int64_t C, int64_t r,
+                                               int64_t c, bool in, int tid, const uint4 v)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    const float a = __uint_as_float(block_max<4>(chunk_absmax_bits(v)) << 16);
+    const uint32_t byte = e8m0_byte<FP4>(a, MX_SCALE_RCEIL);
+    const float scale = __uint_as_float(byte << 23);
+    if constexpr (!FP4) {
+        uint32_t lo = e4m3x4_hw(bf16_lo(w[0]), bf16_hi(w[0]), bf16_lo(w[1]), bf16_hi(w[1]), scale);
+        uint32_t hi = e4m3x4_hw(bf16_lo(w[2]), bf16_hi(w[2]), bf16_lo(w[3]), bf16_hi(w[3]), scale);
+        if (__builtin_amdgcn_ballot_w64(byte == 0xFFu)) { // rare: non-finite input
+            if (byte == 0xFFu) {
+                lo = nan_codes_e4m3(w[0], w[1]);
+                hi = nan_codes_e4m3(w[2], w[3]);
+            }
+        }
+        if (in)
+            *reinterpret_cast<uint2 *>(codes + r * C + c) = make_uint2(lo, hi);
+    } else {
+        uint32_t q = 0;
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, bf16_lo(w[0]), bf16_hi(w[0]), scale, 0);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, bf16_lo(w[1]), bf16_hi(w[1]), scale, 1);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, bf16_lo(w[2]), bf16_hi(w[2]), scale, 2);
+        q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, bf16_lo(w[3]), bf16_hi(w[3]), scale, 3);
+        if (__builtin_amdgcn_ballot_w64(byte == 0xFFu)) {
+            if (byte == 0xFFu)
+                q = 0x77777777u | sign_nibbles(v);
+        }
+        if (in)
+            *reinterpret_cast<uint32_t *>(codes + (r * C + c) / 2) = q;
+    }
+    uint32_t b4 = byte << (8 * ((tid >> 2) & 3));
+    b4 |= dpp_mov<0x124>(b4); // row_ror:4
+    b4 |= dpp_mov<0x128>(b4); // row_ror:8
+    if (in && (tid & 15) == 0)
+        *reinterpret_cast<uint32_t *>(scales + r * (C / 32) + c / 32) = b4;
+}
+
 template <bool FP4, int COLS, int NTH>
 __device__ __forceinline__ void cast_rows(const CastTArgs &A, uint8_t *codes, uint8_t *scales,
                                           int64_t r0, int64_t c0, int tid,
@@ -334,41 +374,7 @@ __device__ __forceinline__ void cast_rows(const CastTArgs &A, uint8_t *codes, ui
 #pragma unroll
     for (int k = 0; k < S::NLD; ++k) {
         const int64_t r = r0 + rbase + S::RPP * k;
-        const uint4 v = L.v[k];
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-        const float a = __uint_as_float(block_max<4>(chunk_absmax_bits(v)) << 16);
-        const uint32_t byte = e8m0_byte<FP4>(a, MX_SCALE_RCEIL);
-        const float scale = __uint_as_float(byte << 23);
-        const bool in = r < A.R && c < A.C;
-        if constexpr (!FP4) {
-            uint32_t lo = e4m3x4_hw(bf16_lo(w[0]), bf16_hi(w[0]), bf16_lo(w[1]), bf16_hi(w[1]), scale);
-            uint32_t hi = e4m3x4_hw(bf16_lo(w[2]), bf16_hi(w[2]), bf16_lo(w[3]), bf16_hi(w[3]), scale);
-            if (__builtin_amdgcn_ballot_w64(byte == 0xFFu)) { // rare: non-finite input
-                if (byte == 0xFFu) {
-                    lo = nan_codes_e4m3(w[0], w[1]);
-                    hi = nan_codes_e4m3(w[2], w[3]);
-                }
-            }
-            if (in)
-                *reinterpret_cast<uint2 *>(codes + r * A.C + c) = make_uint2(lo, hi);
-        } else {
-            uint32_t q = 0;
-            q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, bf16_lo(w[0]), bf16_hi(w[0]), scale, 0);
-            q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, bf16_lo(w[1]), bf16_hi(w[1]), scale, 1);
-            q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, bf16_lo(w[2]), bf16_hi(w[2]), scale, 2);
-            q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, bf16_lo(w[3]), bf16_hi(w[3]), scale, 3);
-            if (__builtin_amdgcn_ballot_w64(byte == 0xFFu)) {
-                if (byte == 0xFFu)
-                    q = 0x77777777u | sign_nibbles(v);
-            }
-            if (in)
-                *reinterpret_cast<uint32_t *>(codes + (r * A.C + c) / 2) = q;
-        }
-        uint32_t b4 = byte << (8 * ((tid >> 2) & 3));
-        b4 |= dpp_mov<0x124>(b4); // row_ror:4
-        b4 |= dpp_mov<0x128>(b4); // row_ror:8
-        if (in && (tid & 15) == 0)
-            *reinterpret_cast<uint32_t *>(scales + r * (A.C / 32) + c / 32) = b4;
+        cast_row_chunk<FP4>(codes, scales, A.C, r, c, r < A.rows && c < A.C, tid, L.v[k]);
     }
 }
 
@@ -697,7 +703,7 @@ ste_bwd_kernel(SteArgs A)
 }
 
 // grad_gamma[j] = RN(sum of the P partial rows, in double, in a fixed
-// order), in one launch.  Block b (1024 threads) sums columns [64 b, +64):
+// order), in one launch (bf16: rounded to float and then to bf16).  Block b (1024 threads) sums columns [64 b, +64):
 // thread (g, q), g = 0 .. 63, q = 0 .. 15, adds rows g, g + 64, g + 128, ...
 // of columns 64 b + 4 q .. +3 in order, 16 bytes per row, so every thread has
 // several loads in flight; the 64 row groups' sums are then added in order
@@ -705,8 +711,9 @@ ste_bwd_kernel(SteArgs A)
 // sum of the slices, took about 10 us at [32768, 4096]; 256 threads with
 // 4-byte loads per column were latency-bound.)
 constexpr int GG_GROUPS = 64;
+template <int OUT>
 __global__ void __launch_bounds__(1024) ggamma_reduce_kernel(const float *part, int64_t P, int d,
-                                                             float *out)
+                                                             void *out)
 {
     __shared__ double red[GG_GROUPS][64];
     const int q = threadIdx.x & 15, g = threadIdx.x >> 4;
@@ -732,7 +739,11 @@ __global__ void __launch_bounds__(1024) ggamma_reduce_kernel(const float *part, 
         double t = 0.0;
         for (int i = 0; i < GG_GROUPS; ++i)
             t += red[i][c];
-        out[blockIdx.x * 64 + c] = (float)t;
+        const int j = blockIdx.x * 64 + c;
+        if constexpr (OUT == MX_OUT_F32)
+            static_cast<float *>(out)[j] = (float)t;
+        else
+            static_cast<uint16_t *>(out)[j] = f32_to_bf16((float)t);
     }
 }
 
@@ -911,7 +922,7 @@ mx_status mx_cast_t_fwd(const void *x, const float *rho, int64_t R, int64_t C, i
     A.rho = rho;
     A.codes = codes;
     A.scales = scales;
-    A.R = R;
+    A.R = A.rows = R;
     A.C = C;
     A.mode = scale_mode;
     // one 128 x 256 tile per workgroup (see the kernel), at most 65535 row
@@ -952,34 +963,8 @@ mx_status mxnorm_ste_bwd(const void *x, const void *grad_z, const void *gamma, c
                                         workspace, workspace_bytes);
     if (ok != MX_OK || T == 0)
         return ok;
-    mxb::SteArgs A;
-    A.x = static_cast<const uint16_t *>(x);
-    A.gz = static_cast<const uint16_t *>(grad_z);
-    A.gamma = static_cast<const uint16_t *>(gamma);
-    A.rho = rho;
-    A.gx = grad_x;
-    A.part = grad_gamma ? static_cast<float *>(workspace) : nullptr;
-    A.T = T;
-    A.rpw = mxb::ste_rpw(T);
-    A.d = (int)d;
-    A.nc = (int)(d / 8);
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    hipError_t e;
-    if (out_dtype == MX_OUT_F32)
-        e = gamma ? mxb::launch_ste_out<MX_OUT_F32, true>(A, st)
-                  : mxb::launch_ste_out<MX_OUT_F32, false>(A, st);
-    else
-        e = gamma ? mxb::launch_ste_out<MX_OUT_BF16, true>(A, st)
-                  : mxb::launch_ste_out<MX_OUT_BF16, false>(A, st);
-    if (e == hipSuccess && grad_gamma) {
-        hipLaunchKernelGGL(mxb::ggamma_reduce_kernel, dim3((unsigned)((d + 63) / 64)), dim3(1024), 0,
-                           st, static_cast<const float *>(workspace), ste_workgroups(T), (int)d,
-                           grad_gamma);
-        e = hipGetLastError();
-    }
-    if (e != hipSuccess)
-        return mxk::fail(MX_EHIP, "kernel launch failed: %s", hipGetErrorString(e));
-    return MX_OK;
+    return mxb::ste(x, grad_z, gamma, rho, T, d, out_dtype, grad_x, MX_OUT_F32, grad_gamma, workspace,
+                    stream);
 }
 
 size_t mxnorm_ste_bwd_noalloc_max_workspace(void) { return kScratchBytes; }
@@ -1011,12 +996,50 @@ mx_status mxnorm_ste_bwd_noalloc(const void *x, const void *grad_z, const void *
 
 namespace mxb {
 
+mx_status ste(const void *x, const void *grad_z, const void *gamma, const float *rho, int64_t T,
+              int64_t d, int out_dtype, void *grad_x, int gamma_dtype, void *grad_gamma,
+              void *workspace, hipStream_t stream)
+{
+    SteArgs A;
+    A.x = static_cast<const uint16_t *>(x);
+    A.gz = static_cast<const uint16_t *>(grad_z);
+    A.gamma = static_cast<const uint16_t *>(gamma);
+    A.rho = rho;
+    A.gx = grad_x;
+    A.part = grad_gamma ? static_cast<float *>(workspace) : nullptr;
+    A.T = T;
+    A.rpw = ste_rpw(T);
+    A.d = (int)d;
+    A.nc = (int)(d / 8);
+    hipStream_t st = stream;
+    hipError_t e;
+    if (out_dtype == MX_OUT_F32)
+        e = gamma ? launch_ste_out<MX_OUT_F32, true>(A, st)
+                  : launch_ste_out<MX_OUT_F32, false>(A, st);
+    else
+        e = gamma ? launch_ste_out<MX_OUT_BF16, true>(A, st)
+                  : launch_ste_out<MX_OUT_BF16, false>(A, st);
+    if (e == hipSuccess && grad_gamma) {
+        const dim3 grid((unsigned)((d + 63) / 64));
+        if (gamma_dtype == MX_OUT_F32)
+            hipLaunchKernelGGL((ggamma_reduce_kernel<MX_OUT_F32>), grid, dim3(1024), 0, st, A.part,
+                               ste_workgroups(T), (int)d, grad_gamma);
+        else
+            hipLaunchKernelGGL((ggamma_reduce_kernel<MX_OUT_BF16>), grid, dim3(1024), 0, st, A.part,
+                               ste_workgroups(T), (int)d, grad_gamma);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess)
+        return mxk::fail(MX_EHIP, "kernel launch failed: %s", hipGetErrorString(e));
+    return MX_OK;
+}
+
 mx_status backward_casts(const void *grad_h, const void *x, const float *rho, const void *w,
-                         int64_t T, int64_t N, int64_t d, int elem, const BackwardCasts &o,
-                         hipStream_t stream)
+                         int64_t T, int64_t Tp, int64_t N, int64_t d, int elem,
+                         const BackwardCasts &o, hipStream_t stream)
 {
     CastJobs J;
-    auto job = [](const void *m, const float *r, int64_t R, int64_t C, uint8_t *codes,
+    auto job = [](const void *m, const float *r, int64_t rows, int64_t R, int64_t C, uint8_t *codes,
                   uint8_t *scales) {
         CastTArgs A;
         A.x = static_cast<const uint16_t *>(m);
@@ -1025,14 +1048,15 @@ mx_status backward_casts(const void *grad_h, const void *x, const float *rho, co
         A.scales = scales;
         A.R = R;
         A.C = C;
+        A.rows = rows;
         A.tile_r0 = 0;
         A.mode = MX_SCALE_RCEIL;
         A.order = cast_order(C);
         return A;
     };
-    J.job[0] = job(grad_h, nullptr, T, N, o.ght, o.ght_s);
-    J.job[1] = job(w, nullptr, N, d, o.wt, o.wt_s);
-    J.job[2] = job(x, rho, T, d, o.xt, o.xt_s);
+    J.job[0] = job(grad_h, nullptr, T, Tp, N, o.ght, o.ght_s);
+    J.job[1] = job(w, nullptr, N, N, d, o.wt, o.wt_s);
+    J.job[2] = job(x, rho, T, Tp, d, o.xt, o.xt_s);
     J.row_codes = o.gh;
     J.row_scales = o.gh_s;
     int64_t at = 0;

@@ -12,6 +12,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
+#include "gate.h"
 #include "mx_gemm_gated.h"
 #include "mx_gemm_plan.h"
 #include "mxnorm.h"
@@ -92,6 +95,47 @@ mx_status check_gated(const GatedProduct &P, int block, int elem)
     return MX_OK;
 }
 
+mx_status check_gated_bwd(const void *grad_h, const void *gu, int64_t T, int64_t F, int act,
+                          const void *grad_gu)
+{
+    if (T < 0 || F < 0)
+        return mxk::fail(MX_EINVAL, "T and F must be >= 0");
+    if (act != MX_ACT_SILU && act != MX_ACT_GELU_TANH)
+        return mxk::fail(MX_EINVAL, "act must be MX_ACT_SILU or MX_ACT_GELU_TANH");
+    if (F % 8 != 0)
+        return mxk::fail(MX_EINVAL, "F must be a multiple of 8");
+    if (T > INT32_MAX || F > MX_MATMUL_MAX_N / 2)
+        return mxk::fail(MX_EUNSUPPORTED, "matrix too large (F at most %d)", MX_MATMUL_MAX_N / 2);
+    if (T == 0 || F == 0)
+        return MX_OK;
+    if (!grad_h || !gu || !grad_gu)
+        return mxk::fail(MX_EINVAL, "grad_h, gu and grad_gu must be non-NULL");
+    if (!aligned(grad_h, 16) || !aligned(gu, 16) || !aligned(grad_gu, 16))
+        return mxk::fail(MX_EINVAL, "grad_h, gu and grad_gu must be 16-byte aligned");
+    return MX_OK;
+}
+
+// The gradients of both projections, bf16 [T, 2F] from grad_h [T, F] and the
+// kept products [T, 2F]: a lane takes 8 columns of a row.
+template <int ACT>
+__global__ void __launch_bounds__(256) gated_bwd_kernel(const uint16_t *gh, const uint16_t *gu,
+                                                        uint16_t *out, int64_t T, int64_t F)
+{
+    const int64_t per = F / 8, n = T * per;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t t = i / per, at = t * 2 * F + 8 * (i - t * per);
+        const uint4 h = mxk::load_stream(reinterpret_cast<const uint4 *>(gh) + i);
+        const uint4 g = mxk::load_stream(reinterpret_cast<const uint4 *>(gu + at));
+        const uint4 u = mxk::load_stream(reinterpret_cast<const uint4 *>(gu + at + F));
+        uint4 dg, du;
+        mxk::gate_gradients<ACT>(g, u, h, dg, du);
+        __builtin_nontemporal_store(mxk::u32x4_t{dg.x, dg.y, dg.z, dg.w},
+                                    reinterpret_cast<mxk::u32x4_t *>(out + at));
+        __builtin_nontemporal_store(mxk::u32x4_t{du.x, du.y, du.z, du.w},
+                                    reinterpret_cast<mxk::u32x4_t *>(out + at + F));
+    }
+}
+
 } // namespace mxg
 
 extern "C" {
@@ -112,6 +156,24 @@ mx_status mx_gated_fwd(const uint8_t *a_codes, const uint8_t *a_scales, const ui
     return launched(by_type(elem, out_dtype, [&](auto e, auto o) {
         return mxg::multiply<decltype(e)::value, decltype(o)::value>(A, stream);
     }));
+}
+
+mx_status mx_gated_bwd(const void *grad_h, const void *gu, int64_t T, int64_t F, int act,
+                       void *grad_gu, hipStream_t stream)
+{
+    mxk::clear_error();
+    const mx_status ok = mxg::check_gated_bwd(grad_h, gu, T, F, act, grad_gu);
+    if (ok != MX_OK || T == 0 || F == 0)
+        return ok;
+    const unsigned grid = (unsigned)std::min<int64_t>((T * (F / 8) + 255) / 256, 1 << 20);
+    const auto *h = static_cast<const uint16_t *>(grad_h), *p = static_cast<const uint16_t *>(gu);
+    auto *o = static_cast<uint16_t *>(grad_gu);
+    if (act == MX_ACT_SILU)
+        hipLaunchKernelGGL((mxg::gated_bwd_kernel<MX_ACT_SILU>), dim3(grid), dim3(256), 0, stream, h, p, o, T, F);
+    else
+        hipLaunchKernelGGL((mxg::gated_bwd_kernel<MX_ACT_GELU_TANH>), dim3(grid), dim3(256), 0, stream, h, p, o,
+                           T, F);
+    return launched(hipGetLastError());
 }
 
 int mxt_gated_plan(int64_t M, int64_t F, int64_t K, int elem, int units, int *whole, int *tail,

@@ -49,21 +49,42 @@ struct FwdSpace {
 struct BwdSpace {
     uint8_t *gh, *gh_s, *wt, *wt_s, *ght, *ght_s, *xt, *xt_s, *gz, *ste;
     size_t ste_bytes, bytes;
-    BwdSpace(void *ws, int64_t T, int64_t N, int64_t d, int elem)
+    // Tp: the length of the casts along T
+    BwdSpace(void *ws, int64_t T, int64_t Tp, int64_t N, int64_t d, int elem)
     {
         Carver c{static_cast<uint8_t *>(ws)};
         gh = c.take(code_bytes(T, N, elem));
         gh_s = c.take((size_t)T * (size_t)(N / 32));
         wt = c.take(code_bytes(d, N, elem));
         wt_s = c.take((size_t)d * (size_t)(N / 32));
-        ght = c.take(code_bytes(N, T, elem));
-        ght_s = c.take((size_t)N * (size_t)(T / 32));
-        xt = c.take(code_bytes(d, T, elem));
-        xt_s = c.take((size_t)d * (size_t)(T / 32));
+        ght = c.take(code_bytes(N, Tp, elem));
+        ght_s = c.take((size_t)N * (size_t)(Tp / 32));
+        xt = c.take(code_bytes(d, Tp, elem));
+        xt_s = c.take((size_t)d * (size_t)(Tp / 32));
         gz = c.take((size_t)T * (size_t)d * 2);
         ste_bytes = mxnorm_ste_bwd_workspace_bytes(T, d);
         ste = c.take(ste_bytes);
         bytes = c.used;
+    }
+};
+
+// T rounded up to what a product contracts over
+int64_t padded(int64_t T, int elem)
+{
+    const int64_t step = elem == MX_ELEM_E2M1 ? 256 : 128;
+    return (T + step - 1) / step * step;
+}
+
+// The projections' gradient (bf16 [T, 2F]) and then the backward's space.
+struct GatedSpace {
+    uint8_t *gg;
+    size_t own;
+    BwdSpace b;
+    size_t bytes;
+    GatedSpace(void *ws, int64_t T, int64_t F, int64_t d, int elem)
+        : gg(static_cast<uint8_t *>(ws)), own(((size_t)T * (size_t)F * 4 + 255) & ~(size_t)255),
+          b(ws ? gg + own : nullptr, T, padded(T, elem), 2 * F, d, elem), bytes(own + b.bytes)
+    {
     }
 };
 
@@ -147,7 +168,7 @@ size_t mxnorm_linear_bwd_workspace_bytes(int64_t T, int64_t N, int64_t d, int el
 {
     if (T <= 0 || N <= 0 || d <= 0 || !known(elem))
         return 0;
-    return BwdSpace(nullptr, T, N, d, elem).bytes;
+    return BwdSpace(nullptr, T, T, N, d, elem).bytes;
 }
 
 mx_status mxnorm_linear_bwd(const void *grad_h, const void *x, const float *rho,
@@ -161,7 +182,7 @@ mx_status mxnorm_linear_bwd(const void *grad_h, const void *x, const float *rho,
                                    mxnorm_linear_bwd_workspace_bytes(T, N, d, elem));
     if (st != MX_OK)
         return st;
-    const BwdSpace s(workspace, T, N, d, elem);
+    const BwdSpace s(workspace, T, T, N, d, elem);
     const int mode = MX_SCALE_RCEIL;
     const mxg::Product gz{s.gh, s.gh_s, s.wt, s.wt_s, T, d, N, nullptr, s.gz};
     const mxg::Product gw{s.ght, s.ght_s, s.xt, s.xt_s, N, d, T, gamma, grad_w};
@@ -179,13 +200,63 @@ mx_status mxnorm_linear_bwd(const void *grad_h, const void *x, const float *rho,
     // grad_Z = MXCast(grad_H) MXCast_N(W), both blocked along N; grad_W =
     // (MXCast(grad_H^T) MXCast(rho~ X)^T) . gamma, blocked along T; then
     // grad_X and grad_gamma
-    if ((st = mxb::backward_casts(grad_h, x, rho, w, T, N, d, elem,
+    if ((st = mxb::backward_casts(grad_h, x, rho, w, T, T, N, d, elem,
                                   {s.gh, s.gh_s, s.ght, s.ght_s, s.wt, s.wt_s, s.xt, s.xt_s},
                                   stream)) != MX_OK ||
-        (st = mxg::matmul_pair(gw, gz, elem, stream)) != MX_OK)
+        (st = mxg::matmul_pair(gw, MX_OUT_F32, gz, elem, stream)) != MX_OK)
         return st;
     return mxnorm_ste_bwd(x, s.gz, gamma, rho, T, d, out_dtype, grad_x, grad_gamma, s.ste,
                           s.ste_bytes, stream);
+}
+
+size_t mxnorm_gated_bwd_workspace_bytes(int64_t T, int64_t F, int64_t d, int elem)
+{
+    if (T <= 0 || F <= 0 || d <= 0 || !known(elem))
+        return 0;
+    return GatedSpace(nullptr, T, F, d, elem).bytes;
+}
+
+mx_status mxnorm_gated_bwd(const void *grad_h, const void *gu, const void *x, const float *rho,
+                           const void *gamma, const void *w, int64_t T, int64_t F, int64_t d,
+                           int block, int elem, int act, int out_dtype, int grad_dtype, void *grad_x,
+                           void *grad_gamma, void *grad_w, void *workspace, size_t workspace_bytes,
+                           hipStream_t stream)
+{
+    mxk::clear_error();
+    if (T <= 0 || F <= 0 || d <= 0)
+        return mxk::fail(MX_EINVAL, "T, F and d must be positive");
+    if (T > MX_MATMUL_MAX_K || F > MX_MATMUL_MAX_K / 2)
+        return mxk::fail(MX_EUNSUPPORTED, "T or 2 F exceeds %d", MX_MATMUL_MAX_K);
+    if (elem != MX_ELEM_E4M3 && elem != MX_ELEM_E2M1)
+        return mxk::fail(MX_EINVAL, "elem must be MX_ELEM_E4M3 or MX_ELEM_E2M1");
+    if (F % (elem == MX_ELEM_E2M1 ? 128 : 64) != 0)
+        return mxk::fail(MX_EUNSUPPORTED, "F must be a multiple of 64 (E4M3) or 128 (E2M1)");
+    mx_status st = check_workspace(workspace, workspace_bytes,
+                                   mxnorm_gated_bwd_workspace_bytes(T, F, d, elem));
+    if (st != MX_OK)
+        return st;
+    const GatedSpace s(workspace, T, F, d, elem);
+    const int64_t N = 2 * F, Tp = padded(T, elem);
+    const mxg::Product gz{s.b.gh, s.b.gh_s, s.b.wt, s.b.wt_s, T, d, N, nullptr, s.b.gz};
+    const mxg::Product gw{s.b.ght, s.b.ght_s, s.b.xt, s.b.xt_s, N, d, Tp, gamma, grad_w};
+    // every check before the first launch
+    if ((st = mxg::check_gated_bwd(grad_h, gu, T, F, act, s.gg)) != MX_OK ||
+        (st = mxb::check_cast_t(w, nullptr, N, d, block, elem, MX_SCALE_RCEIL, s.b.wt, s.b.wt_s)) != MX_OK ||
+        (st = mxg::check_product(gz, block, elem, MX_OUT_BF16)) != MX_OK ||
+        (st = mxb::check_ste(x, s.b.gz, gamma, rho, T, d, out_dtype, grad_x,
+                             static_cast<float *>(grad_gamma), s.b.ste, s.b.ste_bytes)) != MX_OK ||
+        (st = mxb::check_cast_t(x, rho, Tp, d, block, elem, MX_SCALE_RCEIL, s.b.xt, s.b.xt_s)) != MX_OK ||
+        (st = mxg::check_product(gw, block, elem, grad_dtype)) != MX_OK)
+        return st;
+    if ((st = mx_gated_bwd(grad_h, gu, T, F, act, s.gg, stream)) != MX_OK ||
+        (st = mxb::backward_casts(s.gg, x, rho, w, T, Tp, N, d, elem,
+                                  {s.b.gh, s.b.gh_s, s.b.ght, s.b.ght_s, s.b.wt, s.b.wt_s, s.b.xt,
+                                   s.b.xt_s},
+                                  stream)) != MX_OK ||
+        (st = mxg::matmul_pair(gw, grad_dtype, gz, elem, stream)) != MX_OK)
+        return st;
+    return mxb::ste(x, s.b.gz, gamma, rho, T, d, out_dtype, grad_x, grad_dtype, grad_gamma, s.b.ste,
+                    stream);
 }
 
 } // extern "C"

@@ -38,7 +38,7 @@ namespace mxg {
 // us, 6144 x 4096 x 4096 with 4096 x 4096 x 6144 142 -> 130 us (E2M1) and 216
 // -> 199 us (E4M3).
 // Workgroup b is of class b >= split; a workgroup of class c takes n[c][0]
-// tiles of product 0 (float output), then n[c][1] of product 1 (bf16 output).
+// tiles of product 0 (output OUT0), then n[c][1] of product 1 (bf16 output).
 struct PairArgs {
     Args p[2];
     int split; // workgroups of class 0
@@ -57,7 +57,8 @@ __device__ __forceinline__ int pair_tile(const PairArgs &W, int i, int j, int b,
     return j < W.n[c][i] && v < W.p[i].cells ? v : -1;
 }
 
-template <int ELEM> __global__ void __launch_bounds__(NT) mx_gemm_pair_kernel(PairArgs W)
+template <int ELEM, int OUT0>
+__global__ void __launch_bounds__(NT) mx_gemm_pair_kernel(PairArgs W)
 {
     constexpr int SB = Op<ELEM>::SB;
     constexpr int STAGE = Op<ELEM>::STAGE;
@@ -109,8 +110,8 @@ template <int ELEM> __global__ void __launch_bounds__(NT) mx_gemm_pair_kernel(Pa
         const int steps = W.p[i].steps;
         for (int s = 0; s < steps; ++s, ++gs) {
             const int cur = gs & 1;
-            if (s == 0 && stores == kTileStores<MX_OUT_F32, FM, FN>)
-                wait_vmcnt<kTileStores<MX_OUT_F32, FM, FN>>();
+            if (s == 0 && stores == kTileStores<OUT0, FM, FN>)
+                wait_vmcnt<kTileStores<OUT0, FM, FN>>();
             else if (s == 0 && stores == kTileStores<MX_OUT_BF16, FM, FN>)
                 wait_vmcnt<kTileStores<MX_OUT_BF16, FM, FN>>();
             else
@@ -133,8 +134,8 @@ template <int ELEM> __global__ void __launch_bounds__(NT) mx_gemm_pair_kernel(Pa
         }
         const bool full = m0 + BM <= W.p[i].M && n0 + BN <= W.p[i].N;
         if (i == 0) {
-            store_tile<MX_OUT_F32, FM, FN>(W.p[0], acc, m0, n0, wm, wn, g, qd);
-            stores = full ? kTileStores<MX_OUT_F32, FM, FN> : 0;
+            store_tile<OUT0, FM, FN>(W.p[0], acc, m0, n0, wm, wn, g, qd);
+            stores = full ? kTileStores<OUT0, FM, FN> : 0;
         } else {
             store_tile<MX_OUT_BF16, FM, FN>(W.p[1], acc, m0, n0, wm, wn, g, qd);
             stores = full ? kTileStores<MX_OUT_BF16, FM, FN> : 0;
@@ -241,29 +242,29 @@ inline void plan_pair(PairPlan &P, const Args &A0, const Args &A1)
                                                             : PAIR_APART;
 }
 
-// Products 0 (float output) and 1 (bf16 output) on one stream.
-template <int ELEM>
+// Products 0 (output OUT0) and 1 (bf16 output) on one stream.
+template <int ELEM, int OUT0>
 hipError_t multiply_pair_as(const PairPlan &P, const Args &A0, const Args &A1, hipStream_t stream)
 {
     if (P.mode == PAIR_SMALL) {
-        hipLaunchKernelGGL((mx_gemm_ring_pair_kernel<ELEM, R64x128>),
+        hipLaunchKernelGGL((mx_gemm_ring_pair_kernel<ELEM, OUT0, R64x128>),
                            dim3((unsigned)(P.Q.n0 + P.Q.n1)), dim3(R64x128::NT), 0, stream, P.Q);
         return hipGetLastError();
     }
     if (P.mode == PAIR_LARGE) {
-        hipLaunchKernelGGL((mx_gemm_pair_kernel<ELEM>), dim3((unsigned)A0.grid_max), dim3(NT), 0,
+        hipLaunchKernelGGL((mx_gemm_pair_kernel<ELEM, OUT0>), dim3((unsigned)A0.grid_max), dim3(NT), 0,
                            stream, P.W);
         return hipGetLastError();
     }
     const hipError_t e = multiply<ELEM, MX_OUT_BF16>(A1, stream);
-    return e != hipSuccess ? e : multiply<ELEM, MX_OUT_F32>(A0, stream);
+    return e != hipSuccess ? e : multiply<ELEM, OUT0>(A0, stream);
 }
 
-template <int ELEM> hipError_t multiply_pair(const Args &A0, const Args &A1, hipStream_t stream)
+template <int ELEM, int OUT0> hipError_t multiply_pair(const Args &A0, const Args &A1, hipStream_t stream)
 {
     PairPlan P;
     plan_pair(P, A0, A1);
-    return multiply_pair_as<ELEM>(P, A0, A1, stream);
+    return multiply_pair_as<ELEM, OUT0>(P, A0, A1, stream);
 }
 
 } // namespace mxg
@@ -388,13 +389,19 @@ mx_status mx_matmul_fwd(const uint8_t *a_codes, const uint8_t *a_scales, const u
 
 namespace mxg {
 
-mx_status matmul_pair(const Product &f32, const Product &bf16, int elem, hipStream_t stream)
+mx_status matmul_pair(const Product &first, int out0, const Product &bf16, int elem,
+                      hipStream_t stream)
 {
     Args A0, A1;
-    product_args(A0, f32, elem, stream);
+    product_args(A0, first, elem, stream);
     product_args(A1, bf16, elem, stream);
-    const hipError_t e = elem == MX_ELEM_E4M3 ? multiply_pair<MX_ELEM_E4M3>(A0, A1, stream)
-                                              : multiply_pair<MX_ELEM_E2M1>(A0, A1, stream);
+    hipError_t e;
+    if (elem == MX_ELEM_E4M3)
+        e = out0 == MX_OUT_F32 ? multiply_pair<MX_ELEM_E4M3, MX_OUT_F32>(A0, A1, stream)
+                               : multiply_pair<MX_ELEM_E4M3, MX_OUT_BF16>(A0, A1, stream);
+    else
+        e = out0 == MX_OUT_F32 ? multiply_pair<MX_ELEM_E2M1, MX_OUT_F32>(A0, A1, stream)
+                               : multiply_pair<MX_ELEM_E2M1, MX_OUT_BF16>(A0, A1, stream);
     return e == hipSuccess ? MX_OK
                            : mxk::fail(MX_EHIP, "kernel launch failed: %s", hipGetErrorString(e));
 }
@@ -509,8 +516,8 @@ mx_status mxt_matmul_pair(const MxtProduct *f32, const MxtProduct *bf16, int ele
         return mxk::fail(MX_EINVAL, "no such pair launch");
     P.mode = mode;
     const hipError_t e = elem == MX_ELEM_E4M3
-                             ? mxg::multiply_pair_as<MX_ELEM_E4M3>(P, A0, A1, stream)
-                             : mxg::multiply_pair_as<MX_ELEM_E2M1>(P, A0, A1, stream);
+                             ? mxg::multiply_pair_as<MX_ELEM_E4M3, MX_OUT_F32>(P, A0, A1, stream)
+                             : mxg::multiply_pair_as<MX_ELEM_E2M1, MX_OUT_F32>(P, A0, A1, stream);
     return e == hipSuccess ? MX_OK
                            : mxk::fail(MX_EHIP, "kernel launch failed: %s", hipGetErrorString(e));
 }

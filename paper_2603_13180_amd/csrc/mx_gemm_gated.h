@@ -3,36 +3,17 @@
 // float, bf16 or MX codes, and the products themselves where a backward pass
 // will need them.
 //
-// act(g) = g sigma(z(g)) with z = g (SiLU) or 2 sqrt(2/pi) (g + 0.044715 g^3)
-// (GELU in its tanh form, since (1 + tanh y) / 2 = sigma(2 y)).
-//
 // In accumulator layout lane (g, qd) of tile i holds row qd, columns 16 i + 4 g
 // .. + 3, and a wave holds 32 output columns: the two tiles of a row are one MX
 // block over four lanes, so its absmax is two lane swaps away and nothing
 // passes through LDS.
 #pragma once
 
+#include "gate.h"
 #include "mx_gemm.h"
 #include "norm_cast.h"
 
 namespace mxg {
-
-// sigma(z(g)) from the hardware's exp2 and reciprocal, one unit in the last
-// place each: for |z| up to 20 the result is within 2^-19 of its value
-// relatively (the argument's rounding), far below a bf16 or MX rounding.  z
-// beyond the exponential's range gives exactly 0 or 1.
-template <int ACT> __device__ __forceinline__ float gate_sigma(float g)
-{
-    constexpr float kLog2e = 1.44269504f;
-    float t; // -z log2(e)
-    if constexpr (ACT == MX_ACT_SILU) {
-        t = g * -kLog2e;
-    } else {
-        constexpr float c = 1.5957691216f * kLog2e; // 2 sqrt(2/pi) log2(e)
-        t = g * __builtin_fmaf(g * g, -c * 0.044715f, -c);
-    }
-    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));
-}
 
 // The tiles v0, v1 of one row group as 32 bf16 columns: as in store_tile, lane
 // row g stores 8 adjacent columns of tile g & 1 from column 8 (g >> 1).
@@ -75,7 +56,7 @@ __device__ __forceinline__ uint32_t gated_rows(const GatedArgs &A, const v4f (&p
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            h[i][e] = p[i][e] * gate_sigma<ACT>(p[i][e]) * p[i + 2][e];
+            h[i][e] = p[i][e] * mxk::gate_sigma<ACT>(p[i][e]) * p[i + 2][e];
 
     if constexpr (O == MX_OUT_F32) {
         const __amdgpu_buffer_rsrc_t rs = rows_rsrc(A.out, mr * A.N * 4);

@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ring_kernel(ArgsOf<OUT> A)
 }
 
 // Two products whose tiles are all resident at once, one tile per workgroup:
-// product 0 (float output) in workgroups 0 .. n0 - 1 or, if product 1 (bf16)
+// product 0 (output OUT0) in workgroups 0 .. n0 - 1 or, if product 1 (bf16)
 // has the longer K, in those after product 1's.  Each alone leaves compute
 // units idle (1024 x 768 x 2304 has 96 tiles): both in one launch, 1024 x 768 x
 // 2304 and 2304 x 768 x 1024 (E4M3), 14.2 us against 16.2 apart.
@@ -239,7 +239,7 @@ struct RingPair {
     int second_first;
 };
 
-template <int ELEM, class C>
+template <int ELEM, int OUT0, class C>
 __global__ void __launch_bounds__(C::NT) mx_gemm_ring_pair_kernel(RingPair W)
 {
     __shared__ __attribute__((aligned(16))) uint8_t lds[C::S * RingOp<C, ELEM>::STAGE];
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ring_pair_kernel(RingPair W)
         ring_tiles<ELEM, MX_OUT_BF16, C>(W.p[1], (LDS_AS uint8_t *)lds, v, W.n1);
     } else {
         const int v = W.second_first ? b - W.n1 : b;
-        ring_tiles<ELEM, MX_OUT_F32, C>(W.p[0], (LDS_AS uint8_t *)lds, v, W.n0);
+        ring_tiles<ELEM, OUT0, C>(W.p[0], (LDS_AS uint8_t *)lds, v, W.n0);
     }
 }
 

@@ -44,11 +44,16 @@ struct GatedProduct {
     void *gu;
 };
 mx_status check_gated(const GatedProduct &P, int block, int elem);
+// mx_gated_bwd's checks.
+mx_status check_gated_bwd(const void *grad_h, const void *gu, int64_t T, int64_t F, int act,
+                          const void *grad_gu);
 
-// A product with float output and one with bf16 output that do not depend on
-// each other, on one stream: within mx_matmul_fwd's bound, in one launch or
-// two, so the sums may be taken in another order than by two mx_matmul_fwd calls.
-mx_status matmul_pair(const Product &f32, const Product &bf16, int elem, hipStream_t stream);
+// A product with output of type out0 and one with bf16 output that do not
+// depend on each other, on one stream: within mx_matmul_fwd's bound, in one
+// launch or two, so the sums may be taken in another order than by two
+// mx_matmul_fwd calls.
+mx_status matmul_pair(const Product &first, int out0, const Product &bf16, int elem,
+                      hipStream_t stream);
 
 } // namespace mxg
 
@@ -61,6 +66,11 @@ mx_status check_ste(const void *x, const void *grad_z, const void *gamma, const 
                     int64_t T, int64_t d, int out_dtype, const void *grad_x, const float *grad_gamma,
                     const void *workspace, size_t workspace_bytes);
 
+// mxnorm_ste_bwd after its checks, T > 0, with grad_gamma in gamma_dtype.
+mx_status ste(const void *x, const void *grad_z, const void *gamma, const float *rho, int64_t T,
+              int64_t d, int out_dtype, void *grad_x, int gamma_dtype, void *grad_gamma,
+              void *workspace, hipStream_t stream);
+
 // Codes and scales of the backward's casts, laid out as the entry points of
 // the single casts do (RCEIL, blocks of 32).
 struct BackwardCasts {
@@ -70,9 +80,10 @@ struct BackwardCasts {
     uint8_t *xt, *xt_s;   // (rho X)^T [d, T] along T
 };
 
-// T and N multiples of 128, d of 16; grad_h, x, w 16-byte aligned.
+// The casts along T are of T rows and then zeros up to Tp.  Tp and N multiples
+// of 128, d of 16; grad_h, x, w 16-byte aligned.
 mx_status backward_casts(const void *grad_h, const void *x, const float *rho, const void *w,
-                         int64_t T, int64_t N, int64_t d, int elem, const BackwardCasts &o,
-                         hipStream_t stream);
+                         int64_t T, int64_t Tp, int64_t N, int64_t d, int elem,
+                         const BackwardCasts &o, hipStream_t stream);
 
 } // namespace mxb

@@ -70,6 +70,10 @@ def load():
         "mxnorm_gated_fwd_workspace_bytes": (ctypes.c_size_t, [I64, I64, I, I]),
         "mxnorm_gated_fwd": (I, [P, I64, I64, P, P, I64, I, I, I, F, F, I, I, I, P, P, P, P, P,
                                  ctypes.c_size_t, P]),
+        "mx_gated_bwd": (I, [P, P, I64, I64, I, P, P]),
+        "mxnorm_gated_bwd_workspace_bytes": (ctypes.c_size_t, [I64, I64, I64, I]),
+        "mxnorm_gated_bwd": (I, [P, P, P, P, P, P, I64, I64, I64, I, I, I, I, I, P, P, P, P,
+                                 ctypes.c_size_t, P]),
         "mxnorm_linear_bwd_workspace_bytes": (ctypes.c_size_t, [I64, I64, I64, I]),
         "mxnorm_linear_bwd": (I, [P, P, P, P, P, I64, I64, I64, I, I, I, P, P, P, P,
                                   ctypes.c_size_t, P]),
@@ -419,6 +423,73 @@ def mxnorm_gated_fwd(x, w_codes, w_scales, block=32, elem="e4m3", p=2, coef=0.0,
           w_scales.data_ptr(), F, block, e, p, coef, eps, mode, ACTS[act], GATED_DTYPES[out_dtype],
           out.data_ptr(), _ptr(scales), _ptr(gu), _ptr(rho), ws.data_ptr(), ws_bytes)
     return (out if scales is None else (out, scales)), gu, rho
+
+
+def _gated_gradient(grad_h, gu, act):
+    """(T, F) of a gated product's gradient and kept products."""
+    T, F = _input(grad_h)
+    _input(gu)
+    if gu.shape != (T, 2 * F) or gu.device != grad_h.device:
+        raise ValueError("gu must be [T, 2F] for a grad_h [T, F], on its device")
+    if act not in ACTS:
+        raise ValueError("act must be 'silu' or 'gelu_tanh'")
+    return T, F
+
+
+def mx_gated_bwd(grad_h, gu, act="silu", grad_gu=None):
+    """The gradient of both projections of mx_gated_fwd: bfloat16 [T, 2F] (gate
+    columns, then up columns) from grad_h bfloat16 [T, F] and the forward's gu
+    [T, 2F], which grad_gu may be."""
+    T, F = _gated_gradient(grad_h, gu, act)
+    grad_gu = _out(grad_gu, (T, 2 * F), torch.bfloat16, grad_h.device)
+    _call(load().mx_gated_bwd, grad_h.device, grad_h.data_ptr(), gu.data_ptr(), T, F, ACTS[act],
+          grad_gu.data_ptr())
+    return grad_gu
+
+
+def mxnorm_gated_bwd(grad_h, gu, x, rho, gamma, w, block=32, elem="e4m3", act="silu",
+                     grad_x_dtype=torch.bfloat16, grad_dtype=torch.float32):
+    """The backward of mxnorm_gated_fwd, every product and cast in the library,
+    for any number of tokens:
+      grad_P = mx_gated_bwd(grad_h, gu)                 [T, 2F]
+      grad_Z = MXCast(grad_P) MXCast_2F(W)
+      grad_X, grad_gamma = STE(X, grad_Z, gamma, rho~)
+      grad_W = (MXCast(grad_P^T) MXCast(rho~ X)^T) . gamma
+    grad_h bf16 [T, F]; gu bf16 [T, 2F] and rho float32 [T] from the forward; x
+    bf16 [T, d]; gamma bf16 [d] or None; w bf16 [2F, d], before its cast.
+    Returns (grad_x, grad_gamma [d], grad_w [2F, d]), the last two in
+    grad_dtype (float32 or bfloat16)."""
+    T, F = _gated_gradient(grad_h, gu, act)
+    if _input(x)[0] != T:
+        raise ValueError("x must have grad_h's rows")
+    d = x.shape[1]
+    _input(w)
+    if w.shape != (2 * F, d):
+        raise ValueError("w must be [2F, d]")
+    if block not in (16, 32, 64) or elem not in ELEMS:
+        raise ValueError("block must be 16, 32 or 64 and elem 'e4m3' or 'e2m1'")
+    if x.device != grad_h.device or w.device != grad_h.device:
+        raise ValueError("grad_h, x and w must be on one device")
+    if rho.dtype != torch.float32 or rho.shape != (T,) or rho.device != x.device \
+            or not rho.is_contiguous():
+        raise ValueError("rho must be a contiguous float32 [T] tensor on x's device")
+    if gamma is not None:
+        _gamma(gamma, x)
+        if not gamma.is_contiguous():
+            raise ValueError("gamma must be contiguous")
+    if grad_x_dtype not in OUT_DTYPES or grad_dtype not in OUT_DTYPES:
+        raise ValueError("grad_x_dtype and grad_dtype must be float32 or bfloat16")
+    lib, e = load(), ELEMS[elem]
+    grad_x = torch.empty((T, d), dtype=grad_x_dtype, device=x.device)
+    grad_gamma = torch.empty((d,), dtype=grad_dtype, device=x.device)
+    grad_w = torch.empty((2 * F, d), dtype=grad_dtype, device=x.device)
+    ws_bytes = lib.mxnorm_gated_bwd_workspace_bytes(T, F, d, e)
+    ws = torch.empty((ws_bytes,), dtype=torch.uint8, device=x.device)
+    _call(lib.mxnorm_gated_bwd, x.device, grad_h.data_ptr(), gu.data_ptr(), x.data_ptr(),
+          rho.data_ptr(), _ptr(gamma), w.data_ptr(), T, F, d, block, e, ACTS[act],
+          OUT_DTYPES[grad_x_dtype], OUT_DTYPES[grad_dtype], grad_x.data_ptr(), grad_gamma.data_ptr(),
+          grad_w.data_ptr(), ws.data_ptr(), ws_bytes)
+    return grad_x, grad_gamma, grad_w
 
 
 def mx_cast_t_fwd(x, rho=None, block=32, elem="e4m3", scale_mode="rceil", codes=None,
