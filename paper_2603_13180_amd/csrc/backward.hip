@@ -24,7 +24,9 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
+#include "gate.h"
 #include "mxnorm.h"
 #include "norm_cast.h"
 #include "products.h"
@@ -251,7 +253,10 @@ __device__ __forceinline__ void cast_tile_of(int order, int64_t v, int64_t nc, i
 // 32 b + 31 (cast_block).  A column's four scale bytes (blocks 0..3 of the
 // tile) reach the quad's first lane through DPP and go out as one dword when
 // the tile is whole and R a multiple of 128, else byte by byte.
-template <bool FP4, int COLS, int NTH>
+// Output row of tile column cc: c0 + cc; HALF > 0 (a gated tile): the first
+// HALF columns are columns c0 .. of the first half of A.C, the others the same
+// columns of its second half.
+template <bool FP4, int COLS, int NTH, int HALF = 0>
 __device__ __forceinline__ void cast_columns(const CastTArgs &A, const uint8_t *tile,
                                              const float *rs, int64_t r0, int64_t c0, int tid)
 {
@@ -264,15 +269,20 @@ __device__ __forceinline__ void cast_columns(const CastTArgs &A, const uint8_t *
 #pragma unroll
     for (int h = 0; h < COLS / (16 * NW); ++h) {
         const int cc = 16 * NW * h + 16 * w + (lane >> 2); // column in the tile
-        const int64_t orow = c0 + cc;
+        int64_t orow = c0 + cc;
+        bool in_c = orow < A.C;
+        if constexpr (HALF > 0) {
+            in_c = c0 + cc % HALF < A.C / 2;
+            orow = c0 + cc % HALF + (cc < HALF ? 0 : A.C / 2);
+        }
         uint32_t byte = 0;
-        if (rb < A.R && orow < A.C)
+        if (rb < A.R && in_c)
             byte = cast_block<FP4, COLS>(A, tile, rs, cc, blk, orow, rb);
         // every lane of the quad takes part: quad_perm broadcasts of lanes 1, 2, 3
         const uint32_t b1 = (uint32_t)__builtin_amdgcn_mov_dpp((int)byte, 0x55, 0xF, 0xF, false);
         const uint32_t b2 = (uint32_t)__builtin_amdgcn_mov_dpp((int)byte, 0xAA, 0xF, 0xF, false);
         const uint32_t b3 = (uint32_t)__builtin_amdgcn_mov_dpp((int)byte, 0xFF, 0xF, 0xF, false);
-        if (blk == 0 && orow < A.C) {
+        if (blk == 0 && in_c) {
             uint8_t *sdst = A.scales + orow * (A.R / 32) + r0 / 32;
             if (whole) {
                 *reinterpret_cast<uint32_t *>(sdst) = byte | (b1 << 8) | (b2 << 16) | (b3 << 24);
@@ -324,9 +334,13 @@ __global__ void __launch_bounds__(NTH) cast_t_kernel(CastTArgs A)
 // lanes one row's 256 or 128.  The four blocks of 16 lanes gather their scale
 // bytes by two rotations and store them as one dword.  RCEIL scales (no clamp
 // is needed before the conversion); C a multiple of 128.
-template <bool FP4>
+//
+// valid: how many of the 16 lanes' 128 columns are this matrix's (128, or 64
+// where a gated half ends with half a tile: its scale bytes go out in pairs,
+// which are also aligned where the halves meet).
+template <bool FP4, bool PAIRS>
 __device__ __forceinline__ void cast_row_chunk(uint8_t *codes, uint8_t *scales, int64_t C, int64_t r,
-                                               int64_t c, bool in, int tid, const uint4 v)
+                                               int64_t c, bool in, int tid, const uint4 v, int valid)
 {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
     const float a = __uint_as_float(block_max<4>(chunk_absmax_bits(v)) << 16);
@@ -359,8 +373,16 @@ __device__ __forceinline__ void cast_row_chunk(uint8_t *codes, uint8_t *scales, 
     uint32_t b4 = byte << (8 * ((tid >> 2) & 3));
     b4 |= dpp_mov<0x124>(b4); // row_ror:4
     b4 |= dpp_mov<0x128>(b4); // row_ror:8
-    if (in && (tid & 15) == 0)
-        *reinterpret_cast<uint32_t *>(scales + r * (C / 32) + c / 32) = b4;
+    if (in && (tid & 15) == 0) {
+        uint8_t *dst = scales + r * (C / 32) + c / 32;
+        if constexpr (PAIRS) {
+            reinterpret_cast<uint16_t *>(dst)[0] = (uint16_t)b4;
+            if (valid > 64)
+                reinterpret_cast<uint16_t *>(dst)[1] = (uint16_t)(b4 >> 16);
+        } else {
+            *reinterpret_cast<uint32_t *>(dst) = b4;
+        }
+    }
 }
 
 template <bool FP4, int COLS, int NTH>
@@ -374,7 +396,7 @@ __device__ __forceinline__ void cast_rows(const CastTArgs &A, uint8_t *codes, ui
 #pragma unroll
     for (int k = 0; k < S::NLD; ++k) {
         const int64_t r = r0 + rbase + S::RPP * k;
-        cast_row_chunk<FP4>(codes, scales, A.C, r, c, r < A.rows && c < A.C, tid, L.v[k]);
+        cast_row_chunk<FP4, false>(codes, scales, A.C, r, c, r < A.rows && c < A.C, tid, L.v[k], 128);
     }
 }
 
@@ -384,13 +406,66 @@ __device__ __forceinline__ void cast_rows(const CastTArgs &A, uint8_t *codes, ui
 // and latency bound at small ones: 1024 x 2304 x 768 23 -> 9 us.  Workgroups from start[j] on
 // take job j's tiles (starts are multiples of 8, so that a tile's number
 // keeps its XCD).
+//
+// With a gate (GATE = its mx_act; else -1) grad_H is not in memory but formed
+// here: job 0's tile is 128 rows of COLS / 2 columns of H's gradient and of both
+// kept products, which give COLS / 2 columns of each projection's gradient,
+// rounded to bf16 as a matrix in memory would be.  At 8192 x 14336 (with W and
+// X of d = 4096) that saves writing and reading 0.47 GB.
 struct CastJobs {
     CastTArgs job[3];
     uint8_t *row_codes, *row_scales; // job 0's row cast
+    const uint16_t *gh, *gu;         // the gate's operands: [T, F], [T, 2F]
     int start[3];
 };
 
-template <bool FP4, int COLS, int NTH>
+// The gated tile: thread t moves the 16-byte chunk t % 16 of rows t / 16 + 32 k
+// of H's gradient, the gate and the up products.
+template <bool FP4, int ACT, int NTH>
+__device__ __forceinline__ void gated_tile(const CastJobs &J, int64_t r0, int64_t c0, int tid,
+                                           uint8_t *tile, float *rs)
+{
+    constexpr int COLS = 256, CH = COLS / 16, RPP = NTH / CH, NLD = CT_ROWS / RPP;
+    using S = CtShape<COLS, NTH>;
+    const CastTArgs &A = J.job[0];
+    const int64_t F = A.C / 2;
+    const int ch = tid % CH, rbase = tid / CH;
+    const int64_t c = c0 + 8 * ch;
+    const uint32_t pitch = (uint32_t)F * 2u;
+    const uint32_t rows = (uint32_t)max((int64_t)0, min((int64_t)CT_ROWS, A.rows - r0));
+    const __amdgpu_buffer_rsrc_t hr = buffer_rsrc(J.gh + r0 * F + c0, rows * pitch);
+    const __amdgpu_buffer_rsrc_t gr = buffer_rsrc(J.gu + r0 * 2 * F + c0, rows * pitch * 2u);
+    uint4 h[NLD], g[NLD], u[NLD];
+    auto load = [](__amdgpu_buffer_rsrc_t rsrc, uint32_t off) {
+        const u32x4_t t = __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)off, 0, kBufNT);
+        return make_uint4(t.x, t.y, t.z, t.w);
+    };
+#pragma unroll
+    for (int k = 0; k < NLD; ++k) {
+        const uint32_t r = (uint32_t)(rbase + RPP * k);
+        const bool in = c < F && r < rows; // else zeros
+        h[k] = load(hr, in ? r * pitch + 16u * ch : kOutside);
+        g[k] = load(gr, in ? r * pitch * 2u + 16u * ch : kOutside);
+        u[k] = load(gr, in ? r * pitch * 2u + pitch + 16u * ch : kOutside);
+    }
+#pragma unroll
+    for (int k = 0; k < NLD; ++k) {
+        const int r = rbase + RPP * k;
+        uint4 dg, du;
+        gate_gradients<ACT>(g[k], u[k], h[k], dg, du);
+        *reinterpret_cast<uint4 *>(&tile[S::off(r) + 16 * ch]) = dg;
+        *reinterpret_cast<uint4 *>(&tile[S::off(r) + 16 * (CH + ch)]) = du;
+        const bool in = r0 + r < A.rows && c < F;
+        // (E2M1: F is a multiple of 128)
+        const int valid = (int)min((int64_t)COLS / 2, F - c0);
+        cast_row_chunk<FP4, !FP4>(J.row_codes, J.row_scales, A.C, r0 + r, c, in, tid, dg, valid);
+        cast_row_chunk<FP4, !FP4>(J.row_codes, J.row_scales, A.C, r0 + r, F + c, in, tid, du, valid);
+    }
+    if (tid < CT_ROWS)
+        rs[tid] = 1.0f;
+}
+
+template <bool FP4, int COLS, int NTH, int GATE>
 __global__ void __launch_bounds__(NTH) cast_jobs_kernel(CastJobs J)
 {
     using S = CtShape<COLS, NTH>;
@@ -405,12 +480,21 @@ __global__ void __launch_bounds__(NTH) cast_jobs_kernel(CastJobs J)
         return;
     int64_t ct, rt;
     cast_tile_of(A.order, v, nc, nr, ct, rt);
+    if constexpr (GATE >= 0) {
+        if (j == 0) { // F = C / 2 columns in steps of COLS / 2: as many tiles
+            const int64_t c0 = ct * (COLS / 2), r0 = rt * CT_ROWS;
+            gated_tile<FP4, GATE, NTH>(J, r0, c0, tid, tile, rs);
+            lds_barrier();
+            cast_columns<FP4, COLS, NTH, COLS / 2>(A, tile, rs, r0, c0, tid);
+            return;
+        }
+    }
     const int64_t c0 = ct * COLS, r0 = rt * CT_ROWS;
     {
         TileLoad<COLS, NTH> L;
         fetch_tile<COLS, NTH>(A, r0, c0, tid, L);
         stage_tile<COLS, NTH>(L, tid, tile, rs);
-        if (j == 0)
+        if (GATE < 0 && j == 0)
             cast_rows<FP4, COLS, NTH>(A, J.row_codes, J.row_scales, r0, c0, tid, L);
     }
     lds_barrier();
@@ -1036,9 +1120,11 @@ mx_status ste(const void *x, const void *grad_z, const void *gamma, const float 
 
 mx_status backward_casts(const void *grad_h, const void *x, const float *rho, const void *w,
                          int64_t T, int64_t Tp, int64_t N, int64_t d, int elem,
-                         const BackwardCasts &o, hipStream_t stream)
+                         const BackwardCasts &o, const Gate *gate, hipStream_t stream)
 {
     CastJobs J;
+    J.gh = static_cast<const uint16_t *>(grad_h);
+    J.gu = gate ? static_cast<const uint16_t *>(gate->gu) : nullptr;
     auto job = [](const void *m, const float *r, int64_t rows, int64_t R, int64_t C, uint8_t *codes,
                   uint8_t *scales) {
         CastTArgs A;
@@ -1068,12 +1154,22 @@ mx_status backward_casts(const void *grad_h, const void *x, const float *rho, co
         if (at > (int64_t)(UINT32_MAX / kThreads))
             return mxk::fail(MX_EUNSUPPORTED, "too many tiles to cast in one launch");
     }
+    auto launch = [&](auto fp4, auto act) {
+        hipLaunchKernelGGL((cast_jobs_kernel<decltype(fp4)::value, kCols, kThreads, decltype(act)::value>),
+                           dim3((unsigned)at), dim3(kThreads), 0, stream, J);
+    };
+    auto launch_act = [&](auto fp4) {
+        if (!gate)
+            launch(fp4, std::integral_constant<int, -1>{});
+        else if (gate->act == MX_ACT_SILU)
+            launch(fp4, std::integral_constant<int, MX_ACT_SILU>{});
+        else
+            launch(fp4, std::integral_constant<int, MX_ACT_GELU_TANH>{});
+    };
     if (elem == MX_ELEM_E4M3)
-        hipLaunchKernelGGL((cast_jobs_kernel<false, kCols, kThreads>), dim3((unsigned)at),
-                           dim3(kThreads), 0, stream, J);
+        launch_act(std::false_type{});
     else
-        hipLaunchKernelGGL((cast_jobs_kernel<true, kCols, kThreads>), dim3((unsigned)at),
-                           dim3(kThreads), 0, stream, J);
+        launch_act(std::true_type{});
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? MX_OK
                            : mxk::fail(MX_EHIP, "kernel launch failed: %s", hipGetErrorString(e));

@@ -75,19 +75,6 @@ int64_t padded(int64_t T, int elem)
     return (T + step - 1) / step * step;
 }
 
-// The projections' gradient (bf16 [T, 2F]) and then the backward's space.
-struct GatedSpace {
-    uint8_t *gg;
-    size_t own;
-    BwdSpace b;
-    size_t bytes;
-    GatedSpace(void *ws, int64_t T, int64_t F, int64_t d, int elem)
-        : gg(static_cast<uint8_t *>(ws)), own(((size_t)T * (size_t)F * 4 + 255) & ~(size_t)255),
-          b(ws ? gg + own : nullptr, T, padded(T, elem), 2 * F, d, elem), bytes(own + b.bytes)
-    {
-    }
-};
-
 bool known(int elem) { return elem == MX_ELEM_E4M3 || elem == MX_ELEM_E2M1; }
 
 mx_status check_workspace(const void *ws, size_t have, size_t need)
@@ -202,7 +189,7 @@ mx_status mxnorm_linear_bwd(const void *grad_h, const void *x, const float *rho,
     // grad_X and grad_gamma
     if ((st = mxb::backward_casts(grad_h, x, rho, w, T, T, N, d, elem,
                                   {s.gh, s.gh_s, s.ght, s.ght_s, s.wt, s.wt_s, s.xt, s.xt_s},
-                                  stream)) != MX_OK ||
+                                  nullptr, stream)) != MX_OK ||
         (st = mxg::matmul_pair(gw, MX_OUT_F32, gz, elem, stream)) != MX_OK)
         return st;
     return mxnorm_ste_bwd(x, s.gz, gamma, rho, T, d, out_dtype, grad_x, grad_gamma, s.ste,
@@ -213,7 +200,7 @@ size_t mxnorm_gated_bwd_workspace_bytes(int64_t T, int64_t F, int64_t d, int ele
 {
     if (T <= 0 || F <= 0 || d <= 0 || !known(elem))
         return 0;
-    return GatedSpace(nullptr, T, F, d, elem).bytes;
+    return BwdSpace(nullptr, T, padded(T, elem), 2 * F, d, elem).bytes;
 }
 
 mx_status mxnorm_gated_bwd(const void *grad_h, const void *gu, const void *x, const float *rho,
@@ -235,27 +222,26 @@ mx_status mxnorm_gated_bwd(const void *grad_h, const void *gu, const void *x, co
                                    mxnorm_gated_bwd_workspace_bytes(T, F, d, elem));
     if (st != MX_OK)
         return st;
-    const GatedSpace s(workspace, T, F, d, elem);
     const int64_t N = 2 * F, Tp = padded(T, elem);
-    const mxg::Product gz{s.b.gh, s.b.gh_s, s.b.wt, s.b.wt_s, T, d, N, nullptr, s.b.gz};
-    const mxg::Product gw{s.b.ght, s.b.ght_s, s.b.xt, s.b.xt_s, N, d, Tp, gamma, grad_w};
+    const BwdSpace s(workspace, T, Tp, N, d, elem);
+    const mxb::Gate gate{gu, act};
+    const mxg::Product gz{s.gh, s.gh_s, s.wt, s.wt_s, T, d, N, nullptr, s.gz};
+    const mxg::Product gw{s.ght, s.ght_s, s.xt, s.xt_s, N, d, Tp, gamma, grad_w};
     // every check before the first launch
-    if ((st = mxg::check_gated_bwd(grad_h, gu, T, F, act, s.gg)) != MX_OK ||
-        (st = mxb::check_cast_t(w, nullptr, N, d, block, elem, MX_SCALE_RCEIL, s.b.wt, s.b.wt_s)) != MX_OK ||
+    if ((st = mxg::check_gated_bwd(grad_h, gu, T, F, act, s.gh)) != MX_OK ||
+        (st = mxb::check_cast_t(w, nullptr, N, d, block, elem, MX_SCALE_RCEIL, s.wt, s.wt_s)) != MX_OK ||
         (st = mxg::check_product(gz, block, elem, MX_OUT_BF16)) != MX_OK ||
-        (st = mxb::check_ste(x, s.b.gz, gamma, rho, T, d, out_dtype, grad_x,
-                             static_cast<float *>(grad_gamma), s.b.ste, s.b.ste_bytes)) != MX_OK ||
-        (st = mxb::check_cast_t(x, rho, Tp, d, block, elem, MX_SCALE_RCEIL, s.b.xt, s.b.xt_s)) != MX_OK ||
+        (st = mxb::check_ste(x, s.gz, gamma, rho, T, d, out_dtype, grad_x,
+                             static_cast<float *>(grad_gamma), s.ste, s.ste_bytes)) != MX_OK ||
+        (st = mxb::check_cast_t(x, rho, Tp, d, block, elem, MX_SCALE_RCEIL, s.xt, s.xt_s)) != MX_OK ||
         (st = mxg::check_product(gw, block, elem, grad_dtype)) != MX_OK)
         return st;
-    if ((st = mx_gated_bwd(grad_h, gu, T, F, act, s.gg, stream)) != MX_OK ||
-        (st = mxb::backward_casts(s.gg, x, rho, w, T, Tp, N, d, elem,
-                                  {s.b.gh, s.b.gh_s, s.b.ght, s.b.ght_s, s.b.wt, s.b.wt_s, s.b.xt,
-                                   s.b.xt_s},
+    if ((st = mxb::backward_casts(grad_h, x, rho, w, T, Tp, N, d, elem,
+                                  {s.gh, s.gh_s, s.ght, s.ght_s, s.wt, s.wt_s, s.xt, s.xt_s}, &gate,
                                   stream)) != MX_OK ||
         (st = mxg::matmul_pair(gw, grad_dtype, gz, elem, stream)) != MX_OK)
         return st;
-    return mxb::ste(x, s.b.gz, gamma, rho, T, d, out_dtype, grad_x, grad_dtype, grad_gamma, s.b.ste,
+    return mxb::ste(x, s.gz, gamma, rho, T, d, out_dtype, grad_x, grad_dtype, grad_gamma, s.ste,
                     stream);
 }
 

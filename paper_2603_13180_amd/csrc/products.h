@@ -81,9 +81,15 @@ struct BackwardCasts {
 };
 
 // The casts along T are of T rows and then zeros up to Tp.  Tp and N multiples
-// of 128, d of 16; grad_h, x, w 16-byte aligned.
+// of 128, d of 16; grad_h, x, w 16-byte aligned.  With a gate grad_h is H's
+// gradient [T, N/2], and what is cast are both projections' gradients [T, N],
+// mx_gated_bwd's values.
+struct Gate {
+    const void *gu;
+    int act;
+};
 mx_status backward_casts(const void *grad_h, const void *x, const float *rho, const void *w,
                          int64_t T, int64_t Tp, int64_t N, int64_t d, int elem,
-                         const BackwardCasts &o, hipStream_t stream);
+                         const BackwardCasts &o, const Gate *gate, hipStream_t stream);
 
 } // namespace mxb

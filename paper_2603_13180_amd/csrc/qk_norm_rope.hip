@@ -340,23 +340,42 @@ template <int G, bool INTER> __global__ void __launch_bounds__(NT) bwd_kernel(Ar
 }
 
 // Gain gradients: the workgroups' partial rows [P][2][D] added in double in a
-// fixed order.  Block (j, which) sums elements 64 j ..; thread (g, e) adds rows
-// g, g + 16, ... of element e.
+// fixed order.  Block (j, which) sums elements 8 j .. 8 j + 7 (D is a multiple
+// of 8); thread (g, q) adds rows g, g + 512, ... of four of them, so that with
+// 1024 rows a thread waits for two loads (64 elements a block and 64 loads one
+// after the other took 20 us).
+constexpr int GAIN_GROUPS = 512;
 __global__ void __launch_bounds__(1024) gain_kernel(const float *part, int P, int D, float *gq, float *gk)
 {
-    __shared__ double red[16][64];
-    const int e = threadIdx.x & 63, g = threadIdx.x >> 6, j = blockIdx.x * 64 + e, which = blockIdx.y;
-    double s = 0.0;
-    if (j < D)
-        for (int p = g; p < P; p += 16)
-            s += (double)part[((int64_t)p * 2 + which) * D + j];
-    red[g][e] = s;
+    __shared__ double red[16][8];
+    const int q = threadIdx.x & 1, g = threadIdx.x >> 1, which = blockIdx.y;
+    const int j = blockIdx.x * 8 + 4 * q;
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int p = g; p < P; p += GAIN_GROUPS) {
+        const float4 v = *reinterpret_cast<const float4 *>(part + ((int64_t)p * 2 + which) * D + j);
+        s[0] += (double)v.x;
+        s[1] += (double)v.y;
+        s[2] += (double)v.z;
+        s[3] += (double)v.w;
+    }
+    // the 32 rows of a wave, then the waves in order
+#pragma unroll
+    for (int m = 2; m < 64; m *= 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            s[e] += __shfl_xor(s[e], m);
+    const int w = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) < 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            red[w][4 * q + e] = s[e];
     __syncthreads();
     float *out = which ? gk : gq;
-    if (g == 0 && j < D && out) {
-        for (int i = 1; i < 16; ++i)
-            s += red[i][e];
-        out[j] = (float)s;
+    if (threadIdx.x < 8 && out) {
+        double t = 0.0;
+        for (int i = 0; i < 16; ++i)
+            t += red[i][threadIdx.x];
+        out[blockIdx.x * 8 + threadIdx.x] = (float)t;
     }
 }
 
@@ -552,7 +571,7 @@ mx_status qk_norm_rope_bwd(const mx_heads *grad_q_out, const mx_heads *grad_k_ou
     if (T == 0) { // the sums over no tokens
         if (!gains)
             return MX_OK;
-        hipLaunchKernelGGL(mxq::gain_kernel, dim3((unsigned)((D + 63) / 64), 2), dim3(1024), 0, stream,
+        hipLaunchKernelGGL(mxq::gain_kernel, dim3((unsigned)(D / 8), 2), dim3(1024), 0, stream,
                            nullptr, 0, (int)D, grad_q_gamma, grad_k_gamma);
         return launched();
     }
@@ -572,7 +591,7 @@ mx_status qk_norm_rope_bwd(const mx_heads *grad_q_out, const mx_heads *grad_k_ou
     const unsigned grid = mxq::workgroups(T, true);
     mxq::launch<true>(A, interleaved != 0, grid, stream);
     if (gains)
-        hipLaunchKernelGGL(mxq::gain_kernel, dim3((unsigned)((D + 63) / 64), 2), dim3(1024), 0, stream,
+        hipLaunchKernelGGL(mxq::gain_kernel, dim3((unsigned)(D / 8), 2), dim3(1024), 0, stream,
                            A.part, (int)grid, (int)D, grad_q_gamma, grad_k_gamma);
     return launched();
 }

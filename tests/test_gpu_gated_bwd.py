@@ -189,6 +189,41 @@ def test_whole_backward(elem, T, F, d, grad_dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("elem", ELEMS)
+@pytest.mark.parametrize("T,F,d", [(1, 128, 16), (37, 384, 48), (128, 128, 272), (300, 640, 512), (1025, 1152, 256),
+                                   (160, 6272, 64), (150, 64, 32), (70, 192, 16), (200, 6208, 32)])
+def test_casts_byte_for_byte(elem, act, T, F, d):
+    if elem == "e2m1" and F % 128:
+        F += 64
+    # what the products take, in a workspace of the test's own: the casts of the
+    # gradient that mx_gated_bwd gives, padded with rows of zeros.  6272: from 48
+    # column tiles on they are visited in another order.  Infinities and NaN too
+    c = Case(T, F, d, seed=9)
+    c.gh[T // 2, 5] = float("inf")
+    c.gh[0, F - 1] = float("nan")
+    c.gu[T - 1, 7] = -float("inf")
+    c.gu[T - 1, F + 40] = 0.0
+    lib, e = mxnorm.load(), mxnorm.ELEMS[elem]
+    size = lib.mxnorm_gated_bwd_workspace_bytes(T, F, d, e)
+    ws = torch.full((size + 256,), 7, dtype=torch.uint8, device=DEV)
+    gx, gg, gw = [torch.empty(s, dtype=torch.bfloat16, device=DEV) for s in ((T, d), (d,), (2 * F, d))]
+    mxnorm._check(lib.mxnorm_gated_bwd(
+        c.gh.data_ptr(), c.gu.data_ptr(), c.x.data_ptr(), c.rho.data_ptr(), c.gamma.data_ptr(), c.w.data_ptr(),
+        T, F, d, 32, e, mxnorm.ACTS[act], 1, 1, gx.data_ptr(), gg.data_ptr(), gw.data_ptr(), ws.data_ptr(), size,
+        mxnorm._stream(c.x.device)))
+    assert (ws[size:] == 7).all()
+    at = 0
+    parts = c.parts(elem, act)
+    for name in ("gh", "wt", "ght", "xt"):
+        for want, what in zip(parts[name], ("codes", "scales")):
+            got = ws[at:at + want.numel()].view(want.shape)
+            bad = (got != want).nonzero()
+            assert not len(bad), (name, what, len(bad), bad[0].tolist(), got[tuple(bad[0])], want[tuple(bad[0])])
+            at += (want.numel() + 255) // 256 * 256
+
+
+@pytest.mark.gpu
 def test_without_a_gain_and_narrow_feed_forward():
     for F in (64, 192):                       # a single partial tile of columns
         c = Case(200, F, 128, gain=False)
