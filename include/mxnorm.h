@@ -432,8 +432,9 @@ typedef struct {
  *   (n_2i, n_(2i+1)) if interleaved:  t = pos[token] inv_freq[i],
  *   y_a = a cos t - b sin t,  y_b = b cos t + a sin t;
  *   elements from R on: y = n.
- * r comes from a double sum, is formed in double and rounded once to float (a
- * zero or infinite radicand gives 0); the angle is formed in double turns and
+ * r comes from a float sum, or where the squares leave float's range from a
+ * double one, and is within 2^-20 of its value (a zero or infinite radicand
+ * gives 0); the angle is formed in double turns and
  * its fraction rounded to float, so far and negative positions keep their
  * angles (to 2^-23 of a turn up to |pos inv_freq| of 2^29); the rest is float,
  * rounded once to bf16.
@@ -452,10 +453,10 @@ mx_status qk_norm_rope_fwd(const mx_heads *q, const mx_heads *k, const void *q_g
 /*
  * Its gradients from those of q_out and k_out, q and k as the forward took
  * them.  Per head, with m the gradient turned back by the angles and v = gamma
- * m:  u = sum_e v_e x_e (in double);  grad_x = RN(RN(r v) - RN(c x)), c = r^3 u /
- * D in double rounded to float;  grad_gamma_e = sum over the tokens and heads of
- * RN(RN(x r) m), in float within a workgroup's heads (at most 1024 workgroups),
- * then in double, in a fixed order: the same call gives the same bits.
+ * m:  grad_x = r (v - k n) with n = x r and k = (1/D) sum_e v_e n_e, in float;
+ * grad_gamma_e = sum over the tokens and heads of n m, in float within a
+ * workgroup's heads (at most 512 workgroups), then in double, in a fixed order:
+ * the same call gives the same bits.
  * grad_q, grad_k: bf16; each may be the incoming gradient itself (data and
  * strides).  grad_q_gamma, grad_k_gamma: float [D] or NULL (not computed); with
  * no tokens or heads they are 0.  They need `workspace`, caller-owned device

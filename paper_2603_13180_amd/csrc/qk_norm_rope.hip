@@ -12,16 +12,23 @@
 // A lane holds the two 16-byte chunks of a head whose elements are paired
 // (chunks l and l + R/16 of the rotated part, two chunks of the rest), so a
 // pair never crosses lanes, and a head is a group of G = 4 .. 32 lanes; a wave
-// takes 64 / G heads of one token.  An angle costs a double product and a
-// sine, and every head of the token needs it: the workgroup computes its
-// tokens' angles once into LDS.  HBM bound: 4 bytes an element forward, 6
-// backward.
+// takes 64 / G heads of one token, the next one's loads in flight.  An angle
+// costs a double product and a sine, and every head of the token needs it: the
+// workgroup computes its tokens' angles once into LDS.
+//
+// What bounds it: HBM, 4 bytes an element forward and 6 backward.  32768 tokens
+// of 32 + 8 heads of 128 out of a projection of 48: forward 120 us, 5.6 TB/s (a
+// copy of as much 125 us); backward 190 us, 5.3 TB/s (an addition of as much
+// 167).  Neither changes with angles and arithmetic left out (120 and 196 us);
+// 15 us of the backward are for writing rows with gaps (the values' part of the
+// projection's gradient), 166 us into a tensor of its own.
 #include <hip/hip_runtime.h>
 
 #include <math.h>
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "mxnorm.h"
 #include "norm_cast.h"
@@ -35,7 +42,7 @@ using namespace mxk;
 
 constexpr int NT = 256, NW = NT / 64;
 constexpr int MAX_D = 512;
-constexpr int TOKENS = 4; // tokens whose angles a workgroup holds at once
+constexpr int ANGLES = 1024; // angles a workgroup holds at once
 
 struct Heads {
     const uint16_t *in;  // x
@@ -44,15 +51,17 @@ struct Heads {
     const uint16_t *gamma;
     int64_t in_t, in_h, gy_t, gy_h, out_t, out_h; // strides, elements
     int heads, blocks;   // blocks of 64 / G heads
+    int tb;              // tokens a workgroup takes at a time
+    int64_t steps;       // of tb tokens
 };
 
 struct Args {
     Heads q, k;
     const int64_t *pos;    // NULL: 0, 1, ...
     const float *inv_freq; // [R/2]
-    float *part;           // backward: [workgroups][2][D] gain gradients, or NULL
+    float *part;           // backward: [2][workgroups][D] gain gradients, or NULL
     int64_t T;
-    int D, R, tb;          // tb: tokens a workgroup takes at a time
+    int D, R;
     float eps;
     double inv_d; // 1 / D
 };
@@ -83,6 +92,7 @@ template <bool INTER>
 __device__ __forceinline__ void fill_angles(const Args &A, int64_t t0, int nt, float *cs, float *sn)
 {
     const int half = A.R / 2;
+#pragma unroll 1
     for (int i = threadIdx.x; i < nt * half; i += NT) {
         const int t = i / half, p = i - t * half; // p = 8 l + e
         const int l = p >> 3, e = p & 7;
@@ -110,24 +120,40 @@ template <int G> __device__ __forceinline__ double head_sum(double s)
     return s;
 }
 
-// (S / D + eps)^(-1/2), 0 for a radicand that is zero or infinite: the
-// hardware's estimate and one Newton step in double, rounded to float.
-__device__ __forceinline__ float inverse_rms(double S, double inv_d, float eps)
+template <int G> __device__ __forceinline__ float head_sum(float s)
 {
-    const double u = S * inv_d + (double)eps;
-    const double y = __builtin_amdgcn_rsq(u);
-    const double z = __builtin_fma(y, __builtin_fma(-0.5 * u * y, y, 0.5), y);
-    return u == 0.0 || u == INFINITY ? 0.0f : (float)z;
+    auto step = [](float v, auto c) {
+        return v + __uint_as_float(dpp_mov<decltype(c)::value>(__float_as_uint(v)));
+    };
+    s = step(s, std::integral_constant<int, 0xB1>{});
+    s = step(s, std::integral_constant<int, 0x4E>{});
+    if constexpr (G >= 8)
+        s = step(s, std::integral_constant<int, 0x141>{});
+    if constexpr (G >= 16)
+        s = step(s, std::integral_constant<int, 0x140>{});
+    if constexpr (G >= 32)
+        s += __shfl_xor(s, 16);
+    return s;
 }
 
-struct Chunk {
-    float v[8];
+// Two adjacent elements of each of the lane's chunks.
+struct Quad {
+    float a0, a1, b0, b1;
 };
 
-__device__ __forceinline__ Chunk widen(uint4 w)
+__device__ __forceinline__ Quad widen(const uint4 &a, const uint4 &b, int i)
 {
-    return {{bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y), bf16_lo(w.z), bf16_hi(w.z),
-             bf16_lo(w.w), bf16_hi(w.w)}};
+    const uint32_t x = i == 0 ? a.x : i == 1 ? a.y : i == 2 ? a.z : a.w;
+    const uint32_t y = i == 0 ? b.x : i == 1 ? b.y : i == 2 ? b.z : b.w;
+    return {bf16_lo(x), bf16_hi(x), bf16_lo(y), bf16_hi(y)};
+}
+
+// The compiler takes v as new: nothing computed from it before is kept.
+__device__ __forceinline__ void opaque(uint4 (&v)[2])
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        asm volatile("" : "+v"(v[i].x), "+v"(v[i].y), "+v"(v[i].z), "+v"(v[i].w));
 }
 
 __device__ __forceinline__ uint32_t pack2(float a, float b)
@@ -136,15 +162,10 @@ __device__ __forceinline__ uint32_t pack2(float a, float b)
     return (uint32_t)__builtin_bit_cast(uint16_t, x) | ((uint32_t)__builtin_bit_cast(uint16_t, y) << 16);
 }
 
-__device__ __forceinline__ uint4 narrow(const Chunk &c)
-{
-    return make_uint4(pack2(c.v[0], c.v[1]), pack2(c.v[2], c.v[3]), pack2(c.v[4], c.v[5]),
-                      pack2(c.v[6], c.v[7]));
-}
-
-// Turn the lane's pairs by its angles, or (BACK) by their negatives.
+// Turn elements 2 i, 2 i + 1 of the chunks by the lane's angles, or (BACK) by
+// their negatives.
 template <bool INTER, bool BACK>
-__device__ __forceinline__ void turn(Chunk &a, Chunk &b, const float *cs, const float *sn)
+__device__ __forceinline__ void turn(Quad &q, const float *cs, const float *sn, int i)
 {
     auto one = [](float &x, float &y, float c, float s) {
         if (BACK)
@@ -153,193 +174,284 @@ __device__ __forceinline__ void turn(Chunk &a, Chunk &b, const float *cs, const 
         y = __builtin_fmaf(y, c, x * s);
         x = t;
     };
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        if constexpr (!INTER)
-            one(a.v[e], b.v[e], cs[e], sn[e]);
-        else if (e < 4)
-            one(a.v[2 * e], a.v[2 * e + 1], cs[e], sn[e]);
-        else
-            one(b.v[2 * e - 8], b.v[2 * e - 7], cs[e], sn[e]);
+    if constexpr (INTER) {
+        one(q.a0, q.a1, cs[i], sn[i]);
+        one(q.b0, q.b1, cs[4 + i], sn[4 + i]);
+    } else {
+        const float2 c = reinterpret_cast<const float2 *>(cs)[i], s = reinterpret_cast<const float2 *>(sn)[i];
+        one(q.a0, q.b0, c.x, s.x);
+        one(q.a1, q.b1, c.y, s.y);
     }
 }
 
-__device__ __forceinline__ uint4 load16(const uint16_t *p, bool in)
+// 16 bytes at p, or zeros: without a branch, which would end with a wait for
+// its own load.  `some` is an address that can be read.
+__device__ __forceinline__ uint4 load16(const uint16_t *p, bool in, const uint16_t *some)
 {
-    return in ? load_stream(reinterpret_cast<const uint4 *>(p)) : make_uint4(0, 0, 0, 0);
+    const uint4 v = load_stream(reinterpret_cast<const uint4 *>(in ? p : some));
+    return make_uint4(in ? v.x : 0, in ? v.y : 0, in ? v.z : 0, in ? v.w : 0);
 }
 
-__device__ __forceinline__ void store16(uint16_t *p, const uint4 &v)
+// The lane's two chunks at p and p + step.
+template <bool FULL>
+__device__ __forceinline__ void load_chunks(uint4 (&v)[2], const uint16_t *p, int step, bool in_a,
+                                            bool in_b, const uint16_t *some)
 {
-    __builtin_nontemporal_store(u32x4_t{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4_t *>(p));
+    if constexpr (FULL) {
+        v[0] = load_stream(reinterpret_cast<const uint4 *>(p));
+        v[1] = load_stream(reinterpret_cast<const uint4 *>(p + step));
+    } else {
+        v[0] = load16(p, in_a, some);
+        v[1] = load16(p + step, in_b, some);
+    }
 }
 
-// A lane's place in its head and the gains of its chunks.
-template <int G> struct Lane {
+__device__ __forceinline__ void store16(uint16_t *p, const uint32_t (&v)[4])
+{
+    __builtin_nontemporal_store(u32x4_t{v[0], v[1], v[2], v[3]}, reinterpret_cast<u32x4_t *>(p));
+}
+
+// A lane's place in its head and the gains of its chunks.  FULL: every lane of
+// a wave holds two chunks that turn (R = D = 16 G, and the numbers of heads are
+// multiples of 64 / G).
+template <int G, bool FULL> struct Lane {
     int l, sub, ca, cb;
     bool in_a, in_b, rot;
-    __device__ Lane(const Args &A)
+    __device__ __forceinline__ Lane(const Args &A)
     {
         const int lane = threadIdx.x & 63;
         l = lane % G;
         sub = lane / G;
-        chunks_of(A.D, A.R, l, ca, cb);
-        in_a = l < lanes_of(A.D, A.R);
-        in_b = in_a && 8 * cb < A.D;
-        rot = l < A.R / 16;
+        if constexpr (FULL) {
+            ca = l;
+            cb = l + G;
+            in_a = in_b = rot = true;
+        } else {
+            chunks_of(A.D, A.R, l, ca, cb);
+            in_a = l < lanes_of(A.D, A.R);
+            in_b = in_a && 8 * cb < A.D;
+            rot = l < A.R / 16;
+        }
     }
-    __device__ void gains(const uint16_t *gamma, uint4 &ga, uint4 &gb) const
+    __device__ __forceinline__ void gains(const uint16_t *gamma, uint4 (&g)[2]) const
     {
         const uint32_t one = 0x3F803F80u;
-        ga = gb = make_uint4(one, one, one, one);
+        g[0] = g[1] = make_uint4(one, one, one, one);
         if (gamma && in_a)
-            ga = *reinterpret_cast<const uint4 *>(gamma + 8 * ca);
+            g[0] = *reinterpret_cast<const uint4 *>(gamma + 8 * ca);
         if (gamma && in_b)
-            gb = *reinterpret_cast<const uint4 *>(gamma + 8 * cb);
+            g[1] = *reinterpret_cast<const uint4 *>(gamma + 8 * cb);
     }
 };
 
-template <int G, bool INTER> __global__ void __launch_bounds__(NT) fwd_kernel(Args A)
+// What a lane has loaded of one head: its chunks of x and, backward, of the
+// gradient.
+template <bool BWD> struct Loaded {
+    uint4 x[2], gy[BWD ? 2 : 1];
+};
+
+// The lane's 16 elements, widened: four at a time.
+struct Item {
+    Quad q[4];
+};
+
+__device__ __forceinline__ Item widen(const uint4 (&v)[2])
 {
-    __shared__ float cs[TOKENS * MAX_D / 2], sn[TOKENS * MAX_D / 2];
-    const int w = threadIdx.x >> 6, half = A.R / 2;
-    const Lane<G> L(A);
-    uint4 gq[2], gk[2];
-    L.gains(A.q.gamma, gq[0], gq[1]);
-    L.gains(A.k.gamma, gk[0], gk[1]);
-    const int per = A.q.blocks + A.k.blocks;
-    for (int64_t t0 = (int64_t)blockIdx.x * A.tb; t0 < A.T; t0 += (int64_t)gridDim.x * A.tb) {
-        const int nt = (int)min((int64_t)A.tb, A.T - t0);
+    return {{widen(v[0], v[1], 0), widen(v[0], v[1], 1), widen(v[0], v[1], 2), widen(v[0], v[1], 3)}};
+}
+
+// r = (sum x^2 / D + eps)^(-1/2) of the lane's head: the sum in float where its
+// squares cannot leave float's range (between 2^-100 and 2^100), else, for the
+// whole wave and rarely, in double; 0 for a radicand that is zero or infinite.
+template <int G>
+__device__ __forceinline__ float inverse_rms(const Args &A, const Item &x)
+{
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        s = __builtin_fmaf(x.q[i].a0, x.q[i].a0, s);
+        s = __builtin_fmaf(x.q[i].a1, x.q[i].a1, s);
+        s = __builtin_fmaf(x.q[i].b0, x.q[i].b0, s);
+        s = __builtin_fmaf(x.q[i].b1, x.q[i].b1, s);
+    }
+    s = head_sum<G>(s);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(s > 0x1p-100f && s < 0x1p100f)) != 0, 0)) {
+        double S = 0.0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const double a = x.q[i].a0, b = x.q[i].a1, c = x.q[i].b0, d = x.q[i].b1;
+            S += a * a + b * b + c * c + d * d;
+        }
+        const double u = head_sum<G>(S) * A.inv_d + (double)A.eps;
+        return u == 0.0 || u == INFINITY ? 0.0f : (float)(1.0 / sqrt(u));
+    }
+    return __builtin_amdgcn_rsqf(__builtin_fmaf(s, (float)A.inv_d, A.eps));
+}
+
+template <int G, bool INTER, bool FULL>
+__device__ __forceinline__ void forward_item(const Args &A, const Lane<G, FULL> &L, const Loaded<false> &v,
+                                             const uint4 (&gain)[2], const float *cs, const float *sn,
+                                             uint32_t (&a)[4], uint32_t (&b)[4])
+{
+    const Item x = widen(v.x);
+    const float r = inverse_rms<G>(A, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const Quad g = widen(gain[0], gain[1], i), q = x.q[i];
+        Quad y = {q.a0 * r * g.a0, q.a1 * r * g.a1, q.b0 * r * g.b0, q.b1 * r * g.b1};
+        if (L.rot)
+            turn<INTER, false>(y, cs, sn, i);
+        a[i] = pack2(y.a0, y.a1);
+        b[i] = pack2(y.b0, y.b1);
+    }
+}
+
+// The gradient of x is r (v - k n) with n = x r and k = (1/D) sum v n: no term
+// overflows or underflows where x is huge or tiny.
+template <int G, bool INTER, bool FULL>
+__device__ __forceinline__ void backward_item(const Args &A, const Lane<G, FULL> &L, const Loaded<true> &v,
+                                              const uint4 (&gain)[2], const float *cs, const float *sn,
+                                              uint32_t (&a)[4], uint32_t (&b)[4], float (&sum)[16])
+{
+    Item n = widen(v.x), w;
+    const float r = inverse_rms<G>(A, n);
+    float u = 0.0f;
+    auto one = [&](float &x, float m, float g, float &to) {
+        x = x * r;
+        to = __builtin_fmaf(x, m, to);
+        const float t = m * g;
+        u = __builtin_fmaf(x, t, u);
+        return t;
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const Quad g = widen(gain[0], gain[1], i);
+        Quad m = widen(v.gy[0], v.gy[1], i);
+        if (L.rot)
+            turn<INTER, true>(m, cs, sn, i);
+        w.q[i] = {one(n.q[i].a0, m.a0, g.a0, sum[2 * i]), one(n.q[i].a1, m.a1, g.a1, sum[2 * i + 1]),
+                  one(n.q[i].b0, m.b0, g.b0, sum[8 + 2 * i]), one(n.q[i].b1, m.b1, g.b1, sum[9 + 2 * i])};
+    }
+    const float k = head_sum<G>(u) * (float)A.inv_d;
+    auto grad = [&](float x, float t) { return r * __builtin_fmaf(-k, x, t); };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        a[i] = pack2(grad(n.q[i].a0, w.q[i].a0), grad(n.q[i].a1, w.q[i].a1));
+        b[i] = pack2(grad(n.q[i].b0, w.q[i].b0), grad(n.q[i].b1, w.q[i].b1));
+    }
+}
+
+// Steps s, s + nwg, ... below H.steps of one kind of heads, a step being H.tb
+// tokens: wave w takes items w, w + NW, ... of their blocks of heads, an item's
+// loads issued before the item ahead of it is computed, the first before the
+// tokens' angles.  Returns the first step past them.
+template <int G, bool INTER, bool FULL, bool BWD>
+__device__ __forceinline__ int64_t heads_of_kind(const Args &A, const Heads &H, int64_t s, int64_t nwg,
+                                                 float *cs, float *sn, float (&sum)[16])
+{
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = A.R / 2;
+    const Lane<G, FULL> L(A);
+    uint4 gain[2];
+    L.gains(H.gamma, gain);
+    // an item is the wave's, so its first head's address is scalar; a lane adds
+    // its own head and chunk
+    const int64_t xl = L.sub * H.in_h + 8 * L.ca, gl = BWD ? L.sub * H.gy_h + 8 * L.ca : 0,
+                  yl = L.sub * H.out_h + 8 * L.ca;
+    const int step = 8 * (L.cb - L.ca);
+#pragma unroll 1
+    for (; s < H.steps; s += nwg) {
+        const int64_t t0 = s * H.tb;
+        const int nt = (int)min((int64_t)H.tb, A.T - t0), n = nt * H.blocks;
+        auto load = [&](int i, Loaded<BWD> &v) {
+            const int t = i / H.blocks, h = (i - t * H.blocks) * (64 / G);
+            // past the last item every lane reads the tensor's first bytes: a
+            // branch around the loads would end with a wait for them
+            const bool more = i < n, on = FULL || (more && h + L.sub < H.heads);
+            const int sp = more ? step : 0;
+            const uint16_t *x = more ? H.in + (t0 + t) * H.in_t + h * H.in_h : H.in;
+            load_chunks<FULL>(v.x, x + (more ? xl : 0), sp, on && L.in_a, on && L.in_b, H.in);
+            if constexpr (BWD) {
+                const uint16_t *gy = more ? H.gy + (t0 + t) * H.gy_t + h * H.gy_h : H.gy;
+                load_chunks<FULL>(v.gy, gy + (more ? gl : 0), sp, on && L.in_a, on && L.in_b, H.gy);
+            }
+        };
+        Loaded<BWD> next;
+        load(w, next);
         __syncthreads(); // the angles of the tokens before are read
         fill_angles<INTER>(A, t0, nt, cs, sn);
         __syncthreads();
-        for (int i = w; i < nt * per; i += NW) {
-            const int t = i / per, blk = i - t * per;
-            const bool key = blk >= A.q.blocks;
-            const Heads &H = key ? A.k : A.q;
-            const int h = (key ? blk - A.q.blocks : blk) * (64 / G) + L.sub;
-            const bool on = h < H.heads;
-            const uint16_t *x = H.in + (t0 + t) * H.in_t + h * H.in_h;
-            Chunk a = widen(load16(x + 8 * L.ca, on && L.in_a));
-            Chunk b = widen(load16(x + 8 * L.cb, on && L.in_b));
-            double S = 0.0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                S = __builtin_fma((double)a.v[e], (double)a.v[e], S);
-                S = __builtin_fma((double)b.v[e], (double)b.v[e], S);
-            }
-            const float r = inverse_rms(head_sum<G>(S), A.inv_d, A.eps);
-            const Chunk ga = widen(key ? gk[0] : gq[0]), gb = widen(key ? gk[1] : gq[1]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                a.v[e] = a.v[e] * r * ga.v[e];
-                b.v[e] = b.v[e] * r * gb.v[e];
-            }
-            if (L.rot)
-                turn<INTER, false>(a, b, cs + t * half + 8 * L.l, sn + t * half + 8 * L.l);
-            uint16_t *y = H.out + (t0 + t) * H.out_t + h * H.out_h;
+#pragma unroll 1
+        for (int i = w; i < n; i += NW) {
+            const Loaded<BWD> v = next;
+            load(i + NW, next);
+            const int t = i / H.blocks, h = (i - t * H.blocks) * (64 / G);
+            const float *c = cs + t * half + 8 * L.l, *d = sn + t * half + 8 * L.l;
+            uint16_t *y = H.out + (t0 + t) * H.out_t + h * H.out_h + yl;
+            const bool on = FULL || h + L.sub < H.heads;
+            opaque(gain); // or they are all kept widened, 16 registers more
+            uint32_t a[4], b[4];
+            if constexpr (BWD)
+                backward_item<G, INTER, FULL>(A, L, v, gain, c, d, a, b, sum);
+            else
+                forward_item<G, INTER, FULL>(A, L, v, gain, c, d, a, b);
             if (on && L.in_a)
-                store16(y + 8 * L.ca, narrow(a));
+                store16(y, a);
             if (on && L.in_b)
-                store16(y + 8 * L.cb, narrow(b));
+                store16(y + step, b);
         }
     }
+    return s;
 }
 
-// As the forward; each lane also keeps the gain gradients of its chunks, of
-// queries and of keys, in float over its heads.  At the end the workgroup's
-// lanes are added in a fixed order into its row of the partial sums.
-template <int G, bool INTER> __global__ void __launch_bounds__(NT) bwd_kernel(Args A)
+// The steps of queries and then those of keys, dealt to the workgroups in one
+// sequence.
+template <int G, bool INTER, bool FULL> __global__ void __launch_bounds__(NT) fwd_kernel(Args A)
 {
-    __shared__ float cs[TOKENS * MAX_D / 2], sn[TOKENS * MAX_D / 2];
+    __shared__ __attribute__((aligned(16))) float cs[ANGLES], sn[ANGLES];
+    float none[16];
+    const int64_t s =
+        heads_of_kind<G, INTER, FULL, false>(A, A.q, blockIdx.x, gridDim.x, cs, sn, none);
+    heads_of_kind<G, INTER, FULL, false>(A, A.k, s - A.q.steps, gridDim.x, cs, sn, none);
+}
+
+// As the forward; each lane also keeps the gain gradients of its chunks in
+// float over its heads.  After each kind the workgroup's lanes are added in a
+// fixed order into its row of the partial sums.
+template <int G, bool INTER, bool FULL>
+__global__ void __launch_bounds__(NT) bwd_kernel(Args A)
+{
+    __shared__ __attribute__((aligned(16))) float cs[ANGLES], sn[ANGLES];
     __shared__ float red[NW * 64 / G][16 * G]; // D <= 16 G
-    const int w = threadIdx.x >> 6, half = A.R / 2;
-    const Lane<G> L(A);
-    uint4 gq[2], gk[2];
-    L.gains(A.q.gamma, gq[0], gq[1]);
-    L.gains(A.k.gamma, gk[0], gk[1]);
-    float sum[2][16] = {};
-    const int per = A.q.blocks + A.k.blocks;
-    for (int64_t t0 = (int64_t)blockIdx.x * A.tb; t0 < A.T; t0 += (int64_t)gridDim.x * A.tb) {
-        const int nt = (int)min((int64_t)A.tb, A.T - t0);
-        __syncthreads();
-        fill_angles<INTER>(A, t0, nt, cs, sn);
-        __syncthreads();
-        for (int i = w; i < nt * per; i += NW) {
-            const int t = i / per, blk = i - t * per;
-            const bool key = blk >= A.q.blocks;
-            const Heads &H = key ? A.k : A.q;
-            const int h = (key ? blk - A.q.blocks : blk) * (64 / G) + L.sub;
-            const bool on = h < H.heads;
-            const uint16_t *x = H.in + (t0 + t) * H.in_t + h * H.in_h;
-            const uint16_t *gy = H.gy + (t0 + t) * H.gy_t + h * H.gy_h;
-            const Chunk a = widen(load16(x + 8 * L.ca, on && L.in_a));
-            const Chunk b = widen(load16(x + 8 * L.cb, on && L.in_b));
-            Chunk ma = widen(load16(gy + 8 * L.ca, on && L.in_a));
-            Chunk mb = widen(load16(gy + 8 * L.cb, on && L.in_b));
-            if (L.rot)
-                turn<INTER, true>(ma, mb, cs + t * half + 8 * L.l, sn + t * half + 8 * L.l);
-            const Chunk ga = widen(key ? gk[0] : gq[0]), gb = widen(key ? gk[1] : gq[1]);
-            Chunk va, vb;
-            double S = 0.0, u = 0.0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                va.v[e] = ma.v[e] * ga.v[e];
-                vb.v[e] = mb.v[e] * gb.v[e];
-                S = __builtin_fma((double)a.v[e], (double)a.v[e], S);
-                S = __builtin_fma((double)b.v[e], (double)b.v[e], S);
-                u = __builtin_fma((double)a.v[e], (double)va.v[e], u);
-                u = __builtin_fma((double)b.v[e], (double)vb.v[e], u);
-            }
-            const float r = inverse_rms(head_sum<G>(S), A.inv_d, A.eps);
-            const double rd = (double)r;
-            const float c = (float)(rd * rd * rd * head_sum<G>(u) * A.inv_d);
-            auto gain_terms = [&](float (&to)[16]) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    to[e] += a.v[e] * r * ma.v[e];
-                    to[8 + e] += b.v[e] * r * mb.v[e];
-                }
-            };
-            if (key) // the same for the whole wave
-                gain_terms(sum[1]);
-            else
-                gain_terms(sum[0]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                va.v[e] = r * va.v[e] - c * a.v[e];
-                vb.v[e] = r * vb.v[e] - c * b.v[e];
-            }
-            uint16_t *y = H.out + (t0 + t) * H.out_t + h * H.out_h;
-            if (on && L.in_a)
-                store16(y + 8 * L.ca, narrow(va));
-            if (on && L.in_b)
-                store16(y + 8 * L.cb, narrow(vb));
-        }
-    }
-    if (!A.part)
-        return;
-    for (int which = 0; which < 2; ++which) {
-        __syncthreads();
-        float *row = red[w * (64 / G) + L.sub];
+    const Lane<G, FULL> L(A);
+    auto finish = [&](float (&sum)[16], int which) {
+        if (!A.part)
+            return;
+        float *row = red[(threadIdx.x >> 6) * (64 / G) + L.sub];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             if (L.in_a)
-                row[8 * L.ca + e] = sum[which][e];
+                row[8 * L.ca + e] = sum[e];
             if (L.in_b)
-                row[8 * L.cb + e] = sum[which][8 + e];
+                row[8 * L.cb + e] = sum[8 + e];
         }
         __syncthreads();
         for (int e = threadIdx.x; e < A.D; e += NT) {
-            float s = 0.0f;
+            float t = 0.0f;
             for (int g = 0; g < NW * 64 / G; ++g)
-                s += red[g][e];
-            A.part[((int64_t)blockIdx.x * 2 + which) * A.D + e] = s;
+                t += red[g][e];
+            A.part[((int64_t)which * gridDim.x + blockIdx.x) * A.D + e] = t;
         }
-    }
+        __syncthreads();
+    };
+    float sq[16] = {};
+    const int64_t s = heads_of_kind<G, INTER, FULL, true>(A, A.q, blockIdx.x, gridDim.x, cs, sn, sq);
+    finish(sq, 0);
+    float sk[16] = {};
+    heads_of_kind<G, INTER, FULL, true>(A, A.k, s - A.q.steps, gridDim.x, cs, sn, sk);
+    finish(sk, 1);
 }
 
-// Gain gradients: the workgroups' partial rows [P][2][D] added in double in a
+// Gain gradients: the workgroups' partial rows [2][P][D] added in double in a
 // fixed order.  Block (j, which) sums elements 8 j .. 8 j + 7 (D is a multiple
 // of 8); thread (g, q) adds rows g, g + 512, ... of four of them, so that with
 // 1024 rows a thread waits for two loads (64 elements a block and 64 loads one
@@ -351,8 +463,9 @@ __global__ void __launch_bounds__(1024) gain_kernel(const float *part, int P, in
     const int q = threadIdx.x & 1, g = threadIdx.x >> 1, which = blockIdx.y;
     const int j = blockIdx.x * 8 + 4 * q;
     double s[4] = {0.0, 0.0, 0.0, 0.0};
+    part += (int64_t)which * P * D;
     for (int p = g; p < P; p += GAIN_GROUPS) {
-        const float4 v = *reinterpret_cast<const float4 *>(part + ((int64_t)p * 2 + which) * D + j);
+        const float4 v = *reinterpret_cast<const float4 *>(part + (int64_t)p * D + j);
         s[0] += (double)v.x;
         s[1] += (double)v.y;
         s[2] += (double)v.z;
@@ -388,39 +501,53 @@ inline int group_of(int D, int R)
     return g;
 }
 
-template <bool BWD, int G> void launch_group(const Args &A, bool inter, unsigned grid, hipStream_t st)
+template <bool BWD, int G, bool INTER> void launch_group(const Args &A, unsigned grid, hipStream_t st)
 {
-    if constexpr (BWD) {
-        if (inter)
-            hipLaunchKernelGGL((bwd_kernel<G, true>), dim3(grid), dim3(NT), 0, st, A);
+    if (A.D == 16 * G && A.R == A.D && A.q.heads % (64 / G) == 0 && A.k.heads % (64 / G) == 0) {
+        if constexpr (BWD)
+            hipLaunchKernelGGL((bwd_kernel<G, INTER, true>), dim3(grid), dim3(NT), 0, st, A);
         else
-            hipLaunchKernelGGL((bwd_kernel<G, false>), dim3(grid), dim3(NT), 0, st, A);
+            hipLaunchKernelGGL((fwd_kernel<G, INTER, true>), dim3(grid), dim3(NT), 0, st, A);
     } else {
-        if (inter)
-            hipLaunchKernelGGL((fwd_kernel<G, true>), dim3(grid), dim3(NT), 0, st, A);
+        if constexpr (BWD)
+            hipLaunchKernelGGL((bwd_kernel<G, INTER, false>), dim3(grid), dim3(NT), 0, st, A);
         else
-            hipLaunchKernelGGL((fwd_kernel<G, false>), dim3(grid), dim3(NT), 0, st, A);
+            hipLaunchKernelGGL((fwd_kernel<G, INTER, false>), dim3(grid), dim3(NT), 0, st, A);
     }
 }
 
 template <bool BWD> void launch(const Args &A, bool inter, unsigned grid, hipStream_t st)
 {
     switch (group_of(A.D, A.R)) {
-    case 4: return launch_group<BWD, 4>(A, inter, grid, st);
-    case 8: return launch_group<BWD, 8>(A, inter, grid, st);
-    case 16: return launch_group<BWD, 16>(A, inter, grid, st);
-    default: return launch_group<BWD, 32>(A, inter, grid, st);
+    case 4: return inter ? launch_group<BWD, 4, true>(A, grid, st)
+                         : launch_group<BWD, 4, false>(A, grid, st);
+    case 8: return inter ? launch_group<BWD, 8, true>(A, grid, st)
+                         : launch_group<BWD, 8, false>(A, grid, st);
+    case 16: return inter ? launch_group<BWD, 16, true>(A, grid, st)
+                         : launch_group<BWD, 16, false>(A, grid, st);
+    default: return inter ? launch_group<BWD, 32, true>(A, grid, st)
+                         : launch_group<BWD, 32, false>(A, grid, st);
     }
 }
 
-// tokens a workgroup takes at a time: one where that gives the chip no more
-// than a few workgroups a compute unit
-inline int tokens_at_once(int64_t T) { return T >= 4096 ? TOKENS : 1; }
-
-inline unsigned workgroups(int64_t T, bool bwd)
+// Tokens of a step: four items (one a wave), and up to 16 as far as the angles
+// fit and that leaves every compute unit several steps.
+inline void steps_of(Heads &H, int64_t T, int R)
 {
-    const int tb = tokens_at_once(T);
-    return (unsigned)std::min<int64_t>((T + tb - 1) / tb, bwd ? 1024 : 1 << 20);
+    H.tb = 1;
+    while (2 * H.tb * std::max(R / 2, 1) <= ANGLES &&
+           (2 * H.tb * H.blocks <= NW || (2 * H.tb * H.blocks <= 4 * NW && T / (2 * H.tb) >= 1024)))
+        H.tb *= 2;
+    H.steps = H.heads ? (T + H.tb - 1) / H.tb : 0;
+}
+
+// Workgroups: forward one for each step, backward at most two a compute unit,
+// each with a row of partial sums for either gain (32768 tokens of 40 heads of
+// 128: 190 us with 512, 195 with 768, 198 with 1024, 223 with 256).
+constexpr int MAX_ROWS = 512;
+inline unsigned workgroups(const Args &A, bool bwd)
+{
+    return (unsigned)std::min<int64_t>(A.q.steps + A.k.steps, bwd ? MAX_ROWS : 1 << 20);
 }
 
 } // namespace mxq
@@ -531,10 +658,11 @@ mx_status qk_norm_rope_fwd(const mx_heads *q, const mx_heads *k, const void *q_g
     A.T = T;
     A.D = (int)D;
     A.R = (int)R;
-    A.tb = mxq::tokens_at_once(T);
     A.eps = eps;
     A.inv_d = 1.0 / (double)D;
-    mxq::launch<false>(A, interleaved != 0, mxq::workgroups(T, false), stream);
+    mxq::steps_of(A.q, T, A.R);
+    mxq::steps_of(A.k, T, A.R);
+    mxq::launch<false>(A, interleaved != 0, mxq::workgroups(A, false), stream);
     return launched();
 }
 
@@ -542,7 +670,8 @@ size_t qk_norm_rope_bwd_workspace_bytes(int64_t T, int64_t D)
 {
     if (T <= 0 || D <= 0 || T > ((int64_t)1 << 40) || D > mxq::MAX_D)
         return 0;
-    return (size_t)mxq::workgroups(T, true) * 2 * (size_t)D * sizeof(float);
+    // no more steps than tokens of each kind
+    return 2 * (size_t)std::min<int64_t>(mxq::MAX_ROWS, 2 * T) * (size_t)D * sizeof(float);
 }
 
 mx_status qk_norm_rope_bwd(const mx_heads *grad_q_out, const mx_heads *grad_k_out, const mx_heads *q,
@@ -585,11 +714,13 @@ mx_status qk_norm_rope_bwd(const mx_heads *grad_q_out, const mx_heads *grad_k_ou
     A.T = T;
     A.D = (int)D;
     A.R = (int)R;
-    A.tb = mxq::tokens_at_once(T);
     A.eps = eps;
     A.inv_d = 1.0 / (double)D;
-    const unsigned grid = mxq::workgroups(T, true);
-    mxq::launch<true>(A, interleaved != 0, grid, stream);
+    mxq::steps_of(A.q, T, A.R);
+    mxq::steps_of(A.k, T, A.R);
+    const unsigned grid = mxq::workgroups(A, true);
+    if (grid > 0)
+        mxq::launch<true>(A, interleaved != 0, grid, stream);
     if (gains)
         hipLaunchKernelGGL(mxq::gain_kernel, dim3((unsigned)(D / 8), 2), dim3(1024), 0, stream,
                            A.part, (int)grid, (int)D, grad_q_gamma, grad_k_gamma);
