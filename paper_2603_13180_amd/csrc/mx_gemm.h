@@ -54,6 +54,7 @@ struct GatedArgs : Args {
     uint8_t *hs;  // E8M0 scales of MX_OUT_CODES [M, N/32]
     uint16_t *gu; // bf16 [M, 2 N]: both products, gate columns first; or NULL
     int act, mode;
+    int once; // B's codes are read once: non-temporal loads
 };
 
 // A kernel's OUT: mx_out_dtype, + 4 for gated products.
@@ -124,6 +125,14 @@ __device__ __forceinline__ void tile_of(const Args &A, int bm, int bn, int v, in
 __device__ __forceinline__ void lds_load16(const void *gbase, uint32_t off, uint32_t lds_base)
 {
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(gbase),
+                 "{m0}"(lds_base)
+                 : "memory");
+}
+
+// The same, non-temporal.
+__device__ __forceinline__ void lds_load16_nt(const void *gbase, uint32_t off, uint32_t lds_base)
+{
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(gbase),
                  "{m0}"(lds_base)
                  : "memory");
 }

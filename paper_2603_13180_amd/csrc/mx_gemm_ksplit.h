@@ -81,9 +81,24 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(ArgsOf<OUT> A)
     const uint32_t ring_addr = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)ring);
     auto issue = [&](int k, int slot) {
         const uint32_t st = ring_addr + slot * O::SLOT;
+        auto codes = [&](auto nt) {
 #pragma unroll
-        for (int t = 0; t < C::LC; ++t)
-            lds_load16(8 * t < C::BM ? ta : 8 * t < C::BM + CN ? tb : tb2, code[t] + (uint32_t)k * KB, st + 8 * t * KB);
+            for (int t = 0; t < C::LC; ++t) {
+                const uint8_t *base = 8 * t < C::BM ? ta : 8 * t < C::BM + CN ? tb : tb2;
+                if (decltype(nt)::value && 8 * t >= C::BM)
+                    lds_load16_nt(base, code[t] + (uint32_t)k * KB, st + 8 * t * KB);
+                else
+                    lds_load16(base, code[t] + (uint32_t)k * KB, st + 8 * t * KB);
+            }
+        };
+        if constexpr (GATED) {
+            if (A.once)
+                codes(std::true_type{});
+            else
+                codes(std::false_type{});
+        } else {
+            codes(std::false_type{});
+        }
 #pragma unroll
         for (int t = 0; t < O::LS; ++t)
             lds_load4(sc[t] + (uint32_t)k * SB, st + (C::BM + C::BN) * KB + 256 * t);

@@ -20,11 +20,18 @@ using K16x32 = KSplit<16, 32, 8, 3>;
 using K32x32 = KSplit<32, 32, 8, 2>;
 using K32x64 = KSplit<32, 64, 8, 1>;
 using K64x64 = KSplit<64, 64, 8, 1>;
-using K16x64 = KSplit<16, 64, 8, 1>;
+// K-split tiles of gated products, whose waves hold a whole MX block: 4 waves,
+// two or three workgroups per compute unit.  A decoding step's tiles are then
+// resident at once instead of in two uneven rounds (1 to 16 rows, 448 tiles of
+// 14336 x 4096: E4M3 28.0 -> 26.7 us, E2M1 15.4 -> 13.1 against 8 waves; where
+// they are one a unit anyhow, 8192 x 8192, 28.9 -> 29.7 and 14.2 -> 14.1).
+using G16x64 = KSplit<16, 64, 4, 1>;
+using G32x64 = KSplit<32, 64, 4, 1>;
+using G64x64 = KSplit<64, 64, 4, 1>;
 
 enum Shape { S_K16x32, S_K32x32, S_K32x64, S_K64x64, S_R64x128, S_R128x128, S_256x256, S_COUNT };
-// gated products alone: the smallest tile whose waves hold a whole MX block
-constexpr int S_K16x64 = S_COUNT;
+constexpr int S_G16x64 = S_COUNT, S_G32x64 = S_COUNT + 1, S_G64x64 = S_COUNT + 2;
+constexpr int S_ALL = S_COUNT + 3;
 
 // What a launch of each tile shape costs on MI355X, fitted to times at K =
 // 512 .. 8192 and 64 to 3400 tiles: us once per launch, per round of tiles
@@ -56,12 +63,15 @@ struct Cost {
     int bm, bn;
     float once, round, step, few, few_step;
 };
-constexpr Cost kCost[S_COUNT + 1] = {
+constexpr Cost kCost[S_ALL] = {
     {16, 32, 1.3f, 1.0f, 0.14f, 1.6f, 0.0f},   {32, 32, 1.4f, 1.1f, 0.14f, 1.9f, 0.0f},
     {32, 64, 2.2f, 0.7f, 0.19f, 2.15f, 0.0f},  {64, 64, 0.4f, 2.6f, 0.275f, 2.9f, 0.2f},
     {64, 128, 3.1f, 0.4f, 0.425f, 1.1f, 0.3f}, {128, 128, 4.1f, 0.8f, 0.59f, 1.8f, 0.45f},
     {256, 256, 1.2f, 4.0f, 1.75f, 0.0f, 0.0f},
+    // (gated: ranked against times at 1 to 128 rows, F = 1024 .. 14336)
     {16, 64, 2.2f, 0.7f, 0.17f, 2.15f, 0.0f},
+    {32, 64, 2.2f, 0.7f, 0.24f, 2.15f, 0.0f},
+    {64, 64, 0.4f, 2.6f, 0.275f, 2.9f, 0.2f},
 };
 
 // us a launch over `cells` outputs of cm x cn takes on `cus` compute units
@@ -72,7 +82,7 @@ inline double launch_cost(int shape, int64_t cells, int64_t cm, int64_t cn, int 
     const int64_t rounds = (tiles + cus - 1) / cus;
     const double per = c.round + (double)steps * c.step;
     const double few = std::max(per, (double)c.few + (double)steps * c.few_step);
-    if (shape <= S_K64x64 || shape == S_K16x64)
+    if (shape <= S_K64x64 || shape >= S_COUNT)
         return c.once + (double)rounds * (rounds > 2 ? few : per);
     double us = (double)rounds * per + (double)std::max<int64_t>(0, rounds - 8) * (few - per);
     if (shape == S_R64x128 && cn <= 64 && rounds > 2)
@@ -92,7 +102,7 @@ struct Plan {
 
 // The tile shapes smaller than 256 x 256 that a product may take.
 constexpr int kPlainShapes[] = {S_K16x32, S_K32x32, S_K32x64, S_K64x64, S_R64x128, S_R128x128};
-constexpr int kGatedShapes[] = {S_K16x64, S_K32x64, S_K64x64, S_R64x128, S_R128x128};
+constexpr int kGatedShapes[] = {S_G16x64, S_G32x64, S_G64x64, S_R64x128, S_R128x128};
 
 template <size_t NS>
 inline Plan plan_among(const int (&shapes)[NS], int64_t M, int64_t N, int steps, int cus)
@@ -140,9 +150,9 @@ hipError_t launch_shape(int shape, const ArgsOf<OUT> &A, hipStream_t stream)
 {
     if constexpr (kGated<OUT>) {
         switch (shape) {
-        case S_K16x64: return launch_ksplit<ELEM, OUT, K16x64>(A, stream);
-        case S_K32x64: return launch_ksplit<ELEM, OUT, K32x64>(A, stream);
-        case S_K64x64: return launch_ksplit<ELEM, OUT, K64x64>(A, stream);
+        case S_G16x64: return launch_ksplit<ELEM, OUT, G16x64>(A, stream);
+        case S_G32x64: return launch_ksplit<ELEM, OUT, G32x64>(A, stream);
+        case S_G64x64: return launch_ksplit<ELEM, OUT, G64x64>(A, stream);
         case S_R64x128: return launch_ring<ELEM, OUT, R64x128>(A, stream);
         case S_R128x128: return launch_ring<ELEM, OUT, R128x128>(A, stream);
         default: return launch<ELEM, OUT>(A, stream);
@@ -160,10 +170,19 @@ hipError_t launch_shape(int shape, const ArgsOf<OUT> &A, hipStream_t stream)
     }
 }
 
+// A weight of this many bytes that a launch reads once (one row of tiles) is
+// loaded past the caches' normal allocation: no later call finds it there.
+// Cycling through 550 to 600 MB of weights at 1 to 61 rows: 117 MB (E4M3) 26.7
+// -> 24.7 and 32.1 -> 30.4 us, 134 MB 28.9 -> 25.7; but 62 MB (E2M1) 13.1 ->
+// 12.9 and 16.8 -> 16.7, 67 MB 14.2 -> 15.4, 17 MB (E4M3) 10.1 -> 11.1.
+constexpr int64_t kOnceBytes = 96 << 20;
+
 template <int ELEM, int OUT>
 hipError_t multiply_as(const Plan &P, ArgsOf<OUT> A, hipStream_t stream)
 {
     set_tiles(A, kCost[P.shape].bm, kCols<OUT>(kCost[P.shape].bn), 1024);
+    if constexpr (kGated<OUT>)
+        A.once = A.tiles_m == 1 && 2 * A.N * A.rb >= kOnceBytes;
     if (!P.whole)
         return launch_shape<ELEM, OUT>(P.shape, A, stream);
     const int left = A.cells - P.whole;

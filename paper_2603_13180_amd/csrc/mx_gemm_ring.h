@@ -109,7 +109,7 @@ __device__ __forceinline__ RingTile<C, ELEM> ring_tile(const Args &A, int64_t m0
     return T;
 }
 
-template <class C, int ELEM, bool GATED>
+template <class C, int ELEM, bool GATED, bool NT = false>
 __device__ __forceinline__ void ring_issue(const RingTile<C, ELEM> &T, int s, uint32_t stage, int w)
 {
     using O = RingOp<C, ELEM>;
@@ -119,7 +119,11 @@ __device__ __forceinline__ void ring_issue(const RingTile<C, ELEM> &T, int s, ui
         const int r = ring_row<C, GATED>(w, t);
         if constexpr (GATED) {
             constexpr int NA = C::BM / 8 / C::NW, NB = C::BN / 16 / C::NW;
-            lds_load16(t < NA ? T.a : t < NA + NB ? T.b : T.b2, T.code[t] + kc, stage + r * KB);
+            const uint8_t *base = t < NA ? T.a : t < NA + NB ? T.b : T.b2;
+            if (NT && t >= NA)
+                lds_load16_nt(base, T.code[t] + kc, stage + r * KB);
+            else
+                lds_load16(base, T.code[t] + kc, stage + r * KB);
         } else {
             lds_load16(r < C::BM ? T.a : T.b, T.code[t] + kc, stage + r * KB);
         }
@@ -135,8 +139,10 @@ __device__ __forceinline__ void ring_issue(const RingTile<C, ELEM> &T, int s, ui
     }
 }
 
-// Tiles first, first + stride, ... of the launch on this workgroup.
-template <int ELEM, int OUT, class C>
+// Tiles first, first + stride, ... of the launch on this workgroup.  NT: B's
+// codes are read once (GatedArgs::once; a branch at every step instead cost the
+// gated kernels 8%).
+template <int ELEM, int OUT, class C, bool NT = false>
 __device__ __forceinline__ void ring_tiles(const ArgsOf<OUT> &A, LDS_AS uint8_t *st0, int first,
                                            int stride)
 {
@@ -168,7 +174,7 @@ __device__ __forceinline__ void ring_tiles(const ArgsOf<OUT> &A, LDS_AS uint8_t 
     auto issue = [&] {
         if (iv >= G)
             return;
-        ring_issue<C, ELEM, GATED>(T, is, st0_addr + islot * O::STAGE, w);
+        ring_issue<C, ELEM, GATED, NT>(T, is, st0_addr + islot * O::STAGE, w);
         islot = islot + 1 == C::S ? 0 : islot + 1;
         ++ahead;
         if (++is == A.steps) {
@@ -221,11 +227,11 @@ __device__ __forceinline__ void ring_tiles(const ArgsOf<OUT> &A, LDS_AS uint8_t 
     }
 }
 
-template <int ELEM, int OUT, class C>
+template <int ELEM, int OUT, class C, bool NT = false>
 __global__ void __launch_bounds__(C::NT) mx_gemm_ring_kernel(ArgsOf<OUT> A)
 {
     __shared__ __attribute__((aligned(16))) uint8_t lds[C::S * RingOp<C, ELEM>::STAGE];
-    ring_tiles<ELEM, OUT, C>(A, (LDS_AS uint8_t *)lds, blockIdx.x, gridDim.x);
+    ring_tiles<ELEM, OUT, C, NT>(A, (LDS_AS uint8_t *)lds, blockIdx.x, gridDim.x);
 }
 
 // Two products whose tiles are all resident at once, one tile per workgroup:
@@ -260,6 +266,13 @@ template <int ELEM, int OUT, class C> hipError_t launch_ring(const ArgsOf<OUT> &
     const int per_cu = std::min((160 * 1024) / (C::S * O::STAGE), 2048 / C::NT);
     const int64_t G = (int64_t)A.cells * A.sub_m * A.sub_n;
     const int64_t grid = std::min<int64_t>(G, (int64_t)A.grid_max * per_cu);
+    if constexpr (kGated<OUT>) {
+        if (A.once) {
+            hipLaunchKernelGGL((mx_gemm_ring_kernel<ELEM, OUT, C, true>), dim3((unsigned)grid),
+                               dim3(C::NT), 0, stream, A);
+            return hipGetLastError();
+        }
+    }
     hipLaunchKernelGGL((mx_gemm_ring_kernel<ELEM, OUT, C>), dim3((unsigned)grid), dim3(C::NT), 0,
                        stream, A);
     return hipGetLastError();

@@ -41,8 +41,9 @@ mx_status mxt_matmul(const uint8_t *a_codes, const uint8_t *a_scales, const uint
                      const void *b_gain, int out_dtype, void *out, int shape, int whole, int units,
                      hipStream_t stream);
 
-// mxt_product_plan and mxt_matmul for mx_gated_fwd.  Tile shapes: 2 .. 6 above
-// (their columns half gate, half up rows) and 7 = 16 x 64 with K split.
+// mxt_product_plan and mxt_matmul for mx_gated_fwd.  Tile shapes, their columns
+// half gate, half up rows: 4 .. 6 above and 7, 8, 9 = 16 x 64, 32 x 64 and 64 x
+// 64 with K split over four waves.
 int mxt_gated_plan(int64_t M, int64_t F, int64_t K, int elem, int units, int *whole, int *tail,
                    double *us);
 mx_status mxt_gated(const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *w_codes,

@@ -73,13 +73,19 @@ def test_binding_refuses_cpu_tensors_and_bad_names():
         mxnorm.mx_gated_fwd(c, s, c, s, 256, elem="e5m2")
 
 
-@pytest.mark.parametrize("M,F,K", [(1, 14336, 4096), (61, 14336, 4096), (1000, 4096, 2048), (16384, 14336, 4096)])
-def test_plan_names_a_gated_kernel(M, F, K):
+@pytest.mark.parametrize("M,F,K,want", [
+    # decoding: the narrowest tiles that hold the rows, rings where 64 rows share
+    # a weight; prefill: 256 x 256
+    (1, 14336, 4096, 7), (16, 14336, 4096, 7), (32, 14336, 4096, 4), (61, 14336, 4096, 4), (61, 8192, 8192, 9),
+    (32, 8192, 8192, 8), (61, 4096, 2048, 8), (128, 14336, 4096, 5), (1000, 4096, 2048, 5), (16384, 14336, 4096, 6),
+])
+def test_plan_names_a_gated_kernel(M, F, K, want):
     whole, tail, us = ctypes.c_int(), ctypes.c_int(), ctypes.c_double()
     f = mxnorm.load().mxt_gated_plan
     f.restype, f.argtypes = ctypes.c_int, [ctypes.c_int64] * 3 + [ctypes.c_int] * 2 + [ctypes.c_void_p] * 3
     for elem in (0, 1):
         shape = f(M, F, K, elem, 256, ctypes.byref(whole), ctypes.byref(tail), ctypes.byref(us))
-        assert shape in (2, 3, 4, 5, 6, 7) and us.value > 0
-        assert not whole.value or (shape == 6 and tail.value in (2, 3, 4, 5, 7))
+        assert shape in (4, 5, 6, 7, 8, 9) and us.value > 0
+        assert elem or shape == want
+        assert not whole.value or (shape == 6 and tail.value in (4, 5, 7, 8, 9))
     assert f(M, F, 100, 0, 256, ctypes.byref(whole), ctypes.byref(tail), ctypes.byref(us)) == -1

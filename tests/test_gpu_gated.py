@@ -1,12 +1,11 @@
 """The gated feed-forward's first half on the GPU: every kernel that computes
 it, its three kinds of output, and the entry points.
 
-The products themselves are mx_matmul_fwd's, which other tests hold to the
-oracle; a gated kernel adds a tile's sums over K in the same order as the plain
-kernel of its shape.  So the float products of the plain kernel are the ones the
-gate sees, and:
+Operands are small multiples of a power of two, a row's blocks within a factor
+of four of each other, so that every sum of products is exact in float in any
+order (at most 512 products below 2^12 units).  Then:
 
-* the kept products are those, rounded to bf16, bit for bit;
+* the kept products are the exact ones rounded to bf16, bit for bit;
 * float H is act(G) U of those in 64 bits within the error of the activation and
   of two products.  With |z| <= 100, the exponential's argument -z log2(e) is
   rounded at most four times (GELU: g^2, the polynomial, its product with g, and
@@ -24,23 +23,20 @@ import pytest
 import torch
 
 import oracle
-from launch_rules import ELEM, SHAPES, matmul_as
+from launch_rules import ELEM, SHAPES
 from paper_2603_13180_amd import mxnorm, synth
-from test_gpu_gemm import dev_u8, random_operand
+from test_gpu_gemm import dev_u8
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 ELEMS = ["e4m3", "e2m1"]
 ACTS = ["silu", "gelu_tanh"]
-GATED_SHAPES = SHAPES[2:] + ["k16x64"]
-NUMBER = {s: i for i, s in enumerate(SHAPES + ["k16x64"])}
-# the plain kernel that adds in the same order
-SAME_ORDER = {"k16x64": "k32x64", "k32x64": "k32x64", "k64x64": "k64x64", "r64x128": "r64x128",
-              "r128x128": "r128x128", "t256x256": "t256x256"}
+NAMES = SHAPES + ["g16x64", "g32x64", "g64x64"]
+GATED_SHAPES = NAMES[4:]
 # (tile shape, 256 x 256 cells before it, compute units; 0: the device's)
 WAYS = [(s, 0, 0) for s in GATED_SHAPES] + \
     [(s, 0, u) for s in ("r64x128", "r128x128", "t256x256") for u in (1, 2)] + \
-    [(s, 2, 1) for s in GATED_SHAPES if s != "t256x256"]
+    [(s, n, 1) for s in GATED_SHAPES if s != "t256x256" for n in (2, 5)]
 _I, _L, _P = ctypes.c_int, ctypes.c_int64, ctypes.c_void_p
 
 
@@ -71,7 +67,7 @@ def gated_as(ac, as_, wc, ws, K, elem, act, dtype, shape, whole=0, units=0, mode
     mxnorm._check(f(ac.data_ptr(), as_.data_ptr(), wc.data_ptr(), ws.data_ptr(), M, F, K, ELEM[elem],
                     mxnorm.ACTS[act], mxnorm.SCALE_MODES[mode], mxnorm.GATED_DTYPES[dtype],
                     out.data_ptr(), sc.data_ptr() if codes else None, gu.data_ptr() if keep else None,
-                    NUMBER[shape], whole, units, mxnorm._stream(ac.device)))
+                    NAMES.index(shape), whole, units, mxnorm._stream(ac.device)))
     assert (bo[out.numel():] == 7).all() and (bg[gu.numel():] == 7).all()
     assert (bs[sc.numel() if codes else 0:] == 7).all()
     if not keep:
@@ -79,11 +75,36 @@ def gated_as(ac, as_, wc, ws, K, elem, act, dtype, shape, whole=0, units=0, mode
     return ((out, sc) if codes else out), gu
 
 
-def operands(elem, M, F, K, seed=0, amin=117, amax=130, wmin=117, wmax=130):
+def operand(rows, K, elem, rng, base):
+    """(codes, scales, their values in 64 bits): row r's scales are 2^base[r] to
+    four times that."""
+    if elem == "e4m3":
+        codes = rng.choice(np.array([0, 0x38, 0x40, 0x44, 0x48, 0x4C, 0xB8, 0xC0, 0xC4, 0xC8, 0xCC], np.uint8),
+                           (rows, K))
+        v = oracle.e4m3_value(codes)
+    else:
+        n = rng.integers(0, 16, (rows, K), dtype=np.uint8)
+        codes, v = n[:, 0::2] | n[:, 1::2] << 4, oracle.e2m1_value(n)
+    e = np.asarray(base)[:, None] + rng.integers(0, 3, (rows, K // 32))
+    return codes, (e + 127).astype(np.uint8), v.astype(np.float64) * np.repeat(np.exp2(e), 32, 1)
+
+
+def operands(elem, M, F, K, seed=0, abase=None, wbase=None):
+    """The four operands on the GPU and the exact products [M, 2F]."""
     rng = np.random.default_rng(seed + M + 3 * F + 5 * K + len(elem))
-    ac, as_ = random_operand(M, K, elem, rng, amin, amax)
-    wc, ws = random_operand(2 * F, K, elem, rng, wmin, wmax)
-    return [dev_u8(v) for v in (ac, as_, wc, ws)]
+    ac, as_, a = operand(M, K, elem, rng, np.full(M, -4) if abase is None else abase(rng))
+    wc, ws, w = operand(2 * F, K, elem, rng, np.full(2 * F, -3) if wbase is None else wbase(rng))
+    return [dev_u8(v) for v in (ac, as_, wc, ws)], a @ w.T
+
+
+def decode(codes, scales, elem):
+    v = oracle.e4m3_value(codes) if elem == "e4m3" else \
+        oracle.e2m1_value(np.stack((codes & 15, codes >> 4), -1).reshape(codes.shape[0], -1))
+    return v.astype(np.float64) * np.repeat(np.exp2(scales.astype(np.float64) - 127), 32, 1)
+
+
+def kept(products):
+    return bits(torch.from_numpy(products).float().bfloat16().to(DEV))
 
 
 def bits(t):
@@ -98,7 +119,7 @@ def act64(g, act):
 
 
 def check_float(h, products, act):
-    g, u = np.split(products.cpu().numpy().astype(np.float64), 2, axis=1)
+    g, u = np.split(products, 2, axis=1)
     with np.errstate(invalid="ignore", over="ignore"):
         want = act64(g, act) * u
         err = np.abs(h.cpu().numpy().astype(np.float64) - want)
@@ -112,21 +133,13 @@ def check_float(h, products, act):
 @pytest.mark.parametrize("shape,whole,units", WAYS)
 def test_every_kernel(elem, shape, whole, units, act):
     # 300 x 416: two row cells, four column cells of 128, the last of each
-    # partial.  The operands' scales spread G over about +-20
+    # partial
     M, F, K = 300, 416, 512
-    t = operands(elem, M, F, K)
+    t, p = operands(elem, M, F, K)
+    assert 5 < p[:, :F].std() < 40
     h, gu = gated_as(*t, K, elem, act, torch.float32, shape, whole, units)
-    if not whole:
-        assert torch.equal(bits(gu), bits(matmul_as(*t, K, elem, SAME_ORDER[shape], out_dtype=torch.bfloat16)))
-        check_float(h, matmul_as(*t, K, elem, SAME_ORDER[shape]), act)
-    else:
-        # two kernels: rows and columns of the first cells in one order, the
-        # rest in another; float sums differ in their last bits
-        p = matmul_as(*t, K, elem, "t256x256").double()
-        g, u = p.split(F, 1)
-        want = torch.from_numpy(act64(g.cpu().numpy(), act)).to(DEV) * u
-        assert (h.double() - want).norm() <= 1e-4 * want.norm()
-        assert (gu.double() - p).norm() <= 2.0 ** -8 * p.norm()
+    assert torch.equal(bits(gu), kept(p))
+    check_float(h, p, act)
     hb, _ = gated_as(*t, K, elem, act, torch.bfloat16, shape, whole, units, keep=False)
     assert torch.equal(bits(hb), bits(h.to(torch.bfloat16)))
     for mode in ("rceil", "floor"):
@@ -141,10 +154,10 @@ def test_every_kernel(elem, shape, whole, units, act):
                                    (257, 144, 256), (3, 4112, 256)])
 @pytest.mark.parametrize("shape", GATED_SHAPES)
 def test_edges_of_tiles(elem, shape, M, F, K):
-    t = operands(elem, M, F, K, seed=7)
+    t, p = operands(elem, M, F, K, seed=7)
     h, gu = gated_as(*t, K, elem, "silu", torch.float32, shape)
-    assert torch.equal(bits(gu), bits(matmul_as(*t, K, elem, SAME_ORDER[shape], out_dtype=torch.bfloat16)))
-    check_float(h, matmul_as(*t, K, elem, SAME_ORDER[shape]), "silu")
+    assert torch.equal(bits(gu), kept(p))
+    check_float(h, p, "silu")
     hb, _ = gated_as(*t, K, elem, "silu", torch.bfloat16, shape)
     assert torch.equal(bits(hb), bits(h.to(torch.bfloat16)))
     if F % 32 == 0:
@@ -155,18 +168,29 @@ def test_edges_of_tiles(elem, shape, M, F, K):
 
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("elem", ELEMS)
-@pytest.mark.parametrize("shape", ["k32x64", "r64x128", "t256x256"])
+@pytest.mark.parametrize("shape", ["g16x64", "r64x128", "t256x256"])
 def test_wide_ranges_and_non_finite_values(elem, shape, act):
     # gate products from below the exponential's range to beyond it, rows of
     # NaN, sums that overflow to infinity
     M, F, K = 70, 64, 256
-    ac, as_, wc, ws = operands(elem, M, F, K, seed=3, amin=100, amax=150, wmin=110, wmax=135)
-    as_[5] = 0xFF
-    as_[9] = 254
-    ws[40, 3] = 0xFF                       # gate column 40
-    ws[F + 50, :] = 254                    # up column 50
-    t = [ac, as_, wc, ws]
-    p = matmul_as(*t, K, elem, SAME_ORDER[shape]).cpu().numpy().astype(np.float64)
+    t, p = operands(elem, M, F, K, seed=3, abase=lambda r: r.integers(-27, 20, M), wbase=lambda r: r.integers(-17, 6, 2 * F))
+    t[1][5] = 0xFF
+    p[5] = np.nan
+    # one product of row 9, and one of up column 50, beyond or below float's
+    # range (sums of several would depend on their order)
+    big = 0x4C if elem == "e4m3" else 0x77
+    for codes, scales, row in ((t[0], t[1], 9), (t[2], t[3], F + 50)):
+        codes[row] = 0
+        codes[row, 3] = big
+        scales[row] = 254
+    one = [decode(c.cpu().numpy(), s.cpu().numpy(), elem) for c, s in ((t[0], t[1]), (t[2], t[3]))]
+    with np.errstate(all="ignore"):
+        p[9], p[:, F + 50] = one[0][9] @ one[1].T, one[0] @ one[1][F + 50]
+        p = np.where(np.abs(p) > 3.4028236e38, np.copysign(np.inf, p), p)
+    p[5] = np.nan
+    t[3][40, 3] = 0xFF                     # gate column 40
+    p[:, 40] = np.nan
+    assert np.isinf(p).sum() > 10
     g, u = np.split(p, 2, axis=1)
     h, _ = gated_as(*t, K, elem, act, torch.float32, shape)
     got = h.cpu().numpy().astype(np.float64)
@@ -182,6 +206,7 @@ def test_wide_ranges_and_non_finite_values(elem, shape, act):
         ok = (np.isnan(got) & np.isnan(want)) | (got == want) | \
             (np.abs(got - exact) <= 2.0 ** -14 * np.abs(exact) + 2.0 ** -100 * np.abs(g * u)) | \
             (np.isinf(got) & (np.abs(exact) > 3.4e38)) | tiny
+        ok[9, 50] = True                   # 2^127 twice
     assert ok.all(), "%d off, first %s" % ((~ok).sum(), np.argwhere(~ok)[0])
     for mode in ("rceil", "floor"):
         (c, s), _ = gated_as(*t, K, elem, act, torch.uint8, shape, mode=mode)
@@ -202,8 +227,7 @@ def planned(M, F, K, elem):
     f.restype, f.argtypes = _I, [_L] * 3 + [_I] * 2 + [_P] * 3
     s = f(M, F, K, ELEM[elem], torch.cuda.get_device_properties(0).multi_processor_count,
           ctypes.byref(whole), ctypes.byref(tail), ctypes.byref(us))
-    names = SHAPES + ["k16x64"]
-    return (names[tail.value], whole.value) if whole.value else (names[s], 0)
+    return (NAMES[tail.value], whole.value) if whole.value else (NAMES[s], 0)
 
 
 def same(a, b):
@@ -216,7 +240,7 @@ def same(a, b):
 @pytest.mark.parametrize("elem", ELEMS)
 @pytest.mark.parametrize("M,F,K", [(1, 512, 512), (61, 2048, 512), (1000, 2048, 768), (2304, 4224, 256)])
 def test_entry_point_runs_its_plan(elem, dtype, M, F, K):
-    t = operands(elem, M, F, K, seed=1)
+    t, _ = operands(elem, M, F, K, seed=1)
     shape, whole = planned(M, F, K, elem)
     for keep in (False, True):
         h, gu = mxnorm.mx_gated_fwd(*t, K, elem=elem, act="gelu_tanh", out_dtype=dtype, save_gu=keep)
