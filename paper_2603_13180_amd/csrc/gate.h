@@ -29,22 +29,23 @@ template <int ACT> __device__ __forceinline__ float gate_sigma(float g)
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));
 }
 
-// Gradients of act(g) u: dg = gh u act'(g), act' = sigma + g sigma (1 - sigma)
-// z'(g), and du = gh act(g).  The second term of act' is 0 beyond |g| = 128 in
-// float, where its g is held there: a finite polynomial times 0, also for
-// infinite g.  A NaN g fails the comparison and stays.
+// Gradients of act(g) u: dg = gh u act'(g), act' = sigma (1 + g (1 - sigma)
+// z'(g)), and du = gh act(g).  Beyond |g| = 128 the second term is 0 in float,
+// or sigma is: its g is held there, a finite polynomial times 0, also for
+// infinite g.  (A NaN g, which the clamp would drop, is in sigma.)
 template <int ACT>
 __device__ __forceinline__ void gate_gradient(float g, float u, float gh, float &dg, float &du)
 {
     const float s = gate_sigma<ACT>(g);
-    const float gc = __builtin_fabsf(g) > 128.0f ? __builtin_copysignf(128.0f, g) : g;
-    float t = gc * s * (1.0f - s);
+    const float gc = __builtin_amdgcn_fmed3f(g, -128.0f, 128.0f);
+    float t = gc;
     if constexpr (ACT == MX_ACT_GELU_TANH) {
         constexpr float c = 1.5957691216f;
         t *= __builtin_fmaf(gc * gc, c * 3.0f * 0.044715f, c);
     }
-    dg = gh * u * (s + t);
-    du = gh * (g * s);
+    const float hs = gh * s;
+    dg = hs * u * __builtin_fmaf(t, 1.0f - s, 1.0f);
+    du = hs * g;
 }
 
 // gate_gradient of 8 bf16 columns, rounded to bf16: what the casts of a
