@@ -405,7 +405,7 @@ __device__ __forceinline__ void store_gated(const GatedArgs &A, const v4f (&acc)
 template <int OUT, int FM>
 constexpr int kGatedStores = OUT == kGate + MX_OUT_F32    ? 2 * FM
                              : OUT == kGate + MX_OUT_BF16 ? FM
-                                                          : FM + (FM + 3) / 4;
+                                                          : (FM + 1) / 2 + (FM + 3) / 4;
 template <int FM> constexpr int kKeptStores = 2 * FM;
 
 } // namespace mxg

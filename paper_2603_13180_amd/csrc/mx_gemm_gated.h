@@ -34,12 +34,48 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(void *p, int64_t byt
     return __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t *>(p) + byte, 0, 0x7FFFFFFF, 0x00020000);
 }
 
+// The codes of two row groups from mr as gated_rows leaves them: lane rows 0 and
+// 1 store 16 columns each of the first group's rows, lane rows 2 and 3 of the
+// second's.  One row group at a time, 8 columns a lane: E2M1 [8192, 14336] over
+// K 4096 500 us instead of 491, with gate and up 580 instead of 551.
+// Ordinary stores, since a product reads the codes next; beside gate and up,
+// five times their size in E4M3, the codes would lose their place in the caches
+// anyway, and non-temporal stores make [8192, 14336] 874 us instead of 926,
+// [16384, 14336] 1743 instead of 2031 (E2M1: 551 instead of 513 for the codes
+// alone, so ordinary).
+template <int ELEM>
+__device__ __forceinline__ void store_codes(const GatedArgs &A, const uint32_t (&c0)[2],
+                                            const uint32_t (&c1)[2], int64_t mr, int64_t nc, int g, int qd)
+{
+    const int r = 16 * (g >> 1) + qd;
+    const int64_t n = nc + 16 * (g & 1);
+    const bool in = mr + r < A.M && n < A.N;
+    const uint32_t off = (uint32_t)(r * A.N + n);
+    const auto x = __builtin_amdgcn_permlane32_swap(c0[0], c1[0], false, false);
+    if constexpr (ELEM == MX_ELEM_E4M3) {
+        const auto y = __builtin_amdgcn_permlane32_swap(c0[1], c1[1], false, false);
+        const __amdgpu_buffer_rsrc_t rs = rows_rsrc(A.out, mr * A.N);
+        const u32x4 v = {x[0], y[0], x[1], y[1]};
+        if (in) {
+            if (A.gu)
+                __builtin_amdgcn_raw_buffer_store_b128(v, rs, (int)off, 0, mxk::kBufNT);
+            else
+                __builtin_amdgcn_raw_buffer_store_b128(v, rs, (int)off, 0, 0);
+        }
+    } else {
+        if (in)
+            __builtin_amdgcn_raw_buffer_store_b64(mxk::u32x2_t{x[0], x[1]},
+                                                  rows_rsrc(A.out, mr * (A.N / 2)), (int)(off / 2), 0, 0);
+    }
+}
+
 // 16 rows from mr, 32 output columns from nc: gate products p[0], p[1], up
-// products p[2], p[3].  Returns the block's E8M0 byte (MX_OUT_CODES), the same
-// in the four lanes of a row.
+// products p[2], p[3].  MX_OUT_CODES: returns the block's E8M0 byte, the same in
+// the four lanes of a row, and in `codes` the codes of this lane's 8 columns
+// (E2M1: in codes[0]); the other outputs are stored.
 template <int ELEM, int OUT, int ACT>
 __device__ __forceinline__ uint32_t gated_rows(const GatedArgs &A, const v4f (&p)[4], int64_t mr,
-                                               int64_t nc, int g, int qd)
+                                               int64_t nc, int g, int qd, uint32_t (&codes)[2])
 {
     constexpr int O = OUT - kGate;
     const bool row = mr + qd < A.M;
@@ -125,17 +161,8 @@ __device__ __forceinline__ uint32_t gated_rows(const GatedArgs &A, const v4f (&p
             }
         }
         const auto s = __builtin_amdgcn_permlane16_swap(q[0], q[1], false, false);
-        if constexpr (ELEM == MX_ELEM_E4M3) {
-            const __amdgpu_buffer_rsrc_t rs = rows_rsrc(A.out, mr * A.N);
-            if (in8)
-                __builtin_amdgcn_raw_buffer_store_b64(mxk::u32x2_t{s[0], s[1]}, rs,
-                                                      (int)(uint32_t)(qd * A.N + n8), 0, 0);
-        } else {
-            const __amdgpu_buffer_rsrc_t rs = rows_rsrc(A.out, mr * (A.N / 2));
-            if (in8)
-                __builtin_amdgcn_raw_buffer_store_b32(s[0] | (s[1] << 16), rs,
-                                                      (int)(uint32_t)((qd * A.N + n8) / 2), 0, 0);
-        }
+        codes[0] = ELEM == MX_ELEM_E4M3 ? s[0] : s[0] | (s[1] << 16);
+        codes[1] = s[1];
         return byte;
     }
 }
@@ -144,13 +171,29 @@ template <int ELEM, int OUT, int ACT, int FM>
 __device__ __forceinline__ void store_gated_act(const GatedArgs &A, const v4f (&acc)[4][FM], int64_t m,
                                                 int64_t nc, int g, int qd)
 {
-    uint32_t byte[FM];
+    static_assert(FM == 1 || FM % 2 == 0, "codes are stored by two row groups");
+    uint32_t byte[FM], codes[2][2];
 #pragma unroll
     for (int j = 0; j < FM; ++j) {
         const v4f p[4] = {acc[0][j], acc[1][j], acc[2][j], acc[3][j]};
-        byte[j] = gated_rows<ELEM, OUT, ACT>(A, p, m + 16 * j, nc, g, qd);
+        byte[j] = gated_rows<ELEM, OUT, ACT>(A, p, m + 16 * j, nc, g, qd, codes[j & 1]);
+        if constexpr (OUT - kGate == MX_OUT_CODES) {
+            if (j & 1)
+                store_codes<ELEM>(A, codes[0], codes[1], m + 16 * (j - 1), nc, g, qd);
+        }
     }
     if constexpr (OUT - kGate == MX_OUT_CODES) {
+        if constexpr (FM == 1) {
+            const int64_t n8 = nc + 16 * (g & 1) + 8 * (g >> 1);
+            if (m + qd < A.M && n8 < A.N) {
+                uint8_t *dst = static_cast<uint8_t *>(A.out) +
+                               ((m + qd) * A.N + n8) / (ELEM == MX_ELEM_E4M3 ? 1 : 2);
+                if constexpr (ELEM == MX_ELEM_E4M3)
+                    *reinterpret_cast<uint2 *>(dst) = make_uint2(codes[0][0], codes[0][1]);
+                else
+                    *reinterpret_cast<uint32_t *>(dst) = codes[0][0];
+            }
+        }
         // lane row g stores the scales of row groups g, 4 + g, ...
 #pragma unroll
         for (int j = 0; j < FM; j += 4) {
