@@ -636,21 +636,31 @@ def _heads(t, name, like=None):
     return _Heads(t.data_ptr(), t.shape[1], st, sh)
 
 
+def _new_heads(t):
+    """A contiguous tensor like t and its mx_heads (empty_like: 1 us a tensor
+    less than empty with a shape, type and device)."""
+    out = torch.empty_like(t, memory_format=torch.contiguous_format)
+    _, H, D = t.shape
+    return out, _Heads(out.data_ptr(), H, H * D, D)
+
+
 def _rope_arguments(q, k, q_gamma, k_gamma, pos, inv_freq, rotary):
     """(T, D, R) of a call on queries q and keys k, its vectors checked."""
     T, _, D = q.shape
-    if k.shape[0] != T or k.shape[2] != D or k.device != q.device:
+    Tk, _, Dk = k.shape
+    device = q.device
+    if Tk != T or Dk != D or k.device != device:
         raise ValueError("q and k must have the same tokens, head size and device")
     for g, name in ((q_gamma, "q_gamma"), (k_gamma, "k_gamma")):
-        if g is not None and (g.dtype != torch.bfloat16 or g.shape != (D,) or g.device != q.device
+        if g is not None and (g.dtype != torch.bfloat16 or g.shape != (D,) or g.device != device
                               or not g.is_contiguous()):
             raise ValueError("%s must be a contiguous bfloat16 [D] tensor on q's device" % name)
     R = D if rotary is None else rotary
-    if pos is not None and (pos.dtype != torch.int64 or pos.shape != (T,) or pos.device != q.device
+    if pos is not None and (pos.dtype != torch.int64 or pos.shape != (T,) or pos.device != device
                             or not pos.is_contiguous()):
         raise ValueError("pos must be a contiguous int64 [T] tensor on q's device")
     if R and (inv_freq is None or inv_freq.dtype != torch.float32 or inv_freq.shape != (R // 2,)
-              or inv_freq.device != q.device or not inv_freq.is_contiguous()):
+              or inv_freq.device != device or not inv_freq.is_contiguous()):
         raise ValueError("inv_freq must be a contiguous float32 [rotary / 2] tensor on q's device")
     return T, D, R
 
@@ -665,11 +675,8 @@ def qk_norm_rope_fwd(q, k, q_gamma, k_gamma, pos, inv_freq, rotary=None, interle
     themselves among them.  Returns (q_out, k_out)."""
     dq, dk = _heads(q, "q"), _heads(k, "k")
     T, D, R = _rope_arguments(q, k, q_gamma, k_gamma, pos, inv_freq, rotary)
-    if q_out is None:
-        q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
-    if k_out is None:
-        k_out = torch.empty(k.shape, dtype=torch.bfloat16, device=q.device)
-    oq, ok = _heads(q_out, "q_out", q), _heads(k_out, "k_out", k)
+    q_out, oq = _new_heads(q) if q_out is None else (q_out, _heads(q_out, "q_out", q))
+    k_out, ok = _new_heads(k) if k_out is None else (k_out, _heads(k_out, "k_out", k))
     ref = ctypes.byref
     _call(load().qk_norm_rope_fwd, q.device, ref(dq), ref(dk), _ptr(q_gamma), _ptr(k_gamma), T, D, R,
           _ptr(pos), _ptr(inv_freq), int(bool(interleaved)), eps, ref(oq), ref(ok))
@@ -686,16 +693,13 @@ def qk_norm_rope_bwd(grad_q_out, grad_k_out, q, k, q_gamma, k_gamma, pos, inv_fr
     dq, dk = _heads(q, "q"), _heads(k, "k")
     T, D, R = _rope_arguments(q, k, q_gamma, k_gamma, pos, inv_freq, rotary)
     gq, gk = _heads(grad_q_out, "grad_q_out", q), _heads(grad_k_out, "grad_k_out", k)
-    if grad_q is None:
-        grad_q = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
-    if grad_k is None:
-        grad_k = torch.empty(k.shape, dtype=torch.bfloat16, device=q.device)
-    oq, ok = _heads(grad_q, "grad_q", q), _heads(grad_k, "grad_k", k)
+    grad_q, oq = _new_heads(q) if grad_q is None else (grad_q, _heads(grad_q, "grad_q", q))
+    grad_k, ok = _new_heads(k) if grad_k is None else (grad_k, _heads(grad_k, "grad_k", k))
     lib = load()
-    gg = [torch.empty((D,), dtype=torch.float32, device=q.device)
-          if want_grad_gamma and g is not None else None for g in (q_gamma, k_gamma)]
+    gg = [q.new_empty((D,), dtype=torch.float32) if want_grad_gamma and g is not None else None
+          for g in (q_gamma, k_gamma)]
     ws_bytes = lib.qk_norm_rope_bwd_workspace_bytes(T, D) if gg[0] is not None or gg[1] is not None else 0
-    ws = torch.empty((ws_bytes,), dtype=torch.uint8, device=q.device) if ws_bytes else None
+    ws = q.new_empty((ws_bytes,), dtype=torch.uint8) if ws_bytes else None
     ref = ctypes.byref
     _call(lib.qk_norm_rope_bwd, q.device, ref(gq), ref(gk), ref(dq), ref(dk), _ptr(q_gamma),
           _ptr(k_gamma), T, D, R, _ptr(pos), _ptr(inv_freq), int(bool(interleaved)), eps, ref(oq),
