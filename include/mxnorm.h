@@ -340,7 +340,8 @@ mx_status mxnorm_linear_bwd(const void *grad_h, const void *x, const float *rho,
  *   G = dec(A) dec(W[0 .. F))^T,  U = dec(A) dec(W[F .. 2F))^T,
  *   H = act(G) . U                                               [M, F]
  * G and U are the float sums of mx_matmul_fwd (its bound, its note on the order
- * of additions); activation and product are computed in float.  Non-finite
+ * of additions, with four partial sums); activation and product are computed in
+ * float.  Non-finite
  * values follow the formula: a NaN gives NaN, act(-inf) is NaN, act(+inf) is
  * inf; a finite G too negative for the exponential gives act(G) = -0.
  * out_dtype MX_OUT_F32, MX_OUT_BF16: out [M, F] in that type, out_scales NULL.
@@ -364,9 +365,11 @@ mx_status mx_gated_fwd(const uint8_t *a_codes, const uint8_t *a_scales, const ui
 /*
  * mxnorm_mx_fwd of x [T, d] and mx_gated_fwd with the weight W [2F, d] as one
  * call: same arguments, outputs (bit for bit) and errors as the two calls, the
- * errors of both before the first launch; rho float [T] or NULL.  The codes of
- * the normed activations live in `workspace`: caller-owned device memory of
- * mxnorm_gated_fwd_workspace_bytes() bytes, 256-byte aligned, overwritten.
+ * errors of both before the first launch; rho float [T] or NULL.  (With up to
+ * four rows one launch does both, the norm's sums in another order; they are
+ * exact in double short of block absmaxes 2^15 apart.)  The codes of the normed
+ * activations may live in `workspace`: caller-owned device memory of
+ * mxnorm_gated_fwd_workspace_bytes() bytes, 256-byte aligned.
  */
 size_t mxnorm_gated_fwd_workspace_bytes(int64_t T, int64_t d, int block, int elem);
 mx_status mxnorm_gated_fwd(const void *x, int64_t T, int64_t d, const uint8_t *w_codes,

@@ -115,6 +115,35 @@ mx_status check_gated_bwd(const void *grad_h, const void *gu, int64_t T, int64_t
     return MX_OK;
 }
 
+// Whether a product of M rows takes the tile that can norm them, and they fit.
+static bool fits_normed(int64_t M, int64_t F, int steps, int elem, int units)
+{
+    if (!(elem == MX_ELEM_E2M1 ? Normed<MX_ELEM_E2M1, G16x64::NW>::fits(M, steps)
+                               : Normed<MX_ELEM_E4M3, G16x64::NW>::fits(M, steps)))
+        return false;
+    const Plan plan = plan_gated(M, F, steps, units);
+    return plan.shape == S_G16x64 && !plan.whole;
+}
+
+bool normed_product(const GatedProduct &P, const RowNorm &n, int elem, hipStream_t stream, mx_status &st)
+{
+    NormedArgs A;
+    gated_args(A, P, elem, stream);
+    if (!fits_normed(P.M, P.F, A.steps, elem, A.grid_max))
+        return false;
+    A.x = static_cast<const uint16_t *>(n.x);
+    A.rho = n.rho;
+    A.p = n.p;
+    A.coef = n.coef;
+    A.eps = n.eps;
+    set_tiles(A, G16x64::BM, G16x64::BN / 2, 1024);
+    A.once = read_once(A);
+    st = launched(by_type(elem, P.out_dtype, [&](auto e, auto o) {
+        return launch_ksplit<decltype(e)::value, decltype(o)::value, G16x64, true>(A, stream);
+    }));
+    return true;
+}
+
 // The gradients of both projections, bf16 [T, 2F] from grad_h [T, F] and the
 // kept products [T, 2F]: a lane takes 8 columns of a row.
 template <int ACT>
@@ -187,6 +216,13 @@ int mxt_gated_plan(int64_t M, int64_t F, int64_t K, int elem, int units, int *wh
     *tail = P.tail;
     *us = P.us;
     return P.shape;
+}
+
+int mxt_gated_normed(int64_t M, int64_t F, int64_t K, int elem, int units)
+{
+    const int64_t rb = elem == MX_ELEM_E2M1 ? K / 2 : K;
+    return M > 0 && F > 0 && K > 0 && units > 0 &&
+           mxg::fits_normed(M, F, (int)(rb / mxg::KB), elem, units);
 }
 
 mx_status mxt_gated(const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *w_codes,

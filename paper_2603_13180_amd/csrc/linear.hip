@@ -143,8 +143,14 @@ mx_status mxnorm_gated_fwd(const void *x, int64_t T, int64_t d, const uint8_t *w
                                 rho)) != MX_OK ||
         (st = mxg::check_gated({s.codes, s.scales, w_codes, w_scales, T, F, d, act, scale_mode,
                                 out_dtype, out, out_scales, gu},
-                               block, elem)) != MX_OK ||
-        (st = mxnorm_mx_fwd(x, T, d, block, elem, p, coef, eps, scale_mode, s.codes, s.scales, rho,
+                               block, elem)) != MX_OK)
+        return st;
+    if (T > 0 && F > 0 &&
+        mxg::normed_product({s.codes, s.scales, w_codes, w_scales, T, F, d, act, scale_mode, out_dtype,
+                             out, out_scales, gu},
+                            {x, rho, p, c, eps}, elem, stream, st))
+        return st;
+    if ((st = mxnorm_mx_fwd(x, T, d, block, elem, p, coef, eps, scale_mode, s.codes, s.scales, rho,
                             stream)) != MX_OK)
         return st;
     return mx_gated_fwd(s.codes, s.scales, w_codes, w_scales, T, F, d, block, elem, act, scale_mode,

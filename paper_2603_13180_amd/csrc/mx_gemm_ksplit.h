@@ -14,6 +14,7 @@
 #pragma once
 
 #include "mx_gemm.h"
+#include "mx_gemm_normed.h"
 
 namespace mxg {
 
@@ -34,14 +35,22 @@ template <class C, int ELEM> struct KSplitOp {
     static_assert(C::NW * PART <= 160 * 1024, "LDS");
 };
 
-template <int ELEM, int OUT, class C>
-__global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(ArgsOf<OUT> A)
+// NORM: A's rows are normed and cast here (mx_gemm_normed.h), not loaded.
+template <int OUT, bool NORM> using KSplitArgs = std::conditional_t<NORM, NormedArgs, ArgsOf<OUT>>;
+
+template <int ELEM, int OUT, class C, bool NORM>
+__global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(KSplitArgs<OUT, NORM> A)
 {
+    static_assert(!NORM || (C::FM == 1 && C::S == 1), "normed rows are one tile row");
+    using R = Normed<ELEM, C::NW>;
     using O = KSplitOp<C, ELEM>;
     constexpr bool GATED = kGated<OUT>;
     constexpr int CN = kCols<OUT>(C::BN); // output columns of a tile
     constexpr int SB = O::SB, DW = SB / 4;
+    constexpr int T0 = NORM ? C::BM / 8 : 0; // the first code load
     __shared__ __attribute__((aligned(16))) uint8_t lds[C::NW * O::PART];
+    __shared__ __attribute__((aligned(16))) uint8_t act[NORM ? C::NW * R::AREA : 16];
+    __shared__ double red[NORM ? C::NW * R::ROWS : 1];
 
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l = threadIdx.x & 63;
@@ -62,7 +71,7 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(ArgsOf<OUT> A)
     const int rr = l >> 3, ch = (l & 7) ^ rr;
     uint32_t code[C::LC];
 #pragma unroll
-    for (int t = 0; t < C::LC; ++t) {
+    for (int t = T0; t < C::LC; ++t) {
         const int r = 8 * t;
         const int64_t off = r < C::BM ? min(m0 + r + rr, A.M - 1) - m0
                                       : min(n0 + brow(r) + rr, A.N - 1) - n0;
@@ -71,7 +80,8 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(ArgsOf<OUT> A)
     const uint8_t *sc[O::LS];
 #pragma unroll
     for (int t = 0; t < O::LS; ++t) {
-        const int dw = 64 * t + l, r = min(dw / DW, C::BM + C::BN - 1);
+        // (NORM: B's first row in place of A's)
+        const int dw = 64 * t + l, r = max(min(dw / DW, C::BM + C::BN - 1), NORM ? C::BM : 0);
         sc[t] = (r < C::BM ? A.as + min(m0 + r, A.M - 1) * A.rs
                            : A.bs + (min(n0 + brow(r), A.N - 1) +
                                      (GATED && r >= C::BM + CN ? A.N : 0)) * A.rs) + 4 * (dw % DW);
@@ -83,7 +93,7 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(ArgsOf<OUT> A)
         const uint32_t st = ring_addr + slot * O::SLOT;
         auto codes = [&](auto nt) {
 #pragma unroll
-            for (int t = 0; t < C::LC; ++t) {
+            for (int t = T0; t < C::LC; ++t) {
                 const uint8_t *base = 8 * t < C::BM ? ta : 8 * t < C::BM + CN ? tb : tb2;
                 if (decltype(nt)::value && 8 * t >= C::BM)
                     lds_load16_nt(base, code[t] + (uint32_t)k * KB, st + 8 * t * KB);
@@ -113,9 +123,20 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(ArgsOf<OUT> A)
         for (int i = 0; i < C::FN; ++i)
             acc[j][i] = v4f{0.f, 0.f, 0.f, 0.f};
     const int mine = w < A.steps ? (A.steps - w - 1) / C::NW + 1 : 0; // this wave's steps
+    LDS_AS uint8_t *area = (LDS_AS uint8_t *)act + w * R::AREA;
+    if constexpr (NORM)
+        R::load(A, __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)area), w, l);
 #pragma unroll 1
     for (int p = 0; p < C::S && p < mine; ++p)
         issue(w + p * C::NW, p);
+    if constexpr (NORM) {
+        if (mine)
+            wait_vmcnt<O::L - T0>();
+        else
+            wait_vmcnt<0>();
+        R::cast(A, area, (LDS_AS double *)red, n0 == 0, w, l);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
     int slot = 0;
 #pragma unroll 1
     for (int p = 0; p < mine; ++p) {
@@ -123,7 +144,10 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(ArgsOf<OUT> A)
         const LDS_AS uint8_t *st = ring + slot * O::SLOT;
         Frag fa[C::FM], fb[C::FN];
         read_frags<ELEM, GATED ? CN : 0>(fb, st, bb, std::make_integer_sequence<int, C::FN>{});
-        read_frags<ELEM, 0>(fa, st, ba, std::make_integer_sequence<int, C::FM>{});
+        if constexpr (NORM)
+            fa[0] = R::frag(A, area, p, g, qd);
+        else
+            read_frags<ELEM, 0>(fa, st, ba, std::make_integer_sequence<int, C::FM>{});
         // the slot is in registers: its next step may land in it
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         if (p + C::S < mine)
@@ -182,9 +206,10 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(ArgsOf<OUT> A)
     }
 }
 
-template <int ELEM, int OUT, class C> hipError_t launch_ksplit(const ArgsOf<OUT> &A, hipStream_t stream)
+template <int ELEM, int OUT, class C, bool NORM = false>
+hipError_t launch_ksplit(const KSplitArgs<OUT, NORM> &A, hipStream_t stream)
 {
-    hipLaunchKernelGGL((mx_gemm_ksplit_kernel<ELEM, OUT, C>), dim3((unsigned)(A.cells * A.sub_m * A.sub_n)),
+    hipLaunchKernelGGL((mx_gemm_ksplit_kernel<ELEM, OUT, C, NORM>), dim3((unsigned)(A.cells * A.sub_m * A.sub_n)),
                        dim3(C::NT), 0, stream, A);
     return hipGetLastError();
 }

@@ -176,13 +176,14 @@ hipError_t launch_shape(int shape, const ArgsOf<OUT> &A, hipStream_t stream)
 // -> 24.7 and 32.1 -> 30.4 us, 134 MB 28.9 -> 25.7; but 62 MB (E2M1) 13.1 ->
 // 12.9 and 16.8 -> 16.7, 67 MB 14.2 -> 15.4, 17 MB (E4M3) 10.1 -> 11.1.
 constexpr int64_t kOnceBytes = 96 << 20;
+inline bool read_once(const GatedArgs &A) { return A.tiles_m == 1 && 2 * A.N * A.rb >= kOnceBytes; }
 
 template <int ELEM, int OUT>
 hipError_t multiply_as(const Plan &P, ArgsOf<OUT> A, hipStream_t stream)
 {
     set_tiles(A, kCost[P.shape].bm, kCols<OUT>(kCost[P.shape].bn), 1024);
     if constexpr (kGated<OUT>)
-        A.once = A.tiles_m == 1 && 2 * A.N * A.rb >= kOnceBytes;
+        A.once = read_once(A);
     if (!P.whole)
         return launch_shape<ELEM, OUT>(P.shape, A, stream);
     const int left = A.cells - P.whole;

@@ -336,6 +336,47 @@ __device__ __forceinline__ double team_sum(double s, double *red, int tid)
     return s;
 }
 
+// The codes of a lane's 8 elements x of a block with absmax pattern m, normed by
+// rho: t = RN(x rho), E4M3 in lo and hi or E2M1 in lo; returns the block's E8M0
+// byte.  As the kernel below computes them with blocks of 32 and no gain.
+template <bool FP4>
+__device__ __forceinline__ uint32_t cast_chunk(const uint4 &v, float rho, uint32_t m, int mode,
+                                               uint32_t &lo, uint32_t &hi)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    float t[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        t[2 * i] = bf16_lo(w[i]) * rho;
+        t[2 * i + 1] = bf16_hi(w[i]) * rho;
+    }
+    const uint32_t byte = e8m0_byte<FP4>(__uint_as_float(m << 16) * rho, mode);
+    const float scale = __uint_as_float(byte << 23);
+    if constexpr (!FP4) {
+        if (mode == MX_SCALE_FLOOR) { // saturate before the conversion
+            const float lim = __uint_as_float(((byte + 8u) << 23) | 0x600000u);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                t[k] = __builtin_amdgcn_fmed3f(t[k], -lim, lim);
+        }
+        lo = e4m3x4_hw(t[0], t[1], t[2], t[3], scale);
+        hi = e4m3x4_hw(t[4], t[5], t[6], t[7], scale);
+        if (byte == 0xFFu) {
+            lo = nan_codes_e4m3(w[0], w[1]);
+            hi = nan_codes_e4m3(w[2], w[3]);
+        }
+    } else {
+        lo = hi = 0;
+        lo = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(lo, t[0], t[1], scale, 0);
+        lo = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(lo, t[2], t[3], scale, 1);
+        lo = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(lo, t[4], t[5], scale, 2);
+        lo = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(lo, t[6], t[7], scale, 3);
+        if (byte == 0xFFu)
+            lo = 0x77777777u | sign_nibbles(v);
+    }
+    return byte;
+}
+
 // ------------------------------------------------------------------ kernel --
 
 template <int TL>

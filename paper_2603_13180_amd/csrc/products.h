@@ -44,6 +44,16 @@ struct GatedProduct {
     void *gu;
 };
 mx_status check_gated(const GatedProduct &P, int block, int elem);
+// mxnorm_gated_fwd's norm: x bf16 [M, K] in place of the product's operand.
+struct RowNorm {
+    const void *x;
+    float *rho;
+    int p;
+    float coef, eps;
+};
+// The norm and the product (M, F > 0, both checked) in one launch, with the
+// bits of two, where so few rows allow it; false: nothing was launched.
+bool normed_product(const GatedProduct &P, const RowNorm &n, int elem, hipStream_t stream, mx_status &st);
 // mx_gated_bwd's checks.
 mx_status check_gated_bwd(const void *grad_h, const void *gu, int64_t T, int64_t F, int act,
                           const void *grad_gu);

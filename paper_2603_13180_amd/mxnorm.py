@@ -357,19 +357,20 @@ def _call(fn, device, *args):
     _check(status)
 
 
-def _gated_outputs(T, F, elem, act, out_dtype, save_gu, device):
-    """(out, scales or None, gu or None) of a gated product."""
+def _gated_outputs(T, F, elem, act, out_dtype, save_gu, a):
+    """(out, scales or None, gu or None) of a gated product of a.  (new_empty:
+    0.5 us a tensor less than empty with a device.)"""
     if elem not in ELEMS or act not in ACTS:
         raise ValueError("elem must be 'e4m3' or 'e2m1', act 'silu' or 'gelu_tanh'")
     if out_dtype not in GATED_DTYPES:
         raise ValueError("out_dtype must be float32, bfloat16 or uint8 (MX codes)")
     if out_dtype is torch.uint8:
-        out = torch.empty((T, F if elem == "e4m3" else F // 2), dtype=torch.uint8, device=device)
-        scales = torch.empty((T, F // 32), dtype=torch.uint8, device=device)
+        out = a.new_empty((T, F if elem == "e4m3" else F // 2), dtype=torch.uint8)
+        scales = a.new_empty((T, F // 32), dtype=torch.uint8)
     else:
-        out = torch.empty((T, F), dtype=out_dtype, device=device)
+        out = a.new_empty((T, F), dtype=out_dtype)
         scales = None
-    gu = torch.empty((T, 2 * F), dtype=torch.bfloat16, device=device) if save_gu else None
+    gu = a.new_empty((T, 2 * F), dtype=torch.bfloat16) if save_gu else None
     return out, scales, gu
 
 
@@ -395,7 +396,7 @@ def mx_gated_fwd(a_codes, a_scales, w_codes, w_scales, K, block=32, elem="e4m3",
     if a_scales.device != a_codes.device:
         raise ValueError("A: codes and scales must be on one device")
     mode = SCALE_MODES[scale_mode]
-    out, scales, gu = _gated_outputs(M, F, elem, act, out_dtype, save_gu, a_codes.device)
+    out, scales, gu = _gated_outputs(M, F, elem, act, out_dtype, save_gu, a_codes)
     _call(load().mx_gated_fwd, a_codes.device, a_codes.data_ptr(), a_scales.data_ptr(),
           w_codes.data_ptr(), w_scales.data_ptr(), M, F, K, block, ELEMS[elem], ACTS[act], mode,
           GATED_DTYPES[out_dtype], out.data_ptr(), _ptr(scales), _ptr(gu))
@@ -414,11 +415,11 @@ def mxnorm_gated_fwd(x, w_codes, w_scales, block=32, elem="e4m3", p=2, coef=0.0,
     _mx_out_shapes(T, d, block, elem)
     F = _gated_weight(w_codes, w_scales, d, block, elem, x.device)
     mode = SCALE_MODES[scale_mode]
-    out, scales, gu = _gated_outputs(T, F, elem, act, out_dtype, save_gu, x.device)
-    rho = torch.empty((T,), dtype=torch.float32, device=x.device) if want_rho else None
+    out, scales, gu = _gated_outputs(T, F, elem, act, out_dtype, save_gu, x)
+    rho = x.new_empty((T,), dtype=torch.float32) if want_rho else None
     lib, e = load(), ELEMS[elem]
     ws_bytes = lib.mxnorm_gated_fwd_workspace_bytes(T, d, block, e)
-    ws = torch.empty((ws_bytes,), dtype=torch.uint8, device=x.device)
+    ws = x.new_empty((ws_bytes,), dtype=torch.uint8)
     _call(lib.mxnorm_gated_fwd, x.device, x.data_ptr(), T, d, w_codes.data_ptr(),
           w_scales.data_ptr(), F, block, e, p, coef, eps, mode, ACTS[act], GATED_DTYPES[out_dtype],
           out.data_ptr(), _ptr(scales), _ptr(gu), _ptr(rho), ws.data_ptr(), ws_bytes)
@@ -480,11 +481,11 @@ def mxnorm_gated_bwd(grad_h, gu, x, rho, gamma, w, block=32, elem="e4m3", act="s
     if grad_x_dtype not in OUT_DTYPES or grad_dtype not in OUT_DTYPES:
         raise ValueError("grad_x_dtype and grad_dtype must be float32 or bfloat16")
     lib, e = load(), ELEMS[elem]
-    grad_x = torch.empty((T, d), dtype=grad_x_dtype, device=x.device)
-    grad_gamma = torch.empty((d,), dtype=grad_dtype, device=x.device)
-    grad_w = torch.empty((2 * F, d), dtype=grad_dtype, device=x.device)
+    grad_x = x.new_empty((T, d), dtype=grad_x_dtype)
+    grad_gamma = x.new_empty((d,), dtype=grad_dtype)
+    grad_w = x.new_empty((2 * F, d), dtype=grad_dtype)
     ws_bytes = lib.mxnorm_gated_bwd_workspace_bytes(T, F, d, e)
-    ws = torch.empty((ws_bytes,), dtype=torch.uint8, device=x.device)
+    ws = x.new_empty((ws_bytes,), dtype=torch.uint8)
     _call(lib.mxnorm_gated_bwd, x.device, grad_h.data_ptr(), gu.data_ptr(), x.data_ptr(),
           rho.data_ptr(), _ptr(gamma), w.data_ptr(), T, F, d, block, e, ACTS[act],
           OUT_DTYPES[grad_x_dtype], OUT_DTYPES[grad_dtype], grad_x.data_ptr(), grad_gamma.data_ptr(),
