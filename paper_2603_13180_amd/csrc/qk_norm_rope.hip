@@ -12,9 +12,10 @@
 // A lane holds the two 16-byte chunks of a head whose elements are paired
 // (chunks l and l + R/16 of the rotated part, two chunks of the rest), so a
 // pair never crosses lanes, and a head is a group of G = 4 .. 32 lanes; a wave
-// takes 64 / G heads of one token, the next one's loads in flight.  An angle
-// costs a double product and a sine, and every head of the token needs it: the
-// workgroup computes its tokens' angles once into LDS.
+// takes 64 / G heads of one token, or several tokens' if they have so few, the
+// next ones' loads in flight.  An angle costs a double product and a sine, and
+// every head of the token needs it: the workgroup computes its tokens' angles
+// once into LDS.
 //
 // What bounds it: HBM, 4 bytes an element forward and 6 backward.  32768 tokens
 // of 32 + 8 heads of 128 out of a projection of 48: forward 120 us, 5.6 TB/s (a
@@ -51,6 +52,10 @@ struct Heads {
     const uint16_t *gamma;
     int64_t in_t, in_h, gy_t, gy_h, out_t, out_h; // strides, elements
     int heads, blocks;   // blocks of 64 / G heads
+    // Tokens of an item: as many as have room in a wave.  (One token an item, and
+    // a load for each angle after the other: 4831 tokens of 4 + 2 heads of 128
+    // backward 24.6 us, now 17.4; 26066 of 2 + 1 forward 38.7, now 20.0.)
+    int tpi;
     int tb;              // tokens a workgroup takes at a time
     int64_t steps;       // of tb tokens
 };
@@ -68,6 +73,13 @@ struct Args {
 
 // lanes that hold a head's chunks
 __host__ __device__ inline int lanes_of(int D, int R) { return R / 16 + (D - R + 15) / 16; }
+
+// a / b for 0 <= a < 4096 and b > 0: (a + 1/2) / b is at least 1 / (2 b) from an
+// integer, its rounding and the reciprocal's are below 2^-20 a / b.
+__device__ __forceinline__ int quotient(int a, int b)
+{
+    return (int)(((float)a + 0.5f) * __builtin_amdgcn_rcpf((float)b));
+}
 
 // The two chunks of lane l; the second may lie past the head (an odd number of
 // chunks that do not turn).
@@ -91,16 +103,29 @@ __device__ __forceinline__ void chunks_of(int D, int R, int l, int &a, int &b)
 template <bool INTER>
 __device__ __forceinline__ void fill_angles(const Args &A, int64_t t0, int nt, float *cs, float *sn)
 {
-    const int half = A.R / 2;
-#pragma unroll 1
-    for (int i = threadIdx.x; i < nt * half; i += NT) {
-        const int t = i / half, p = i - t * half; // p = 8 l + e
+    const int half = A.R / 2, n = nt * half;
+    constexpr int UP = ANGLES / NT; // a lane's angles: their loads are in flight together
+    float turn[UP];
+#pragma unroll
+    for (int k = 0; k < UP; ++k) {
+        if (k * NT >= n)
+            break;
+        const int i = min(k * NT + (int)threadIdx.x, n - 1);
+        const int t = quotient(i, half), p = i - t * half; // p = 8 l + e
         const int l = p >> 3, e = p & 7;
         const int pair = !INTER ? p : e < 4 ? 4 * l + e : A.R / 4 + 4 * l + e - 4;
         const int64_t pos = A.pos ? A.pos[t0 + t] : t0 + t;
         const double turns = (double)pos * (double)A.inv_freq[pair] * 0.15915494309189535;
+        turn[k] = 2.0f * (float)(turns - rint(turns));
+    }
+#pragma unroll
+    for (int k = 0; k < UP; ++k)
+        if (k * NT < n)
+            cs[k * NT + threadIdx.x] = turn[k];
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += NT) {
         float s, c;
-        sincospif(2.0f * (float)(turns - rint(turns)), &s, &c);
+        sincospif(cs[i], &s, &c);
         cs[i] = c;
         sn[i] = s;
     }
@@ -211,22 +236,33 @@ __device__ __forceinline__ void store16(uint16_t *p, const uint32_t (&v)[4])
     __builtin_nontemporal_store(u32x4_t{v[0], v[1], v[2], v[3]}, reinterpret_cast<u32x4_t *>(p));
 }
 
-// A lane's place in its head and the gains of its chunks.  FULL: every lane of
+// A lane's place in its head, its item's head and token, and the gains of its
+// chunks.  FULL: every lane of
 // a wave holds two chunks that turn (R = D = 16 G, and the numbers of heads are
 // multiples of 64 / G).
 template <int G, bool FULL> struct Lane {
     int l, sub, ca, cb;
     bool in_a, in_b, rot;
-    __device__ __forceinline__ Lane(const Args &A)
+    int hs, ts; // the lane's head and token within an item
+    bool used;
+    __device__ __forceinline__ Lane(const Args &A, const Heads &H)
     {
         const int lane = threadIdx.x & 63;
         l = lane % G;
         sub = lane / G;
+        hs = sub;
+        ts = 0;
+        used = true;
         if constexpr (FULL) {
             ca = l;
             cb = l + G;
             in_a = in_b = rot = true;
         } else {
+            if (H.tpi > 1) {
+                ts = quotient(sub, H.heads);
+                hs = sub - ts * H.heads;
+                used = ts < H.tpi;
+            }
             chunks_of(A.D, A.R, l, ca, cb);
             in_a = l < lanes_of(A.D, A.R);
             in_b = in_a && 8 * cb < A.D;
@@ -350,23 +386,32 @@ __device__ __forceinline__ int64_t heads_of_kind(const Args &A, const Heads &H, 
                                                  float *cs, float *sn, float (&sum)[16])
 {
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = A.R / 2;
-    const Lane<G, FULL> L(A);
+    const Lane<G, FULL> L(A, H);
     uint4 gain[2];
     L.gains(H.gamma, gain);
     // an item is the wave's, so its first head's address is scalar; a lane adds
     // its own head and chunk
-    const int64_t xl = L.sub * H.in_h + 8 * L.ca, gl = BWD ? L.sub * H.gy_h + 8 * L.ca : 0,
-                  yl = L.sub * H.out_h + 8 * L.ca;
+    const int64_t xl = L.hs * H.in_h + L.ts * H.in_t + 8 * L.ca,
+                  gl = BWD ? L.hs * H.gy_h + L.ts * H.gy_t + 8 * L.ca : 0,
+                  yl = L.hs * H.out_h + L.ts * H.out_t + 8 * L.ca;
     const int step = 8 * (L.cb - L.ca);
 #pragma unroll 1
     for (; s < H.steps; s += nwg) {
         const int64_t t0 = s * H.tb;
-        const int nt = (int)min((int64_t)H.tb, A.T - t0), n = nt * H.blocks;
+        const int nt = (int)min((int64_t)H.tb, A.T - t0), n = (nt + H.tpi - 1) / H.tpi * H.blocks;
+        auto place = [&](int i, int &t, int &h) {
+            t = i / H.blocks;
+            h = (i - t * H.blocks) * (64 / G);
+            if constexpr (!FULL)
+                t *= H.tpi;
+        };
         auto load = [&](int i, Loaded<BWD> &v) {
-            const int t = i / H.blocks, h = (i - t * H.blocks) * (64 / G);
+            int t, h;
+            place(i, t, h);
             // past the last item every lane reads the tensor's first bytes: a
             // branch around the loads would end with a wait for them
-            const bool more = i < n, on = FULL || (more && h + L.sub < H.heads);
+            const bool more = i < n;
+            const bool on = FULL || (more && L.used && h + L.hs < H.heads && t + L.ts < nt);
             const int sp = more ? step : 0;
             const uint16_t *x = more ? H.in + (t0 + t) * H.in_t + h * H.in_h : H.in;
             load_chunks<FULL>(v.x, x + (more ? xl : 0), sp, on && L.in_a, on && L.in_b, H.in);
@@ -384,10 +429,13 @@ __device__ __forceinline__ int64_t heads_of_kind(const Args &A, const Heads &H, 
         for (int i = w; i < n; i += NW) {
             const Loaded<BWD> v = next;
             load(i + NW, next);
-            const int t = i / H.blocks, h = (i - t * H.blocks) * (64 / G);
-            const float *c = cs + t * half + 8 * L.l, *d = sn + t * half + 8 * L.l;
+            int t, h;
+            place(i, t, h);
+            const bool on = FULL || (L.used && h + L.hs < H.heads && t + L.ts < nt);
+            // (a lane without a token turns zeros, by any angles)
+            const int at = (on ? t + L.ts : 0) * half + 8 * L.l;
+            const float *c = cs + at, *d = sn + at;
             uint16_t *y = H.out + (t0 + t) * H.out_t + h * H.out_h + yl;
-            const bool on = FULL || h + L.sub < H.heads;
             opaque(gain); // or they are all kept widened, 16 registers more
             uint32_t a[4], b[4];
             if constexpr (BWD)
@@ -422,7 +470,7 @@ __global__ void __launch_bounds__(NT) bwd_kernel(Args A)
 {
     __shared__ __attribute__((aligned(16))) float cs[ANGLES], sn[ANGLES];
     __shared__ float red[NW * 64 / G][16 * G]; // D <= 16 G
-    const Lane<G, FULL> L(A);
+    const Lane<G, FULL> L(A, A.q);
     auto finish = [&](float (&sum)[16], int which, bool any) {
         if (!A.part)
             return;
@@ -537,8 +585,8 @@ template <bool BWD> void launch(const Args &A, bool inter, unsigned grid, hipStr
     }
 }
 
-// Tokens of a step: four items (one a wave), and up to 16 as far as the angles
-// fit and that leaves a step for each of `least` workgroups: the next item's
+// Tokens of a step: four items (one a wave) with an angle a lane, and up to 16
+// as far as the angles fit and that leaves a step for each of `least` workgroups: the next item's
 // loads then hide behind the one at hand, and backward a workgroup's sums are
 // added once.  12 + 4 heads of 64, 2000 tokens backward: 13.9 us, 17.1 with
 // four times as many steps; 8000 tokens 28.7 and 35.7, forward 14.4 and 18.8.
@@ -548,8 +596,11 @@ template <bool BWD> void launch(const Args &A, bool inter, unsigned grid, hipStr
 inline void steps_of(Heads &H, int64_t T, int R, int64_t least)
 {
     H.tb = 1;
-    while (2 * H.tb * std::max(R / 2, 1) <= ANGLES &&
-           (2 * H.tb * H.blocks <= NW || (2 * H.tb * H.blocks <= 4 * NW && T / (2 * H.tb) >= least)))
+    auto items = [&](int tb) { return (tb + H.tpi - 1) / H.tpi * H.blocks; };
+    auto angles = [&](int tb) { return tb * (R / 2); };
+    while (angles(2 * H.tb) <= ANGLES &&
+           ((items(2 * H.tb) <= NW && angles(2 * H.tb) <= NT) ||
+            (items(2 * H.tb) <= 4 * NW && T / (2 * H.tb) >= least)))
         H.tb *= 2;
     H.steps = H.heads ? (T + H.tb - 1) / H.tb : 0;
 }
@@ -635,6 +686,7 @@ mxq::Heads heads_of(const mx_heads *in, const mx_heads *gy, const mx_heads *out,
     H.gamma = static_cast<const uint16_t *>(gamma);
     H.heads = (int)in->heads;
     H.blocks = (int)((in->heads + 64 / G - 1) / (64 / G));
+    H.tpi = H.heads ? std::max(64 / G / H.heads, 1) : 1;
     return H;
 }
 
