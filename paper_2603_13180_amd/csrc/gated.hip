@@ -115,21 +115,28 @@ mx_status check_gated_bwd(const void *grad_h, const void *gu, int64_t T, int64_t
     return MX_OK;
 }
 
-// Whether a product of M rows takes the tile that can norm them, and they fit.
-static bool fits_normed(int64_t M, int64_t F, int steps, int elem, int units)
+// The chunks a lane needs (4 or 8) if a product of M rows takes the tile that can
+// norm them, and they fit; else 0.
+static int fits_normed(int64_t M, int64_t F, int steps, int elem, int units)
 {
-    if (!(elem == MX_ELEM_E2M1 ? Normed<MX_ELEM_E2M1, G16x64::NW>::fits(M, steps)
-                               : Normed<MX_ELEM_E4M3, G16x64::NW>::fits(M, steps)))
-        return false;
+    auto fits = [&](auto nch) {
+        constexpr int N = decltype(nch)::value;
+        return elem == MX_ELEM_E2M1 ? Normed<MX_ELEM_E2M1, G16x64::NW, N>::fits(M, steps)
+                                    : Normed<MX_ELEM_E4M3, G16x64::NW, N>::fits(M, steps);
+    };
+    const int n = fits(std::integral_constant<int, 4>{}) ? 4 : fits(std::integral_constant<int, 8>{}) ? 8 : 0;
+    if (n == 0)
+        return 0;
     const Plan plan = plan_gated(M, F, steps, units);
-    return plan.shape == S_G16x64 && !plan.whole;
+    return plan.shape == S_G16x64 && !plan.whole ? n : 0;
 }
 
 bool normed_product(const GatedProduct &P, const RowNorm &n, int elem, hipStream_t stream, mx_status &st)
 {
     NormedArgs A;
     gated_args(A, P, elem, stream);
-    if (!fits_normed(P.M, P.F, A.steps, elem, A.grid_max))
+    const int chunks = fits_normed(P.M, P.F, A.steps, elem, A.grid_max);
+    if (chunks == 0)
         return false;
     A.x = static_cast<const uint16_t *>(n.x);
     A.rho = n.rho;
@@ -139,7 +146,8 @@ bool normed_product(const GatedProduct &P, const RowNorm &n, int elem, hipStream
     set_tiles(A, G16x64::BM, G16x64::BN / 2, 1024);
     A.once = read_once(A);
     st = launched(by_type(elem, P.out_dtype, [&](auto e, auto o) {
-        return launch_ksplit<decltype(e)::value, decltype(o)::value, G16x64, true>(A, stream);
+        constexpr int E = decltype(e)::value, O = decltype(o)::value;
+        return chunks == 4 ? launch_ksplit<E, O, G16x64, 4>(A, stream) : launch_ksplit<E, O, G16x64, 8>(A, stream);
     }));
     return true;
 }
@@ -221,8 +229,7 @@ int mxt_gated_plan(int64_t M, int64_t F, int64_t K, int elem, int units, int *wh
 int mxt_gated_normed(int64_t M, int64_t F, int64_t K, int elem, int units)
 {
     const int64_t rb = elem == MX_ELEM_E2M1 ? K / 2 : K;
-    return M > 0 && F > 0 && K > 0 && units > 0 &&
-           mxg::fits_normed(M, F, (int)(rb / mxg::KB), elem, units);
+    return M > 0 && F > 0 && K > 0 && units > 0 ? mxg::fits_normed(M, F, (int)(rb / mxg::KB), elem, units) : 0;
 }
 
 mx_status mxt_gated(const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *w_codes,

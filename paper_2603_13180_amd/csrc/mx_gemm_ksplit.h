@@ -21,33 +21,36 @@ namespace mxg {
 template <int BM_, int BN_, int NW_, int S_> struct KSplit {
     static constexpr int BM = BM_, BN = BN_, NW = NW_, S = S_, NT = 64 * NW;
     static constexpr int FM = BM / 16, FN = BN / 16;
-    static constexpr int LC = (BM + BN) / 8; // code loads per step
 };
 
-template <class C, int ELEM> struct KSplitOp {
+// NORM > 0: A's rows are normed and cast here (mx_gemm_normed.h: NORM chunks), not
+// loaded; the ring's slots are then B's rows alone.
+template <class C, int ELEM, int NORM> struct KSplitOp {
+    using R = Normed<ELEM, C::NW, NORM>;
     static constexpr int SB = kSB<ELEM>;
-    static constexpr int LS = ((C::BM + C::BN) * SB + 255) / 256; // scale loads per step
-    static constexpr int L = C::LC + LS;
-    static constexpr int SLOT = (C::BM + C::BN) * KB + LS * 256;
-    static_assert((C::S - 1) * L <= 63, "vmcnt range");
+    static constexpr int AR = NORM ? 0 : C::BM, ROWS = AR + C::BN; // rows of a slot: A's, then B's
+    static constexpr int S = NORM ? R::S : C::S;
+    static constexpr int LC = ROWS / 8;                 // code loads per step
+    static constexpr int LS = (ROWS * SB + 255) / 256; // scale loads per step
+    static constexpr int L = LC + LS;
+    static constexpr int SLOT = ROWS * KB + LS * 256;
+    static_assert((S - 1) * L <= 63, "vmcnt range");
     // a wave's part of LDS: its ring, then its partial sums
-    static constexpr int PART = C::S * SLOT > C::FM * C::FN * 1024 ? C::S * SLOT : C::FM * C::FN * 1024;
+    static constexpr int PART = S * SLOT > C::FM * C::FN * 1024 ? S * SLOT : C::FM * C::FN * 1024;
     static_assert(C::NW * PART <= 160 * 1024, "LDS");
 };
 
-// NORM: A's rows are normed and cast here (mx_gemm_normed.h), not loaded.
-template <int OUT, bool NORM> using KSplitArgs = std::conditional_t<NORM, NormedArgs, ArgsOf<OUT>>;
+template <int OUT, int NORM> using KSplitArgs = std::conditional_t<(NORM > 0), NormedArgs, ArgsOf<OUT>>;
 
-template <int ELEM, int OUT, class C, bool NORM>
+template <int ELEM, int OUT, class C, int NORM>
 __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(KSplitArgs<OUT, NORM> A)
 {
-    static_assert(!NORM || (C::FM == 1 && C::S == 1), "normed rows are one tile row");
-    using R = Normed<ELEM, C::NW>;
-    using O = KSplitOp<C, ELEM>;
+    using O = KSplitOp<C, ELEM, NORM>;
+    using R = typename O::R;
+    static_assert(!NORM || (C::FM == 1 && R::ROWS <= C::BM && R::NCH * 1024 <= O::SLOT), "normed rows");
     constexpr bool GATED = kGated<OUT>;
     constexpr int CN = kCols<OUT>(C::BN); // output columns of a tile
-    constexpr int SB = O::SB, DW = SB / 4;
-    constexpr int T0 = NORM ? C::BM / 8 : 0; // the first code load
+    constexpr int SB = O::SB, DW = SB / 4, AR = O::AR;
     __shared__ __attribute__((aligned(16))) uint8_t lds[C::NW * O::PART];
     __shared__ __attribute__((aligned(16))) uint8_t act[NORM ? C::NW * R::AREA : 16];
     __shared__ double red[NORM ? C::NW * R::ROWS : 1];
@@ -67,24 +70,23 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(KSplitArgs<OUT, N
     // Gated: the second half of B's rows are up rows, N rows further on.
     const uint8_t *ta = A.a + m0 * A.rb, *tb = A.b + n0 * A.rb;
     const uint8_t *tb2 = GATED ? tb + A.N * A.rb : tb;
-    auto brow = [](int r) { return GATED ? (r - C::BM) % (C::BN / 2) : r - C::BM; };
+    auto brow = [](int r) { return GATED ? (r - AR) % (C::BN / 2) : r - AR; };
     const int rr = l >> 3, ch = (l & 7) ^ rr;
-    uint32_t code[C::LC];
+    uint32_t code[O::LC];
 #pragma unroll
-    for (int t = T0; t < C::LC; ++t) {
+    for (int t = 0; t < O::LC; ++t) {
         const int r = 8 * t;
-        const int64_t off = r < C::BM ? min(m0 + r + rr, A.M - 1) - m0
+        const int64_t off = r < AR ? min(m0 + r + rr, A.M - 1) - m0
                                       : min(n0 + brow(r) + rr, A.N - 1) - n0;
         code[t] = (uint32_t)(off * A.rb) + 16 * ch;
     }
     const uint8_t *sc[O::LS];
 #pragma unroll
     for (int t = 0; t < O::LS; ++t) {
-        // (NORM: B's first row in place of A's)
-        const int dw = 64 * t + l, r = max(min(dw / DW, C::BM + C::BN - 1), NORM ? C::BM : 0);
-        sc[t] = (r < C::BM ? A.as + min(m0 + r, A.M - 1) * A.rs
+        const int dw = 64 * t + l, r = min(dw / DW, O::ROWS - 1);
+        sc[t] = (r < AR ? A.as + min(m0 + r, A.M - 1) * A.rs
                            : A.bs + (min(n0 + brow(r), A.N - 1) +
-                                     (GATED && r >= C::BM + CN ? A.N : 0)) * A.rs) + 4 * (dw % DW);
+                                     (GATED && r >= AR + CN ? A.N : 0)) * A.rs) + 4 * (dw % DW);
     }
 
     LDS_AS uint8_t *ring = (LDS_AS uint8_t *)lds + w * O::PART;
@@ -93,9 +95,9 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(KSplitArgs<OUT, N
         const uint32_t st = ring_addr + slot * O::SLOT;
         auto codes = [&](auto nt) {
 #pragma unroll
-            for (int t = T0; t < C::LC; ++t) {
-                const uint8_t *base = 8 * t < C::BM ? ta : 8 * t < C::BM + CN ? tb : tb2;
-                if (decltype(nt)::value && 8 * t >= C::BM)
+            for (int t = 0; t < O::LC; ++t) {
+                const uint8_t *base = 8 * t < AR ? ta : 8 * t < AR + CN ? tb : tb2;
+                if (decltype(nt)::value && 8 * t >= AR)
                     lds_load16_nt(base, code[t] + (uint32_t)k * KB, st + 8 * t * KB);
                 else
                     lds_load16(base, code[t] + (uint32_t)k * KB, st + 8 * t * KB);
@@ -111,10 +113,10 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(KSplitArgs<OUT, N
         }
 #pragma unroll
         for (int t = 0; t < O::LS; ++t)
-            lds_load4(sc[t] + (uint32_t)k * SB, st + (C::BM + C::BN) * KB + 256 * t);
+            lds_load4(sc[t] + (uint32_t)k * SB, st + O::ROWS * KB + 256 * t);
     };
-    const FragBase ba = frag_base<ELEM>(0, (C::BM + C::BN) * KB, 0, qd, g);
-    const FragBase bb = frag_base<ELEM>(C::BM * KB, (C::BM + C::BN) * KB + C::BM * SB, 0, qd, g);
+    const FragBase ba = frag_base<ELEM>(0, O::ROWS * KB, 0, qd, g);
+    const FragBase bb = frag_base<ELEM>(AR * KB, O::ROWS * KB + AR * SB, 0, qd, g);
 
     v4f acc[C::FM][C::FN];
 #pragma unroll
@@ -124,38 +126,45 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(KSplitArgs<OUT, N
             acc[j][i] = v4f{0.f, 0.f, 0.f, 0.f};
     const int mine = w < A.steps ? (A.steps - w - 1) / C::NW + 1 : 0; // this wave's steps
     LDS_AS uint8_t *area = (LDS_AS uint8_t *)act + w * R::AREA;
-    if constexpr (NORM)
-        R::load(A, __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)area), w, l);
-#pragma unroll 1
-    for (int p = 0; p < C::S && p < mine; ++p)
-        issue(w + p * C::NW, p);
-    if constexpr (NORM) {
-        if (mine)
-            wait_vmcnt<O::L - T0>();
-        else
+    if constexpr (NORM > 0) {
+        LDS_AS uint8_t *xs = O::S == 2 ? ring + O::SLOT : area;
+        R::load(A, __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)xs), w, l);
+        if (mine > 0) {
+            issue(w, 0);
+            wait_vmcnt<O::L>();
+        } else {
             wait_vmcnt<0>();
-        R::cast(A, area, (LDS_AS double *)red, n0 == 0, w, l);
+        }
+        uint4 x[R::NCH];
+        R::read(xs, l, x);
+        if (O::S == 2 && mine > 1)
+            issue(w + C::NW, 1);
+        R::cast(A, x, area, (LDS_AS double *)red, n0 == 0, w, l);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    } else {
+#pragma unroll 1
+        for (int p = 0; p < O::S && p < mine; ++p)
+            issue(w + p * C::NW, p);
     }
     int slot = 0;
 #pragma unroll 1
     for (int p = 0; p < mine; ++p) {
-        wait_steps<O::L, C::S - 1>(mine - 1 - p);
+        wait_steps<O::L, O::S - 1>(mine - 1 - p);
         const LDS_AS uint8_t *st = ring + slot * O::SLOT;
         Frag fa[C::FM], fb[C::FN];
         read_frags<ELEM, GATED ? CN : 0>(fb, st, bb, std::make_integer_sequence<int, C::FN>{});
-        if constexpr (NORM)
+        if constexpr (NORM > 0)
             fa[0] = R::frag(A, area, p, g, qd);
         else
             read_frags<ELEM, 0>(fa, st, ba, std::make_integer_sequence<int, C::FM>{});
         // the slot is in registers: its next step may land in it
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (p + C::S < mine)
-            issue(w + (p + C::S) * C::NW, slot);
+        if (p + O::S < mine)
+            issue(w + (p + O::S) * C::NW, slot);
 #pragma unroll
         for (int j = 0; j < C::FM; ++j)
             mma_column<ELEM, C::FN>(acc[j], fb, fa[j]);
-        slot = slot + 1 == C::S ? 0 : slot + 1;
+        slot = slot + 1 == O::S ? 0 : slot + 1;
     }
 
     // partial sums, each wave's in its own ring
@@ -206,7 +215,7 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(KSplitArgs<OUT, N
     }
 }
 
-template <int ELEM, int OUT, class C, bool NORM = false>
+template <int ELEM, int OUT, class C, int NORM = 0>
 hipError_t launch_ksplit(const KSplitArgs<OUT, NORM> &A, hipStream_t stream)
 {
     hipLaunchKernelGGL((mx_gemm_ksplit_kernel<ELEM, OUT, C, NORM>), dim3((unsigned)(A.cells * A.sub_m * A.sub_n)),

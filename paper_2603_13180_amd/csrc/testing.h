@@ -46,7 +46,8 @@ mx_status mxt_matmul(const uint8_t *a_codes, const uint8_t *a_scales, const uint
 // 64 with K split over four waves.
 int mxt_gated_plan(int64_t M, int64_t F, int64_t K, int elem, int units, int *whole, int *tail,
                    double *us);
-// Whether mxnorm_gated_fwd norms M rows within its product's launch.
+// The chunks of x per lane (4 or 8) with which mxnorm_gated_fwd norms M rows within
+// its product's launch; 0: in a launch before it.
 int mxt_gated_normed(int64_t M, int64_t F, int64_t K, int elem, int units);
 mx_status mxt_gated(const uint8_t *a_codes, const uint8_t *a_scales, const uint8_t *w_codes,
                     const uint8_t *w_scales, int64_t M, int64_t F, int64_t K, int elem, int act,

@@ -22,14 +22,14 @@ _I, _L, _P = ctypes.c_int, ctypes.c_int64, ctypes.c_void_p
 def normed(T, F, d, elem, units=UNITS):
     f = mxnorm.load().mxt_gated_normed
     f.restype, f.argtypes = _I, [_L] * 3 + [_I] * 2
-    return bool(f(T, F, d, ELEM[elem], units))
+    return f(T, F, d, ELEM[elem], units)
 
 
 @pytest.mark.parametrize("T,d,elem,want", [
-    (1, 128, "e4m3", True), (4, 4096, "e4m3", True), (5, 4096, "e4m3", False), (4, 4224, "e4m3", False),
-    (1, 16384, "e4m3", True), (1, 16512, "e4m3", False), (2, 8192, "e2m1", True), (4, 256, "e2m1", True),
-    (4, 4096, "e2m1", True), (4, 4352, "e2m1", False), (1, 16384, "e2m1", True), (0, 256, "e4m3", False),
-    (16, 256, "e4m3", False)])
+    (1, 128, "e4m3", 4), (4, 2048, "e4m3", 4), (4, 2176, "e4m3", 8), (4, 4096, "e4m3", 8), (5, 4096, "e4m3", 0),
+    (4, 4224, "e4m3", 0), (1, 8192, "e4m3", 4), (1, 16384, "e4m3", 8), (1, 16512, "e4m3", 0),
+    (2, 4096, "e2m1", 4), (2, 8192, "e2m1", 8), (4, 256, "e2m1", 4), (4, 4096, "e2m1", 8), (4, 4352, "e2m1", 0),
+    (1, 16384, "e2m1", 8), (0, 256, "e4m3", 0), (16, 256, "e4m3", 0)])
 def test_which_rows_are_normed_in_the_product(T, d, elem, want):
     assert normed(T, 4096, d, elem) == want
 
@@ -95,11 +95,11 @@ def two_calls(x, wc, ws, elem, p, mode, act, dtype, keep, want_rho):
 
 
 # one K step (three waves without one), steps that no four waves share evenly,
-# the longest rows that fit; F of half a tile, of a tile and a half, of many
-SIZES = {"e4m3": [(1, 128, 32), (2, 384, 96), (3, 640, 32), (4, 1152, 1024), (4, 4096, 64), (2, 8192, 32),
-                  (1, 16384, 64)],
-         "e2m1": [(1, 256, 32), (2, 768, 96), (3, 1280, 32), (4, 2304, 1024), (4, 4096, 64), (2, 8192, 32),
-                  (1, 16384, 64)]}
+# the longest rows that fit, for both numbers of chunks; F of half a tile, of a tile and a half, of many
+SIZES = {"e4m3": [(1, 128, 32), (2, 384, 96), (3, 640, 32), (4, 1152, 1024), (2, 4096, 64), (1, 8192, 96),
+                  (3, 2176, 32), (4, 4096, 64), (2, 8192, 32), (1, 16384, 64)],
+         "e2m1": [(1, 256, 32), (2, 768, 96), (3, 1280, 32), (4, 1792, 1024), (2, 4096, 64), (1, 8192, 96),
+                  (3, 2304, 32), (4, 4096, 64), (2, 8192, 32), (1, 16384, 64)]}
 
 
 @gpu
