@@ -335,10 +335,11 @@ __global__ void __launch_bounds__(NTH) cast_t_kernel(CastTArgs A)
 // bytes by two rotations and store them as one dword.  RCEIL scales (no clamp
 // is needed before the conversion); C a multiple of 128.
 //
-// valid: how many of the 16 lanes' 128 columns are this matrix's (128, or 64
-// where a gated half ends with half a tile: its scale bytes go out in pairs,
-// which are also aligned where the halves meet).
-template <bool FP4, bool PAIRS>
+// LANES: of a row's columns, 16 or, in narrow gated tiles, 8.  valid: how many of
+// 16 lanes' 128 columns are this matrix's (128, or 64 where a gated half ends with
+// half a tile: its scale bytes go out in pairs, which are also aligned where the
+// halves meet).
+template <bool FP4, bool PAIRS, int LANES = 16>
 __device__ __forceinline__ void cast_row_chunk(uint8_t *codes, uint8_t *scales, int64_t C, int64_t r,
                                                int64_t c, bool in, int tid, const uint4 v, int valid)
 {
@@ -373,9 +374,11 @@ __device__ __forceinline__ void cast_row_chunk(uint8_t *codes, uint8_t *scales, 
     uint32_t b4 = byte << (8 * ((tid >> 2) & 3));
     b4 |= dpp_mov<0x124>(b4); // row_ror:4
     b4 |= dpp_mov<0x128>(b4); // row_ror:8
-    if (in && (tid & 15) == 0) {
+    if (in && (tid & (LANES - 1)) == 0) {
         uint8_t *dst = scales + r * (C / 32) + c / 32;
-        if constexpr (PAIRS) {
+        if constexpr (LANES == 8) { // two rows' pairs in the 16 lanes
+            *reinterpret_cast<uint16_t *>(dst) = (uint16_t)(tid & 8 ? b4 >> 16 : b4);
+        } else if constexpr (PAIRS) {
             reinterpret_cast<uint16_t *>(dst)[0] = (uint16_t)b4;
             if (valid > 64)
                 reinterpret_cast<uint16_t *>(dst)[1] = (uint16_t)(b4 >> 16);
@@ -419,13 +422,13 @@ struct CastJobs {
     int start[3];
 };
 
-// The gated tile: thread t moves the 16-byte chunk t % 16 of rows t / 16 + 32 k
+// The gated tile: thread t moves the 16-byte chunk t % CH of rows t / CH + RPP k
 // of H's gradient, the gate and the up products.
-template <bool FP4, int ACT, int NTH>
+template <bool FP4, int ACT, int COLS, int NTH>
 __device__ __forceinline__ void gated_tile(const CastJobs &J, int64_t r0, int64_t c0, int tid,
                                            uint8_t *tile, float *rs)
 {
-    constexpr int COLS = 256, CH = COLS / 16, RPP = NTH / CH, NLD = CT_ROWS / RPP;
+    constexpr int CH = COLS / 16, RPP = NTH / CH, NLD = CT_ROWS / RPP;
     using S = CtShape<COLS, NTH>;
     const CastTArgs &A = J.job[0];
     const int64_t F = A.C / 2;
@@ -456,10 +459,10 @@ __device__ __forceinline__ void gated_tile(const CastJobs &J, int64_t r0, int64_
         *reinterpret_cast<uint4 *>(&tile[S::off(r) + 16 * ch]) = dg;
         *reinterpret_cast<uint4 *>(&tile[S::off(r) + 16 * (CH + ch)]) = du;
         const bool in = r0 + r < A.rows && c < F;
-        // (E2M1: F is a multiple of 128)
+        // (E2M1: F is a multiple of 128; E4M3, of 64)
         const int valid = (int)min((int64_t)COLS / 2, F - c0);
-        cast_row_chunk<FP4, !FP4>(J.row_codes, J.row_scales, A.C, r0 + r, c, in, tid, dg, valid);
-        cast_row_chunk<FP4, !FP4>(J.row_codes, J.row_scales, A.C, r0 + r, F + c, in, tid, du, valid);
+        cast_row_chunk<FP4, !FP4, CH>(J.row_codes, J.row_scales, A.C, r0 + r, c, in, tid, dg, valid);
+        cast_row_chunk<FP4, !FP4, CH>(J.row_codes, J.row_scales, A.C, r0 + r, F + c, in, tid, du, valid);
     }
     if (tid < CT_ROWS)
         rs[tid] = 1.0f;
@@ -483,7 +486,7 @@ __global__ void __launch_bounds__(NTH) cast_jobs_kernel(CastJobs J)
     if constexpr (GATE >= 0) {
         if (j == 0) { // F = C / 2 columns in steps of COLS / 2: as many tiles
             const int64_t c0 = ct * (COLS / 2), r0 = rt * CT_ROWS;
-            gated_tile<FP4, GATE, NTH>(J, r0, c0, tid, tile, rs);
+            gated_tile<FP4, GATE, COLS, NTH>(J, r0, c0, tid, tile, rs);
             lds_barrier();
             cast_columns<FP4, COLS, NTH, COLS / 2>(A, tile, rs, r0, c0, tid);
             return;
@@ -1118,6 +1121,13 @@ mx_status ste(const void *x, const void *grad_z, const void *gamma, const float 
     return MX_OK;
 }
 
+// A gated launch of up to this many tiles takes tiles of half the columns: with few
+// tiles the gate's arithmetic on one compute unit, 11 us a tile, is the launch's
+// time.  Whole backwards, E4M3: 1024 x 2048 x 768 (248 tiles) 46.7 -> 43.6 us, 64 x
+// 1024 x 512 (42) 25.6 -> 23.3, 2048 x 5632 x 2048 (1536) 204 -> 198; 2560 tiles
+// 236 and 235, E2M1 174 and 179, 10240 1379 and 1422.
+constexpr int64_t kNarrowTiles = 2048;
+
 mx_status backward_casts(const void *grad_h, const void *x, const float *rho, const void *w,
                          int64_t T, int64_t Tp, int64_t N, int64_t d, int elem,
                          const BackwardCasts &o, const Gate *gate, hipStream_t stream)
@@ -1145,17 +1155,31 @@ mx_status backward_casts(const void *grad_h, const void *x, const float *rho, co
     J.job[2] = job(x, rho, T, Tp, d, o.xt, o.xt_s);
     J.row_codes = o.gh;
     J.row_scales = o.gh_s;
-    int64_t at = 0;
-    for (int j = 0; j < 3; ++j) {
-        J.start[j] = (int)at;
-        const int64_t tiles = ((J.job[j].C + kCols - 1) / kCols) * ((J.job[j].R + CT_ROWS - 1) / CT_ROWS);
-        at += (tiles + 7) / 8 * 8;
-        // (no matrices that fit 288 GB of memory come near this)
-        if (at > (int64_t)(UINT32_MAX / kThreads))
-            return mxk::fail(MX_EUNSUPPORTED, "too many tiles to cast in one launch");
-    }
+    auto tiles = [&](int cols) {
+        int64_t at = 0;
+        for (int j = 0; j < 3; ++j) {
+            J.start[j] = (int)at;
+            at += (((J.job[j].C + cols - 1) / cols) * ((J.job[j].R + CT_ROWS - 1) / CT_ROWS) + 7) / 8 * 8;
+        }
+        return at;
+    };
+    int64_t at = tiles(kCols);
+    // (no matrices that fit 288 GB of memory come near this)
+    if (at > (int64_t)(UINT32_MAX / kThreads))
+        return mxk::fail(MX_EUNSUPPORTED, "too many tiles to cast in one launch");
+    const bool narrow = gate && at <= kNarrowTiles;
+    if (narrow)
+        at = tiles(kCols / 2);
     auto launch = [&](auto fp4, auto act) {
-        hipLaunchKernelGGL((cast_jobs_kernel<decltype(fp4)::value, kCols, kThreads, decltype(act)::value>),
+        constexpr int ACT = decltype(act)::value;
+        if constexpr (ACT >= 0) {
+            if (narrow) {
+                hipLaunchKernelGGL((cast_jobs_kernel<decltype(fp4)::value, kCols / 2, kThreads, ACT>),
+                                   dim3((unsigned)at), dim3(kThreads), 0, stream, J);
+                return;
+            }
+        }
+        hipLaunchKernelGGL((cast_jobs_kernel<decltype(fp4)::value, kCols, kThreads, ACT>),
                            dim3((unsigned)at), dim3(kThreads), 0, stream, J);
     };
     auto launch_act = [&](auto fp4) {

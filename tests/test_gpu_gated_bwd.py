@@ -192,13 +192,15 @@ def test_whole_backward(elem, T, F, d, grad_dtype):
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("elem", ELEMS)
 @pytest.mark.parametrize("T,F,d", [(1, 128, 16), (37, 384, 48), (128, 128, 272), (300, 640, 512), (1025, 1152, 256),
-                                   (160, 6272, 64), (150, 64, 32), (70, 192, 16), (200, 6208, 32)])
+                                   (160, 6272, 64), (150, 64, 32), (70, 192, 16), (200, 6208, 32),
+                                   (4130, 8256, 48), (2100, 14400, 32)])
 def test_casts_byte_for_byte(elem, act, T, F, d):
     if elem == "e2m1" and F % 128:
         F += 64
     # what the products take, in a workspace of the test's own: the casts of the
     # gradient that mx_gated_bwd gives, padded with rows of zeros.  6272: from 48
-    # column tiles on they are visited in another order.  Infinities and NaN too
+    # column tiles on they are visited in another order; the last two have over 2048
+    # tiles, which are then of 128 columns, not 64.  Infinities and NaN too
     c = Case(T, F, d, seed=9)
     c.gh[T // 2, 5] = float("inf")
     c.gh[0, F - 1] = float("nan")
