@@ -196,7 +196,7 @@ mx_status mxnorm_linear_bwd(const void *grad_h, const void *x, const float *rho,
     if ((st = mxb::backward_casts(grad_h, x, rho, w, T, T, N, d, elem,
                                   {s.gh, s.gh_s, s.ght, s.ght_s, s.wt, s.wt_s, s.xt, s.xt_s},
                                   nullptr, stream)) != MX_OK ||
-        (st = mxg::matmul_pair(gw, MX_OUT_F32, gz, elem, stream)) != MX_OK)
+        (st = mxg::matmul_pair(gw, MX_OUT_F32, gz, elem, false, stream)) != MX_OK)
         return st;
     return mxnorm_ste_bwd(x, s.gz, gamma, rho, T, d, out_dtype, grad_x, grad_gamma, s.ste,
                           s.ste_bytes, stream);
@@ -245,7 +245,7 @@ mx_status mxnorm_gated_bwd(const void *grad_h, const void *gu, const void *x, co
     if ((st = mxb::backward_casts(grad_h, x, rho, w, T, Tp, N, d, elem,
                                   {s.gh, s.gh_s, s.ght, s.ght_s, s.wt, s.wt_s, s.xt, s.xt_s}, &gate,
                                   stream)) != MX_OK ||
-        (st = mxg::matmul_pair(gw, grad_dtype, gz, elem, stream)) != MX_OK)
+        (st = mxg::matmul_pair(gw, grad_dtype, gz, elem, true, stream)) != MX_OK)
         return st;
     return mxb::ste(x, s.gz, gamma, rho, T, d, out_dtype, grad_x, grad_dtype, grad_gamma, s.ste,
                     stream);

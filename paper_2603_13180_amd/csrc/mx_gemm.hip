@@ -198,19 +198,40 @@ inline int64_t pair_plan(PairArgs &W, int cus)
     return best;
 }
 
+// As mx_gemm_ring_pair_kernel, but product 1 on 64 x 64 tiles with K split over
+// four waves: where it has few tiles and many steps (a gated backward's grad_Z,
+// whose K is 2F), its workgroups' chains of steps are the launch's time, and here a
+// quarter as long.  W.second_first: its tiles come first.
+template <int ELEM, int OUT0>
+__global__ void __launch_bounds__(R64x128::NT) mx_gemm_split_pair_kernel(RingPair W)
+{
+    using O = KSplitOp<G64x64, ELEM, 0>;
+    static_assert(R64x128::NT == G64x64::NT, "one launch");
+    constexpr int RING = R64x128::S * RingOp<R64x128, ELEM>::STAGE, PARTS = G64x64::NW * O::PART;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[RING > PARTS ? RING : PARTS];
+    const int b = blockIdx.x;
+    const int first = W.second_first ? W.n1 : W.n0;
+    if ((b < first) == (W.second_first != 0))
+        ksplit_tile<ELEM, MX_OUT_BF16, G64x64, 0>(W.p[1], (LDS_AS uint8_t *)lds, nullptr, nullptr,
+                                                  W.second_first ? b : b - first);
+    else
+        ring_tiles<ELEM, OUT0, R64x128>(W.p[0], (LDS_AS uint8_t *)lds, W.second_first ? b - first : b, W.n0);
+}
+
 // How two products are computed: one launch each, or in one launch on 256 x
 // 256 tiles shared out by load or on 64 x 128 tiles that are all resident at
-// once, where that is 3% cheaper.
-enum PairMode { PAIR_APART, PAIR_LARGE, PAIR_SMALL };
+// once, where that is 3% cheaper; or (where the caller allows sums in the order of
+// K-split tiles) on 64 x 128 and K-split tiles.
+enum PairMode { PAIR_APART, PAIR_LARGE, PAIR_SMALL, PAIR_SPLIT };
 struct PairPlan {
     int mode;
     bool can_large;             // the shares of the large tiles were found
-    double apart, large, small; // us; large or small = apart: not possible
+    double apart, large, small, split; // us; large, small or split = apart: not possible
     PairArgs W;
-    RingPair Q;
+    RingPair Q, K; // small, split
 };
 
-inline void plan_pair(PairPlan &P, const Args &A0, const Args &A1)
+inline void plan_pair(PairPlan &P, const Args &A0, const Args &A1, bool may_split)
 {
     const int cus = A0.grid_max;
     P.apart = plan_product(A0.M, A0.N, A0.steps, cus).us + plan_product(A1.M, A1.N, A1.steps, cus).us;
@@ -240,6 +261,25 @@ inline void plan_pair(PairPlan &P, const Args &A0, const Args &A1)
     P.mode = P.small <= P.large && P.small < 0.97 * P.apart ? PAIR_SMALL
              : P.large < 0.97 * P.apart                     ? PAIR_LARGE
                                                             : PAIR_APART;
+
+    // Product 1 on K-split tiles.  us of a compute unit: 0.45 and 0.3 for the
+    // operands of a step of either tile at 55 GB/s, 0.6 of which the longer chain
+    // of steps does not cover (1 us a step of a K-split wave, 0.5 of a ring).
+    // On 56 sizes of T = 50 .. 3000, F = 512 .. 6144, d = 384 .. 3328 that it was not
+    // fitted to the choice is 1.2% slower than the faster one on average and 12% at
+    // most; without this launch 5.7% and 42%.  (With more than six tiles a compute
+    // unit up to 25%.)  F = 2048, d = 768, E4M3, T = 1024: 23.8 -> 19.4 us; F = d =
+    // 2048, T = 128 19.5 -> 15.9.
+    P.K = P.Q;
+    set_tiles(P.K.p[1], G64x64::BM, G64x64::BN, 1024);
+    P.K.n1 = P.K.p[1].cells;
+    const double own = (A1.steps + G64x64::NW - 1) / G64x64::NW, ring = 0.5 * A0.steps;
+    P.K.second_first = own >= ring;
+    const double bytes = (0.45 * P.K.n0 * A0.steps + 0.3 * P.K.n1 * A1.steps) / cus;
+    P.split = 3.0 + 0.6 * bytes + std::max(own, ring);
+    const double now = P.mode == PAIR_SMALL ? P.small : P.mode == PAIR_LARGE ? P.large : P.apart;
+    if (may_split && (int64_t)P.K.n0 + P.K.n1 <= 6 * (int64_t)cus && P.split < now)
+        P.mode = PAIR_SPLIT;
 }
 
 // Products 0 (output OUT0) and 1 (bf16 output) on one stream.
@@ -251,6 +291,11 @@ hipError_t multiply_pair_as(const PairPlan &P, const Args &A0, const Args &A1, h
                            dim3((unsigned)(P.Q.n0 + P.Q.n1)), dim3(R64x128::NT), 0, stream, P.Q);
         return hipGetLastError();
     }
+    if (P.mode == PAIR_SPLIT) {
+        hipLaunchKernelGGL((mx_gemm_split_pair_kernel<ELEM, OUT0>), dim3((unsigned)(P.K.n0 + P.K.n1)),
+                           dim3(R64x128::NT), 0, stream, P.K);
+        return hipGetLastError();
+    }
     if (P.mode == PAIR_LARGE) {
         hipLaunchKernelGGL((mx_gemm_pair_kernel<ELEM, OUT0>), dim3((unsigned)A0.grid_max), dim3(NT), 0,
                            stream, P.W);
@@ -260,10 +305,11 @@ hipError_t multiply_pair_as(const PairPlan &P, const Args &A0, const Args &A1, h
     return e != hipSuccess ? e : multiply<ELEM, OUT0>(A0, stream);
 }
 
-template <int ELEM, int OUT0> hipError_t multiply_pair(const Args &A0, const Args &A1, hipStream_t stream)
+template <int ELEM, int OUT0>
+hipError_t multiply_pair(const Args &A0, const Args &A1, bool may_split, hipStream_t stream)
 {
     PairPlan P;
-    plan_pair(P, A0, A1);
+    plan_pair(P, A0, A1, may_split);
     return multiply_pair_as<ELEM, OUT0>(P, A0, A1, stream);
 }
 
@@ -389,7 +435,7 @@ mx_status mx_matmul_fwd(const uint8_t *a_codes, const uint8_t *a_scales, const u
 
 namespace mxg {
 
-mx_status matmul_pair(const Product &first, int out0, const Product &bf16, int elem,
+mx_status matmul_pair(const Product &first, int out0, const Product &bf16, int elem, bool may_split,
                       hipStream_t stream)
 {
     Args A0, A1;
@@ -397,11 +443,11 @@ mx_status matmul_pair(const Product &first, int out0, const Product &bf16, int e
     product_args(A1, bf16, elem, stream);
     hipError_t e;
     if (elem == MX_ELEM_E4M3)
-        e = out0 == MX_OUT_F32 ? multiply_pair<MX_ELEM_E4M3, MX_OUT_F32>(A0, A1, stream)
-                               : multiply_pair<MX_ELEM_E4M3, MX_OUT_BF16>(A0, A1, stream);
+        e = out0 == MX_OUT_F32 ? multiply_pair<MX_ELEM_E4M3, MX_OUT_F32>(A0, A1, may_split, stream)
+                               : multiply_pair<MX_ELEM_E4M3, MX_OUT_BF16>(A0, A1, may_split, stream);
     else
-        e = out0 == MX_OUT_F32 ? multiply_pair<MX_ELEM_E2M1, MX_OUT_F32>(A0, A1, stream)
-                               : multiply_pair<MX_ELEM_E2M1, MX_OUT_BF16>(A0, A1, stream);
+        e = out0 == MX_OUT_F32 ? multiply_pair<MX_ELEM_E2M1, MX_OUT_F32>(A0, A1, may_split, stream)
+                               : multiply_pair<MX_ELEM_E2M1, MX_OUT_BF16>(A0, A1, may_split, stream);
     return e == hipSuccess ? MX_OK
                            : mxk::fail(MX_EHIP, "kernel launch failed: %s", hipGetErrorString(e));
 }
@@ -452,6 +498,17 @@ int mxt_product_plan(int64_t M, int64_t N, int64_t K, int elem, int units, int *
     return P.shape;
 }
 
+int mxt_gated_pair_plan(int64_t M0, int64_t N0, int64_t K0, int64_t M1, int64_t N1, int64_t K1,
+                        int elem, int units)
+{
+    mxg::Args A0, A1;
+    if (!plan_args(A0, M0, N0, K0, elem, units) || !plan_args(A1, M1, N1, K1, elem, units))
+        return -1;
+    mxg::PairPlan P;
+    mxg::plan_pair(P, A0, A1, true);
+    return P.mode;
+}
+
 int mxt_pair_plan(int64_t M0, int64_t N0, int64_t K0, int64_t M1, int64_t N1, int64_t K1, int elem,
                   int units, double *us)
 {
@@ -459,7 +516,7 @@ int mxt_pair_plan(int64_t M0, int64_t N0, int64_t K0, int64_t M1, int64_t N1, in
     if (!plan_args(A0, M0, N0, K0, elem, units) || !plan_args(A1, M1, N1, K1, elem, units))
         return -1;
     mxg::PairPlan P;
-    mxg::plan_pair(P, A0, A1);
+    mxg::plan_pair(P, A0, A1, false);
     us[0] = P.apart;
     us[1] = P.large;
     us[2] = P.small;
@@ -511,8 +568,8 @@ mx_status mxt_matmul_pair(const MxtProduct *f32, const MxtProduct *bf16, int ele
     if (units)
         A0.grid_max = A1.grid_max = units;
     mxg::PairPlan P;
-    mxg::plan_pair(P, A0, A1);
-    if (mode < 0 || mode > mxg::PAIR_SMALL || (mode == mxg::PAIR_LARGE && !P.can_large))
+    mxg::plan_pair(P, A0, A1, false);
+    if (mode < 0 || mode > mxg::PAIR_SPLIT || (mode == mxg::PAIR_LARGE && !P.can_large))
         return mxk::fail(MX_EINVAL, "no such pair launch");
     P.mode = mode;
     const hipError_t e = elem == MX_ELEM_E4M3

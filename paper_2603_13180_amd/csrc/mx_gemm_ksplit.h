@@ -42,8 +42,11 @@ template <class C, int ELEM, int NORM> struct KSplitOp {
 
 template <int OUT, int NORM> using KSplitArgs = std::conditional_t<(NORM > 0), NormedArgs, ArgsOf<OUT>>;
 
+// Tile v of the launch on this workgroup.  lds: NW PART bytes; NORM: act, NW AREA
+// bytes, and red, NW ROWS sums.
 template <int ELEM, int OUT, class C, int NORM>
-__global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(KSplitArgs<OUT, NORM> A)
+__device__ __forceinline__ void ksplit_tile(const KSplitArgs<OUT, NORM> &A, LDS_AS uint8_t *lds,
+                                            LDS_AS uint8_t *act, LDS_AS double *red, int v)
 {
     using O = KSplitOp<C, ELEM, NORM>;
     using R = typename O::R;
@@ -51,15 +54,12 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(KSplitArgs<OUT, N
     constexpr bool GATED = kGated<OUT>;
     constexpr int CN = kCols<OUT>(C::BN); // output columns of a tile
     constexpr int SB = O::SB, DW = SB / 4, AR = O::AR;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[C::NW * O::PART];
-    __shared__ __attribute__((aligned(16))) uint8_t act[NORM ? C::NW * R::AREA : 16];
-    __shared__ double red[NORM ? C::NW * R::ROWS : 1];
 
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l = threadIdx.x & 63;
     const int g = l >> 4, qd = l & 15;
     int64_t m0, n0;
-    tile_of(A, C::BM, CN, blockIdx.x, m0, n0);
+    tile_of(A, C::BM, CN, v, m0, n0);
     if (m0 >= A.M || n0 >= A.N) // a part of a cell that lies outside H
         return;
 
@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(KSplitArgs<OUT, N
                                      (GATED && r >= AR + CN ? A.N : 0)) * A.rs) + 4 * (dw % DW);
     }
 
-    LDS_AS uint8_t *ring = (LDS_AS uint8_t *)lds + w * O::PART;
+    LDS_AS uint8_t *ring = lds + w * O::PART;
     const uint32_t ring_addr = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)ring);
     auto issue = [&](int k, int slot) {
         const uint32_t st = ring_addr + slot * O::SLOT;
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(KSplitArgs<OUT, N
         for (int i = 0; i < C::FN; ++i)
             acc[j][i] = v4f{0.f, 0.f, 0.f, 0.f};
     const int mine = w < A.steps ? (A.steps - w - 1) / C::NW + 1 : 0; // this wave's steps
-    LDS_AS uint8_t *area = (LDS_AS uint8_t *)act + w * R::AREA;
+    LDS_AS uint8_t *area = act + w * R::AREA;
     if constexpr (NORM > 0) {
         LDS_AS uint8_t *xs = O::S == 2 ? ring + O::SLOT : area;
         R::load(A, __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)xs), w, l);
@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(KSplitArgs<OUT, N
         R::read(xs, l, x);
         if (O::S == 2 && mine > 1)
             issue(w + C::NW, 1);
-        R::cast(A, x, area, (LDS_AS double *)red, n0 == 0, w, l);
+        R::cast(A, x, area, red, n0 == 0, w, l);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     } else {
 #pragma unroll 1
@@ -179,8 +179,7 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(KSplitArgs<OUT, N
         v4f v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int u = 0; u < C::NW; ++u)
-            v += reinterpret_cast<const LDS_AS v4f *>((LDS_AS uint8_t *)lds +
-                                                      u * O::PART)[f * 64 + l];
+            v += reinterpret_cast<const LDS_AS v4f *>(lds + u * O::PART)[f * 64 + l];
         return v;
     };
     if constexpr (GATED) {
@@ -212,6 +211,21 @@ __global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(KSplitArgs<OUT, N
                 *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(A.out) + m * A.N + n) =
                     make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
         }
+    }
+}
+
+template <int ELEM, int OUT, class C, int NORM>
+__global__ void __launch_bounds__(C::NT) mx_gemm_ksplit_kernel(KSplitArgs<OUT, NORM> A)
+{
+    using O = KSplitOp<C, ELEM, NORM>;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[C::NW * O::PART];
+    if constexpr (NORM > 0) {
+        __shared__ __attribute__((aligned(16))) uint8_t act[C::NW * O::R::AREA];
+        __shared__ double red[C::NW * O::R::ROWS];
+        ksplit_tile<ELEM, OUT, C, NORM>(A, (LDS_AS uint8_t *)lds, (LDS_AS uint8_t *)act, (LDS_AS double *)red,
+                                        blockIdx.x);
+    } else {
+        ksplit_tile<ELEM, OUT, C, 0>(A, (LDS_AS uint8_t *)lds, nullptr, nullptr, blockIdx.x);
     }
 }
 

@@ -61,8 +61,9 @@ mx_status check_gated_bwd(const void *grad_h, const void *gu, int64_t T, int64_t
 // A product with output of type out0 and one with bf16 output that do not
 // depend on each other, on one stream: within mx_matmul_fwd's bound, in one
 // launch or two, so the sums may be taken in another order than by two
-// mx_matmul_fwd calls.
-mx_status matmul_pair(const Product &first, int out0, const Product &bf16, int elem,
+// mx_matmul_fwd calls.  may_split: the second's also as four partial sums, where
+// that is faster.
+mx_status matmul_pair(const Product &first, int out0, const Product &bf16, int elem, bool may_split,
                       hipStream_t stream);
 
 } // namespace mxg

@@ -30,6 +30,11 @@ int mxt_product_plan(int64_t M, int64_t N, int64_t K, int elem, int units, int *
 int mxt_pair_plan(int64_t M0, int64_t N0, int64_t K0, int64_t M1, int64_t N1, int64_t K1, int elem,
                   int units, double *us);
 
+// The same of mxnorm_gated_bwd, which may also take 3: one launch of 64 x 128
+// tiles and, for product 1, 64 x 64 tiles with K split over four waves.
+int mxt_gated_pair_plan(int64_t M0, int64_t N0, int64_t K0, int64_t M1, int64_t N1, int64_t K1,
+                        int elem, int units);
+
 // mx_matmul_fwd with blocks of 32 in a given way, so that every kernel is
 // reached at sizes the oracle can check: in tiles of `shape`, or, whole > 0,
 // that many cells of 256 x 256 in a first launch and the rest in tiles of
@@ -63,7 +68,7 @@ typedef struct MxtProduct {
 } MxtProduct;
 
 // Two products as mxnorm_linear_bwd computes them, one with float and one with
-// bf16 output, in a given way (mxt_pair_plan's numbers).  MX_EINVAL if the
+// bf16 output, in a given way (mxt_gated_pair_plan's numbers).  MX_EINVAL if the
 // large tiles cannot be shared out.
 mx_status mxt_matmul_pair(const MxtProduct *f32, const MxtProduct *bf16, int elem, int mode,
                           int units, hipStream_t stream);
