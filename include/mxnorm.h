@@ -340,7 +340,7 @@ mx_status mxnorm_linear_bwd(const void *grad_h, const void *x, const float *rho,
  *   G = dec(A) dec(W[0 .. F))^T,  U = dec(A) dec(W[F .. 2F))^T,
  *   H = act(G) . U                                               [M, F]
  * G and U are the float sums of mx_matmul_fwd (its bound, its note on the order
- * of additions, with four partial sums); activation and product are computed in
+ * of additions, with four partial sums, and K from any step on); activation and product are computed in
  * float.  Non-finite
  * values follow the formula: a NaN gives NaN, act(-inf) is NaN, act(+inf) is
  * inf; a finite G too negative for the exponential gives act(G) = -0.

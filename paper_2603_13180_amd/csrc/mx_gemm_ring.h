@@ -167,6 +167,13 @@ __device__ __forceinline__ void ring_tiles(const ArgsOf<OUT> &A, LDS_AS uint8_t 
     // being multiplied
     const int G = A.cells * A.sub_m * A.sub_n;
     int iv = first, is = 0, islot = 0, ahead = -1;
+    // NT: the tile's K steps in turn from `from` on.  Weights that are read once come
+    // from HBM, and workgroups that all start at step 0 ask few of its channels for
+    // the same columns of rows a power of two apart (61 rows of 28672 x 8192: E4M3
+    // 111.8 -> 107.8 us, E2M1 60.7 -> 58.0; 32 of 14336 x 4096 E4M3 29.0 -> 27.6.  The
+    // K-split tiles, whose waves are at different steps anyhow, lose up to 11%, and
+    // rings over weights below 96 MB up to 4%.)
+    int from = NT ? iv * 7 % A.steps : 0;
     RingTile<C, ELEM> T;
     int64_t im, in;
     tile_of(A, C::BM, CN, iv, im, in);
@@ -174,7 +181,8 @@ __device__ __forceinline__ void ring_tiles(const ArgsOf<OUT> &A, LDS_AS uint8_t 
     auto issue = [&] {
         if (iv >= G)
             return;
-        ring_issue<C, ELEM, GATED, NT>(T, is, st0_addr + islot * O::STAGE, w);
+        const int k = !NT || is + from < A.steps ? is + from : is + from - A.steps;
+        ring_issue<C, ELEM, GATED, NT>(T, k, st0_addr + islot * O::STAGE, w);
         islot = islot + 1 == C::S ? 0 : islot + 1;
         ++ahead;
         if (++is == A.steps) {
@@ -183,6 +191,7 @@ __device__ __forceinline__ void ring_tiles(const ArgsOf<OUT> &A, LDS_AS uint8_t 
             if (iv < G) {
                 tile_of(A, C::BM, CN, iv, im, in);
                 T = ring_tile<C, ELEM, GATED>(A, im, in, w, l);
+                from = NT ? iv * 7 % A.steps : 0;
             }
         }
     };

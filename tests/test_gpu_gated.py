@@ -324,3 +324,29 @@ def test_feed_forward_forward():
     # differs by at most one step, 2^-3 of the element, in few places
     err = np.linalg.norm(y.cpu().numpy() - want) / np.linalg.norm(want)
     assert err <= 2.0 ** -8, err
+
+
+@pytest.mark.parametrize("elem", ELEMS)
+@pytest.mark.parametrize("M", [1, 5, 29, 61, 120])
+def test_large_weights_read_once(elem, M):
+    # over 96 MB: a tile's K steps in an order of its own.  Codes of 0, 1 and -1 and
+    # scales of 1 and 2: sums below 2^16, exact in any order
+    F, K = (12800, 4096) if elem == "e4m3" else (12800, 8192)
+    gen = torch.Generator(device=DEV).manual_seed(M)
+    val = torch.tensor([0.0, 1.0, -1.0, 0.0], device=DEV)
+    code = torch.tensor([0x00, 0x38, 0xB8, 0x00] if elem == "e4m3" else [0, 2, 10, 0], dtype=torch.uint8, device=DEV)
+
+    def operand(rows):
+        i = torch.randint(0, 4, (rows, K), generator=gen, device=DEV)
+        e = torch.randint(0, 2, (rows, K // 32), generator=gen, device=DEV)
+        c = code[i]
+        if elem == "e2m1":
+            c = c[:, 0::2] | (c[:, 1::2] << 4)
+        return c.contiguous(), (127 + e).to(torch.uint8), val[i] * torch.exp2(e.float()).repeat_interleave(32, 1)
+    (ac, as_, a), (wc, ws, w) = operand(M), operand(2 * F)
+    assert wc.numel() >= 96 << 20
+    h, gu = mxnorm.mx_gated_fwd(ac, as_, wc, ws, K, elem=elem, out_dtype=torch.float32, save_gu=True)
+    exact = torch.cat([a.double() @ p.double().t() for p in w.split(3200)], 1)
+    assert exact.abs().max() < 1 << 16 and torch.equal(gu, exact.to(torch.bfloat16))
+    want = act64(exact.cpu().numpy()[:, :F], "silu") * exact.cpu().numpy()[:, F:]
+    assert (np.abs(h.cpu().numpy() - want) <= 2.0 ** -14 * np.abs(want) + 2.0 ** -120 * np.abs(exact.cpu().numpy()[:, :F] * exact.cpu().numpy()[:, F:])).all()

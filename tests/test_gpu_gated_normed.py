@@ -97,9 +97,9 @@ def two_calls(x, wc, ws, elem, p, mode, act, dtype, keep, want_rho):
 # one K step (three waves without one), steps that no four waves share evenly,
 # the longest rows that fit, for both numbers of chunks; F of half a tile, of a tile and a half, of many
 SIZES = {"e4m3": [(1, 128, 32), (2, 384, 96), (3, 640, 32), (4, 1152, 1024), (2, 4096, 64), (1, 8192, 96),
-                  (3, 2176, 32), (4, 4096, 64), (2, 8192, 32), (1, 16384, 64)],
+                  (3, 2176, 32), (4, 4096, 64), (2, 8192, 32), (1, 16384, 64), (2, 4096, 12800), (3, 4096, 12800)],
          "e2m1": [(1, 256, 32), (2, 768, 96), (3, 1280, 32), (4, 1792, 1024), (2, 4096, 64), (1, 8192, 96),
-                  (3, 2304, 32), (4, 4096, 64), (2, 8192, 32), (1, 16384, 64)]}
+                  (3, 2304, 32), (4, 4096, 64), (2, 8192, 32), (1, 16384, 64), (1, 8192, 12800), (2, 8192, 12800)]}
 
 
 @gpu
