@@ -173,7 +173,8 @@ hipError_t launch_shape(int shape, const ArgsOf<OUT> &A, hipStream_t stream)
 // A weight of this many bytes that a launch reads once (one row of tiles) is
 // loaded past the caches' normal allocation: no later call finds it there.
 // Cycling through 550 to 600 MB of weights at 1 to 61 rows: 117 MB (E4M3) 26.7
-// -> 24.7 and 32.1 -> 30.4 us, 134 MB 28.9 -> 25.7; but 62 MB (E2M1) 13.1 ->
+// -> 24.7 and 32.1 -> 30.4 us (and 29.5 with the rings' K steps in turn), 134 MB
+// 28.9 -> 25.7; but 62 MB (E2M1) 13.1 ->
 // 12.9 and 16.8 -> 16.7, 67 MB 14.2 -> 15.4, 17 MB (E4M3) 10.1 -> 11.1.
 constexpr int64_t kOnceBytes = 96 << 20;
 inline bool read_once(const GatedArgs &A) { return A.tiles_m == 1 && 2 * A.N * A.rb >= kOnceBytes; }
