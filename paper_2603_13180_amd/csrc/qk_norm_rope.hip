@@ -596,13 +596,16 @@ template <bool BWD> void launch(const Args &A, bool inter, unsigned grid, hipStr
 inline void steps_of(Heads &H, int64_t T, int R, int64_t least)
 {
     H.tb = 1;
+    H.steps = 0;
+    if (H.heads == 0) // no items, however many tokens: nothing below would bound tb
+        return;
     auto items = [&](int tb) { return (tb + H.tpi - 1) / H.tpi * H.blocks; };
     auto angles = [&](int tb) { return tb * (R / 2); };
     while (angles(2 * H.tb) <= ANGLES &&
            ((items(2 * H.tb) <= NW && angles(2 * H.tb) <= NT) ||
             (items(2 * H.tb) <= 4 * NW && T / (2 * H.tb) >= least)))
         H.tb *= 2;
-    H.steps = H.heads ? (T + H.tb - 1) / H.tb : 0;
+    H.steps = (T + H.tb - 1) / H.tb;
 }
 
 // Workgroups: forward one for each step, backward at most two a compute unit,
@@ -784,6 +787,8 @@ mx_status qk_norm_rope_bwd(const mx_heads *grad_q_out, const mx_heads *grad_k_ou
     mxq::steps_of(A.q, T, A.R, 224);
     mxq::steps_of(A.k, T, A.R, 224);
     const unsigned grid = mxq::workgroups(A, true);
+    if (grid == 0 && !gains)
+        return MX_OK;
     if (grid > 0)
         mxq::launch<true>(A, interleaved != 0, grid, stream);
     if (gains)
