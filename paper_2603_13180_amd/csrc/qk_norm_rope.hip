@@ -297,10 +297,13 @@ __device__ __forceinline__ Item widen(const uint4 (&v)[2])
 }
 
 // r = (sum x^2 / D + eps)^(-1/2) of the lane's head: the sum in float where its
-// squares cannot leave float's range (between 2^-100 and 2^100), else, for the
-// whole wave and rarely, in double; 0 for a radicand that is zero or infinite.
+// squares cannot leave float's range (between 2^-100 and 2^100), else in double;
+// 0 for a radicand that is zero or infinite.  A wave computes the double sums if
+// one of its heads needs them, but each head takes its own, so that its bits do
+// not depend on the others.  Lanes without a head (`on` false), whose elements
+// are zeros, ask for none, and get an r that is finite for any eps.
 template <int G>
-__device__ __forceinline__ float inverse_rms(const Args &A, const Item &x)
+__device__ __forceinline__ float inverse_rms(const Args &A, const Item &x, bool on)
 {
     float s = 0.0f;
 #pragma unroll
@@ -311,7 +314,10 @@ __device__ __forceinline__ float inverse_rms(const Args &A, const Item &x)
         s = __builtin_fmaf(x.q[i].b1, x.q[i].b1, s);
     }
     s = head_sum<G>(s);
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(s > 0x1p-100f && s < 0x1p100f)) != 0, 0)) {
+    s = on ? s : 1.0f;
+    const bool far = !(s > 0x1p-100f && s < 0x1p100f);
+    float r = __builtin_amdgcn_rsqf(__builtin_fmaf(s, (float)A.inv_d, A.eps));
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(far) != 0, 0)) {
         double S = 0.0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -319,18 +325,19 @@ __device__ __forceinline__ float inverse_rms(const Args &A, const Item &x)
             S += a * a + b * b + c * c + d * d;
         }
         const double u = head_sum<G>(S) * A.inv_d + (double)A.eps;
-        return u == 0.0 || u == INFINITY ? 0.0f : (float)(1.0 / sqrt(u));
+        if (far)
+            r = u == 0.0 || u == INFINITY ? 0.0f : (float)(1.0 / sqrt(u));
     }
-    return __builtin_amdgcn_rsqf(__builtin_fmaf(s, (float)A.inv_d, A.eps));
+    return r;
 }
 
 template <int G, bool INTER, bool FULL>
-__device__ __forceinline__ void forward_item(const Args &A, const Lane<G, FULL> &L, const Loaded<false> &v,
+__device__ __forceinline__ void forward_item(const Args &A, const Lane<G, FULL> &L, bool on, const Loaded<false> &v,
                                              const uint4 (&gain)[2], const float *cs, const float *sn,
                                              uint32_t (&a)[4], uint32_t (&b)[4])
 {
     const Item x = widen(v.x);
-    const float r = inverse_rms<G>(A, x);
+    const float r = inverse_rms<G>(A, x, on);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const Quad g = widen(gain[0], gain[1], i), q = x.q[i];
@@ -345,12 +352,12 @@ __device__ __forceinline__ void forward_item(const Args &A, const Lane<G, FULL> 
 // The gradient of x is r (v - k n) with n = x r and k = (1/D) sum v n: no term
 // overflows or underflows where x is huge or tiny.
 template <int G, bool INTER, bool FULL>
-__device__ __forceinline__ void backward_item(const Args &A, const Lane<G, FULL> &L, const Loaded<true> &v,
+__device__ __forceinline__ void backward_item(const Args &A, const Lane<G, FULL> &L, bool on, const Loaded<true> &v,
                                               const uint4 (&gain)[2], const float *cs, const float *sn,
                                               uint32_t (&a)[4], uint32_t (&b)[4], float (&sum)[16])
 {
     Item n = widen(v.x), w;
-    const float r = inverse_rms<G>(A, n);
+    const float r = inverse_rms<G>(A, n, on);
     float u = 0.0f;
     auto one = [&](float &x, float m, float g, float &to) {
         x = x * r;
@@ -439,9 +446,9 @@ __device__ __forceinline__ int64_t heads_of_kind(const Args &A, const Heads &H, 
             opaque(gain); // or they are all kept widened, 16 registers more
             uint32_t a[4], b[4];
             if constexpr (BWD)
-                backward_item<G, INTER, FULL>(A, L, v, gain, c, d, a, b, sum);
+                backward_item<G, INTER, FULL>(A, L, on, v, gain, c, d, a, b, sum);
             else
-                forward_item<G, INTER, FULL>(A, L, v, gain, c, d, a, b);
+                forward_item<G, INTER, FULL>(A, L, on, v, gain, c, d, a, b);
             if (on && L.in_a)
                 store16(y, a);
             if (on && L.in_b)

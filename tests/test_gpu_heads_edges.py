@@ -1,5 +1,6 @@
 """Query and key heads at the edges of what the entry points take, on the GPU:
-kinds without heads.  Bounds as in test_gpu_qk_norm_rope."""
+kinds without heads,
+heads beside others that have no norm or are missing.  Bounds as in test_gpu_qk_norm_rope."""
 import pytest
 import torch
 
@@ -32,3 +33,30 @@ def test_kinds_without_heads(T, Hq, Hk, R):
             c.check_backward(g, gg, heads, gy, i)
         else:
             assert (gg == 0).all()
+
+
+@pytest.mark.parametrize("D,R,inter", [(128, 128, False), (64, 32, True), (256, 0, False), (512, 512, False)])
+def test_a_head_does_not_depend_on_its_neighbours(D, R, inter):
+    # the same heads by themselves, beside others, and beside heads of zeros, of
+    # tiny and of huge values (whose squares leave the float range), NaN among them
+    T, H = 3000, 3
+    c = Case(T, 16, 16, D, R, inter)
+    q, gq = c.qkv[:, :16 * D].view(T, 16, D).to(DEV), c.gq.to(DEV)
+    beside = q.clone()
+    beside[:, H] = 0
+    beside[:, H + 1] *= 1e-30
+    beside[:, H + 2] *= 1e30
+    beside[1::2, H + 3] = float("nan")
+    # and, of every other token, one of the heads itself
+    beside[::2, 1] = 0
+    keep = torch.ones(T, H, dtype=torch.bool, device=DEV)
+    keep[::2, 1] = False
+    args = (c.on_gpu()[0], None, *c.on_gpu()[2:])
+
+    def both(x, gy):
+        y, _ = mxnorm.qk_norm_rope_fwd(x, x[:, :0], *args, **c.kw())
+        g = mxnorm.qk_norm_rope_bwd(gy, gy[:, :0], x, x[:, :0], *args, **c.kw())
+        return y[:, :H], g[0][:, :H]
+    for got in (both(q[:, :H], gq[:, :H]), both(q[:, :H + 1], gq[:, :H + 1]), both(beside, gq)):
+        for a, b in zip(got, both(q, gq)):
+            assert torch.equal(a[keep], b[keep])
