@@ -437,7 +437,8 @@ typedef struct {
  *   elements from R on: y = n.
  * r comes from a float sum, or where the squares leave float's range from a
  * double one, and is within 2^-20 of its value (a zero or infinite radicand
- * gives 0); the angle is formed in double turns and
+ * gives 0; beyond 2^126, without eps, it keeps its exponent apart), each head's
+ * from its own elements alone; the angle is formed in double turns and
  * its fraction rounded to float, so far and negative positions keep their
  * angles (to 2^-23 of a turn up to |pos inv_freq| of 2^29); the rest is float,
  * rounded once to bf16.

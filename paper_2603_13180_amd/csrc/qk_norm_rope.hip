@@ -302,9 +302,14 @@ __device__ __forceinline__ Item widen(const uint4 (&v)[2])
 // one of its heads needs them, but each head takes its own, so that its bits do
 // not depend on the others.  Lanes without a head (`on` false), whose elements
 // are zeros, ask for none, and get an r that is finite for any eps.
+// Without eps a head of subnormals has an r of up to 2^138, beyond float: r is
+// then 2^-64 of it and v becomes 2^64 v, exactly, so that x r is what it should
+// be.  (v and not its widened elements, which need not be kept for it: twice the
+// registers made the forward up to 11% slower.)  Returns 2^64 there, else 1.
 template <int G>
-__device__ __forceinline__ float inverse_rms(const Args &A, const Item &x, bool on)
+__device__ __forceinline__ float inverse_rms(const Args &A, uint4 (&v)[2], bool on, float &r)
 {
+    const Item x = widen(v);
     float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -316,7 +321,8 @@ __device__ __forceinline__ float inverse_rms(const Args &A, const Item &x, bool 
     s = head_sum<G>(s);
     s = on ? s : 1.0f;
     const bool far = !(s > 0x1p-100f && s < 0x1p100f);
-    float r = __builtin_amdgcn_rsqf(__builtin_fmaf(s, (float)A.inv_d, A.eps));
+    float up = 1.0f;
+    r = __builtin_amdgcn_rsqf(__builtin_fmaf(s, (float)A.inv_d, A.eps));
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(far) != 0, 0)) {
         double S = 0.0;
 #pragma unroll
@@ -325,19 +331,32 @@ __device__ __forceinline__ float inverse_rms(const Args &A, const Item &x, bool 
             S += a * a + b * b + c * c + d * d;
         }
         const double u = head_sum<G>(S) * A.inv_d + (double)A.eps;
+        const double w = u == 0.0 || u == INFINITY ? 0.0 : 1.0 / sqrt(u);
+        up = far && w > 0x1p126 ? 0x1p64f : 1.0f;
         if (far)
-            r = u == 0.0 || u == INFINITY ? 0.0f : (float)(1.0 / sqrt(u));
+            r = (float)(up > 1.0f ? w * 0x1p-64 : w);
+        if (up > 1.0f) {
+            auto raise = [&](uint32_t &w) { w = pack2(bf16_lo(w) * up, bf16_hi(w) * up); };
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                raise(v[i].x);
+                raise(v[i].y);
+                raise(v[i].z);
+                raise(v[i].w);
+            }
+        }
     }
-    return r;
+    return up;
 }
 
 template <int G, bool INTER, bool FULL>
-__device__ __forceinline__ void forward_item(const Args &A, const Lane<G, FULL> &L, bool on, const Loaded<false> &v,
+__device__ __forceinline__ void forward_item(const Args &A, const Lane<G, FULL> &L, bool on, Loaded<false> &v,
                                              const uint4 (&gain)[2], const float *cs, const float *sn,
                                              uint32_t (&a)[4], uint32_t (&b)[4])
 {
+    float r;
+    inverse_rms<G>(A, v.x, on, r);
     const Item x = widen(v.x);
-    const float r = inverse_rms<G>(A, x, on);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const Quad g = widen(gain[0], gain[1], i), q = x.q[i];
@@ -350,14 +369,15 @@ __device__ __forceinline__ void forward_item(const Args &A, const Lane<G, FULL> 
 }
 
 // The gradient of x is r (v - k n) with n = x r and k = (1/D) sum v n: no term
-// overflows or underflows where x is huge or tiny.
+// overflows or underflows where x is huge or tiny, unless the gradient does.
 template <int G, bool INTER, bool FULL>
-__device__ __forceinline__ void backward_item(const Args &A, const Lane<G, FULL> &L, bool on, const Loaded<true> &v,
+__device__ __forceinline__ void backward_item(const Args &A, const Lane<G, FULL> &L, bool on, Loaded<true> &v,
                                               const uint4 (&gain)[2], const float *cs, const float *sn,
                                               uint32_t (&a)[4], uint32_t (&b)[4], float (&sum)[16])
 {
+    float r;
+    const float up = inverse_rms<G>(A, v.x, on, r);
     Item n = widen(v.x), w;
-    const float r = inverse_rms<G>(A, n, on);
     float u = 0.0f;
     auto one = [&](float &x, float m, float g, float &to) {
         x = x * r;
@@ -376,12 +396,18 @@ __device__ __forceinline__ void backward_item(const Args &A, const Lane<G, FULL>
                   one(n.q[i].b0, m.b0, g.b0, sum[8 + 2 * i]), one(n.q[i].b1, m.b1, g.b1, sum[9 + 2 * i])};
     }
     const float k = head_sum<G>(u) * (float)A.inv_d;
-    auto grad = [&](float x, float t) { return r * __builtin_fmaf(-k, x, t); };
+    auto store = [&](auto grad) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        a[i] = pack2(grad(n.q[i].a0, w.q[i].a0), grad(n.q[i].a1, w.q[i].a1));
-        b[i] = pack2(grad(n.q[i].b0, w.q[i].b0), grad(n.q[i].b1, w.q[i].b1));
-    }
+        for (int i = 0; i < 4; ++i) {
+            a[i] = pack2(grad(n.q[i].a0, w.q[i].a0), grad(n.q[i].a1, w.q[i].a1));
+            b[i] = pack2(grad(n.q[i].b0, w.q[i].b0), grad(n.q[i].b1, w.q[i].b1));
+        }
+    };
+    // (the common case apart: no multiplication, and no copies of w kept for one)
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(up > 1.0f) != 0, 0))
+        store([&](float x, float t) { return r * (up * __builtin_fmaf(-k, x, t)); });
+    else
+        store([&](float x, float t) { return r * __builtin_fmaf(-k, x, t); });
 }
 
 // Steps s, s + nwg, ... below H.steps of one kind of heads, a step being H.tb
@@ -434,7 +460,7 @@ __device__ __forceinline__ int64_t heads_of_kind(const Args &A, const Heads &H, 
         __syncthreads();
 #pragma unroll 1
         for (int i = w; i < n; i += NW) {
-            const Loaded<BWD> v = next;
+            Loaded<BWD> v = next;
             load(i + NW, next);
             int t, h;
             place(i, t, h);

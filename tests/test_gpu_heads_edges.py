@@ -1,6 +1,7 @@
 """Query and key heads at the edges of what the entry points take, on the GPU:
 kinds without heads,
-heads beside others that have no norm or are missing.  Bounds as in test_gpu_qk_norm_rope."""
+heads beside others that have no norm or are missing, heads of subnormals.
+Bounds as in test_gpu_qk_norm_rope."""
 import pytest
 import torch
 
@@ -60,3 +61,30 @@ def test_a_head_does_not_depend_on_its_neighbours(D, R, inter):
     for got in (both(q[:, :H], gq[:, :H]), both(q[:, :H + 1], gq[:, :H + 1]), both(beside, gq)):
         for a, b in zip(got, both(q, gq)):
             assert torch.equal(a[keep], b[keep])
+
+
+@pytest.mark.parametrize("D,R,inter,Hq,Hk", [(128, 128, False, 8, 8), (64, 32, True, 3, 1), (512, 0, False, 2, 1),
+                                             (512, 512, False, 2, 2), (8, 0, False, 5, 1)])
+def test_heads_of_subnormals_without_eps(D, R, inter, Hq, Hk):
+    # multiples of 2^-133, the least value: an inverse RMS of up to 2^133 sqrt(D)
+    T = 12
+    c = Case(T, Hq, Hk, D, R, inter, eps=0.0)
+    g = torch.Generator().manual_seed(D + R)
+    k = torch.randint(-127, 128, (T, Hq + 2 * Hk, D), generator=g)
+    k[1] %= 2
+    k[2] = 0
+    k[1:3, :, 3] = -1                    # one element alone
+    k = k.reshape(T, -1)
+    bits = k.abs() | (k < 0).long() << 15
+    some = torch.arange(T) % 4 != 3      # and tokens of ordinary heads beside them
+    c.qkv = torch.where(some[:, None], bits.to(torch.int16).view(torch.bfloat16), c.qkv)
+    q, kk = c.views(c.qkv.to(DEV))
+    hq, hk = c.views(c.qkv)
+    y = mxnorm.qk_norm_rope_fwd(q, kk, *c.on_gpu(), **c.kw())
+    c.check_forward(y[0], hq, 0)
+    c.check_forward(y[1], hk, 1)
+    # output gradients under which those of x stay below the largest bf16: 2^-30 2^138
+    c.gq, c.gk = c.gq * 2.0 ** -30, c.gk * 2.0 ** -30
+    gx = mxnorm.qk_norm_rope_bwd(c.gq.to(DEV), c.gk.to(DEV), q, kk, *c.on_gpu(), **c.kw())
+    c.check_backward(gx[0], gx[2], hq, c.gq, 0)
+    c.check_backward(gx[1], gx[3], hk, c.gk, 1)
