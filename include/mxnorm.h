@@ -458,9 +458,10 @@ mx_status qk_norm_rope_fwd(const mx_heads *q, const mx_heads *k, const void *q_g
  * Its gradients from those of q_out and k_out, q and k as the forward took
  * them.  Per head, with m the gradient turned back by the angles and v = gamma
  * m:  grad_x = r (v - k n) with n = x r and k = (1/D) sum_e v_e n_e, in float;
- * grad_gamma_e = sum over the tokens and heads of n m, in float within a
- * workgroup's heads (at most 512 workgroups), then in double, in a fixed order:
- * the same call gives the same bits.
+ * grad_gamma_e = sum over the tokens and heads of n m, in float over at most 64
+ * heads and (only where a workgroup has no more for each) 64 of those sums, else
+ * in double, rounded to float for each of at most 512 workgroups and at the end,
+ * in a fixed order: the same call gives the same bits.
  * grad_q, grad_k: bf16; each may be the incoming gradient itself (data and
  * strides).  grad_q_gamma, grad_k_gamma: float [D] or NULL (not computed); with
  * no tokens or heads they are 0.  They need `workspace`, caller-owned device

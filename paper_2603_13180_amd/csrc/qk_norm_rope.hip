@@ -413,11 +413,14 @@ __device__ __forceinline__ void backward_item(const Args &A, const Lane<G, FULL>
 // Steps s, s + nwg, ... below H.steps of one kind of heads, a step being H.tb
 // tokens: wave w takes items w, w + NW, ... of their blocks of heads, an item's
 // loads issued before the item ahead of it is computed, the first before the
-// tokens' angles.  Returns the first step past them.
-template <int G, bool INTER, bool FULL, bool BWD>
+// tokens' angles.  Backward, fold() takes the sums after every CHAIN items.
+// Returns the first step past them.
+constexpr int CHAIN = 64;
+template <int G, bool INTER, bool FULL, bool BWD, class Fold>
 __device__ __forceinline__ int64_t heads_of_kind(const Args &A, const Heads &H, int64_t s, int64_t nwg,
-                                                 float *cs, float *sn, float (&sum)[16])
+                                                 float *cs, float *sn, float (&sum)[16], Fold fold)
 {
+    int chain = 0;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = A.R / 2;
     const Lane<G, FULL> L(A, H);
     uint4 gain[2];
@@ -479,6 +482,12 @@ __device__ __forceinline__ int64_t heads_of_kind(const Args &A, const Heads &H, 
                 store16(y, a);
             if (on && L.in_b)
                 store16(y + step, b);
+            if constexpr (BWD) {
+                if (__builtin_expect(++chain == CHAIN, 0)) {
+                    fold();
+                    chain = 0;
+                }
+            }
         }
     }
     return s;
@@ -491,20 +500,43 @@ template <int G, bool INTER, bool FULL> __global__ void __launch_bounds__(NT) fw
     __shared__ __attribute__((aligned(16))) float cs[ANGLES], sn[ANGLES];
     float none[16];
     const int64_t s =
-        heads_of_kind<G, INTER, FULL, false>(A, A.q, blockIdx.x, gridDim.x, cs, sn, none);
-    heads_of_kind<G, INTER, FULL, false>(A, A.k, s - A.q.steps, gridDim.x, cs, sn, none);
+        heads_of_kind<G, INTER, FULL, false>(A, A.q, blockIdx.x, gridDim.x, cs, sn, none, [] {});
+    heads_of_kind<G, INTER, FULL, false>(A, A.k, s - A.q.steps, gridDim.x, cs, sn, none, [] {});
 }
 
-// As the forward; each lane also keeps the gain gradients of its chunks in
-// float over its heads.  After each kind the workgroup's lanes are added in a
-// fixed order into its row of the partial sums.
+// As the forward; each lane also keeps the gain gradients of its chunks, in
+// float over CHAIN heads and from then on in double in LDS, so that their error
+// does not grow with the tokens.  After each kind the workgroup's lanes are added
+// in a fixed order into its row of the partial sums: in float where no wave had
+// more than CHAIN items (in double always: up to 2 us more), else in double.
 template <int G, bool INTER, bool FULL>
 __global__ void __launch_bounds__(NT) bwd_kernel(Args A)
 {
+    constexpr int GW = 64 / G; // groups of a wave
     __shared__ __attribute__((aligned(16))) float cs[ANGLES], sn[ANGLES];
-    __shared__ float red[NW * 64 / G][16 * G]; // D <= 16 G
+    __shared__ float red[NW * GW][16 * G]; // D <= 16 G
+    __shared__ double kept[NW * GW][16 * G];
+    __shared__ bool folded[NW];
     const Lane<G, FULL> L(A, A.q);
-    auto finish = [&](float (&sum)[16], int which, bool any) {
+    const int w = threadIdx.x >> 6, row = w * GW + L.sub;
+    float sum[16] = {};
+    bool some = false; // this wave has folded its sums
+    auto fold = [&] {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if (L.in_a) {
+                double &to = kept[row][8 * L.ca + e];
+                to = (some ? to : 0.0) + (double)sum[e];
+            }
+            if (L.in_b) {
+                double &to = kept[row][8 * L.cb + e];
+                to = (some ? to : 0.0) + (double)sum[8 + e];
+            }
+            sum[e] = sum[8 + e] = 0.0f;
+        }
+        some = true;
+    };
+    auto finish = [&](int which, bool any) {
         if (!A.part)
             return;
         float *to = A.part + ((int64_t)which * gridDim.x + blockIdx.x) * A.D;
@@ -513,30 +545,43 @@ __global__ void __launch_bounds__(NT) bwd_kernel(Args A)
                 to[e] = 0.0f;
             return;
         }
-        float *row = red[(threadIdx.x >> 6) * (64 / G) + L.sub];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             if (L.in_a)
-                row[8 * L.ca + e] = sum[e];
+                red[row][8 * L.ca + e] = sum[e];
             if (L.in_b)
-                row[8 * L.cb + e] = sum[8 + e];
+                red[row][8 * L.cb + e] = sum[8 + e];
+            sum[e] = sum[8 + e] = 0.0f;
         }
+        if ((threadIdx.x & 63) == 0)
+            folded[w] = some;
         __syncthreads();
+        const bool f[NW] = {folded[0], folded[1], folded[2], folded[3]};
+        const bool in_double = f[0] || f[1] || f[2] || f[3];
         for (int e = threadIdx.x; e < A.D; e += NT) {
-            float t = 0.0f;
+            if (in_double) {
+                double t = 0.0;
+#pragma unroll
+                for (int v = 0; v < NW; ++v)
+#pragma unroll 2
+                    for (int g = v * GW; g < (v + 1) * GW; ++g)
+                        t += (f[v] ? kept[g][e] : 0.0) + (double)red[g][e];
+                to[e] = (float)t;
+            } else {
+                float t = 0.0f;
 #pragma unroll 16
-            for (int g = 0; g < NW * 64 / G; ++g)
-                t += red[g][e];
-            to[e] = t;
+                for (int g = 0; g < NW * GW; ++g)
+                    t += red[g][e];
+                to[e] = t;
+            }
         }
         __syncthreads();
+        some = false;
     };
-    float sq[16] = {};
-    const int64_t s = heads_of_kind<G, INTER, FULL, true>(A, A.q, blockIdx.x, gridDim.x, cs, sn, sq);
-    finish(sq, 0, blockIdx.x < A.q.steps);
-    float sk[16] = {};
-    heads_of_kind<G, INTER, FULL, true>(A, A.k, s - A.q.steps, gridDim.x, cs, sn, sk);
-    finish(sk, 1, s - A.q.steps < A.k.steps);
+    const int64_t s = heads_of_kind<G, INTER, FULL, true>(A, A.q, blockIdx.x, gridDim.x, cs, sn, sum, fold);
+    finish(0, blockIdx.x < A.q.steps);
+    heads_of_kind<G, INTER, FULL, true>(A, A.k, s - A.q.steps, gridDim.x, cs, sn, sum, fold);
+    finish(1, s - A.q.steps < A.k.steps);
 }
 
 // Gain gradients: the workgroups' partial rows [2][P][D] added in double in a

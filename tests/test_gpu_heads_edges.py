@@ -1,7 +1,7 @@
 """Query and key heads at the edges of what the entry points take, on the GPU:
 kinds without heads,
-heads beside others that have no norm or are missing, heads of subnormals.
-Bounds as in test_gpu_qk_norm_rope."""
+heads beside others that have no norm or are missing, heads of subnormals,
+gain gradients over many tokens.  Bounds as in test_gpu_qk_norm_rope."""
 import pytest
 import torch
 
@@ -88,3 +88,20 @@ def test_heads_of_subnormals_without_eps(D, R, inter, Hq, Hk):
     gx = mxnorm.qk_norm_rope_bwd(c.gq.to(DEV), c.gk.to(DEV), q, kk, *c.on_gpu(), **c.kw())
     c.check_backward(gx[0], gx[2], hq, c.gq, 0)
     c.check_backward(gx[1], gx[3], hk, c.gk, 1)
+
+
+def test_gain_gradients_do_not_lose_bits_with_the_tokens():
+    # 2^27 equal heads, 4096 of them to a lane: a float sum of so many is 2.5e-5
+    # off in the median.  Bound: r 2^-20, x r and its product 2^-24 each, 64 terms in
+    # float 64 2^-24, then double, rounded to float twice: below 2^-17.6
+    T, H, D = 1 << 21, 64, 8
+    g = torch.Generator().manual_seed(1)
+    x, gy = [torch.randn(1, 1, D, generator=g).bfloat16() for _ in range(2)]
+    gain = torch.ones(D, dtype=torch.bfloat16, device=DEV)
+    q, dq = [t.to(DEV).expand(T, H, D) for t in (x, gy)]
+    got = mxnorm.qk_norm_rope_bwd(dq, dq[:, :1], q, q[:, :1], gain, gain, None, None, rotary=0)
+    xd = x.double().flatten()
+    term = xd * (xd.square().mean() + 1e-6).rsqrt() * gy.double().flatten()
+    for gg, n in ((got[2], T * H), (got[3], T)):
+        err = (gg.cpu().double() / (term * n) - 1).abs()
+        assert (err <= 2.0 ** -17.6).all(), err.max()
