@@ -147,7 +147,7 @@ bool normed_product(const GatedProduct &P, const RowNorm &n, int elem, hipStream
     A.coef = n.coef;
     A.eps = n.eps;
     set_tiles(A, G16x64::BM, G16x64::BN / 2, 1024);
-    A.once = read_once(A);
+    A.once = read_once(A, S_G16x64);
     st = launched(by_type(elem, P.out_dtype, [&](auto e, auto o) {
         constexpr int E = decltype(e)::value, O = decltype(o)::value;
         return chunks == 4 ? launch_ksplit<E, O, G16x64, 4>(A, stream) : launch_ksplit<E, O, G16x64, 8>(A, stream);
@@ -228,6 +228,17 @@ int mxt_gated_plan(int64_t M, int64_t F, int64_t K, int elem, int units, int *wh
     *tail = P.tail;
     *us = P.us;
     return P.shape;
+}
+
+int mxt_gated_once(int64_t M, int64_t F, int64_t K, int elem, int units)
+{
+    mxg::GatedArgs A{};
+    A.M = M;
+    A.N = F;
+    A.rb = elem == MX_ELEM_E2M1 ? K / 2 : K;
+    A.steps = (int)(A.rb / mxg::KB);
+    const mxg::Plan P = mxg::plan_gated(M, F, A.steps, units);
+    return mxg::read_once(A, P.shape) + (P.whole && mxg::read_once(A, P.tail) ? 2 : 0);
 }
 
 int mxt_gated_normed(int64_t M, int64_t F, int64_t K, int elem, int units)

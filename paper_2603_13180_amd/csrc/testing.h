@@ -51,6 +51,9 @@ mx_status mxt_matmul(const uint8_t *a_codes, const uint8_t *a_scales, const uint
 // 64 with K split over four waves.
 int mxt_gated_plan(int64_t M, int64_t F, int64_t K, int elem, int units, int *whole, int *tail,
                    double *us);
+// Whether mx_gated_fwd loads the weight past the caches: 1 in its only or first
+// launch, + 2 in the tail's.
+int mxt_gated_once(int64_t M, int64_t F, int64_t K, int elem, int units);
 // The chunks of x per lane (4 or 8) with which mxnorm_gated_fwd norms M rows within
 // its product's launch; 0: in a launch before it.
 int mxt_gated_normed(int64_t M, int64_t F, int64_t K, int elem, int units);

@@ -89,3 +89,16 @@ def test_plan_names_a_gated_kernel(M, F, K, want):
         assert elem or shape == want
         assert not whole.value or (shape == 6 and tail.value in (4, 5, 7, 8, 9))
     assert f(M, F, 100, 0, 256, ctypes.byref(whole), ctypes.byref(tail), ctypes.byref(us)) == -1
+
+
+@pytest.mark.parametrize("M,F,K,elem,want", [
+    # one row of tiles, from 96 MB of weights on; a first launch of 256 x 256 tiles
+    # has one up to 256 rows, the smaller tiles of its tail do not
+    (1, 14336, 4096, 0, 1), (61, 14336, 4096, 0, 1), (61, 14336, 4096, 1, 0), (129, 14336, 4096, 0, 0),
+    (200, 36096, 4096, 0, 1), (200, 37120, 4096, 0, 1), (200, 65792, 4096, 0, 1), (256, 37120, 8192, 1, 1),
+    (257, 65792, 4096, 0, 0),
+])
+def test_weights_that_are_read_once(M, F, K, elem, want):
+    f = mxnorm.load().mxt_gated_once
+    f.restype, f.argtypes = ctypes.c_int, [ctypes.c_int64] * 3 + [ctypes.c_int] * 2
+    assert f(M, F, K, elem, 256) == want
