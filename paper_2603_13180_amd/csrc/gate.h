@@ -13,8 +13,9 @@
 namespace mxk {
 
 // sigma(z(g)) from the hardware's exp2 and reciprocal, one unit in the last
-// place each: for |z| up to 20 the result is within 2^-19 of its value
-// relatively (the argument's rounding), far below a bf16 or MX rounding.  z
+// place each: for |z| up to 20 the result is within 2^-19 (SiLU) or 2^-18 (GELU,
+// whose polynomial is rounded too) of its value relatively, by the argument's
+// rounding, far below a bf16 or MX rounding.  z
 // beyond the exponential's range gives exactly 0 or 1.
 template <int ACT> __device__ __forceinline__ float gate_sigma(float g)
 {

@@ -18,11 +18,14 @@
 // once into LDS.
 //
 // What bounds it: HBM, 4 bytes an element forward and 6 backward.  32768 tokens
-// of 32 + 8 heads of 128 out of a projection of 48: forward 120 us, 5.6 TB/s (a
-// copy of as much 125 us); backward 190 us, 5.3 TB/s (an addition of as much
-// 167).  Neither changes with angles and arithmetic left out (120 and 196 us);
-// 15 us of the backward are for writing rows with gaps (the values' part of the
-// projection's gradient), 166 us into a tensor of its own.
+// of 32 + 8 heads of 128 out of a projection of 48: forward 118 us, 5.7 TB/s (a
+// copy of as much 125 us); backward 187 us, 5.4 TB/s (an addition of as much
+// 167); 15 us of the backward are for writing rows with gaps (the values' part
+// of the projection's gradient).  There the angles cost nothing (left out: the
+// same and 1% more).  With few heads a token they do, once for its queries and
+// once for its keys: 26066 tokens of 2 + 1 heads of 128 18.0 us forward and 32.6
+// backward, 14.7 and 25.8 without them; 8000 of 12 + 4 of 64 13.3 and 24.2, 12.4
+// and 22.7.
 #include <hip/hip_runtime.h>
 
 #include <math.h>
@@ -52,9 +55,9 @@ struct Heads {
     const uint16_t *gamma;
     int64_t in_t, in_h, gy_t, gy_h, out_t, out_h; // strides, elements
     int heads, blocks;   // blocks of 64 / G heads
-    // Tokens of an item: as many as have room in a wave.  (One token an item, and
-    // a load for each angle after the other: 4831 tokens of 4 + 2 heads of 128
-    // backward 24.6 us, now 17.4; 26066 of 2 + 1 forward 38.7, now 20.0.)
+    // Tokens of an item: as many as have room in a wave.  (One token an item:
+    // 4831 tokens of 4 + 2 heads of 128 backward 23.1 us, so 17.8; 26066 of 2 + 1
+    // forward 29.9, so 18.0.)
     int tpi;
     int tb;              // tokens a workgroup takes at a time
     int64_t steps;       // of tb tokens
@@ -666,11 +669,11 @@ template <bool BWD> void launch(const Args &A, bool inter, unsigned grid, hipStr
 // Tokens of a step: four items (one a wave) with an angle a lane, and up to 16
 // as far as the angles fit and that leaves a step for each of `least` workgroups: the next item's
 // loads then hide behind the one at hand, and backward a workgroup's sums are
-// added once.  12 + 4 heads of 64, 2000 tokens backward: 13.9 us, 17.1 with
-// four times as many steps; 8000 tokens 28.7 and 35.7, forward 14.4 and 18.8.
+// added once.  12 + 4 heads of 64, 2000 tokens backward: 12.4 us, 14.5 with
+// four times as many steps; 8000 tokens 24.1 and 29.0, forward 12.9 and 15.5.
 // Fewer workgroups than 224 backward or 360 forward leave compute units idle:
-// 32 + 8 heads of 128, 500 tokens 10.0 us backward, 11.5 with 128 of them; 4096
-// tokens 17.9 us forward, 18.9 with 256.
+// 32 + 8 heads of 128, 500 tokens 10.6 us backward, 12.1 with 120 of them; 4096
+// tokens 19.1 us forward, 19.8 with 256.
 inline void steps_of(Heads &H, int64_t T, int R, int64_t least)
 {
     H.tb = 1;
@@ -688,7 +691,7 @@ inline void steps_of(Heads &H, int64_t T, int R, int64_t least)
 
 // Workgroups: forward one for each step, backward at most two a compute unit,
 // each with a row of partial sums for either gain (32768 tokens of 40 heads of
-// 128: 190 us with 512, 195 with 768, 198 with 1024, 223 with 256).
+// 128: 188 us with 512, 210 with 768, 187 with 1024, 226 with 256).
 constexpr int MAX_ROWS = 512;
 inline unsigned workgroups(const Args &A, bool bwd)
 {
