@@ -1,7 +1,7 @@
 """Query and key heads at the edges of what the entry points take, on the GPU:
 kinds without heads,
-heads beside others that have no norm or are missing, heads of subnormals,
-gain gradients over many tokens.  Bounds as in test_gpu_qk_norm_rope."""
+heads beside others that have no norm or are missing, heads of subnormals
+and of the largest values, gain gradients over many tokens.  Bounds as in test_gpu_qk_norm_rope."""
 import pytest
 import torch
 
@@ -105,3 +105,25 @@ def test_gain_gradients_do_not_lose_bits_with_the_tokens():
     for gg, n in ((got[2], T * H), (got[3], T)):
         err = (gg.cpu().double() / (term * n) - 1).abs()
         assert (err <= 2.0 ** -17.6).all(), err.max()
+
+
+@pytest.mark.parametrize("D,R,inter,Hq,Hk", [(128, 128, False, 8, 8), (64, 32, True, 3, 1), (512, 512, False, 2, 1)])
+def test_heads_of_the_largest_values(D, R, inter, Hq, Hk):
+    # from 2^126 up to the largest bf16 number: an inverse RMS below 2^-126, a
+    # subnormal with 21 bits or more, 2^-22 of it (the bounds count 2^-20 for it)
+    c = Case(11, Hq, Hk, D, R, inter, eps=0.0)
+    g = torch.Generator().manual_seed(D)
+    bits = torch.randint(0x7E80, 0x7F80, c.qkv.shape, generator=g) | torch.randint(0, 2, c.qkv.shape, generator=g) << 15
+    some = torch.arange(11) % 4 != 3     # and tokens of ordinary heads beside them
+    c.qkv = torch.where(some[:, None], bits.to(torch.int16).view(torch.bfloat16), c.qkv)
+    assert c.qkv.isfinite().all()
+    q, k = c.views(c.qkv.to(DEV))
+    hq, hk = c.views(c.qkv)
+    y = mxnorm.qk_norm_rope_fwd(q, k, *c.on_gpu(), **c.kw())
+    c.check_forward(y[0], hq, 0)
+    c.check_forward(y[1], hk, 1)
+    # gradients of x well above the subnormals: 2^60 2^-128
+    c.gq, c.gk = c.gq * 2.0 ** 60, c.gk * 2.0 ** 60
+    gx = mxnorm.qk_norm_rope_bwd(c.gq.to(DEV), c.gk.to(DEV), q, k, *c.on_gpu(), **c.kw())
+    c.check_backward(gx[0], gx[2], hq, c.gq, 0)
+    c.check_backward(gx[1], gx[3], hk, c.gk, 1)
