@@ -341,8 +341,9 @@ mx_status mxnorm_linear_bwd(const void *grad_h, const void *x, const float *rho,
  *   H = act(G) . U                                               [M, F]
  * G and U are the float sums of mx_matmul_fwd (its bound, its note on the order
  * of additions, with four partial sums, and K from any step on); activation and
- * product are computed in float.  Non-finite values follow the formula: a NaN gives NaN, act(-inf) is NaN, act(+inf) is
- * inf; a finite G too negative for the exponential gives act(G) = -0.
+ * product are computed in float.  Non-finite values follow the formula: a NaN
+ * gives NaN, act(-inf) is NaN, act(+inf) is inf; a finite G too negative for the
+ * exponential gives act(G) = -0.
  * out_dtype MX_OUT_F32, MX_OUT_BF16: out [M, F] in that type, out_scales NULL.
  * MX_OUT_CODES: the MX encoding of the float H along F, with blocks of 32 in
  * `elem` by `scale_mode`, rounding and NaN-block codes as in the casts above:
@@ -461,9 +462,9 @@ mx_status qk_norm_rope_fwd(const mx_heads *q, const mx_heads *k, const void *q_g
  * them.  Per head, with m the gradient turned back by the angles and v = gamma
  * m:  grad_x = r (v - k n) with n = x r and k = (1/D) sum_e v_e n_e, in float;
  * grad_gamma_e = sum over the tokens and heads of n m, in float over at most 64
- * heads and (only where a workgroup has no more for each) 64 of those sums, else
- * in double, rounded to float for each of at most 512 workgroups and at the end,
- * in a fixed order: the same call gives the same bits.
+ * heads; those sums in float where a workgroup has at most 64 of them, else in
+ * double; at most 512 workgroups' sums, each rounded to float, in double; all in
+ * a fixed order: the same call gives the same bits.
  * grad_q, grad_k: bf16; each may be the incoming gradient itself (data and
  * strides).  grad_q_gamma, grad_k_gamma: float [D] or NULL (not computed); with
  * no tokens or heads they are 0.  They need `workspace`, caller-owned device

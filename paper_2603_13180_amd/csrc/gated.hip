@@ -232,6 +232,8 @@ int mxt_gated_plan(int64_t M, int64_t F, int64_t K, int elem, int units, int *wh
 
 int mxt_gated_once(int64_t M, int64_t F, int64_t K, int elem, int units)
 {
+    if (M <= 0 || F <= 0 || K <= 0 || units <= 0)
+        return -1;
     mxg::GatedArgs A{};
     A.M = M;
     A.N = F;
