@@ -58,11 +58,14 @@ struct CastTArgs {
     uint8_t *codes;
     uint8_t *scales;
     int64_t R, C;
-    int64_t rows;    // rows that x has: the others, up to R, are zeros
     int64_t tile_r0; // row tile of blockIdx.y == 0 (launches of at most 65535 row tiles)
-    int mode;
-    int order;       // tile visiting order, see cast_t_kernel
+    int32_t pad;     // rows of x's end, up to R, that are not in memory but zeros
+    int16_t mode;
+    int16_t order;   // tile visiting order, see cast_t_kernel
+    __device__ __forceinline__ int64_t rows() const { return R - pad; }
 };
+// one line of the launch's arguments (in two, small casts take 0.2 us longer)
+static_assert(sizeof(CastTArgs) == 64, "cast arguments");
 
 // Lane (cc, blk) of a cast pass: column cc of the staged tile over rows
 // 32 blk .. 32 blk + 31 (one scale block, rows rb .. of x): reads its 32
@@ -189,7 +192,7 @@ __device__ __forceinline__ void fetch_tile(const CastTArgs &A, int64_t r0, int64
     const int ch = tid % S::CPR, rbase = tid / S::CPR;
     const uint32_t chunk_off = c0 + 8 * ch < A.C ? 16u * (uint32_t)ch : kOutside; // C % 8 == 0
     const uint32_t pitch = (uint32_t)A.C * 2u;
-    const uint32_t rows = (uint32_t)max((int64_t)0, min((int64_t)CT_ROWS, A.rows - r0));
+    const uint32_t rows = (uint32_t)max((int64_t)0, min((int64_t)CT_ROWS, A.rows() - r0));
     const __amdgpu_buffer_rsrc_t xr = buffer_rsrc(A.x + r0 * A.C + c0, rows * pitch);
 #pragma unroll
     for (int k = 0; k < S::NLD; ++k) {
@@ -399,7 +402,7 @@ __device__ __forceinline__ void cast_rows(const CastTArgs &A, uint8_t *codes, ui
 #pragma unroll
     for (int k = 0; k < S::NLD; ++k) {
         const int64_t r = r0 + rbase + S::RPP * k;
-        cast_row_chunk<FP4, false>(codes, scales, A.C, r, c, r < A.rows && c < A.C, tid, L.v[k], 128);
+        cast_row_chunk<FP4, false>(codes, scales, A.C, r, c, r < A.rows() && c < A.C, tid, L.v[k], 128);
     }
 }
 
@@ -435,7 +438,7 @@ __device__ __forceinline__ void gated_tile(const CastJobs &J, int64_t r0, int64_
     const int ch = tid % CH, rbase = tid / CH;
     const int64_t c = c0 + 8 * ch;
     const uint32_t pitch = (uint32_t)F * 2u;
-    const uint32_t rows = (uint32_t)max((int64_t)0, min((int64_t)CT_ROWS, A.rows - r0));
+    const uint32_t rows = (uint32_t)max((int64_t)0, min((int64_t)CT_ROWS, A.rows() - r0));
     const __amdgpu_buffer_rsrc_t hr = buffer_rsrc(J.gh + r0 * F + c0, rows * pitch);
     const __amdgpu_buffer_rsrc_t gr = buffer_rsrc(J.gu + r0 * 2 * F + c0, rows * pitch * 2u);
     uint4 h[NLD], g[NLD], u[NLD];
@@ -458,7 +461,7 @@ __device__ __forceinline__ void gated_tile(const CastJobs &J, int64_t r0, int64_
         gate_gradients<ACT>(g[k], u[k], h[k], dg, du);
         *reinterpret_cast<uint4 *>(&tile[S::off(r) + 16 * ch]) = dg;
         *reinterpret_cast<uint4 *>(&tile[S::off(r) + 16 * (CH + ch)]) = du;
-        const bool in = r0 + r < A.rows && c < F;
+        const bool in = r0 + r < A.rows() && c < F;
         // (E2M1: F is a multiple of 128; E4M3, of 64)
         const int valid = (int)min((int64_t)COLS / 2, F - c0);
         cast_row_chunk<FP4, !FP4, CH>(J.row_codes, J.row_scales, A.C, r0 + r, c, in, tid, dg, valid);
@@ -1009,7 +1012,8 @@ mx_status mx_cast_t_fwd(const void *x, const float *rho, int64_t R, int64_t C, i
     A.rho = rho;
     A.codes = codes;
     A.scales = scales;
-    A.R = A.rows = R;
+    A.R = R;
+    A.pad = 0;
     A.C = C;
     A.mode = scale_mode;
     // one 128 x 256 tile per workgroup (see the kernel), at most 65535 row
@@ -1144,7 +1148,7 @@ mx_status backward_casts(const void *grad_h, const void *x, const float *rho, co
         A.scales = scales;
         A.R = R;
         A.C = C;
-        A.rows = rows;
+        A.pad = (int32_t)(R - rows);
         A.tile_r0 = 0;
         A.mode = MX_SCALE_RCEIL;
         A.order = cast_order(C);
