@@ -59,6 +59,9 @@ extern "C" {
 #define MXNORM_MAX_D 32768
 #define MX_MATMUL_MAX_K (1 << 22)
 #define MX_MATMUL_MAX_N (1 << 24)
+#define MX_ATTN_MAX_D 128
+#define MX_ATTN_MAX_SINKS 256
+#define MX_ATTN_MAX_TOKENS (1 << 28)
 
 typedef enum {
     MX_OK = 0,
@@ -479,6 +482,62 @@ mx_status qk_norm_rope_bwd(const mx_heads *grad_q_out, const mx_heads *grad_k_ou
                            const mx_heads *grad_q, const mx_heads *grad_k, float *grad_q_gamma,
                            float *grad_k_gamma, void *workspace, size_t workspace_bytes,
                            hipStream_t stream);
+
+/*
+ * Causal attention of packed sequences, with a sliding window and a few first
+ * tokens that stay visible (sinks), or without a window.  q, out: Hq heads a
+ * token [Tq, Hq, D]; k, v: Hk heads [Tk, Hk, D], Hq a multiple of Hk; query head
+ * h reads key head h Hk / Hq (mx_heads: views of a projection's output, or
+ * qk_norm_rope_fwd's).
+ * q_start, k_start: device int32 [sequences + 1]; sequence b has the queries
+ * q_start[b] .. q_start[b + 1] - 1 and the keys k_start[b] .. likewise, lq and lk
+ * of them, in ascending order; k_start NULL: q_start's (Tk = Tq).  Both NULL: one
+ * sequence of Tq and Tk (sequences = 1).  A sequence's queries are its last
+ * tokens: query i stands at p = i + lk - lq, and sees key j where j <= p and (p -
+ * j < window or j < sinks); window 0: every j <= p.
+ *   s_ij = scale q_i . k_j,   out_i = sum_j softmax(s_i)_j v_j,
+ *   lse[h, i] = log sum_j exp(s_ij)                       (float [Hq, Tq] or NULL)
+ * over the keys that i sees.  A query that sees none (p < 0) gives 0 and an lse of
+ * -inf.  Products and sums are float, the exponentials, relative to a running
+ * maximum, rounded to bf16 for the product with v, out rounded once more.  What a
+ * masked key or value holds (infinities, NaN) changes nothing; visible ones
+ * follow the formula, and a row whose visible scores are all -inf gives NaN.
+ * Rows of out and lse that no sequence has are left as they were.  Starts past
+ * Tq or Tk count as Tq and Tk; descending ones give unspecified rows.
+ * D a multiple of 8, at most MX_ATTN_MAX_D; at most MX_ATTN_MAX_SINKS sinks,
+ * MX_ATTN_MAX_TOKENS tokens, 4096 heads and 2^20 sequences (else
+ * MX_EUNSUPPORTED); scale from 2^-100 to 2^100.  out must not overlap an input.
+ * The same call gives the same bits.  Tq == 0 is a no-op.
+ */
+mx_status window_attn_fwd(const mx_heads *q, const mx_heads *k, const mx_heads *v, int64_t Tq, int64_t Tk,
+                          int64_t D, const int32_t *q_start, const int32_t *k_start, int64_t sequences,
+                          int64_t window, int64_t sinks, float scale, const mx_heads *out, float *lse,
+                          hipStream_t stream);
+
+/*
+ * Its gradients, from that of out; q, k, v and the rest as the forward took them,
+ * out and lse as it gave them.  With P = exp(s - lse), delta_i = grad_out_i . out_i
+ * and dS_ij = P_ij (grad_out_i . v_j - delta_i):
+ *   grad_q_i = scale sum_j dS_ij k_j,   grad_k_j = scale sum_i dS_ij q_i,
+ *   grad_v_j = sum_i P_ij grad_out_i,
+ * the sums of grad_k and grad_v over the query heads of a key head too.  Products
+ * and sums are float, in a fixed order (the same call gives the same bits), P and
+ * dS rounded to bf16 for the last three products, the gradients once more.  What
+ * a pair that is masked holds changes nothing.  Queries and keys without a
+ * visible partner have a gradient of 0; rows that no sequence has are left as
+ * they were.  grad_q, grad_k and grad_v may be parts of one buffer, and must not
+ * overlap an input.
+ * `workspace`: caller-owned device memory of window_attn_bwd_workspace_bytes()
+ * bytes (of the heads, D, sequences and sinks of the call), 256-byte aligned,
+ * overwritten; calls that overlap in time need one each.
+ */
+size_t window_attn_bwd_workspace_bytes(int64_t Tq, int64_t q_heads, int64_t k_heads, int64_t D,
+                                       int64_t sequences, int64_t sinks);
+mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_heads *k, const mx_heads *v,
+                          const mx_heads *out, const float *lse, int64_t Tq, int64_t Tk, int64_t D,
+                          const int32_t *q_start, const int32_t *k_start, int64_t sequences, int64_t window,
+                          int64_t sinks, float scale, const mx_heads *grad_q, const mx_heads *grad_k,
+                          const mx_heads *grad_v, void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 /*
  * Default NVFP4 tensor decode scales: an output bound divided by 6 * 448, so

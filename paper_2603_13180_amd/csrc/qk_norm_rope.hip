@@ -34,6 +34,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "heads.h"
 #include "mxnorm.h"
 #include "norm_cast.h"
 #include "status.h"
@@ -702,31 +703,9 @@ inline unsigned workgroups(const Args &A, bool bwd)
 
 namespace {
 
-bool aligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
-
-// One tensor of heads: an input (any strides, 0 among them) or an output,
-// whose heads must not share elements.
-mx_status check_heads(const mx_heads *h, const char *name, int64_t T, int64_t D, int64_t heads, bool out)
-{
-    if (!h)
-        return mxk::fail(MX_EINVAL, "%s is NULL", name);
-    if (h->heads != heads)
-        return mxk::fail(MX_EINVAL, "%s has %lld heads, not %lld", name, (long long)h->heads, (long long)heads);
-    if (T == 0 || heads == 0)
-        return MX_OK;
-    const int64_t t = T > 1 ? h->token_stride : 0, s = heads > 1 ? h->head_stride : 0;
-    if (!h->data || !aligned(h->data, 16) || t % 8 != 0 || s % 8 != 0)
-        return mxk::fail(MX_EINVAL, "%s must be non-NULL, 16-byte aligned, its strides multiples of 8", name);
-    if (t < 0 || s < 0 || t > INT64_MAX / 4 / T || s > INT64_MAX / 4 / heads)
-        return mxk::fail(MX_EINVAL, "%s: bad strides", name);
-    if (out) {
-        const bool by_token = (heads == 1 || s >= D) && (T == 1 || t >= s * (heads - 1) + D);
-        const bool by_head = (T == 1 || t >= D) && (heads == 1 || s >= t * (T - 1) + D);
-        if (!by_token && !by_head)
-            return mxk::fail(MX_EINVAL, "%s: its heads overlap", name);
-    }
-    return MX_OK;
-}
+using mxk::aligned;
+using mxk::check_heads;
+using mxk::launched;
 
 mx_status check_common(const mx_heads *q, const mx_heads *k, const void *q_gamma, const void *k_gamma,
                        int64_t T, int64_t D, int64_t R, const int64_t *pos, const float *inv_freq,
@@ -772,12 +751,6 @@ mxq::Heads heads_of(const mx_heads *in, const mx_heads *gy, const mx_heads *out,
     H.blocks = (int)((in->heads + 64 / G - 1) / (64 / G));
     H.tpi = H.heads ? std::max(64 / G / H.heads, 1) : 1;
     return H;
-}
-
-mx_status launched()
-{
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? MX_OK : mxk::fail(MX_EHIP, "kernel launch failed: %s", hipGetErrorString(e));
 }
 
 } // namespace

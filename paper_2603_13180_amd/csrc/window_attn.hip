@@ -1,0 +1,714 @@
+// window_attn.hip -- causal attention of packed sequences with a sliding window
+// and sinks, forward and backward.
+//
+// Query i of a sequence of lq queries and lk keys stands at p = i + lk - lq and
+// sees key j where j <= p and (p - j < window or j < sinks).  With s = scale q.k,
+//   forward:  o = sum_j exp(s_j - m) v_j / l,  l = sum_j exp(s_j - m),  lse = m + log l;
+//   backward: P = exp(s - lse),  delta = grad_o . o,  dS = P (grad_o . v - delta),
+//     grad_q = scale sum_j dS k_j,  grad_k = scale sum_i dS q_i,  grad_v = sum_i P grad_o_i.
+#include "attn.h"
+
+namespace mxa {
+
+constexpr int BK = 64;        // keys of a tile, queries of a backward tile
+constexpr int FAR_CHUNK = 256; // queries that a wave sums for the sinks, at least
+
+struct Args {
+    In q, k, v, go, o;
+    Out out, gk, gv;      // out: the output, or grad_q
+    const float *lse;     // backward: [Hq, Tq]
+    float *lse_out;       // forward: or NULL
+    float *lse2, *delta;  // backward: lse log2(e), grad_o . o, [Hq, Tq]
+    float *part;          // backward: the sinks' sums over queries far behind them
+    const int *qs, *ks;   // [B + 1], or NULL: one sequence
+    int Tq, Tk, B, Hk, G, D;
+    int tiles, window, sinks, chunk;
+    float c, scale;       // scale log2(e), scale
+};
+
+struct Span {
+    int q0, lq, k0, lk, off; // off = lk - lq
+};
+
+__device__ __forceinline__ int start_of(const int *s, int b, int T) { return min(max(s[b], 0), T); }
+
+// The sequence that tile `tile` belongs to and the tile's first row in it.  The
+// sequences' tiles of R rows are numbered from floor(start / R) + b on: that
+// leaves room for each, and starts that are not in order stay within bounds.
+__device__ __forceinline__ bool span_of(const Args &A, const int *s, int T, int tile, int R, bool keys, Span &S, int &b, int &r0)
+{
+    b = 0;
+    if (!s) {
+        S = {0, A.Tq, 0, A.Tk, A.Tk - A.Tq};
+        r0 = tile * R;
+        return r0 < T;
+    }
+    int hi = A.B - 1;
+    while (b < hi) {
+        const int mid = (b + hi + 1) >> 1;
+        if (start_of(s, mid, T) / R + mid <= tile)
+            b = mid;
+        else
+            hi = mid - 1;
+    }
+    S.q0 = start_of(A.qs, b, A.Tq);
+    S.lq = max(start_of(A.qs, b + 1, A.Tq) - S.q0, 0);
+    S.k0 = start_of(A.ks, b, A.Tk);
+    S.lk = max(start_of(A.ks, b + 1, A.Tk) - S.k0, 0);
+    S.off = S.lk - S.lq;
+    r0 = (tile - ((keys ? S.k0 : S.q0) / R + b)) * R;
+    return r0 >= 0 && r0 < (keys ? S.lk : S.lq);
+}
+
+// Workgroup id of a launch over tiles, key heads and their G query heads, so that
+// an XCD has whole key heads, or every (8 / Hk)-th tile of one: its L2 then holds
+// what its workgroups share, and each XCD has long and short tiles alike.
+__device__ __forceinline__ bool item_of(int id, int tiles, int Hk, int G, int &rank, int &hk, int &g)
+{
+    const int per = tiles * G, x = id % NXCD;
+    int r;
+    if (Hk % NXCD == 0) {
+        r = id / NXCD;
+        hk = x + NXCD * (r / per);
+        r %= per;
+    } else if (NXCD % Hk == 0) {
+        hk = x % Hk;
+        r = id / NXCD * (NXCD / Hk) + x / Hk;
+    } else {
+        hk = id % Hk;
+        r = id / Hk;
+    }
+    rank = r / G;
+    g = r % G;
+    return r < per;
+}
+
+inline int64_t items(int64_t tiles, int64_t Hk, int64_t G)
+{
+    if (NXCD % Hk == 0)
+        return NXCD * ((tiles * G * Hk + NXCD - 1) / NXCD);
+    return tiles * G * Hk;
+}
+
+// The key tiles that queries at p0 .. p1 see: those of the sinks, then the window's.
+struct Tiles {
+    int sinks, first, n;
+    __device__ __forceinline__ Tiles(const Args &A, int p0, int p1)
+    {
+        first = max(p0 - A.window + 1, 0) / BK;
+        sinks = min((A.sinks + BK - 1) / BK, first);
+        n = p1 < 0 ? 0 : sinks + p1 / BK - first + 1;
+    }
+    __device__ __forceinline__ int operator[](int i) const { return (i < sinks ? i : first + i - sinks) * BK; }
+};
+
+__device__ __forceinline__ bool sees(const Args &A, int p, int j)
+{
+    return j <= p && (p - j < A.window || j < A.sinks);
+}
+
+// What queries at p0 .. p1 see of keys j0 .. j0 + n - 1: 0 none, 1 some, 2 all.
+__device__ __forceinline__ int seen(const Args &A, int p0, int p1, int j0, int n)
+{
+    if (j0 > p1 || (j0 + n - 1 <= p0 - A.window && j0 >= A.sinks))
+        return 0;
+    return j0 + n - 1 <= p0 && p1 - j0 < A.window ? 2 : 1;
+}
+
+template <int DB> struct Scores {
+    f16v s[2];
+    // the tile's rows times x
+    __device__ __forceinline__ Scores(const LDS_AS uint8_t *tile, const Lane<DB> &L, const b8 (&x)[2 * DB])
+    {
+        s[0] = s[1] = zero16();
+#pragma unroll
+        for (int ks = 0; ks < 2 * DB; ++ks)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+                s[b] = mfma(row_frag<DB>(tile, L, ks, b), x[ks], s[b]);
+    }
+};
+
+// ---------------------------------------------------------------- forward --
+
+template <int DB, int NW, bool CAREFUL>
+__device__ __forceinline__ bool forward(const Args &A, LDS_AS uint8_t *lds, const Span &S, int i0, int hk, int hq)
+{
+    constexpr int TILE = BK * kRow<DB>;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, h = l >> 5;
+    const uint32_t base = lds_address(lds);
+    const Lane<DB> L(l);
+    const uint16_t *kh = A.k.p + S.k0 * A.k.ts + hk * A.k.hs, *vh = A.v.p + S.k0 * A.v.ts + hk * A.v.hs;
+    const Tiles tiles(A, i0 + S.off, min(i0 + 32 * NW, S.lq) - 1 + S.off);
+    auto load = [&](int it) {
+        const uint32_t to = base + (it & 1) * 2 * TILE;
+        load_tile<DB, BK, NW>(kh, A.k.ts, tiles[it], S.lk - 1, A.D, to, w, l);
+        load_tile<DB, BK, NW>(vh, A.v.ts, tiles[it], S.lk - 1, A.D, to + TILE, w, l);
+    };
+    if (tiles.n > 0)
+        load(0);
+    const int iw = i0 + 32 * w;                             // the wave's first query
+    const int p0 = iw + S.off, p1 = min(iw + 31, S.lq - 1) + S.off;
+    const int p = min(iw + n, S.lq - 1) + S.off;
+    b8 q[2 * DB];
+    load_rows<DB>(q, A.q.p + S.q0 * A.q.ts + hq * A.q.hs, A.q.ts, iw, S.lq - 1, A.D, l);
+    f16v o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+        o[d] = zero16();
+    float m = -FLT_MAX, sum = 0.0f; // m: of scores in powers of two; sum: the lane's half of the keys
+    for (int it = 0; it < tiles.n; ++it) {
+        wait_vmcnt<0>();
+        barrier();
+        if (it + 1 < tiles.n)
+            load(it + 1);
+        const int j0 = tiles[it];
+        const int see = iw < S.lq ? seen(A, p0, p1, j0, BK) : 0;
+        if (see == 0)
+            continue;
+        const LDS_AS uint8_t *kt = lds + (it & 1) * 2 * TILE, *vt = kt + TILE;
+        Scores<DB> x(kt, L, q);
+        if (see == 1)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    x.s[b][e] = sees(A, p, j0 + 32 * b + c_row(e, h)) ? x.s[b][e] : -INFINITY;
+        float mt = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                mt = fmaxf(mt, x.s[b][e]);
+        mt = halves_max(mt) * A.c;
+        // The maximum is followed only where it grows by more than 2^8: what
+        // exponentials and sums gain from that stays far inside float and bf16.
+        if (__builtin_amdgcn_ballot_w64(mt > m + 8.0f)) {
+            const float mn = fmaxf(m, mt), by = __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            sum *= by;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+                o[d] *= by;
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                x.s[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x.s[b][e], A.c, -m));
+                sum += x.s[b][e];
+            }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const b8 y = pack8(x.s[s >> 1], s & 1);
+            if (CAREFUL && see == 1)
+                careful_product<DB>(o, vt, L, s, y, h, [&](int r) { return sees(A, p, j0 + r); });
+            else
+                product<DB>(o, vt, L, s, y);
+        }
+    }
+    if (!CAREFUL && __syncthreads_or(iw + n < S.lq && not_finite<DB>(o)))
+        return false;
+    if (CAREFUL)
+        __syncthreads();
+    sum = halves_sum(sum);
+    // a row that sees no key gives 0; one that sees only scores of -inf NaN
+    const float by = p < 0 ? 0.0f : 1.0f / sum;
+    if (A.lse_out && h == 0 && iw + n < S.lq)
+        A.lse_out[(int64_t)hq * A.Tq + S.q0 + iw + n] =
+            p < 0 ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * LN2;
+    store_rows<DB>(o, by, lds + w * 32 * kRow<DB>, A.out.p + (int64_t)(S.q0 + iw) * A.out.ts + hq * A.out.hs, A.out.ts,
+                   S.lq - iw, A.D, l);
+    return true;
+}
+
+template <int DB, int NW>
+__global__ void __launch_bounds__(64 * NW, 2) fwd_kernel(Args A)
+{
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * BK * kRow<DB>];
+    LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
+    int rank, hk, g, b, i0;
+    Span S;
+    if (!item_of(blockIdx.x, A.tiles, A.Hk, A.G, rank, hk, g) ||
+        !span_of(A, A.qs, A.Tq, A.tiles - 1 - rank, 32 * NW, false, S, b, i0))
+        return;
+    if (A.D != 32 * DB)
+        zero_lds<4 * BK * kRow<DB>>(lds, 64 * NW);
+    if (!forward<DB, NW, false>(A, lds, S, i0, hk, hk * A.G + g))
+        forward<DB, NW, true>(A, lds, S, i0, hk, hk * A.G + g);
+}
+
+// --------------------------------------------------------------- backward --
+
+// grad_q, and for the other kernels lse log2(e) and delta.
+template <int DB, int NW, bool CAREFUL>
+__device__ __forceinline__ bool backward_q(const Args &A, LDS_AS uint8_t *lds, const Span &S, int i0, int hk, int hq)
+{
+    constexpr int TILE = BK * kRow<DB>;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, h = l >> 5;
+    const uint32_t base = lds_address(lds);
+    const Lane<DB> L(l);
+    const uint16_t *kh = A.k.p + S.k0 * A.k.ts + hk * A.k.hs, *vh = A.v.p + S.k0 * A.v.ts + hk * A.v.hs;
+    const Tiles tiles(A, i0 + S.off, min(i0 + 32 * NW, S.lq) - 1 + S.off);
+    auto load = [&](int it) {
+        const uint32_t to = base + (it & 1) * 2 * TILE;
+        load_tile<DB, BK, NW>(kh, A.k.ts, tiles[it], S.lk - 1, A.D, to, w, l);
+        load_tile<DB, BK, NW>(vh, A.v.ts, tiles[it], S.lk - 1, A.D, to + TILE, w, l);
+    };
+    if (tiles.n > 0)
+        load(0);
+    const int iw = i0 + 32 * w;
+    const int p0 = iw + S.off, p1 = min(iw + 31, S.lq - 1) + S.off;
+    const int p = min(iw + n, S.lq - 1) + S.off;
+    b8 q[2 * DB], go[2 * DB];
+    load_rows<DB>(go, A.o.p + S.q0 * A.o.ts + hq * A.o.hs, A.o.ts, iw, S.lq - 1, A.D, l);
+    load_rows<DB>(q, A.go.p + S.q0 * A.go.ts + hq * A.go.hs, A.go.ts, iw, S.lq - 1, A.D, l);
+    float delta = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < 2 * DB; ++ks)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            delta = __builtin_fmaf((float)q[ks][e], (float)go[ks][e], delta);
+    delta = halves_sum(delta);
+#pragma unroll
+    for (int ks = 0; ks < 2 * DB; ++ks)
+        go[ks] = q[ks];
+    load_rows<DB>(q, A.q.p + S.q0 * A.q.ts + hq * A.q.hs, A.q.ts, iw, S.lq - 1, A.D, l);
+    const int64_t row = (int64_t)hq * A.Tq + S.q0 + min(iw + n, S.lq - 1);
+    const float lse2 = A.lse[row] * LOG2E;
+    if (h == 0 && iw + n < S.lq) {
+        A.lse2[row] = lse2;
+        A.delta[row] = delta;
+    }
+    f16v o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+        o[d] = zero16();
+    for (int it = 0; it < tiles.n; ++it) {
+        wait_vmcnt<0>();
+        barrier();
+        if (it + 1 < tiles.n)
+            load(it + 1);
+        const int j0 = tiles[it];
+        const int see = iw < S.lq ? seen(A, p0, p1, j0, BK) : 0;
+        if (see == 0)
+            continue;
+        const LDS_AS uint8_t *kt = lds + (it & 1) * 2 * TILE, *vt = kt + TILE;
+        Scores<DB> x(kt, L, q), y(vt, L, go);
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(x.s[b][e], A.c, -lse2));
+                x.s[b][e] = pr * (y.s[b][e] - delta);
+            }
+        if (see == 1)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    x.s[b][e] = sees(A, p, j0 + 32 * b + c_row(e, h)) ? x.s[b][e] : 0.0f;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const b8 z = pack8(x.s[s >> 1], s & 1);
+            if (CAREFUL && see == 1)
+                careful_product<DB>(o, kt, L, s, z, h, [&](int r) { return sees(A, p, j0 + r); });
+            else
+                product<DB>(o, kt, L, s, z);
+        }
+    }
+    if (!CAREFUL && __syncthreads_or(iw + n < S.lq && not_finite<DB>(o)))
+        return false;
+    if (CAREFUL)
+        __syncthreads();
+    store_rows<DB>(o, A.scale, lds + w * 32 * kRow<DB>, A.out.p + (int64_t)(S.q0 + iw) * A.out.ts + hq * A.out.hs, A.out.ts,
+                   S.lq - iw, A.D, l);
+    return true;
+}
+
+template <int DB, int NW>
+__global__ void __launch_bounds__(64 * NW, 2) bwd_q_kernel(Args A)
+{
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * BK * kRow<DB>];
+    LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
+    int rank, hk, g, b, i0;
+    Span S;
+    if (!item_of(blockIdx.x, A.tiles, A.Hk, A.G, rank, hk, g) ||
+        !span_of(A, A.qs, A.Tq, A.tiles - 1 - rank, 32 * NW, false, S, b, i0))
+        return;
+    if (A.D != 32 * DB)
+        zero_lds<4 * BK * kRow<DB>>(lds, 64 * NW);
+    if (!backward_q<DB, NW, false>(A, lds, S, i0, hk, hk * A.G + g))
+        backward_q<DB, NW, true>(A, lds, S, i0, hk, hk * A.G + g);
+}
+
+// The sinks' sums over queries that lie the window or more behind: chunk `at`
+// (numbered as tiles are) of block kb of 32 keys, one plane each for grad_k and
+// grad_v, in the order in which a wave holds them.
+template <int DB> __device__ __forceinline__ float *far_part(const Args &A, int at, int hk, int kb)
+{
+    const int blocks = (A.sinks + 31) / 32;
+    return A.part + (((int64_t)at * A.Hk + hk) * blocks + kb) * (2 * DB * 16 * 64);
+}
+
+// grad_k and grad_v of 32 keys a wave, from queries i0 .. i1 of every head of the
+// group.  FAR: those that see them as sinks, not through the window.
+template <int DB, int NW, bool FAR, bool CAREFUL>
+__device__ __forceinline__ bool backward_kv(const Args &A, LDS_AS uint8_t *lds, const Span &S, int j0, int i0, int i1, int hk,
+                                            int b, int chunk)
+{
+    constexpr int TILE = BK * kRow<DB>, STAGE = 2 * TILE + 8 * BK;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, h = l >> 5;
+    const uint32_t base = lds_address(lds);
+    const Lane<DB> L(l);
+    const int steps = i1 < i0 ? 0 : (i1 - i0) / BK + 1, total = steps * A.G;
+    auto load = [&](int it) {
+        const int hq = hk * A.G + it / steps, r0 = i0 + it % steps * BK;
+        const uint32_t to = base + (it & 1) * STAGE;
+        load_tile<DB, BK, NW>(A.q.p + S.q0 * A.q.ts + hq * A.q.hs, A.q.ts, r0, i1, A.D, to, w, l);
+        load_tile<DB, BK, NW>(A.go.p + S.q0 * A.go.ts + hq * A.go.hs, A.go.ts, r0, i1, A.D, to + TILE, w, l);
+        const int64_t row = (int64_t)hq * A.Tq + S.q0 + min(r0 + l, i1);
+        if (w == 0)
+            mxg::lds_load4(A.lse2 + row, to + 2 * TILE);
+        if (w == NW - 1)
+            mxg::lds_load4(A.delta + row, to + 2 * TILE + 4 * BK);
+    };
+    if (total > 0)
+        load(0);
+    const int jw = j0 + 32 * w, j = jw + n;
+    b8 k[2 * DB], v[2 * DB];
+    load_rows<DB>(k, A.k.p + S.k0 * A.k.ts + hk * A.k.hs, A.k.ts, jw, S.lk - 1, A.D, l);
+    load_rows<DB>(v, A.v.p + S.k0 * A.v.ts + hk * A.v.hs, A.v.ts, jw, S.lk - 1, A.D, l);
+    f16v gk[DB], gv[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+        gk[d] = gv[d] = zero16();
+    auto sees_key = [&](int i) {
+        const int back = i + S.off - j;
+        return i <= i1 && (FAR ? back >= A.window && j < A.sinks : back >= 0 && back < A.window);
+    };
+    for (int it = 0; it < total; ++it) {
+        wait_vmcnt<0>();
+        barrier();
+        if (it + 1 < total)
+            load(it + 1);
+        if (jw >= S.lk)
+            continue;
+        const int r0 = i0 + it % steps * BK;
+        const LDS_AS uint8_t *qt = lds + (it & 1) * STAGE, *gt = qt + TILE, *st = gt + TILE;
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb) {
+            const int ib = r0 + 32 * qb, p0 = ib + S.off, p1 = p0 + 31;
+            if (ib > i1 || (!FAR && (p1 < jw || p0 - (jw + 31) >= A.window)))
+                continue;
+            const bool all = !FAR && p0 >= jw + 31 && p1 - jw < A.window && ib + 31 <= i1;
+            f16v s = zero16(), dp = zero16();
+#pragma unroll
+            for (int ks = 0; ks < 2 * DB; ++ks) {
+                s = mfma(row_frag<DB>(qt, L, ks, qb), k[ks], s);
+                dp = mfma(row_frag<DB>(gt, L, ks, qb), v[ks], dp);
+            }
+            const LDS_AS float *sl = reinterpret_cast<const LDS_AS float *>(st) + 32 * qb + 4 * h, *sd = sl + BK;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int r = 8 * (e >> 2) + (e & 3);
+                s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], A.c, -sl[r]));
+                dp[e] = s[e] * (dp[e] - sd[r]);
+            }
+            if (!all)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const bool see = sees_key(ib + c_row(e, h));
+                    s[e] = see ? s[e] : 0.0f;
+                    dp[e] = see ? dp[e] : 0.0f;
+                }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const b8 x = pack8(s, t), y = pack8(dp, t);
+                if (CAREFUL && !all) {
+                    auto see = [&](int r) { return sees_key(r0 + r); };
+                    careful_product<DB>(gv, gt, L, 2 * qb + t, x, h, see);
+                    careful_product<DB>(gk, qt, L, 2 * qb + t, y, h, see);
+                } else {
+                    product<DB>(gv, gt, L, 2 * qb + t, x);
+                    product<DB>(gk, qt, L, 2 * qb + t, y);
+                }
+            }
+        }
+    }
+    if (!CAREFUL && __syncthreads_or(j < S.lk && (not_finite<DB>(gk) || not_finite<DB>(gv))))
+        return false;
+    if (CAREFUL)
+        __syncthreads();
+    if constexpr (FAR) {
+        float *to = far_part<DB>(A, chunk, hk, j0 / 32) + l;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                to[(d * 16 + e) * 64] = gk[d][e];
+                to[((DB + d) * 16 + e) * 64] = gv[d][e];
+            }
+        return true;
+    }
+    if (jw < S.lk && jw < A.sinks && max(jw + A.window - S.off, 0) < S.lq) { // add the sums that the sinks have from far queries
+        const int at = S.q0 / A.chunk + b;
+        for (int c = max(jw + A.window - S.off, 0) / A.chunk; c <= (S.lq - 1) / A.chunk; ++c) {
+            const float *from = far_part<DB>(A, at + c, hk, jw / 32) + l;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    gk[d][e] += from[(d * 16 + e) * 64];
+                    gv[d][e] += from[((DB + d) * 16 + e) * 64];
+                }
+        }
+    }
+    LDS_AS uint8_t *mine = lds + w * 32 * kRow<DB>;
+    store_rows<DB>(gk, A.scale, mine, A.gk.p + (int64_t)(S.k0 + jw) * A.gk.ts + hk * A.gk.hs, A.gk.ts, S.lk - jw, A.D, l);
+    store_rows<DB>(gv, 1.0f, mine, A.gv.p + (int64_t)(S.k0 + jw) * A.gv.ts + hk * A.gv.hs, A.gv.ts, S.lk - jw, A.D, l);
+    return true;
+}
+
+template <int DB> constexpr int kStageKV = 2 * BK * kRow<DB> + 8 * BK;
+
+template <int DB, int NW>
+__global__ void __launch_bounds__(64 * NW) bwd_kv_kernel(Args A)
+{
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * kStageKV<DB>];
+    LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
+    int rank, hk, g, b, j0;
+    Span S;
+    if (!item_of(blockIdx.x, A.tiles, A.Hk, 1, rank, hk, g) ||
+        !span_of(A, A.ks, A.Tk, rank, 32 * NW, true, S, b, j0))
+        return;
+    if (A.D != 32 * DB)
+        zero_lds<2 * kStageKV<DB>>(lds, 64 * NW);
+    const int i0 = max(j0 - S.off, 0);
+    const int i1 = min(min(j0 + 32 * NW, S.lk) - 2 + A.window - S.off, S.lq - 1);
+    if (!backward_kv<DB, NW, false, false>(A, lds, S, j0, i0, i1, hk, b, 0))
+        backward_kv<DB, NW, false, true>(A, lds, S, j0, i0, i1, hk, b, 0);
+}
+
+template <int DB>
+__global__ void __launch_bounds__(64) bwd_far_kernel(Args A)
+{
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * kStageKV<DB>];
+    LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
+    int b, i0;
+    Span S;
+    const int hk = blockIdx.y, j0 = 32 * blockIdx.z;
+    if (!span_of(A, A.qs, A.Tq, blockIdx.x, A.chunk, false, S, b, i0))
+        return;
+    const int i1 = min(i0 + A.chunk, S.lq) - 1;
+    i0 = max(i0, j0 + A.window - S.off);
+    if (j0 >= S.lk || i0 > i1)
+        return;
+    if (A.D != 32 * DB)
+        zero_lds<2 * kStageKV<DB>>(lds, 64);
+    if (!backward_kv<DB, 1, true, false>(A, lds, S, j0, i0, i1, hk, b, blockIdx.x))
+        backward_kv<DB, 1, true, true>(A, lds, S, j0, i0, i1, hk, b, blockIdx.x);
+}
+
+// ------------------------------------------------------------------- host --
+
+template <int DB, int NW> void launch_fwd(Args &A, hipStream_t st)
+{
+    hipLaunchKernelGGL((fwd_kernel<DB, NW>), dim3((unsigned)items(A.tiles, A.Hk, A.G)), dim3(64 * NW), 0, st, A);
+}
+
+template <int DB, int NW> void launch_bwd_q(Args &A, hipStream_t st)
+{
+    hipLaunchKernelGGL((bwd_q_kernel<DB, NW>), dim3((unsigned)items(A.tiles, A.Hk, A.G)), dim3(64 * NW), 0, st, A);
+}
+
+// tiles of R rows that T rows of B sequences may have, numbered as span_of does
+inline int64_t tiles_of(int64_t T, int64_t R, int64_t B, bool packed)
+{
+    return packed ? T / R + B : (T + R - 1) / R;
+}
+
+// queries of a chunk of the sinks' far sums: at most about 64 chunks
+inline int64_t chunk_of(int64_t Tq)
+{
+    int64_t c = FAR_CHUNK;
+    while (c * 64 < Tq)
+        c *= 2;
+    return c;
+}
+
+inline int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
+inline int64_t row_bytes(int64_t Tq, int64_t Hq) { return round256(4 * Tq * Hq); }
+inline int64_t blocks_of(int64_t D) { return D <= 64 ? 2 : D <= 96 ? 3 : 4; }
+
+} // namespace mxa
+
+namespace {
+
+using mxk::aligned;
+using mxk::check_heads;
+using mxk::fail;
+using mxk::launched;
+
+mx_status check_common(const mx_heads *q, const mx_heads *k, const mx_heads *v, int64_t Tq, int64_t Tk, int64_t D,
+                       const int32_t *q_start, const int32_t *k_start, int64_t sequences, int64_t window, int64_t sinks,
+                       float scale)
+{
+    if (Tq < 0 || Tk < 0)
+        return fail(MX_EINVAL, "Tq and Tk must be >= 0");
+    if (D <= 0 || D % 8 != 0)
+        return fail(MX_EINVAL, "D must be a positive multiple of 8");
+    if (!q || !k || !v || q->heads < 1 || k->heads < 1 || q->heads % k->heads != 0)
+        return fail(MX_EINVAL, "q, k and v must be given, q's heads a multiple of k's");
+    if (window < 0 || sinks < 0)
+        return fail(MX_EINVAL, "window and sinks must be >= 0");
+    if (!(scale >= 0x1p-100f && scale <= 0x1p100f))
+        return fail(MX_EINVAL, "scale must be from 2^-100 to 2^100");
+    if (q_start ? sequences < 1 || !aligned(q_start, 4) || !aligned(k_start, 4) : sequences != 1 || k_start != nullptr)
+        return fail(MX_EINVAL, "q_start must hold sequences + 1 starts; without it there is one sequence, and no k_start");
+    if (q_start && !k_start && Tq != Tk)
+        return fail(MX_EINVAL, "without k_start, k must have the tokens of q");
+    if (D > MX_ATTN_MAX_D || sinks > MX_ATTN_MAX_SINKS)
+        return fail(MX_EUNSUPPORTED, "heads of more than %d elements, or more than %d sinks", MX_ATTN_MAX_D, MX_ATTN_MAX_SINKS);
+    if (Tq > MX_ATTN_MAX_TOKENS || Tk > MX_ATTN_MAX_TOKENS || q->heads > 4096 || sequences > 1 << 20)
+        return fail(MX_EUNSUPPORTED, "at most %d tokens, 4096 heads and 2^20 sequences", MX_ATTN_MAX_TOKENS);
+    if ((mxa::tiles_of(Tq, 128, sequences, true) + 1) * q->heads > 1 << 30)
+        return fail(MX_EUNSUPPORTED, "too many tokens times heads");
+    return MX_OK;
+}
+
+mxa::In in_of(const mx_heads *h)
+{
+    return {static_cast<const uint16_t *>(h->data), h->token_stride, h->head_stride};
+}
+mxa::Out out_of(const mx_heads *h)
+{
+    return {static_cast<uint16_t *>(h->data), h->token_stride, h->head_stride};
+}
+
+mxa::Args arguments(const mx_heads *q, const mx_heads *k, const mx_heads *v, int64_t Tq, int64_t Tk, int64_t D,
+                    const int32_t *q_start, const int32_t *k_start, int64_t sequences, int64_t window, int64_t sinks,
+                    float scale)
+{
+    mxa::Args A{};
+    A.q = in_of(q);
+    A.k = in_of(k);
+    A.v = in_of(v);
+    A.qs = q_start;
+    A.ks = k_start ? k_start : q_start;
+    A.Tq = (int)Tq;
+    A.Tk = (int)Tk;
+    A.B = (int)sequences;
+    A.Hk = (int)k->heads;
+    A.G = (int)(q->heads / k->heads);
+    A.D = (int)D;
+    // no two positions are further apart than 2^30
+    A.window = window == 0 || window > MX_ATTN_MAX_TOKENS ? MX_ATTN_MAX_TOKENS : (int)window;
+    A.sinks = A.window == MX_ATTN_MAX_TOKENS ? 0 : (int)sinks;
+    A.scale = scale;
+    A.c = scale * mxa::LOG2E;
+    return A;
+}
+
+} // namespace
+
+extern "C" {
+
+mx_status window_attn_fwd(const mx_heads *q, const mx_heads *k, const mx_heads *v, int64_t Tq, int64_t Tk, int64_t D,
+                          const int32_t *q_start, const int32_t *k_start, int64_t sequences, int64_t window, int64_t sinks,
+                          float scale, const mx_heads *out, float *lse, hipStream_t stream)
+{
+    mxk::clear_error();
+    mx_status st = check_common(q, k, v, Tq, Tk, D, q_start, k_start, sequences, window, sinks, scale);
+    if (st != MX_OK || (st = check_heads(q, "q", Tq, D, q->heads, false)) != MX_OK ||
+        (st = check_heads(k, "k", Tk, D, k->heads, false)) != MX_OK ||
+        (st = check_heads(v, "v", Tk, D, k->heads, false)) != MX_OK ||
+        (st = check_heads(out, "out", Tq, D, q->heads, true)) != MX_OK)
+        return st;
+    if (!aligned(lse, 4))
+        return fail(MX_EINVAL, "lse must be 4-byte aligned");
+    if (Tq == 0)
+        return MX_OK;
+    mxa::Args A = arguments(q, k, v, Tq, Tk, D, q_start, k_start, sequences, window, sinks, scale);
+    A.out = out_of(out);
+    A.lse_out = lse;
+    A.tiles = (int)mxa::tiles_of(Tq, 256, sequences, q_start != nullptr);
+    switch (mxa::blocks_of(D)) {
+    case 2: mxa::launch_fwd<2, 8>(A, stream); break;
+    case 3: mxa::launch_fwd<3, 8>(A, stream); break;
+    default: mxa::launch_fwd<4, 8>(A, stream); break;
+    }
+    return launched();
+}
+
+size_t window_attn_bwd_workspace_bytes(int64_t Tq, int64_t q_heads, int64_t k_heads, int64_t D, int64_t sequences, int64_t sinks)
+{
+    if (Tq <= 0 || Tq > MX_ATTN_MAX_TOKENS || q_heads < 1 || q_heads > 4096 || k_heads < 1 || k_heads > q_heads || D < 1 ||
+        D > MX_ATTN_MAX_D || sequences < 1 || sequences > 1 << 20 || sinks < 0 || sinks > MX_ATTN_MAX_SINKS)
+        return 0;
+    const int64_t slots = mxa::tiles_of(Tq, mxa::chunk_of(Tq), sequences, true) + 1;
+    return 2 * mxa::row_bytes(Tq, q_heads) + slots * k_heads * ((sinks + 31) / 32) * mxa::blocks_of(D) * (2 * 16 * 64 * 4);
+}
+
+mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_heads *k, const mx_heads *v,
+                          const mx_heads *out, const float *lse, int64_t Tq, int64_t Tk, int64_t D, const int32_t *q_start,
+                          const int32_t *k_start, int64_t sequences, int64_t window, int64_t sinks, float scale,
+                          const mx_heads *grad_q, const mx_heads *grad_k, const mx_heads *grad_v, void *workspace,
+                          size_t workspace_bytes, hipStream_t stream)
+{
+    mxk::clear_error();
+    mx_status st = check_common(q, k, v, Tq, Tk, D, q_start, k_start, sequences, window, sinks, scale);
+    if (st != MX_OK || (st = check_heads(grad_out, "grad_out", Tq, D, q->heads, false)) != MX_OK ||
+        (st = check_heads(q, "q", Tq, D, q->heads, false)) != MX_OK ||
+        (st = check_heads(k, "k", Tk, D, k->heads, false)) != MX_OK ||
+        (st = check_heads(v, "v", Tk, D, k->heads, false)) != MX_OK ||
+        (st = check_heads(out, "out", Tq, D, q->heads, false)) != MX_OK ||
+        (st = check_heads(grad_q, "grad_q", Tq, D, q->heads, true)) != MX_OK ||
+        (st = check_heads(grad_k, "grad_k", Tk, D, k->heads, true)) != MX_OK ||
+        (st = check_heads(grad_v, "grad_v", Tk, D, k->heads, true)) != MX_OK)
+        return st;
+    const size_t need = window_attn_bwd_workspace_bytes(Tq, q->heads, k->heads, D, sequences, sinks);
+    if (Tq > 0 && (!lse || !aligned(lse, 4) || !workspace || !aligned(workspace, 256) || workspace_bytes < need))
+        return fail(MX_EINVAL, "lse must be given, 4-byte aligned, and a 256-byte aligned workspace of %zu bytes", need);
+    mxa::Args A = arguments(q, k, v, Tq, Tk, D, q_start, k_start, sequences, window, sinks, scale);
+    const bool packed = q_start != nullptr;
+    const int DB = (int)mxa::blocks_of(D);
+    if (Tq > 0) {
+        A.go = in_of(grad_out);
+        A.o = in_of(out);
+        A.lse = lse;
+        A.lse2 = static_cast<float *>(workspace);
+        A.delta = A.lse2 + mxa::row_bytes(Tq, q->heads) / 4;
+        A.part = A.delta + mxa::row_bytes(Tq, q->heads) / 4;
+        A.chunk = (int)mxa::chunk_of(Tq);
+        A.out = out_of(grad_q);
+        A.tiles = (int)mxa::tiles_of(Tq, 256, sequences, packed);
+        switch (DB) {
+        case 2: mxa::launch_bwd_q<2, 8>(A, stream); break;
+        case 3: mxa::launch_bwd_q<3, 8>(A, stream); break;
+        default: mxa::launch_bwd_q<4, 8>(A, stream); break;
+        }
+    }
+    if (Tk > 0) {
+        A.gk = out_of(grad_k);
+        A.gv = out_of(grad_v);
+        if (Tq > 0 && A.sinks > 0) {
+            const dim3 grid((unsigned)mxa::tiles_of(Tq, A.chunk, sequences, packed), (unsigned)A.Hk, (unsigned)((A.sinks + 31) / 32));
+            switch (DB) {
+            case 2: hipLaunchKernelGGL((mxa::bwd_far_kernel<2>), grid, dim3(64), 0, stream, A); break;
+            case 3: hipLaunchKernelGGL((mxa::bwd_far_kernel<3>), grid, dim3(64), 0, stream, A); break;
+            default: hipLaunchKernelGGL((mxa::bwd_far_kernel<4>), grid, dim3(64), 0, stream, A); break;
+            }
+        }
+        A.tiles = (int)mxa::tiles_of(Tk, 128, sequences, packed);
+        const dim3 grid((unsigned)mxa::items(A.tiles, A.Hk, 1));
+        switch (DB) {
+        case 2: hipLaunchKernelGGL((mxa::bwd_kv_kernel<2, 4>), grid, dim3(256), 0, stream, A); break;
+        case 3: hipLaunchKernelGGL((mxa::bwd_kv_kernel<3, 4>), grid, dim3(256), 0, stream, A); break;
+        default: hipLaunchKernelGGL((mxa::bwd_kv_kernel<4, 4>), grid, dim3(256), 0, stream, A); break;
+        }
+    }
+    return launched();
+}
+
+} // extern "C"

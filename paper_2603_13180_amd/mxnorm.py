@@ -81,6 +81,10 @@ def load():
         "qk_norm_rope_bwd_workspace_bytes": (ctypes.c_size_t, [I64, I64]),
         "qk_norm_rope_bwd": (I, [P, P, P, P, P, P, I64, I64, I64, P, P, I, F, P, P, P, P, P,
                                  ctypes.c_size_t, P]),
+        "window_attn_fwd": (I, [P, P, P, I64, I64, I64, P, P, I64, I64, I64, F, P, P, P]),
+        "window_attn_bwd_workspace_bytes": (ctypes.c_size_t, [I64, I64, I64, I64, I64, I64]),
+        "window_attn_bwd": (I, [P, P, P, P, P, P, I64, I64, I64, P, P, I64, I64, I64, F, P, P, P, P,
+                                ctypes.c_size_t, P]),
         "mxnorm_default_global_scale": (F, [I64, I, I, F]),
         "rmsnorm_default_global_scale": (F, [I64, F]),
         "mxnorm_coef": (F, [I, I]),
@@ -706,6 +710,72 @@ def qk_norm_rope_bwd(grad_q_out, grad_k_out, q, k, q_gamma, k_gamma, pos, inv_fr
           _ptr(k_gamma), T, D, R, _ptr(pos), _ptr(inv_freq), int(bool(interleaved)), eps, ref(oq),
           ref(ok), _ptr(gg[0]), _ptr(gg[1]), _ptr(ws), ws_bytes)
     return grad_q, grad_k, gg[0], gg[1]
+
+
+def _starts(t, name, device, n=None):
+    """An int32 vector of n elements, if given; None stays None."""
+    if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or t.device != device or not t.is_contiguous()
+                          or (n is not None and t.shape[0] != n)):
+        raise ValueError("%s must be a contiguous int32 tensor%s on q's device" % (name, "" if n is None else " [%d]" % n))
+    return t
+
+
+def _attn_arguments(q, k, v, q_start, k_start, scale):
+    """(mx_heads of q, k, v; Tq, Tk, D, sequences, scale) of a call."""
+    dq, dk, dv = _heads(q, "q"), _heads(k, "k"), _heads(v, "v", k)
+    Tq, Hq, D = q.shape
+    Tk, Hk, Dk = k.shape
+    device = q.device
+    if Dk != D or k.device != device or Hk == 0 or Hq % Hk:
+        raise ValueError("k and v must have q's head size and device, and q a multiple of their heads")
+    sequences = 1
+    if q_start is not None:
+        _starts(q_start, "q_start", device)
+        sequences = q_start.shape[0] - 1
+        _starts(k_start, "k_start", device, sequences + 1)
+    elif k_start is not None:
+        raise ValueError("k_start needs a q_start")
+    return dq, dk, dv, Tq, Tk, D, sequences, D ** -0.5 if scale is None else scale
+
+
+def window_attn_fwd(q, k, v, window=0, sinks=0, scale=None, q_start=None, k_start=None, out=None, lse=None,
+                    want_lse=True):
+    """Causal attention of q [T, Hq, D] over k and v [S, Hk, D] (views of a
+    projection's output among them), packed sequences by q_start and k_start
+    (int32 [sequences + 1]; k_start None: q_start, both None: one sequence whose
+    queries are its last tokens).  Of the keys up to its own place a query sees
+    the last `window` (0: all) and the first `sinks`.  scale None: D ** -0.5.
+    Returns (out [T, Hq, D], lse float32 [Hq, T] or None)."""
+    dq, dk, dv, T, S, D, B, scale = _attn_arguments(q, k, v, q_start, k_start, scale)
+    out, do = _new_heads(q) if out is None else (out, _heads(out, "out", q))
+    if want_lse:
+        lse = _out(lse, (q.shape[1], T), torch.float32, q.device)
+    ref = ctypes.byref
+    _call(load().window_attn_fwd, q.device, ref(dq), ref(dk), ref(dv), T, S, D, _ptr(q_start), _ptr(k_start), B,
+          window, sinks, scale, ref(do), _ptr(lse) if want_lse else None)
+    return out, (lse if want_lse else None)
+
+
+def window_attn_bwd(grad_out, q, k, v, out, lse, window=0, sinks=0, scale=None, q_start=None, k_start=None,
+                    grad_q=None, grad_k=None, grad_v=None):
+    """The gradients of window_attn_fwd from that of its output: q, k, v and the
+    rest as it took them, out and lse as it gave them.  grad_q, grad_k and grad_v
+    may be views of the projection's gradient.  Returns (grad_q, grad_k, grad_v)."""
+    dq, dk, dv, T, S, D, B, scale = _attn_arguments(q, k, v, q_start, k_start, scale)
+    dg, do = _heads(grad_out, "grad_out", q), _heads(out, "out", q)
+    Hq, device = q.shape[1], q.device
+    if lse.shape != (Hq, T) or lse.dtype != torch.float32 or lse.device != device or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous float32 [Hq, T] tensor on q's device")
+    grad_q, gq = _new_heads(q) if grad_q is None else (grad_q, _heads(grad_q, "grad_q", q))
+    grad_k, gk = _new_heads(k) if grad_k is None else (grad_k, _heads(grad_k, "grad_k", k))
+    grad_v, gv = _new_heads(v) if grad_v is None else (grad_v, _heads(grad_v, "grad_v", v))
+    lib = load()
+    ws_bytes = lib.window_attn_bwd_workspace_bytes(T, Hq, k.shape[1], D, B, sinks)
+    ws = q.new_empty((ws_bytes,), dtype=torch.uint8) if ws_bytes else None
+    ref = ctypes.byref
+    _call(lib.window_attn_bwd, device, ref(dg), ref(dq), ref(dk), ref(dv), ref(do), _ptr(lse), T, S, D,
+          _ptr(q_start), _ptr(k_start), B, window, sinks, scale, ref(gq), ref(gk), ref(gv), _ptr(ws), ws_bytes)
+    return grad_q, grad_k, grad_v
 
 
 def mxnorm_default_global_scale(d, block=16, p=2, coef=0.0):
