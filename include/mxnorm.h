@@ -62,6 +62,7 @@ extern "C" {
 #define MX_ATTN_MAX_D 128
 #define MX_ATTN_MAX_SINKS 256
 #define MX_ATTN_MAX_TOKENS (1 << 28)
+#define MX_ATTN_MAX_NEW 64
 
 typedef enum {
     MX_OK = 0,
@@ -538,6 +539,82 @@ mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_
                           const int32_t *q_start, const int32_t *k_start, int64_t sequences, int64_t window,
                           int64_t sinks, float scale, const mx_heads *grad_q, const mx_heads *grad_k,
                           const mx_heads *grad_v, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+typedef enum {
+    MX_CACHE_BF16 = 0,    /* bf16 elements                                */
+    MX_CACHE_E4M3 = 1     /* E4M3 codes, an E8M0 scale for 32 elements    */
+} mx_cache_type;
+
+/*
+ * A paged cache of keys and values (device): pages of page_size slots (a power of
+ * two from 16 on), element (page, head, slot, e) of k and of v at page page_stride
+ * + (head page_size + slot) D + e (strides in elements, whole 16-byte pieces; not
+ * used with one page), so k and v may be halves of one buffer.  MX_CACHE_E4M3: the
+ * codes of mx_cast_fwd along D (RCEIL) and k_scales, v_scales uint8 at page
+ * scale_page_stride + (head page_size + slot) D / 32 + block; D a multiple of 32.
+ * k and v 16-byte aligned.
+ *
+ * Sequence b's token at place j is in slot j % page_size of page table[b
+ * table_width + j / page_size] (int32, device).  A page outside 0 .. pages - 1, or
+ * past the table's end, is not there: nothing is written to it, and no token sees
+ * the keys it would hold.  So pages that a window has left behind may be let go.
+ * length: int32 [sequences] (device), the tokens that a sequence has in the cache,
+ * its new ones not counted (a negative one counts as 0).  start: int32 [sequences
+ * + 1] (device), ascending: sequence b's new tokens are start[b] .. start[b + 1] -
+ * 1 of the call's T; NULL: one each, T = sequences.
+ */
+typedef struct {
+    void *k, *v;
+    uint8_t *k_scales, *v_scales; /* NULL for MX_CACHE_BF16 */
+    int64_t pages, page_size, heads, page_stride, scale_page_stride;
+    int type;                     /* mx_cache_type */
+} mx_kv_cache;
+
+/*
+ * Writes new tokens' keys and values into the cache: sequence b's i-th at place
+ * length[b] + i.  k, v: [S, heads, D] (mx_heads); the call's token t is row t, or
+ * rows[t] (int32 [T], device), so that of drafted tokens those kept are written
+ * again, one behind the other.  MX_CACHE_E4M3: cast as mx_cast_fwd casts, with its
+ * codes for blocks that hold infinities or NaN.  Tokens that no sequence has, and
+ * rows outside 0 .. S - 1, are not written.  length is not changed.  Two tokens at
+ * one place (pages shared by sequences) leave either.  D a multiple of 8 (32), at
+ * most MX_ATTN_MAX_D; T == 0 is a no-op.
+ */
+mx_status kv_cache_append(const mx_kv_cache *cache, const mx_heads *k, const mx_heads *v, int64_t T, int64_t S,
+                          int64_t D, const int32_t *table, int64_t table_width, const int32_t *length,
+                          const int32_t *start, int64_t sequences, const int32_t *rows, hipStream_t stream);
+
+/*
+ * Attention of new tokens over the cache, their own keys and values appended
+ * before: q, out [T, Hq, D] (mx_heads), Hq a multiple of the cache's heads.  At
+ * most max_new (up to MX_ATTN_MAX_NEW) new tokens a sequence; a sequence with more
+ * has unspecified rows.
+ * ancestors: int64 [T] (device) or NULL.  Bit u of a token's: it sees drafted
+ * token u of its sequence (its own bit is not implied); NULL: the ones up to
+ * itself.  A token's place is length + (its bits below the sequence's new tokens)
+ * - 1, so that siblings of a tree have the same; of the cached tokens, and of the
+ * drafted ones its bits name, it sees those whose place is less than `window`
+ * before its own or below `sinks` (window 0: all).
+ * A token that sees none gives 0.  Arithmetic, masked places and rows that no
+ * sequence has as in window_attn_fwd; keys and values of codes are exact.  Where
+ * few sequences and heads would leave compute units idle, shares of a sequence's
+ * keys are summed apart and joined in order: how many depends on the arguments, so
+ * a token's last bits may depend on its batch; the same call gives the same bits.
+ * max_length: a bound of `length` that the caller knows, for that choice (0: what
+ * the table has room for); results do not depend on its being right.
+ * `workspace`: caller-owned device memory of kv_cache_attn_fwd_workspace_bytes()
+ * bytes (0: may be NULL), 256-byte aligned, overwritten; calls that overlap in
+ * time need one each.  Limits else as window_attn_fwd's, and any number of sinks.
+ * out must not overlap an input.
+ */
+size_t kv_cache_attn_fwd_workspace_bytes(int64_t T, int64_t q_heads, int64_t k_heads, int64_t D,
+                                         int64_t sequences, int64_t page_size, int64_t table_width,
+                                         int64_t max_new, int64_t max_length, int64_t window, int64_t sinks);
+mx_status kv_cache_attn_fwd(const mx_kv_cache *cache, const mx_heads *q, int64_t T, int64_t D,
+                            const int32_t *table, int64_t table_width, const int32_t *length,
+                            const int32_t *start, int64_t sequences, int64_t max_new, int64_t max_length,
+                            const int64_t *ancestors, int64_t window, int64_t sinks, float scale,
+                            const mx_heads *out, void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 /*
  * Default NVFP4 tensor decode scales: an output bound divided by 6 * 448, so

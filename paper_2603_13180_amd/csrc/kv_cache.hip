@@ -1,0 +1,740 @@
+// kv_cache.hip -- a paged cache of keys and values: new tokens' heads into it, and
+// attention of new tokens (one a sequence, or a tree of drafted ones) over it.
+//
+// Sequence b has length[b] cached tokens; its new ones stand behind them, drafted
+// token i at key length + i.  Token i sees cached key j where place - j < window or
+// j < sinks, and drafted key u where bit u of its mask is set and the same holds of
+// u's place; a token's place is length + popcount(mask) - 1.
+//
+// The group's query heads and the sequence's new tokens are rows of one product, so
+// the cache is read once for all of them.  A workgroup takes one key head of one
+// sequence, RB blocks of 32 rows and a share of the keys; KW groups of RB waves take
+// tiles of keys in turn, each with its own maximum and sums, joined at the end, and
+// across workgroups by a second kernel.
+#include "attn.h"
+#include "norm_cast.h"
+
+namespace mxa {
+
+struct Cache {
+    uint8_t *k, *v;          // pages [heads, slots, D] of bf16 elements or E4M3 codes
+    uint8_t *ks, *vs;        // E8M0 scales [heads, slots, D / 32] of codes
+    int64_t page_bytes, page_scales; // from page to page
+    int pages, shift;        // 2^shift slots
+    const int *table;        // [B, width] pages of every sequence
+    const int *length;       // [B]
+    int width, B, Hk, D;
+};
+
+// New tokens: sequence b's are start[b] .. start[b + 1] - 1, or without starts
+// token b.
+__device__ __forceinline__ int first_of(const int *start, int b, int T)
+{
+    return start ? min(max(start[b], 0), T) : min(b, T);
+}
+
+// ----------------------------------------------------------------- append --
+
+struct AppendArgs {
+    Cache C;
+    In k, v;
+    const int *start, *rows;
+    int T, S; // new tokens, rows of k and v
+    int tpw;  // tokens of a workgroup
+};
+
+constexpr int APPEND_THREADS = 256, APPEND_TOKENS = 64, APPEND_STARTS = 1024;
+
+template <bool MX> __global__ void __launch_bounds__(APPEND_THREADS) append_kernel(AppendArgs A)
+{
+    __shared__ int starts[APPEND_STARTS];
+    __shared__ int64_t to[APPEND_TOKENS]; // page's first row of the head 0 and slot, or -1
+    __shared__ int from[APPEND_TOKENS];
+    __shared__ int slots[APPEND_TOKENS];
+    const Cache &C = A.C;
+    const int t0 = blockIdx.x * A.tpw, nt = min(A.tpw, A.T - t0);
+    const bool near = A.start && C.B < APPEND_STARTS;
+    if (near)
+        for (int i = threadIdx.x; i <= C.B; i += APPEND_THREADS)
+            starts[i] = first_of(A.start, i, A.T);
+    __syncthreads();
+    if ((int)threadIdx.x < nt) {
+        const int t = t0 + threadIdx.x;
+        auto first = [&](int b) { return near ? starts[b] : first_of(A.start, b, A.T); };
+        int b = A.start ? 0 : t, hi = A.start ? C.B - 1 : t;
+        while (b < hi) {
+            const int mid = (b + hi + 1) >> 1;
+            if (first(mid) <= t)
+                b = mid;
+            else
+                hi = mid - 1;
+        }
+        const int i = t - first(b), src = A.rows ? A.rows[t] : t;
+        int page = -1, slot = 0;
+        if (b < C.B && i >= 0 && t < first(b + 1) && (unsigned)src < (unsigned)A.S) {
+            const int64_t at = (int64_t)C.length[b] + i;
+            slot = (int)(at & ((1 << C.shift) - 1));
+            if (at >= 0 && at >> C.shift < C.width)
+                page = C.table[(int64_t)b * C.width + (at >> C.shift)];
+        }
+        to[threadIdx.x] = (unsigned)page < (unsigned)C.pages ? page : -1;
+        slots[threadIdx.x] = slot;
+        from[threadIdx.x] = src;
+    }
+    __syncthreads();
+    const int row = C.D / 8, per = C.Hk * row; // 16-byte chunks
+    for (int i = threadIdx.x; i < nt * per; i += APPEND_THREADS) {
+        const int t = i / per, h = (i - t * per) / row, c = i - t * per - h * row;
+        const int64_t page = to[t], src = from[t];
+        if (page < 0)
+            continue;
+        const int64_t slot = ((int64_t)h << C.shift) + slots[t];
+        const u32x4 k = *reinterpret_cast<const u32x4 *>(A.k.p + src * A.k.ts + h * A.k.hs + c * 8);
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(A.v.p + src * A.v.ts + h * A.v.hs + c * 8);
+        if constexpr (!MX) {
+            *reinterpret_cast<u32x4 *>(C.k + page * C.page_bytes + (slot * C.D + c * 8) * 2) = k;
+            *reinterpret_cast<u32x4 *>(C.v + page * C.page_bytes + (slot * C.D + c * 8) * 2) = v;
+        } else {
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+                const u32x4 x = which ? v : k;
+                // the block's largest magnitude: four lanes hold its 32 elements
+                uint32_t m = 0;
+                float t8[8];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    m = max(m, max(x[e] & 0x7FFFu, (x[e] >> 16) & 0x7FFFu));
+                    t8[2 * e] = __uint_as_float(x[e] << 16);
+                    t8[2 * e + 1] = __uint_as_float(x[e] & 0xFFFF0000u);
+                }
+                m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0xB1, 0xF, 0xF, true));
+                m = max(m, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, 0x4E, 0xF, 0xF, true));
+                const uint32_t byte = mxk::e8m0_byte<false>(__uint_as_float(m << 16), MX_SCALE_RCEIL);
+                const float scale = __uint_as_float(byte << 23);
+                u32x2 codes = {mxk::e4m3x4_hw(t8[0], t8[1], t8[2], t8[3], scale),
+                               mxk::e4m3x4_hw(t8[4], t8[5], t8[6], t8[7], scale)};
+                if (byte == 0xFFu)
+                    codes = u32x2{mxk::nan_codes_e4m3(x[0], x[1]), mxk::nan_codes_e4m3(x[2], x[3])};
+                *reinterpret_cast<u32x2 *>((which ? C.v : C.k) + page * C.page_bytes + slot * C.D + c * 8) = codes;
+                if (c % 4 == 0)
+                    (which ? C.vs : C.ks)[page * C.page_scales + slot * (C.D / 32) + c / 4] = (uint8_t)byte;
+            }
+        }
+    }
+}
+
+// -------------------------------------------------------------- attention --
+
+constexpr int MAX_NEW = MX_ATTN_MAX_NEW;
+
+struct CachedArgs {
+    Cache C;
+    In q;
+    Out out;
+    const int *start;
+    const int64_t *bits; // [T] or NULL: every token sees the ones before it and itself
+    float *part;         // [T, Hq, splits, D] sums and
+    float2 *stat;        // [T, Hq, splits] maxima (powers of two) and sums of exponentials
+    int T, G, max_new, blocks; // blocks of 32 RB rows
+    int splits, window, sinks;
+    float c;
+};
+
+// A sequence of a workgroup.
+struct Rows {
+    int t0, n, len, R; // first token, tokens, cached tokens, rows
+    int end;           // keys that the table has pages for
+    const int *pages;
+    // the page of key j, or one that the cache does not have
+    __device__ __forceinline__ int page_of(int j, int shift) const { return j < end ? pages[j >> shift] : -1; }
+};
+
+template <int RB> struct Shape {
+    static constexpr int KW = RB >= 4 ? 1 : 4 / RB, NW = RB * KW;
+    static constexpr int NB = RB >= 4 ? 2 : 1, KEYS = 32 * NB; // of a tile
+    static constexpr int STAGES = RB == 1 ? 1 : 2;
+};
+
+// A thread's part of a tile of keys and values on its way to LDS.
+template <int DB, int RB, bool MX> struct Staged {
+    using O = Shape<RB>;
+    static constexpr int PER = kChunks<DB> / (MX ? 2 : 1);      // 16-byte pieces of a row
+    static constexpr int PIECES = O::KEYS * PER, N = (PIECES + 64 * RB - 1) / (64 * RB);
+    u32x4 k[N], v[N];
+    uint32_t sk[N], sv[N]; // scale bytes
+
+    // Keys j0 .. of the tile, those past the end and those of pages that are not
+    // there as zeros.  i: the thread's number among those of its group.
+    __device__ __forceinline__ void load(const Cache &C, const Rows &S, int hk, int j0, int i)
+    {
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+            const int p = x * 64 * RB + i, r = p / PER, c = p % PER, j = j0 + r;
+            k[x] = v[x] = u32x4{0, 0, 0, 0};
+            sk[x] = sv[x] = 127;
+            if (PIECES % (64 * RB) != 0 && p >= PIECES)
+                continue;
+            const int page = S.page_of(j, C.shift);
+            if ((unsigned)page >= (unsigned)C.pages || c * (MX ? 16 : 8) >= C.D)
+                continue;
+            const int64_t slot = ((int64_t)hk << C.shift) + (j & ((1 << C.shift) - 1));
+            const int64_t at = page * C.page_bytes + slot * C.D * (MX ? 1 : 2) + c * 16;
+            k[x] = *reinterpret_cast<const u32x4 *>(C.k + at);
+            v[x] = *reinterpret_cast<const u32x4 *>(C.v + at);
+            if constexpr (MX) {
+                const int64_t s = page * C.page_scales + slot * (C.D / 32) + c / 2;
+                sk[x] = C.ks[s];
+                sv[x] = C.vs[s];
+            }
+        }
+    }
+
+    // 16 codes times 2^(s - 127) as bf16 (exact but for bf16's subnormals)
+    __device__ __forceinline__ static void decode(u32x4 codes, uint32_t s, u32x4 &lo, u32x4 &hi)
+    {
+        const float by = __uint_as_float(s << 23);
+        u32x4 o[2];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            o[e / 2][e % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[e], by, false));
+            o[e / 2][e % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[e], by, true));
+        }
+        if (s == 255) // a scale that is not a number
+            o[0] = o[1] = u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
+        lo = o[0];
+        hi = o[1];
+    }
+
+    __device__ __forceinline__ void store(LDS_AS uint8_t *tile, int i) const
+    {
+        constexpr int TILE = O::KEYS * kRow<DB>;
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+            const int p = x * 64 * RB + i, r = p / PER, c = p % PER;
+            if (PIECES % (64 * RB) != 0 && p >= PIECES)
+                continue;
+            LDS_AS uint8_t *row = tile + r * kRow<DB>;
+            if constexpr (MX) {
+                u32x4 lo, hi;
+                const int a = ((2 * c) ^ swz<DB>(r)) * 16, b = ((2 * c + 1) ^ swz<DB>(r)) * 16;
+                decode(k[x], sk[x], lo, hi);
+                *reinterpret_cast<LDS_AS u32x4 *>(row + a) = lo;
+                *reinterpret_cast<LDS_AS u32x4 *>(row + b) = hi;
+                decode(v[x], sv[x], lo, hi);
+                *reinterpret_cast<LDS_AS u32x4 *>(row + TILE + a) = lo;
+                *reinterpret_cast<LDS_AS u32x4 *>(row + TILE + b) = hi;
+            } else {
+                const int a = (c ^ swz<DB>(r)) * 16;
+                *reinterpret_cast<LDS_AS u32x4 *>(row + a) = k[x];
+                *reinterpret_cast<LDS_AS u32x4 *>(row + TILE + a) = v[x];
+            }
+        }
+    }
+};
+
+template <int DB, int RB, bool MX, bool CAREFUL>
+__device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds, const LDS_AS int *places, const Rows &S,
+                                       int hk, int split, int r0)
+{
+    using O = Shape<RB>;
+    constexpr int TILE = O::KEYS * kRow<DB>, GROUP = O::STAGES * 2 * TILE;
+    const Cache &C = A.C;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, h = l >> 5;
+    const int kw = w / RB, in_group = threadIdx.x - kw * RB * 64;
+    const Lane<DB> L(l);
+    const int rw = r0 + 32 * (w % RB), r = min(rw + n, S.R - 1), i = r / A.G, hq = hk * A.G + r % A.G;
+    const bool mine = rw + n < S.R;
+    b8 q[2 * DB];
+    {
+        const uint16_t *row = A.q.p + (int64_t)(S.t0 + i) * A.q.ts + hq * A.q.hs;
+#pragma unroll
+        for (int ks = 0; ks < 2 * DB; ++ks) {
+            const int e = 16 * ks + 8 * h;
+            u32x4 x = {0, 0, 0, 0};
+            if (e < C.D)
+                x = *reinterpret_cast<const u32x4 *>(row + e);
+            q[ks] = __builtin_bit_cast(b8, x);
+        }
+    }
+    const uint64_t all = S.n >= 64 ? ~0ull : (1ull << S.n) - 1;
+    const uint64_t bits = (A.bits ? (uint64_t)A.bits[S.t0 + i] : (2ull << i) - 1) & all;
+    const int place = S.len + __popcll(bits) - 1;
+    // Tiles: the sinks', then from the first key that the window of a token at
+    // length - 1 holds.  Row blocks differ in their places, not in their tiles.
+    const int first = max(S.len - A.window, 0) / O::KEYS;
+    const int sinks = min((A.sinks + O::KEYS - 1) / O::KEYS, first);
+    const int tiles = sinks + max((S.end + O::KEYS - 1) / O::KEYS - first, 0);
+    const int from = (int)((int64_t)tiles * split / A.splits), to = (int)((int64_t)tiles * (split + 1) / A.splits);
+    auto key_of = [&](int t) { return (t < sinks ? t : first + t - sinks) * O::KEYS; };
+    auto sees = [&](int j) {
+        int at = j;
+        if (j >= S.len) {
+            if (j >= S.end || !(bits >> (j - S.len) & 1))
+                return false;
+            at = places[j - S.len];
+        }
+        return place - at < A.window || at < A.sinks;
+    };
+    Staged<DB, RB, MX> next;
+    f16v o[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+        o[d] = zero16();
+    float m = -FLT_MAX, sum = 0.0f;
+    bool any = false;
+    const int rounds = (to - from + O::KW - 1) / O::KW;
+    auto tile_of = [&](int it) { return from + it * O::KW + kw; };
+    if (tile_of(0) < to)
+        next.load(C, S, hk, key_of(tile_of(0)), in_group);
+    for (int it = 0; it < rounds; ++it) {
+        const int t = tile_of(it);
+        LDS_AS uint8_t *kt = lds + kw * GROUP + (O::STAGES == 2 ? (it & 1) * 2 * TILE : 0), *vt = kt + TILE;
+        if (t < to)
+            next.store(kt, in_group);
+        if (RB > 1)
+            __syncthreads();
+        if (tile_of(it + 1) < to)
+            next.load(C, S, hk, key_of(tile_of(it + 1)), in_group);
+        if (t >= to || rw >= S.R)
+            continue;
+        const int j0 = key_of(t);
+        // pages that are not there: their keys are not seen
+        uint32_t there = 0;
+#pragma unroll
+        for (int x = 0; x < O::KEYS / 16; ++x) {
+            there |= (uint32_t)((unsigned)S.page_of(j0 + 16 * x, C.shift) < (unsigned)C.pages) << x;
+        }
+        const bool full = j0 + O::KEYS <= S.len && there == (1u << O::KEYS / 16) - 1 &&
+                          S.len + S.n - 1 - j0 < A.window;
+        auto seen = [&](int x) { return (there >> (x >> 4) & 1) && sees(j0 + x); };
+        f16v s[O::NB];
+#pragma unroll
+        for (int x = 0; x < O::NB; ++x)
+            s[x] = zero16();
+#pragma unroll
+        for (int ks = 0; ks < 2 * DB; ++ks)
+#pragma unroll
+            for (int x = 0; x < O::NB; ++x)
+                s[x] = mfma(row_frag<DB>(kt, L, ks, x), q[ks], s[x]);
+        if (!full)
+#pragma unroll
+            for (int x = 0; x < O::NB; ++x)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const bool see = seen(32 * x + c_row(e, h));
+                    s[x][e] = see ? s[x][e] : -INFINITY;
+                    any |= see;
+                }
+        any |= full;
+        float mt = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < O::NB; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                mt = fmaxf(mt, s[x][e]);
+        mt = halves_max(mt) * A.c;
+        if (__builtin_amdgcn_ballot_w64(mt > m + 8.0f)) { // as in the packed sequences' kernel
+            const float mn = fmaxf(m, mt), by = __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            sum *= by;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+                o[d] *= by;
+        }
+#pragma unroll
+        for (int x = 0; x < O::NB; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                s[x][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e], A.c, -m));
+                sum += s[x][e];
+            }
+#pragma unroll
+        for (int x = 0; x < 2 * O::NB; ++x) {
+            const b8 y = pack8(s[x >> 1], x & 1);
+            if (CAREFUL && !full)
+                careful_product<DB>(o, vt, L, x, y, h, seen);
+            else
+                product<DB>(o, vt, L, x, y);
+        }
+    }
+    if (!CAREFUL && __syncthreads_or(mine && not_finite<DB>(o)))
+        return false;
+    if (CAREFUL)
+        __syncthreads();
+    sum = halves_sum(sum);
+    any = halves_max(any ? 1.0f : 0.0f) > 0.0f;
+    // join the key groups: group kw takes over blocks of 32 elements
+    if constexpr (O::KW > 1) {
+        LDS_AS float *stat = reinterpret_cast<LDS_AS float *>(lds) + RB * DB * O::KW * 1024;
+        auto cell = [&](int g, int what) { return stat + ((g * RB + w % RB) * 3 + what) * 32 + n; };
+        if (h == 0) {
+            *cell(kw, 0) = m;
+            *cell(kw, 1) = sum;
+            *cell(kw, 2) = any ? 1.0f : 0.0f;
+        }
+        __syncthreads();
+        float mn = m;
+        for (int g = 0; g < O::KW; ++g)
+            mn = fmaxf(mn, *cell(g, 0));
+        sum = 0.0f;
+        for (int g = 0; g < O::KW; ++g) {
+            sum += *cell(g, 1) * __builtin_amdgcn_exp2f(*cell(g, 0) - mn);
+            any |= *cell(g, 2) != 0.0f;
+        }
+        const float by = __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        LDS_AS float *sums = reinterpret_cast<LDS_AS float *>(lds);
+        auto at = [&](int g, int d, int e) { return sums + (((g * RB + w % RB) * DB + d) * 16 + e) * 64 + l; };
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                *at(kw, d, e) = o[d][e] * by;
+        __syncthreads();
+        if (kw != 0)
+            return true;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                float t = 0.0f;
+#pragma unroll
+                for (int g = 0; g < O::KW; ++g)
+                    t += *at(g, d, e);
+                o[d][e] = t;
+            }
+    }
+    if (rw >= S.R)
+        return true;
+    if (A.splits > 1) {
+        // a share that sees nothing is marked by a sum of 0, one that sees only
+        // scores of -inf by -1
+        const int64_t row = ((int64_t)(S.t0 + i) * A.G * C.Hk + hq) * A.splits + split;
+        if (mine && h == 0)
+            A.stat[row] = float2{m, sum > 0.0f || sum != sum ? sum : any ? -1.0f : 0.0f};
+        if (mine)
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    if (32 * d + 8 * g + 4 * h < C.D)
+                        *reinterpret_cast<float4 *>(A.part + row * C.D + 32 * d + 8 * g + 4 * h) =
+                            float4{o[d][4 * g], o[d][4 * g + 1], o[d][4 * g + 2], o[d][4 * g + 3]};
+        return true;
+    }
+    const float by = any ? 1.0f / sum : 0.0f;
+    if (mine)
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                if (32 * d + 8 * g + 4 * h < C.D)
+                    *reinterpret_cast<u32x2 *>(A.out.p + (int64_t)(S.t0 + i) * A.out.ts + hq * A.out.hs + 32 * d + 8 * g + 4 * h) =
+                        u32x2{pack_bf16(o[d][4 * g] * by, o[d][4 * g + 1] * by),
+                              pack_bf16(o[d][4 * g + 2] * by, o[d][4 * g + 3] * by)};
+    return true;
+}
+
+template <int DB, int RB, bool MX> __global__ void __launch_bounds__(64 * Shape<RB>::NW, 2) cached_kernel(CachedArgs A)
+{
+    using O = Shape<RB>;
+    constexpr int TILES = O::KW * O::STAGES * 2 * O::KEYS * kRow<DB>;
+    constexpr int JOIN = O::KW > 1 ? O::KW * RB * (DB * 1024 + 96) * 4 : 0;
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[std::max(TILES, JOIN)];
+    __shared__ int places[MAX_NEW];
+    LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
+    const Cache &C = A.C;
+    int id = blockIdx.x;
+    const int split = id % A.splits;
+    id /= A.splits;
+    const int hk = id % C.Hk;
+    id /= C.Hk;
+    const int block = id % A.blocks, b = id / A.blocks;
+    Rows S;
+    S.t0 = first_of(A.start, b, A.T);
+    S.n = min(min(first_of(A.start, b + 1, A.T) - S.t0, A.max_new), MAX_NEW);
+    S.R = S.n * A.G;
+    const int r0 = block * 32 * RB;
+    if (S.n <= 0 || r0 >= S.R)
+        return;
+    S.len = min(max(C.length[b], 0), MX_ATTN_MAX_TOKENS);
+    S.end = min(S.len + S.n, C.width << C.shift);
+    S.pages = C.table + (int64_t)b * C.width;
+    if ((int)threadIdx.x < S.n) {
+        const uint64_t all = S.n >= 64 ? ~0ull : (1ull << S.n) - 1;
+        places[threadIdx.x] = S.len - 1 + (A.bits ? __popcll((uint64_t)A.bits[S.t0 + threadIdx.x] & all) : (int)threadIdx.x + 1);
+    }
+    __syncthreads();
+    if (!cached<DB, RB, MX, false>(A, lds, (const LDS_AS int *)places, S, hk, split, r0))
+        cached<DB, RB, MX, true>(A, lds, (const LDS_AS int *)places, S, hk, split, r0);
+}
+
+// A row's shares joined: a wave takes one row, four elements a lane at a time.
+__global__ void __launch_bounds__(256) join_kernel(CachedArgs A)
+{
+    const Cache &C = A.C;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int Hq = A.G * C.Hk, l = threadIdx.x & 63;
+    const int64_t t = row / Hq;
+    if (t < first_of(A.start, 0, A.T) || t >= first_of(A.start, C.B, A.T))
+        return;
+    float m = -FLT_MAX;
+    bool any = false;
+    for (int s = l; s < A.splits; s += 64) {
+        const float2 x = A.stat[row * A.splits + s];
+        m = fmaxf(m, x.x);
+        any |= x.y != 0.0f;
+    }
+    for (int x = 32; x; x >>= 1)
+        m = fmaxf(m, __shfl_xor(m, x));
+    any = __builtin_amdgcn_ballot_w64(any) != 0;
+    float sum = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int e = 4 * l;
+    for (int s = 0; s < A.splits; ++s) {
+        const float2 x = A.stat[row * A.splits + s];
+        if (x.y == 0.0f || x.y == -1.0f)
+            continue;
+        const float by = __builtin_amdgcn_exp2f(x.x - m);
+        sum = __builtin_fmaf(x.y, by, sum);
+        if (e < C.D) {
+            const float4 v = *reinterpret_cast<const float4 *>(A.part + (row * A.splits + s) * C.D + e);
+            o[0] = __builtin_fmaf(v.x, by, o[0]);
+            o[1] = __builtin_fmaf(v.y, by, o[1]);
+            o[2] = __builtin_fmaf(v.z, by, o[2]);
+            o[3] = __builtin_fmaf(v.w, by, o[3]);
+        }
+    }
+    const float by = any ? 1.0f / sum : 0.0f;
+    if (e < C.D)
+        *reinterpret_cast<u32x2 *>(A.out.p + t * A.out.ts + (row - (int64_t)t * Hq) * A.out.hs + e) =
+            u32x2{pack_bf16(o[0] * by, o[1] * by), pack_bf16(o[2] * by, o[3] * by)};
+}
+
+// ------------------------------------------------------------------- host --
+
+// Blocks of 32 rows of a workgroup, workgroups a sequence and head takes for its
+// rows, shares of its keys.
+struct CachedPlan {
+    int RB, blocks, splits;
+};
+
+inline CachedPlan cached_plan(int64_t B, int64_t Hk, int64_t G, int64_t max_new, int64_t keys)
+{
+    CachedPlan P;
+    const int64_t rows = max_new * G;
+    P.RB = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
+    P.blocks = (int)((rows + 32 * P.RB - 1) / (32 * P.RB));
+    const int64_t groups = std::max<int64_t>(B * Hk * P.blocks, 1), want = P.RB == 8 ? 512 : 1024;
+    // at least four tiles of 32 keys for each wave of a share
+    const int64_t most = std::max<int64_t>(keys / (P.RB == 1 ? 512 : 256), 1);
+    P.splits = (int)std::min<int64_t>(std::min<int64_t>((want + groups - 1) / groups, most), 128);
+    return P;
+}
+
+template <int DB, bool MX> void launch_cached(const CachedArgs &A, int RB, unsigned grid, hipStream_t st)
+{
+    switch (RB) {
+    case 1: hipLaunchKernelGGL((cached_kernel<DB, 1, MX>), dim3(grid), dim3(256), 0, st, A); break;
+    case 2: hipLaunchKernelGGL((cached_kernel<DB, 2, MX>), dim3(grid), dim3(256), 0, st, A); break;
+    case 4: hipLaunchKernelGGL((cached_kernel<DB, 4, MX>), dim3(grid), dim3(256), 0, st, A); break;
+    default: hipLaunchKernelGGL((cached_kernel<DB, 8, MX>), dim3(grid), dim3(512), 0, st, A); break;
+    }
+}
+
+} // namespace mxa
+
+namespace {
+
+using mxk::aligned;
+using mxk::check_heads;
+using mxk::fail;
+using mxk::launched;
+
+mx_status check_cache(const mx_kv_cache *c, int64_t D, const int32_t *table, int64_t width, const int32_t *length,
+                      const int32_t *start, int64_t T, int64_t sequences)
+{
+    if (!c || c->heads < 1 || c->pages < 0 || width < 0 || T < 0 || sequences < 0)
+        return fail(MX_EINVAL, "the cache must be given, with a head at least; sizes must be >= 0");
+    if (c->type != MX_CACHE_BF16 && c->type != MX_CACHE_E4M3)
+        return fail(MX_EINVAL, "the cache's type must be MX_CACHE_BF16 or MX_CACHE_E4M3");
+    const bool mx = c->type == MX_CACHE_E4M3;
+    const int64_t step = mx ? 32 : 8;
+    if (D <= 0 || D % step != 0)
+        return fail(MX_EINVAL, "D must be a positive multiple of %d", (int)step);
+    if (D > MX_ATTN_MAX_D || c->heads > 4096 || sequences > 1 << 20 || T > MX_ATTN_MAX_TOKENS || c->pages > 0x7FFFFFFF)
+        return fail(MX_EUNSUPPORTED, "at most %d elements a head, 4096 heads, 2^20 sequences, %d tokens, 2^31 pages",
+                    MX_ATTN_MAX_D, MX_ATTN_MAX_TOKENS);
+    if (c->page_size < 16 || (c->page_size & (c->page_size - 1)) != 0)
+        return fail(MX_EINVAL, "page_size must be a power of two from 16 on");
+    if (c->page_size > MX_ATTN_MAX_TOKENS || width > MX_ATTN_MAX_TOKENS / c->page_size)
+        return fail(MX_EUNSUPPORTED, "a sequence's pages hold more than %d tokens", MX_ATTN_MAX_TOKENS);
+    const int64_t page = c->heads * c->page_size * D;
+    if (c->pages > 1 && (c->page_stride < page || c->page_stride % (mx ? 16 : 8) != 0 || c->page_stride > INT64_MAX / 8 / c->pages))
+        return fail(MX_EINVAL, "page_stride must be at least heads page_size D elements, whole 16-byte pieces");
+    if (mx && c->pages > 1 && (c->scale_page_stride < page / 32 || c->scale_page_stride > INT64_MAX / 8 / c->pages))
+        return fail(MX_EINVAL, "scale_page_stride must be at least heads page_size D / 32");
+    if (T == 0 || sequences == 0)
+        return MX_OK;
+    if (c->pages > 0 && (!c->k || !c->v || !aligned(c->k, 16) || !aligned(c->v, 16) || (mx && (!c->k_scales || !c->v_scales))))
+        return fail(MX_EINVAL, "the cache's k and v must be non-NULL and 16-byte aligned, its scales given for codes");
+    if ((width > 0 && !table) || !aligned(table, 4) || !length || !aligned(length, 4) || !aligned(start, 4))
+        return fail(MX_EINVAL, "table and length must be non-NULL; table, length and start 4-byte aligned");
+    if (!start && T != sequences)
+        return fail(MX_EINVAL, "without start every sequence has one new token");
+    return MX_OK;
+}
+
+mxa::Cache cache_of(const mx_kv_cache *c, int64_t D, const int32_t *table, int64_t width, const int32_t *length,
+                    int64_t sequences)
+{
+    mxa::Cache C{};
+    C.k = static_cast<uint8_t *>(c->k);
+    C.v = static_cast<uint8_t *>(c->v);
+    C.ks = c->k_scales;
+    C.vs = c->v_scales;
+    C.page_bytes = c->pages > 1 ? c->page_stride * (c->type == MX_CACHE_E4M3 ? 1 : 2) : 0;
+    C.page_scales = c->pages > 1 ? c->scale_page_stride : 0;
+    C.pages = (int)c->pages;
+    C.shift = __builtin_ctzll((uint64_t)c->page_size);
+    C.table = table;
+    C.length = length;
+    C.width = (int)width;
+    C.B = (int)sequences;
+    C.Hk = (int)c->heads;
+    C.D = (int)D;
+    return C;
+}
+
+// Keys that a token can see at most.
+int64_t keys_of(int64_t width, int64_t page_size, int64_t max_new, int64_t max_length, int64_t window, int64_t sinks)
+{
+    int64_t n = width * page_size;
+    if (max_length > 0)
+        n = std::min(n, max_length + max_new);
+    if (window > 0)
+        n = std::min(n, window + max_new + sinks);
+    return n;
+}
+
+} // namespace
+
+extern "C" {
+
+mx_status kv_cache_append(const mx_kv_cache *cache, const mx_heads *k, const mx_heads *v, int64_t T, int64_t S, int64_t D,
+                          const int32_t *table, int64_t table_width, const int32_t *length, const int32_t *start,
+                          int64_t sequences, const int32_t *rows, hipStream_t stream)
+{
+    mxk::clear_error();
+    mx_status st = check_cache(cache, D, table, table_width, length, start, T, sequences);
+    if (st != MX_OK)
+        return st;
+    if (S < 0 || S > MX_ATTN_MAX_TOKENS || (!rows && S < T) || !aligned(rows, 4))
+        return fail(MX_EINVAL, "k and v must have a row for every new token, or rows (4-byte aligned) name theirs");
+    if ((st = check_heads(k, "k", S, D, cache->heads, false)) != MX_OK ||
+        (st = check_heads(v, "v", S, D, cache->heads, false)) != MX_OK)
+        return st;
+    if (T == 0 || S == 0 || sequences == 0 || cache->pages == 0)
+        return MX_OK;
+    mxa::AppendArgs A{};
+    A.C = cache_of(cache, D, table, table_width, length, sequences);
+    A.k = {static_cast<const uint16_t *>(k->data), k->token_stride, k->head_stride};
+    A.v = {static_cast<const uint16_t *>(v->data), v->token_stride, v->head_stride};
+    A.start = start;
+    A.rows = rows;
+    A.T = (int)T;
+    A.S = (int)S;
+    const int64_t per = cache->heads * D / 8;
+    A.tpw = (int)std::min<int64_t>(std::max<int64_t>(mxa::APPEND_THREADS / per, 1), mxa::APPEND_TOKENS);
+    const dim3 grid((unsigned)((T + A.tpw - 1) / A.tpw));
+    if (cache->type == MX_CACHE_E4M3)
+        hipLaunchKernelGGL((mxa::append_kernel<true>), grid, dim3(mxa::APPEND_THREADS), 0, stream, A);
+    else
+        hipLaunchKernelGGL((mxa::append_kernel<false>), grid, dim3(mxa::APPEND_THREADS), 0, stream, A);
+    return launched();
+}
+
+size_t kv_cache_attn_fwd_workspace_bytes(int64_t T, int64_t q_heads, int64_t k_heads, int64_t D, int64_t sequences,
+                                         int64_t page_size, int64_t table_width, int64_t max_new, int64_t max_length,
+                                         int64_t window, int64_t sinks)
+{
+    if (T <= 0 || T > MX_ATTN_MAX_TOKENS || k_heads < 1 || q_heads < k_heads || q_heads > 4096 || D < 1 || D > MX_ATTN_MAX_D ||
+        sequences < 1 || sequences > 1 << 20 || page_size < 1 || table_width < 0 ||
+        table_width > MX_ATTN_MAX_TOKENS / page_size || max_new < 1 || max_new > MX_ATTN_MAX_NEW || max_length < 0 ||
+        max_length > MX_ATTN_MAX_TOKENS || window < 0 || sinks < 0)
+        return 0;
+    const mxa::CachedPlan P = mxa::cached_plan(sequences, k_heads, q_heads / k_heads, max_new,
+                                               keys_of(table_width, page_size, max_new, max_length, window, sinks));
+    return P.splits == 1 ? 0 : (size_t)T * q_heads * P.splits * (D + 2) * sizeof(float);
+}
+
+mx_status kv_cache_attn_fwd(const mx_kv_cache *cache, const mx_heads *q, int64_t T, int64_t D, const int32_t *table,
+                            int64_t table_width, const int32_t *length, const int32_t *start, int64_t sequences,
+                            int64_t max_new, int64_t max_length, const int64_t *ancestors, int64_t window, int64_t sinks,
+                            float scale, const mx_heads *out, void *workspace, size_t workspace_bytes, hipStream_t stream)
+{
+    mxk::clear_error();
+    mx_status st = check_cache(cache, D, table, table_width, length, start, T, sequences);
+    if (st != MX_OK)
+        return st;
+    if (!q || q->heads < 1 || q->heads % cache->heads != 0)
+        return fail(MX_EINVAL, "q must be given, its heads a multiple of the cache's");
+    if (q->heads > 4096)
+        return fail(MX_EUNSUPPORTED, "at most 4096 heads");
+    if ((st = check_heads(q, "q", T, D, q->heads, false)) != MX_OK ||
+        (st = check_heads(out, "out", T, D, q->heads, true)) != MX_OK)
+        return st;
+    if (max_new < 1 || max_length < 0 || window < 0 || sinks < 0)
+        return fail(MX_EINVAL, "max_new must be >= 1; max_length, window and sinks >= 0");
+    if (max_new > MX_ATTN_MAX_NEW || max_length > MX_ATTN_MAX_TOKENS)
+        return fail(MX_EUNSUPPORTED, "at most %d new tokens a sequence, and %d cached", MX_ATTN_MAX_NEW, MX_ATTN_MAX_TOKENS);
+    if (!(scale >= 0x1p-100f && scale <= 0x1p100f))
+        return fail(MX_EINVAL, "scale must be from 2^-100 to 2^100");
+    if (!aligned(ancestors, 8))
+        return fail(MX_EINVAL, "ancestors must be 8-byte aligned");
+    if (T == 0 || sequences == 0)
+        return MX_OK;
+    const int64_t Hk = cache->heads, G = q->heads / Hk;
+    const mxa::CachedPlan P = mxa::cached_plan(
+        sequences, Hk, G, max_new, keys_of(table_width, cache->page_size, max_new, max_length, window, sinks));
+    const int64_t grid = (int64_t)P.splits * Hk * P.blocks * sequences, rows = T * q->heads;
+    if (grid > 0x7FFFFFFF || rows > (int64_t)1 << 32)
+        return fail(MX_EUNSUPPORTED, "too many sequences times heads");
+    const size_t need = P.splits == 1 ? 0 : (size_t)rows * P.splits * (D + 2) * sizeof(float);
+    if (need && (!workspace || !aligned(workspace, 256) || workspace_bytes < need))
+        return fail(MX_EINVAL, "a 256-byte aligned workspace of %zu bytes is needed", need);
+    mxa::CachedArgs A{};
+    A.C = cache_of(cache, D, table, table_width, length, sequences);
+    A.q = {static_cast<const uint16_t *>(q->data), q->token_stride, q->head_stride};
+    A.out = {static_cast<uint16_t *>(out->data), out->token_stride, out->head_stride};
+    A.start = start;
+    A.bits = ancestors;
+    A.part = static_cast<float *>(workspace);
+    A.stat = reinterpret_cast<float2 *>(A.part + rows * P.splits * D);
+    A.T = (int)T;
+    A.G = (int)G;
+    A.max_new = (int)max_new;
+    A.blocks = P.blocks;
+    A.splits = P.splits;
+    A.window = window == 0 || window > MX_ATTN_MAX_TOKENS ? MX_ATTN_MAX_TOKENS * 2 : (int)window;
+    A.sinks = (int)std::min<int64_t>(sinks, MX_ATTN_MAX_TOKENS);
+    A.c = scale * mxa::LOG2E;
+    const int DB = D <= 64 ? 2 : D <= 96 ? 3 : 4;
+    if (cache->type == MX_CACHE_E4M3) {
+        switch (DB) {
+        case 2: mxa::launch_cached<2, true>(A, P.RB, (unsigned)grid, stream); break;
+        case 3: mxa::launch_cached<3, true>(A, P.RB, (unsigned)grid, stream); break;
+        default: mxa::launch_cached<4, true>(A, P.RB, (unsigned)grid, stream); break;
+        }
+    } else {
+        switch (DB) {
+        case 2: mxa::launch_cached<2, false>(A, P.RB, (unsigned)grid, stream); break;
+        case 3: mxa::launch_cached<3, false>(A, P.RB, (unsigned)grid, stream); break;
+        default: mxa::launch_cached<4, false>(A, P.RB, (unsigned)grid, stream); break;
+        }
+    }
+    if (P.splits > 1)
+        hipLaunchKernelGGL(mxa::join_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, A);
+    return launched();
+}
+
+} // extern "C"

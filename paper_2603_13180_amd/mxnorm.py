@@ -85,6 +85,10 @@ def load():
         "window_attn_bwd_workspace_bytes": (ctypes.c_size_t, [I64, I64, I64, I64, I64, I64]),
         "window_attn_bwd": (I, [P, P, P, P, P, P, I64, I64, I64, P, P, I64, I64, I64, F, P, P, P, P,
                                 ctypes.c_size_t, P]),
+        "kv_cache_append": (I, [P, P, P, I64, I64, I64, P, I64, P, P, I64, P, P]),
+        "kv_cache_attn_fwd_workspace_bytes": (ctypes.c_size_t, [I64] * 11),
+        "kv_cache_attn_fwd": (I, [P, P, I64, I64, P, I64, P, P, I64, I64, I64, P, I64, I64, F, P, P,
+                                  ctypes.c_size_t, P]),
         "mxnorm_default_global_scale": (F, [I64, I, I, F]),
         "rmsnorm_default_global_scale": (F, [I64, F]),
         "mxnorm_coef": (F, [I, I]),
@@ -776,6 +780,106 @@ def window_attn_bwd(grad_out, q, k, v, out, lse, window=0, sinks=0, scale=None, 
     _call(lib.window_attn_bwd, device, ref(dg), ref(dq), ref(dk), ref(dv), ref(do), _ptr(lse), T, S, D,
           _ptr(q_start), _ptr(k_start), B, window, sinks, scale, ref(gq), ref(gk), ref(gv), _ptr(ws), ws_bytes)
     return grad_q, grad_k, grad_v
+
+
+class _Cache(ctypes.Structure):
+    """mx_kv_cache of include/mxnorm.h."""
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("k", "v", "k_scales", "v_scales")]
+                + [(n, ctypes.c_int64) for n in ("pages", "page_size", "heads", "page_stride", "scale_page_stride")]
+                + [("type", ctypes.c_int)])
+
+
+def _paged(t, name, dtype, shape, device):
+    """The page stride of pages whose slots are contiguous."""
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t[:1].is_contiguous():
+        raise ValueError("%s must be %s %s on q's device, every page contiguous" % (name, dtype, list(shape)))
+    return t.stride(0)
+
+
+def _cache(k_cache, v_cache, k_scales, v_scales, table, length, start, T, D, device):
+    """(mx_kv_cache, table width, sequences) of a call."""
+    if k_cache.dim() != 4 or k_cache.dtype not in (torch.bfloat16, torch.uint8):
+        raise TypeError("k_cache must be [pages, heads, slots, D], torch.bfloat16, or torch.uint8 for E4M3 codes")
+    if not k_cache.is_cuda:
+        raise RuntimeError("k_cache must be on the GPU: libmxnorm has no CPU path")
+    shape = k_cache.shape
+    pages, heads, slots, Dc = shape
+    stride = _paged(k_cache, "k_cache", k_cache.dtype, shape, device)
+    if Dc != D or _paged(v_cache, "v_cache", k_cache.dtype, shape, device) != stride:
+        raise ValueError("k_cache and v_cache must have the head size of the call and the same pages")
+    mx, scale_stride = k_cache.dtype == torch.uint8, 0
+    if mx != (k_scales is not None) or mx != (v_scales is not None):
+        raise ValueError("k_scales and v_scales belong to E4M3 codes")
+    if mx:
+        scales = (pages, heads, slots, D // 32)
+        scale_stride = _paged(k_scales, "k_scales", torch.uint8, scales, device)
+        if _paged(v_scales, "v_scales", torch.uint8, scales, device) != scale_stride:
+            raise ValueError("k_scales and v_scales must have the same pages")
+    if table.dim() != 2 or table.dtype != torch.int32 or table.device != device or not table.is_contiguous():
+        raise ValueError("table must be a contiguous int32 [sequences, pages] tensor on q's device")
+    B, width = table.shape
+    _starts(length, "length", device, B)
+    _starts(start, "start", device, B + 1)
+    if start is None and T != B:
+        raise ValueError("without start every sequence has one new token")
+    return _Cache(k_cache.data_ptr(), v_cache.data_ptr(), _ptr(k_scales), _ptr(v_scales), pages, slots, heads, stride,
+                  scale_stride, int(mx)), width, B
+
+
+def kv_cache_append(k, v, k_cache, v_cache, table, length, start=None, rows=None, k_scales=None, v_scales=None):
+    """New tokens' keys and values k, v [S, heads, D] into a paged cache, in place.
+
+    k_cache, v_cache [pages, heads, slots, D]: bf16, or uint8 E4M3 codes with
+    k_scales, v_scales uint8 [pages, heads, slots, D / 32] (E8M0).  Sequence b's
+    new tokens start[b] .. start[b + 1] - 1 (int32 [sequences + 1]; None: one a
+    sequence) go to places length[b] + i, in pages table[b] (int32 [sequences, n];
+    a page that the cache does not have is skipped).  rows int32 or None: the row
+    of k and v of every new token.  Returns (k_cache, v_cache), with scales
+    (k_cache, k_scales, v_cache, v_scales)."""
+    dk, dv = _heads(k, "k"), _heads(v, "v", k)
+    S, heads, D = k.shape
+    device = k.device
+    _starts(rows, "rows", device)
+    T = S if rows is None else rows.shape[0]
+    if start is None and rows is None:
+        T = table.shape[0]
+    cache, width, B = _cache(k_cache, v_cache, k_scales, v_scales, table, length, start, T, D, device)
+    ref = ctypes.byref
+    _call(load().kv_cache_append, device, ref(cache), ref(dk), ref(dv), T, S, D, _ptr(table), width, _ptr(length),
+          _ptr(start), B, _ptr(rows))
+    return (k_cache, v_cache) if k_scales is None else (k_cache, k_scales, v_cache, v_scales)
+
+
+def kv_cache_attn_fwd(q, k_cache, v_cache, table, length, start=None, max_new=None, ancestors=None, window=0, sinks=0,
+                      scale=None, max_length=0, k_scales=None, v_scales=None, out=None):
+    """Attention of new tokens q [T, Hq, D] over the cache that kv_cache_append
+    has written them to (its arguments; length does not count them).
+
+    start None: one new token a sequence; else max_new bounds their number (None:
+    64, the most).  ancestors int64 [T] or None: bit u of a token's says that it
+    sees drafted token u of its sequence (its own bit included); None: those up to
+    itself.  window, sinks and scale as in window_attn_fwd, places counted along a
+    token's own branch.  max_length: a bound of length, if the caller knows one (0:
+    the table's room).  Returns out [T, Hq, D]."""
+    dq = _heads(q, "q")
+    T, Hq, D = q.shape
+    device = q.device
+    cache, width, B = _cache(k_cache, v_cache, k_scales, v_scales, table, length, start, T, D, device)
+    if ancestors is not None and (ancestors.dtype != torch.int64 or ancestors.shape != (T,) or ancestors.device != device
+                                  or not ancestors.is_contiguous()):
+        raise ValueError("ancestors must be a contiguous int64 [T] tensor on q's device")
+    if max_new is None:
+        max_new = 1 if start is None else 64
+    out, do = _new_heads(q) if out is None else (out, _heads(out, "out", q))
+    lib = load()
+    ws_bytes = lib.kv_cache_attn_fwd_workspace_bytes(T, Hq, cache.heads, D, B, cache.page_size, width, max_new, max_length,
+                                                     window, sinks)
+    ws = q.new_empty((ws_bytes,), dtype=torch.uint8) if ws_bytes else None
+    ref = ctypes.byref
+    _call(lib.kv_cache_attn_fwd, device, ref(cache), ref(dq), T, D, _ptr(table), width, _ptr(length), _ptr(start), B,
+          max_new, max_length, _ptr(ancestors), window, sinks, D ** -0.5 if scale is None else scale, ref(do), _ptr(ws),
+          ws_bytes)
+    return out
 
 
 def mxnorm_default_global_scale(d, block=16, p=2, coef=0.0):

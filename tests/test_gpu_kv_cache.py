@@ -1,0 +1,390 @@
+"""The paged cache of keys and values, and attention of new tokens over it, on the
+GPU against a plain implementation in 64 bits (attn_reference.py)."""
+import pytest
+import torch
+
+from attn_reference import HALF, Attention, off
+from paper_2603_13180_amd import mxnorm
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        raise RuntimeError("these tests need a GPU (run them with -m gpu on an MI355X)")
+    mxnorm.load()
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def decode(codes, scales):
+    """float64 values of E4M3 codes and E8M0 scales."""
+    x = codes.view(torch.float8_e4m3fn).double().unflatten(-1, (-1, 32))
+    s = torch.where(scales == 255, torch.nan, torch.ldexp(torch.ones((), dtype=torch.float64, device=DEV), scales.int() - 127))
+    return (x * s[..., None]).flatten(-2)
+
+
+class Case:
+    """Sequences with `cached` and `new` tokens; a cache with every new token in it,
+    NaN in all slots that no token has."""
+
+    def __init__(self, cached, new, Hq, Hk, D, page=16, mx=False, seed=0, tree=False, tail=0, slack=1):
+        g = torch.Generator().manual_seed(seed + 31 * sum(cached) + 7 * sum(new) + D)
+        self.cached, self.new, self.page, self.mx = cached, new, page, mx
+        self.Hq, self.Hk, self.D = Hq, Hk, D
+        self.st = [sum(new[:i]) for i in range(len(new) + 1)]
+        self.T = self.st[-1] + tail
+        need = [-(-(a + b) // page) for a, b in zip(cached, new)]
+        self.pages = sum(need) + 2
+        order = torch.randperm(self.pages, generator=g).tolist()
+        table = torch.full((len(new), max(need + [0]) + slack), -1, dtype=torch.int32)
+        for b, n in enumerate(need):
+            for i in range(n):
+                table[b, i] = order.pop()
+        self.table = table.to(DEV)
+        shape = (self.pages, Hk, page, D)
+        # halves of one buffer
+        self.buf = torch.full((self.pages, 2, Hk, page, D), torch.nan, dtype=torch.bfloat16, device=DEV)
+        self.scales = [None, None]
+        self.kc, self.vc = self.buf[:, 0], self.buf[:, 1]
+        if mx:
+            self.buf = torch.full((self.pages, 2, Hk, page, D), 0x7F, dtype=torch.uint8, device=DEV)
+            self.kc, self.vc = self.buf[:, 0], self.buf[:, 1]
+            self.scales = [torch.full((self.pages, Hk, page, D // 32), 255, dtype=torch.uint8, device=DEV) for _ in range(2)]
+        assert self.kc.shape == shape
+        self.length, self.start = i32(cached), i32(self.st)
+        self.q = torch.randn(self.T, Hq, D, generator=g).bfloat16().to(DEV)
+        # all tokens of a sequence, by the append under test from nothing
+        whole = [a + b for a, b in zip(cached, new)]
+        self.k, self.v = [(torch.randn(sum(whole), Hk, D, generator=g) * 1.5).bfloat16().to(DEV) for _ in range(2)]
+        self.append(self.k, self.v, torch.zeros_like(self.length), i32([sum(whole[:i]) for i in range(len(whole) + 1)]))
+        self.bits = None
+        if tree:
+            bits = []
+            for n in new:
+                mine = []
+                for i in range(n):
+                    parent = int(torch.randint(-1, i, (1,), generator=g)) if i else -1
+                    mine.append((1 << i) | (mine[parent] if parent >= 0 else 0))
+                bits += mine
+            bits = [b - (1 << 64) if b >> 63 else b for b in bits] + [0] * tail
+            self.bits = torch.tensor(bits, dtype=torch.int64, device=DEV)
+
+    def kw(self):
+        return dict(k_scales=self.scales[0], v_scales=self.scales[1])
+
+    def append(self, k, v, length, start, rows=None):
+        return mxnorm.kv_cache_append(k, v, self.kc, self.vc, self.table, length, start=start, rows=rows, **self.kw())
+
+    def run(self, window=0, sinks=0, **kw):
+        args = dict(start=self.start, max_new=max(self.new + [1]), ancestors=self.bits, window=window, sinks=sinks)
+        return mxnorm.kv_cache_attn_fwd(self.q, self.kc, self.vc, self.table, self.length, **self.kw(), **{**args, **kw})
+
+    def keys(self, b, codes, scales):
+        """float64 [keys, heads, D] of sequence b, and whether its page is there."""
+        j = torch.arange(self.cached[b] + self.new[b], device=DEV)
+        i = j // self.page
+        page = torch.where(i < self.table.shape[1], self.table[b].long()[i.clamp(max=self.table.shape[1] - 1)], -1)
+        there = (page >= 0) & (page < self.pages)
+        at = page.clamp(0, self.pages - 1)
+        x = codes[at, :, j % self.page]
+        return (x.double() if scales is None else decode(x, scales[at, :, j % self.page])), there
+
+    def want(self, window=0, sinks=0, scale=None):
+        o = torch.zeros(self.T, self.Hq, self.D, dtype=torch.float64, device=DEV)
+        bound = torch.ones_like(o)
+        scale = self.D ** -0.5 if scale is None else scale
+        for b, (c, n) in enumerate(zip(self.cached, self.new)):
+            (k, there), (v, _) = self.keys(b, self.kc, self.scales[0]), self.keys(b, self.vc, self.scales[1])
+            drafted = torch.ones(n, n, dtype=torch.bool, device=DEV).tril()
+            if self.bits is not None:
+                drafted = self.bits[self.st[b]:self.st[b + 1], None] >> torch.arange(n, device=DEV) & 1 == 1
+            place = c - 1 + drafted.sum(1)
+            at = torch.cat((torch.arange(c, device=DEV), place))
+            see = torch.cat((torch.ones(n, c, dtype=torch.bool, device=DEV), drafted), 1) & there
+            if window:
+                see = see & ((place[:, None] - at < window) | (at < sinks))
+            unseen = ~see.any(0)
+            k, v = [t.masked_fill(unseen[:, None, None], 0) for t in (k, v)]
+            for h in range(self.Hq):
+                x = Attention(self.q[self.st[b]:self.st[b + 1], h].double(), k[:, h * self.Hk // self.Hq],
+                              v[:, h * self.Hk // self.Hq], see, scale)
+                o[self.st[b]:self.st[b + 1], h], bound[self.st[b]:self.st[b + 1], h] = x.o, x.o_bound
+        return o, bound
+
+
+def check(c, window=0, sinks=0, **kw):
+    want, bound = c.want(window, sinks, kw.get("scale"))
+    o = c.run(window, sinks, **kw)
+    n = c.st[-1]
+    worst = off(o[:n], want[:n], bound[:n])
+    assert worst <= 1, worst
+    return o
+
+
+@pytest.mark.parametrize("mx", [False, True])
+@pytest.mark.parametrize("Hk,D,page", [(2, 64, 16), (8, 128, 64), (1, 96, 32), (3, 32, 16)])
+def test_append(mx, Hk, D, page):
+    c = Case([0, 5, 40, 100], [3, 0, 70, 1], 4 * Hk, Hk, D, page, mx)
+    kept = c.kc.clone(), c.vc.clone()
+    S = 200
+    qkv = torch.randn(S, 3 * Hk, D, device=DEV).bfloat16()
+    qkv[7, Hk, 3] = torch.inf
+    qkv[9, 2 * Hk, 1] = torch.nan
+    k, v = qkv[:, Hk:2 * Hk], qkv[:, 2 * Hk:]
+    rows = torch.randperm(S, device=DEV)[:c.T].to(torch.int32)
+    rows[0], rows[1], rows[2] = 7, 9, S  # the last is none
+    got = c.append(k, v, c.length, c.start, rows)
+    assert got[0] is c.kc
+    want = [kept[0], kept[1]]
+    scales = [None, None] if not mx else [s.clone() for s in c.scales]
+    for which, x in ((0, k), (1, v)):
+        for t in range(c.T):
+            b = next(b for b in range(4) if c.st[b] <= t < c.st[b + 1])
+            place = c.cached[b] + t - c.st[b]
+            at, slot = int(c.table[b, place // page]), place % page
+            if t == 2:
+                continue
+            row = x[rows[t].long()]
+            if mx:
+                codes, sc = mxnorm.mx_cast_fwd(row.contiguous())
+                want[which][at, :, slot], scales[which][at, :, slot] = codes, sc
+            else:
+                want[which][at, :, slot] = row
+    for a, b in zip((c.kc, c.vc), want):
+        assert torch.equal(a.view(torch.uint8), b.contiguous().view(torch.uint8))
+    if mx:
+        assert all(torch.equal(a, b) for a, b in zip(c.scales, scales))
+
+
+def test_append_skips_pages_that_are_not_there():
+    c = Case([0, 0], [40, 20], 2, 1, 64)
+    before = c.buf.clone()
+    c.table[0, 1], c.table[1, 0] = c.pages, -1
+    k = torch.full((60, 1, 64), 2.0, dtype=torch.bfloat16, device=DEV)
+    c.append(k, k, c.length, c.start)
+    pages = [int(c.table[0, 0]), int(c.table[0, 2]), int(c.table[1, 1])]
+    rest = [p for p in range(c.pages) if p not in pages]
+    assert torch.equal(c.buf[rest].view(torch.int16), before[rest].view(torch.int16))
+    assert (c.kc[pages[0]] == 2).all() and (c.vc[pages[1], :, :8] == 2).all() and (c.kc[pages[2], :, :4] == 2).all()
+    # past the table, and a negative length past its start
+    c.append(k, k, i32([1 << 20, 0]), c.start)
+    assert torch.equal(c.buf[rest].view(torch.int16), before[rest].view(torch.int16))
+
+
+def test_append_many_sequences():
+    # more starts than the kernel keeps near
+    n = 1500
+    c = Case([17] * n, [1] * n, 1, 1, 64)
+    k = torch.randn(n, 1, 64, device=DEV).bfloat16()
+    c.append(k, k, c.length, c.start)
+    page = c.table[:, 1].long()
+    assert torch.equal(c.kc[page, 0, 1], k[:, 0]) and torch.equal(c.vc[page, 0, 1], k[:, 0])
+    c.append(-k, k, c.length + 1, None)
+    assert torch.equal(c.kc[page, 0, 2], -k[:, 0]) and torch.equal(c.kc[page, 0, 1], k[:, 0])
+
+
+SHAPES = [(4, 2, 128), (3, 1, 64), (2, 2, 96), (8, 1, 80), (12, 3, 32), (32, 1, 128), (5, 5, 40)]
+
+
+@pytest.mark.parametrize("Hq,Hk,D", SHAPES)
+@pytest.mark.parametrize("mx", [False, True])
+def test_one_token(Hq, Hk, D, mx):
+    if mx and D % 32:
+        pytest.skip("codes come in blocks of 32")
+    c = Case([0, 1, 15, 16, 33, 500, 2000], [1] * 7, Hq, Hk, D, mx=mx)
+    check(c)
+    check(c, window=20, sinks=3)
+    check(c, start=None)
+
+
+@pytest.mark.parametrize("mx", [False, True])
+@pytest.mark.parametrize("new", [[64, 1, 0, 17], [3, 2, 3, 1], [33, 31, 5, 9]])
+@pytest.mark.parametrize("Hq,Hk", [(4, 4), (4, 2), (8, 1)])
+def test_chains_and_trees(new, mx, Hq, Hk):
+    for tree in (False, True):
+        c = Case([0, 700, 30, 129], new, Hq, Hk, 64, mx=mx, tree=tree)
+        check(c)
+        check(c, window=40, sinks=5)
+        check(c, window=2, sinks=700)
+
+
+@pytest.mark.parametrize("page", [16, 32, 256, 4096])
+@pytest.mark.parametrize("splits", [False, True])
+def test_pages(page, splits):
+    # with max_length 1 the keys are not shared out
+    c = Case([5000, 4097, 31], [1, 2, 3], 8, 2, 128, page=page)
+    check(c, max_length=0 if splits else 1)
+
+
+def test_any_mask_bits():
+    # masks that name later tokens, none, and tokens that the sequence does not have
+    c = Case([0, 20, 0], [5, 6, 2], 4, 2, 64, tree=True)
+    c.bits[:5] = torch.tensor([0, 1 << 4, -1, 0b10110, 1 << 40], device=DEV)
+    c.bits[5:11] = torch.tensor([0, 1 << 5, -1, 0b111000, -(1 << 63), 32], device=DEV)
+    o = check(c)
+    assert (o[0] == 0).all() and (o[4] == 0).all()
+    check(c, window=3, sinks=1)
+
+
+@pytest.mark.parametrize("mx", [False, True])
+def test_pages_that_are_not_there_are_not_seen(mx):
+    c = Case([300, 100], [4, 2], 4, 2, 64, mx=mx, tree=True)
+    c.table[0, 3], c.table[0, 7], c.table[1, 0] = -1, c.pages, 1 << 30
+    check(c)
+    c.table = c.table[:, :10].contiguous()  # the last keys have no pages
+    check(c, window=64, sinks=70)
+    c.table[:] = -1
+    assert (c.run() == 0).all()
+    c.table = c.table[:, :0].contiguous()
+    assert (c.run() == 0).all()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("new", [1, 40])
+def test_masked_keys_may_hold_anything(bad, new):
+    c = Case([200], [new], 4, 2, 64, tree=new > 1)
+    want, bound = c.want(50, 2)
+    place = 200 + (new > 1)
+    # keys behind the window but above the sinks, in its first tile and the sinks'
+    for j in list(range(2, 20)) + list(range(140, 150)):
+        c.kc[int(c.table[0, j // 16]), :, j % 16] = bad
+        c.vc[int(c.table[0, j // 16]), :, j % 16] = bad
+    assert place - 149 > 50
+    assert off(c.run(50, 2), want, bound) <= 1
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_drafted_tokens_do_not_see_each_other(new):
+    # siblings: whatever one holds, the others' rows stay; it itself is NaN
+    c = Case([37], [new], 2, 1, 64, tree=True)
+    c.bits[:] = 1 << torch.arange(new, device=DEV)
+    want, bound = c.want()
+    at = 37 + new - 1
+    c.vc[int(c.table[0, at // 16]), :, at % 16] = torch.nan
+    o = c.run()
+    if new > 1:
+        assert off(o[:-1], want[:-1], bound[:-1]) <= 1
+    assert o[-1].isnan().all()
+
+
+def test_scale_of_255_is_nan_and_of_0_the_smallest():
+    c = Case([20], [1], 1, 1, 64, mx=True)
+    page = int(c.table[0, 0])
+    c.scales[1][page, 0, 5, 1], c.scales[1][page, 0, 6, 0] = 255, 0
+    c.vc[page, 0, 5, 32:] = 0x38
+    o = c.run()
+    assert o[0, 0, 32:].isnan().all() and not o[0, 0, :32].isnan().any()
+    c.scales[1][page, 0, 5, 1] = 127
+    check(c)
+
+
+def test_rows_behind_the_last_sequence():
+    c = Case([50, 2000], [2, 1], 4, 2, 64, tail=3)
+    for kw in ({}, {"max_length": 1}):
+        out = torch.full_like(c.q, 7.0)
+        c.run(out=out, **kw)
+        assert (out[3:] == 7).all() and torch.equal(out[:3], c.run(**kw)[:3])
+
+
+def test_strided_queries_and_output():
+    c = Case([300, 3000], [2, 5], 6, 2, 96)
+    buf = torch.randn(7, 10, 96, device=DEV).bfloat16()
+    buf[:, :6] = c.q
+    out = torch.zeros(7, 8, 96, dtype=torch.bfloat16, device=DEV)
+    want = c.run()
+    c.q = buf[:, :6]
+    assert torch.equal(c.run(out=out[:, 1:7]), want) and (out[:, 0] == 0).all() and (out[:, 7] == 0).all()
+
+
+def test_far_pages():
+    # a page more than 4 GiB behind the first
+    Hk, D, far = 1, 64, (4 << 30) // 2 + 4096
+    buf = torch.zeros(2 * far, dtype=torch.bfloat16, device=DEV)
+    kc, vc = buf.as_strided((2, Hk, 16, D), (far, 16 * D, D, 1)), buf.as_strided((2, Hk, 16, D), (far, 16 * D, D, 1), 1 << 20)
+    c = Case([10], [1], 2, Hk, D)
+    table = i32([[1]])
+    mxnorm.kv_cache_append(c.k, c.v, kc, vc, table, i32([0]), start=i32([0, 11]))
+    assert torch.equal(kc[1, 0, :11], c.k[:, 0]) and torch.equal(vc[1, 0, :11], c.v[:, 0]) and (kc[0] == 0).all()
+    o = mxnorm.kv_cache_attn_fwd(c.q, kc, vc, table, i32([10]))
+    want, bound = c.want()
+    assert off(o, want, bound) <= 1
+    del buf, kc, vc
+    torch.cuda.empty_cache()
+
+
+def test_captured_and_replayed():
+    # append and attention of one step, lengths moved on between replays
+    c = Case([100, 3000], [1, 1], 8, 2, 128)
+    k, v = torch.randn(2, 2, 2, 128, device=DEV).bfloat16()
+    length, out = c.length.clone(), torch.empty_like(c.q)
+    c.append(k, v, length, None)
+    want = c.run(start=None)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.append(k, v, length, None)
+        mxnorm.kv_cache_attn_fwd(c.q, c.kc, c.vc, c.table, length, out=out)
+    for i in range(3):
+        out.fill_(float(i))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), i
+    length += 1
+    graph.replay()
+    torch.cuda.synchronize()
+    c.length, c.cached = length, [101, 3001]
+    assert torch.equal(out, c.run(start=None))
+    want, bound = c.want()
+    assert off(out, want, bound) <= 1
+
+
+def test_a_prompt_then_steps_then_a_draft():
+    """Norm and rotation, packed attention, the cache and attention over it as a
+    program runs them: token by token and drafted, the same as packed at once."""
+    g = torch.Generator(device=DEV).manual_seed(3)
+    Hq, Hk, D, prompt, steps = 8, 2, 64, [70, 33], 3
+    n = [p + steps for p in prompt]
+    qkv = torch.randn(sum(n), Hq + 2 * Hk, D, generator=g, device=DEV).bfloat16()
+    q, k, v = qkv.split([Hq, Hk, Hk], 1)
+    gain = [(1 + 0.1 * torch.randn(D, generator=g, device=DEV)).bfloat16() for _ in range(2)]
+    pos = torch.cat([torch.arange(m, device=DEV) for m in n])
+    freq = 10000.0 ** (-torch.arange(0, D, 2, device=DEV).float() / D)
+    mxnorm.qk_norm_rope_fwd(q, k, *gain, pos, freq, q_out=q, k_out=k)
+    st = [0, n[0], sum(n)]
+    kw = dict(window=24, sinks=2)
+    whole, _ = mxnorm.window_attn_fwd(q, k, v, q_start=i32(st), want_lse=False, **kw)
+    kc, vc = [torch.full((20, Hk, 16, D), torch.nan, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    table = torch.randperm(20, generator=g, device=DEV).to(torch.int32).view(2, 10)
+    rows = torch.cat([torch.arange(a, a + p, device=DEV) for a, p in zip(st, prompt)])
+    mxnorm.kv_cache_append(k, v, kc, vc, table, i32([0, 0]), start=i32([0, prompt[0], sum(prompt)]), rows=rows.to(torch.int32))
+
+    def near(got, want):
+        # two orders of the same sums of 24 to 26 terms with P and outputs rounded
+        # to bf16: each within (HALF + 2^-10) of the terms' magnitudes and HALF of itself
+        assert ((got.double() - want.double()).abs() <= 2 * (2 * HALF + 2.0 ** -10) * v.double().abs().max()).all()
+
+    for i in range(steps):  # one token at a time
+        t = torch.tensor([a + p + i for a, p in zip(st, prompt)], device=DEV)
+        length = i32([p + i for p in prompt])
+        mxnorm.kv_cache_append(k[t], v[t], kc, vc, table, length)
+        near(mxnorm.kv_cache_attn_fwd(q[t], kc, vc, table, length, **kw), whole[t])
+    # the same three as a draft of two branches: the tokens, and others before each
+    length = i32(prompt)
+    t = torch.cat([torch.tensor([a + p + i for i in range(steps)], device=DEV) for a, p in zip(st, prompt)])
+    dq, dk, dv = [torch.randn(2 * t.numel(), x.shape[1], D, generator=g, device=DEV).bfloat16() for x in (q, k, v)]
+    for x, y in ((dq, q), (dk, k), (dv, v)):
+        x[1::2] = y[t]
+    bits = torch.tensor([1, 2, 5, 10, 21, 42] * 2, device=DEV)
+    start = i32([0, 2 * steps, 4 * steps])
+    mxnorm.kv_cache_append(dk, dv, kc, vc, table, length, start=start)
+    near(mxnorm.kv_cache_attn_fwd(dq, kc, vc, table, length, start=start, max_new=2 * steps, ancestors=bits, **kw)[1::2], whole[t])
+    # those kept, one behind the other
+    mxnorm.kv_cache_append(dk, dv, kc, vc, table, length, start=i32([0, steps, 2 * steps]),
+                           rows=torch.arange(1, 4 * steps, 2, dtype=torch.int32, device=DEV))
+    last = torch.tensor([s - 1 for s in st[1:]], device=DEV)
+    near(mxnorm.kv_cache_attn_fwd(q[last], kc, vc, table, i32([m - 1 for m in n]), **kw), whole[last])
