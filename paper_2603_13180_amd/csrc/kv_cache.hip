@@ -155,36 +155,78 @@ template <int RB> struct Shape {
     static constexpr int STAGES = RB == 1 ? 1 : 2;
 };
 
+// The pages of a tile's runs of 16 keys: the same for every thread of its group.
+template <int RB> struct Pages {
+    static constexpr int RUNS = Shape<RB>::KEYS / 16;
+    int id[RUNS];
+    __device__ __forceinline__ Pages(const Rows &S, int shift, int j0)
+    {
+#pragma unroll
+        for (int y = 0; y < RUNS; ++y)
+            id[y] = __builtin_amdgcn_readfirstlane(S.page_of(j0 + 16 * y, shift));
+    }
+};
+
 // A thread's part of a tile of keys and values on its way to LDS.
 template <int DB, int RB, bool MX> struct Staged {
     using O = Shape<RB>;
     static constexpr int PER = kChunks<DB> / (MX ? 2 : 1);      // 16-byte pieces of a row
     static constexpr int PIECES = O::KEYS * PER, N = (PIECES + 64 * RB - 1) / (64 * RB);
+    static constexpr int RUNS = O::KEYS / 16;
     u32x4 k[N], v[N];
     uint32_t sk[N], sv[N]; // scale bytes
+    uint32_t there;        // bit y: run y's page is there
 
     // Keys j0 .. of the tile, those past the end and those of pages that are not
     // there as zeros.  i: the thread's number among those of its group.
-    __device__ __forceinline__ void load(const Cache &C, const Rows &S, int hk, int j0, int i)
+    __device__ __forceinline__ void load(const Cache &C, const Rows &S, const Pages<RB> &P, int hk, int j0, int i)
     {
+        const uint8_t *kb[RUNS], *vb[RUNS];
+        const uint8_t *ksb[RUNS], *vsb[RUNS];
+        there = 0;
+#pragma unroll
+        for (int y = 0; y < RUNS; ++y) {
+            const bool is = (unsigned)P.id[y] < (unsigned)C.pages;
+            there |= (uint32_t)is << y;
+            const int64_t slot = ((int64_t)hk << C.shift) + ((j0 + 16 * y) & ((1 << C.shift) - 1));
+            const int64_t at = (is ? P.id[y] : 0) * C.page_bytes + slot * C.D * (MX ? 1 : 2);
+            kb[y] = C.k + at;
+            vb[y] = C.v + at;
+            if constexpr (MX) {
+                const int64_t sc = (is ? P.id[y] : 0) * C.page_scales + slot * (C.D / 32);
+                ksb[y] = C.ks + sc;
+                vsb[y] = C.vs + sc;
+            }
+        }
 #pragma unroll
         for (int x = 0; x < N; ++x) {
-            const int p = x * 64 * RB + i, r = p / PER, c = p % PER, j = j0 + r;
+            constexpr int STEP = 64 * RB / PER; // rows that the group's threads take at once
+            const int p = x * 64 * RB + i, r = p / PER, c = p % PER;
             k[x] = v[x] = u32x4{0, 0, 0, 0};
             sk[x] = sv[x] = 127;
-            if (PIECES % (64 * RB) != 0 && p >= PIECES)
-                continue;
-            const int page = S.page_of(j, C.shift);
-            if ((unsigned)page >= (unsigned)C.pages || c * (MX ? 16 : 8) >= C.D)
-                continue;
-            const int64_t slot = ((int64_t)hk << C.shift) + (j & ((1 << C.shift) - 1));
-            const int64_t at = page * C.page_bytes + slot * C.D * (MX ? 1 : 2) + c * 16;
-            k[x] = *reinterpret_cast<const u32x4 *>(C.k + at);
-            v[x] = *reinterpret_cast<const u32x4 *>(C.v + at);
-            if constexpr (MX) {
-                const int64_t s = page * C.page_scales + slot * (C.D / 32) + c / 2;
-                sk[x] = C.ks[s];
-                sv[x] = C.vs[s];
+            int y = x * STEP / 16;
+            const uint8_t *kp = kb[y < RUNS ? y : 0], *vp = vb[y < RUNS ? y : 0], *ksp = ksb[y < RUNS ? y : 0], *vsp = vsb[y < RUNS ? y : 0];
+            if constexpr (STEP > 16) { // several runs: the thread's own
+                y = r / 16;
+#pragma unroll
+                for (int z = 0; z < RUNS; ++z) {
+                    kp = y == z ? kb[z] : kp;
+                    vp = y == z ? vb[z] : vp;
+                    if constexpr (MX) {
+                        ksp = y == z ? ksb[z] : ksp;
+                        vsp = y == z ? vsb[z] : vsp;
+                    }
+                }
+            }
+            if ((PIECES % (64 * RB) == 0 || p < PIECES) && j0 + r < S.end && (there >> y & 1) && c * (MX ? 16 : 8) < C.D) {
+                const uint32_t off = (uint32_t)((r & 15) * C.D * (MX ? 1 : 2) + c * 16);
+                k[x] = *reinterpret_cast<const u32x4 *>(kp + off);
+                v[x] = *reinterpret_cast<const u32x4 *>(vp + off);
+                if constexpr (MX) {
+                    const uint32_t soff = (uint32_t)((r & 15) * (C.D / 32) + c / 2);
+                    sk[x] = ksp[soff];
+                    sv[x] = vsp[soff];
+                }
             }
         }
     }
@@ -284,26 +326,27 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
     bool any = false;
     const int rounds = (to - from + O::KW - 1) / O::KW;
     auto tile_of = [&](int it) { return from + it * O::KW + kw; };
+    // the pages of the tile after the one in flight are on their way as well
+    const int last = max(to - 1, from);
+    Pages<RB> pages(S, C.shift, key_of(min(tile_of(0), last)));
     if (tile_of(0) < to)
-        next.load(C, S, hk, key_of(tile_of(0)), in_group);
+        next.load(C, S, pages, hk, key_of(tile_of(0)), in_group);
+    pages = Pages<RB>(S, C.shift, key_of(min(tile_of(1), last)));
     for (int it = 0; it < rounds; ++it) {
         const int t = tile_of(it);
         LDS_AS uint8_t *kt = lds + kw * GROUP + (O::STAGES == 2 ? (it & 1) * 2 * TILE : 0), *vt = kt + TILE;
+        const uint32_t there = next.there;
         if (t < to)
             next.store(kt, in_group);
         if (RB > 1)
             __syncthreads();
-        if (tile_of(it + 1) < to)
-            next.load(C, S, hk, key_of(tile_of(it + 1)), in_group);
+        if (tile_of(it + 1) < to) {
+            next.load(C, S, pages, hk, key_of(tile_of(it + 1)), in_group);
+            pages = Pages<RB>(S, C.shift, key_of(min(tile_of(it + 2), last)));
+        }
         if (t >= to || rw >= S.R)
             continue;
         const int j0 = key_of(t);
-        // pages that are not there: their keys are not seen
-        uint32_t there = 0;
-#pragma unroll
-        for (int x = 0; x < O::KEYS / 16; ++x) {
-            there |= (uint32_t)((unsigned)S.page_of(j0 + 16 * x, C.shift) < (unsigned)C.pages) << x;
-        }
         const bool full = j0 + O::KEYS <= S.len && there == (1u << O::KEYS / 16) - 1 &&
                           S.len + S.n - 1 - j0 < A.window;
         auto seen = [&](int x) { return (there >> (x >> 4) & 1) && sees(j0 + x); };
@@ -469,45 +512,68 @@ template <int DB, int RB, bool MX> __global__ void __launch_bounds__(64 * Shape<
         cached<DB, RB, MX, true>(A, lds, (const LDS_AS int *)places, S, hk, split, r0);
 }
 
-// A row's shares joined: a wave takes one row, four elements a lane at a time.
+// A row's shares joined, in order: a workgroup takes one row, groups of 32 lanes
+// every eighth share, four elements a lane.
+constexpr int MAX_SPLITS = 128;
 __global__ void __launch_bounds__(256) join_kernel(CachedArgs A)
 {
+    __shared__ float weight[MAX_SPLITS];
+    __shared__ float4 sums[8][32];
+    __shared__ float part[8];
     const Cache &C = A.C;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int Hq = A.G * C.Hk, l = threadIdx.x & 63;
+    const int64_t row = blockIdx.x;
+    const int Hq = A.G * C.Hk, l = threadIdx.x & 63, sub = threadIdx.x >> 5;
     const int64_t t = row / Hq;
     if (t < first_of(A.start, 0, A.T) || t >= first_of(A.start, C.B, A.T))
         return;
-    float m = -FLT_MAX;
-    bool any = false;
-    for (int s = l; s < A.splits; s += 64) {
-        const float2 x = A.stat[row * A.splits + s];
-        m = fmaxf(m, x.x);
-        any |= x.y != 0.0f;
-    }
+    // every wave finds the maximum by itself
+    const float2 none = {-FLT_MAX, 0.0f};
+    const float2 x0 = l < A.splits ? A.stat[row * A.splits + l] : none;
+    const float2 x1 = l + 64 < A.splits ? A.stat[row * A.splits + l + 64] : none;
+    float m = fmaxf(x0.x, x1.x);
     for (int x = 32; x; x >>= 1)
         m = fmaxf(m, __shfl_xor(m, x));
-    any = __builtin_amdgcn_ballot_w64(any) != 0;
-    float sum = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    const int e = 4 * l;
-    for (int s = 0; s < A.splits; ++s) {
-        const float2 x = A.stat[row * A.splits + s];
-        if (x.y == 0.0f || x.y == -1.0f)
+    const bool any = __builtin_amdgcn_ballot_w64(x0.y != 0.0f || x1.y != 0.0f) != 0;
+    if (threadIdx.x < 64) { // shares without a sum have no weight, and their sums are not there
+        auto w = [&](float2 x) { return x.y == 0.0f || x.y == -1.0f ? -1.0f : __builtin_amdgcn_exp2f(x.x - m); };
+        weight[l] = w(x0);
+        weight[l + 64] = w(x1);
+    }
+    __syncthreads();
+    const int e = 4 * (threadIdx.x & 31);
+    float sum = 0.0f;
+    float4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int s = sub; s < A.splits; s += 8) {
+        const float by = weight[s];
+        if (by == -1.0f)
             continue;
-        const float by = __builtin_amdgcn_exp2f(x.x - m);
-        sum = __builtin_fmaf(x.y, by, sum);
+        sum = __builtin_fmaf(A.stat[row * A.splits + s].y, by, sum);
         if (e < C.D) {
             const float4 v = *reinterpret_cast<const float4 *>(A.part + (row * A.splits + s) * C.D + e);
-            o[0] = __builtin_fmaf(v.x, by, o[0]);
-            o[1] = __builtin_fmaf(v.y, by, o[1]);
-            o[2] = __builtin_fmaf(v.z, by, o[2]);
-            o[3] = __builtin_fmaf(v.w, by, o[3]);
+            o.x = __builtin_fmaf(v.x, by, o.x);
+            o.y = __builtin_fmaf(v.y, by, o.y);
+            o.z = __builtin_fmaf(v.z, by, o.z);
+            o.w = __builtin_fmaf(v.w, by, o.w);
         }
     }
+    sums[sub][threadIdx.x & 31] = o;
+    if ((threadIdx.x & 31) == 0)
+        part[sub] = sum;
+    __syncthreads();
+    if (threadIdx.x >= 32 || e >= C.D)
+        return;
+    for (int g = 1; g < 8; ++g) {
+        const float4 v = sums[g][threadIdx.x];
+        o.x += v.x;
+        o.y += v.y;
+        o.z += v.z;
+        o.w += v.w;
+        sum += part[g];
+    }
     const float by = any ? 1.0f / sum : 0.0f;
-    if (e < C.D)
-        *reinterpret_cast<u32x2 *>(A.out.p + t * A.out.ts + (row - (int64_t)t * Hq) * A.out.hs + e) =
-            u32x2{pack_bf16(o[0] * by, o[1] * by), pack_bf16(o[2] * by, o[3] * by)};
+    *reinterpret_cast<u32x2 *>(A.out.p + t * A.out.ts + (row - t * Hq) * A.out.hs + e) =
+        u32x2{pack_bf16(o.x * by, o.y * by), pack_bf16(o.z * by, o.w * by)};
 }
 
 // ------------------------------------------------------------------- host --
@@ -527,7 +593,7 @@ inline CachedPlan cached_plan(int64_t B, int64_t Hk, int64_t G, int64_t max_new,
     const int64_t groups = std::max<int64_t>(B * Hk * P.blocks, 1), want = P.RB == 8 ? 512 : 1024;
     // at least four tiles of 32 keys for each wave of a share
     const int64_t most = std::max<int64_t>(keys / (P.RB == 1 ? 512 : 256), 1);
-    P.splits = (int)std::min<int64_t>(std::min<int64_t>((want + groups - 1) / groups, most), 128);
+    P.splits = (int)std::min<int64_t>(std::min<int64_t>((want + groups - 1) / groups, most), MAX_SPLITS);
     return P;
 }
 
@@ -697,7 +763,7 @@ mx_status kv_cache_attn_fwd(const mx_kv_cache *cache, const mx_heads *q, int64_t
     const mxa::CachedPlan P = mxa::cached_plan(
         sequences, Hk, G, max_new, keys_of(table_width, cache->page_size, max_new, max_length, window, sinks));
     const int64_t grid = (int64_t)P.splits * Hk * P.blocks * sequences, rows = T * q->heads;
-    if (grid > 0x7FFFFFFF || rows > (int64_t)1 << 32)
+    if (grid > 0x7FFFFFFF || rows > 0x7FFFFFFF)
         return fail(MX_EUNSUPPORTED, "too many sequences times heads");
     const size_t need = P.splits == 1 ? 0 : (size_t)rows * P.splits * (D + 2) * sizeof(float);
     if (need && (!workspace || !aligned(workspace, 256) || workspace_bytes < need))
@@ -733,7 +799,7 @@ mx_status kv_cache_attn_fwd(const mx_kv_cache *cache, const mx_heads *q, int64_t
         }
     }
     if (P.splits > 1)
-        hipLaunchKernelGGL(mxa::join_kernel, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, A);
+        hipLaunchKernelGGL(mxa::join_kernel, dim3((unsigned)rows), dim3(256), 0, stream, A);
     return launched();
 }
 

@@ -11,7 +11,7 @@
 namespace mxa {
 
 constexpr int BK = 64;        // keys of a tile, queries of a backward tile
-constexpr int FAR_CHUNK = 256; // queries that a wave sums for the sinks, at least
+constexpr int FAR_CHUNK = 256; // queries that a pair of waves sums for the sinks, at least
 
 struct Args {
     In q, k, v, go, o;
@@ -351,20 +351,32 @@ template <int DB> __device__ __forceinline__ float *far_part(const Args &A, int 
     return A.part + (((int64_t)at * A.Hk + hk) * blocks + kb) * (2 * DB * 16 * 64);
 }
 
-// grad_k and grad_v of 32 keys a wave, from queries i0 .. i1 of every head of the
-// group.  FAR: those that see them as sinks, not through the window.
-template <int DB, int NW, bool FAR, bool CAREFUL>
+// grad_k and grad_v of 32 keys for each of NP pairs of waves, from queries i0 .. i1
+// of every head of the group.  FAR: those that see them as sinks, not through the
+// window.
+//
+// A wave has registers for one of the two sums at two waves a SIMD.  So of a pair
+// the first wave forms the scores, P and grad_v += grad_out^T P, and the second, a
+// tile of queries later, grad_out . v, dS from the P that the first left in LDS,
+// and grad_k += Q^T dS: two products each, one a SIMD's exponentials beside the
+// other's products, one barrier a tile.  P goes over as the upper 24 bits of its
+// float, within 2^-15, so dS is rounded to bf16 from what is nearly float (P in bf16
+// would double that rounding, whole floats do not fit).
+template <int DB> constexpr int kStageKV = 2 * BK * kRow<DB> + 8 * BK;
+template <int DB, int NP> constexpr int kBytesKV = 3 * kStageKV<DB> + NP * 2 * BK * 96;
+template <int DB, int NP, bool FAR, bool CAREFUL>
 __device__ __forceinline__ bool backward_kv(const Args &A, LDS_AS uint8_t *lds, const Span &S, int j0, int i0, int i1, int hk,
                                             int b, int chunk)
 {
-    constexpr int TILE = BK * kRow<DB>, STAGE = 2 * TILE + 8 * BK;
+    constexpr int TILE = BK * kRow<DB>, STAGE = kStageKV<DB>, NW = 2 * NP;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, h = l >> 5;
+    const int pair = w % NP, second = w / NP;
     const uint32_t base = lds_address(lds);
     const Lane<DB> L(l);
     const int steps = i1 < i0 ? 0 : (i1 - i0) / BK + 1, total = steps * A.G;
-    auto load = [&](int it) {
+    auto load = [&](int it, int stage) {
         const int hq = hk * A.G + it / steps, r0 = i0 + it % steps * BK;
-        const uint32_t to = base + (it & 1) * STAGE;
+        const uint32_t to = base + stage * STAGE;
         load_tile<DB, BK, NW>(A.q.p + S.q0 * A.q.ts + hq * A.q.hs, A.q.ts, r0, i1, A.D, to, w, l);
         load_tile<DB, BK, NW>(A.go.p + S.q0 * A.go.ts + hq * A.go.hs, A.go.ts, r0, i1, A.D, to + TILE, w, l);
         const int64_t row = (int64_t)hq * A.Tq + S.q0 + min(r0 + l, i1);
@@ -374,126 +386,157 @@ __device__ __forceinline__ bool backward_kv(const Args &A, LDS_AS uint8_t *lds, 
             mxg::lds_load4(A.delta + row, to + 2 * TILE + 4 * BK);
     };
     if (total > 0)
-        load(0);
-    const int jw = j0 + 32 * w, j = jw + n;
-    b8 k[2 * DB], v[2 * DB];
-    load_rows<DB>(k, A.k.p + S.k0 * A.k.ts + hk * A.k.hs, A.k.ts, jw, S.lk - 1, A.D, l);
-    load_rows<DB>(v, A.v.p + S.k0 * A.v.ts + hk * A.v.hs, A.v.ts, jw, S.lk - 1, A.D, l);
-    f16v gk[DB], gv[DB];
+        load(0, 0);
+    const int jw = j0 + 32 * pair, j = jw + n;
+    b8 x[2 * DB];
+    const In &kv = second ? A.v : A.k;
+    load_rows<DB>(x, kv.p + S.k0 * kv.ts + hk * kv.hs, kv.ts, jw, S.lk - 1, A.D, l);
+    f16v acc[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d)
-        gk[d] = gv[d] = zero16();
+        acc[d] = zero16();
     auto sees_key = [&](int i) {
         const int back = i + S.off - j;
         return i <= i1 && (FAR ? back >= A.window && j < A.sinks : back >= 0 && back < A.window);
     };
-    for (int it = 0; it < total; ++it) {
+    LDS_AS uint8_t *ps = lds + 3 * STAGE + pair * 2 * BK * 96 + l * 16;
+    int mine = second ? 2 : 0, next = 1; // the wave's stage; the one to load next
+    for (int it = 0; it <= total; ++it) {
         wait_vmcnt<0>();
         barrier();
         if (it + 1 < total)
-            load(it + 1);
-        if (jw >= S.lk)
-            continue;
-        const int r0 = i0 + it % steps * BK;
-        const LDS_AS uint8_t *qt = lds + (it & 1) * STAGE, *gt = qt + TILE, *st = gt + TILE;
+            load(it + 1, next);
+        next = next == 2 ? 0 : next + 1;
+        const int t = it - second;
+        if (t >= 0 && t < total && jw < S.lk) {
+            const int r0 = i0 + t % steps * BK, p0 = r0 + S.off, p1 = min(r0 + BK - 1, i1) + S.off;
+            const bool none = !FAR && (p1 < jw || p0 - (jw + 31) >= A.window);
+            const bool all = !FAR && p0 >= jw + 31 && p1 - jw < A.window && r0 + BK - 1 <= i1;
+            if (!none) {
+                const LDS_AS uint8_t *qt = lds + mine * STAGE, *gt = qt + TILE;
+                const LDS_AS float *st = reinterpret_cast<const LDS_AS float *>(qt + 2 * TILE) + second * BK + 4 * h;
+                LDS_AS uint8_t *pt = ps + (t & 1) * BK * 96;
+                Scores<DB> s(second ? gt : qt, L, x);
+                if (second) { // dS: cells 0 .. 3 hold P's upper halves, 4 and 5 the bytes below
+                    u32x4 low[2];
 #pragma unroll
-        for (int qb = 0; qb < 2; ++qb) {
-            const int ib = r0 + 32 * qb, p0 = ib + S.off, p1 = p0 + 31;
-            if (ib > i1 || (!FAR && (p1 < jw || p0 - (jw + 31) >= A.window)))
-                continue;
-            const bool all = !FAR && p0 >= jw + 31 && p1 - jw < A.window && ib + 31 <= i1;
-            f16v s = zero16(), dp = zero16();
+                    for (int c = 0; c < 2; ++c)
+                        low[c] = *reinterpret_cast<const LDS_AS u32x4 *>(pt + (4 + c) * 1024);
 #pragma unroll
-            for (int ks = 0; ks < 2 * DB; ++ks) {
-                s = mfma(row_frag<DB>(qt, L, ks, qb), k[ks], s);
-                dp = mfma(row_frag<DB>(gt, L, ks, qb), v[ks], dp);
-            }
-            const LDS_AS float *sl = reinterpret_cast<const LDS_AS float *>(st) + 32 * qb + 4 * h, *sd = sl + BK;
+                    for (int c = 0; c < 4; ++c) {
+                        const u32x4 up = *reinterpret_cast<const LDS_AS u32x4 *>(pt + c * 1024);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int r = 8 * (e >> 2) + (e & 3);
-                s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], A.c, -sl[r]));
-                dp[e] = s[e] * (dp[e] - sd[r]);
-            }
-            if (!all)
+                        for (int i = 0; i < 8; ++i) {
+                            constexpr uint32_t BYTES[4] = {0x0504000Cu, 0x0706010Cu, 0x0504020Cu, 0x0706030Cu};
+                            const int e = 8 * (c & 1) + i;
+                            const float pr = __uint_as_float(
+                                __builtin_amdgcn_perm(up[i / 2], low[c >> 1][2 * (c & 1) + i / 4], BYTES[i & 3]));
+                            s.s[c >> 1][e] = pr * (s.s[c >> 1][e] - st[32 * (c >> 1) + 8 * (e >> 2) + (e & 3)]);
+                        }
+                    }
+                } else { // P
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const bool see = sees_key(ib + c_row(e, h));
-                    s[e] = see ? s[e] : 0.0f;
-                    dp[e] = see ? dp[e] : 0.0f;
+                    for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            s.s[qb][e] = __builtin_amdgcn_exp2f(
+                                __builtin_fmaf(s.s[qb][e], A.c, -st[32 * qb + 8 * (e >> 2) + (e & 3)]));
                 }
+                if (!all)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const b8 x = pack8(s, t), y = pack8(dp, t);
-                if (CAREFUL && !all) {
-                    auto see = [&](int r) { return sees_key(r0 + r); };
-                    careful_product<DB>(gv, gt, L, 2 * qb + t, x, h, see);
-                    careful_product<DB>(gk, qt, L, 2 * qb + t, y, h, see);
-                } else {
-                    product<DB>(gv, gt, L, 2 * qb + t, x);
-                    product<DB>(gk, qt, L, 2 * qb + t, y);
+                    for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            s.s[qb][e] = sees_key(r0 + 32 * qb + c_row(e, h)) ? s.s[qb][e] : 0.0f;
+                if (!second) {
+                    u32x4 low[2];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        u32x4 up;
+                        uint32_t y[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            y[i] = __float_as_uint(s.s[c >> 1][8 * (c & 1) + i]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            up[i] = __builtin_amdgcn_perm(y[2 * i + 1], y[2 * i], 0x07060302u);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            low[c >> 1][2 * (c & 1) + i] = __builtin_amdgcn_perm(y[4 * i + 1], y[4 * i], 0x0C0C0501u) |
+                                                           __builtin_amdgcn_perm(y[4 * i + 3], y[4 * i + 2], 0x05010C0Cu);
+                        *reinterpret_cast<LDS_AS u32x4 *>(pt + c * 1024) = up;
+                    }
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+                        *reinterpret_cast<LDS_AS u32x4 *>(pt + (4 + c) * 1024) = low[c];
+                }
+                const LDS_AS uint8_t *down = second ? qt : gt;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const b8 z = pack8(s.s[c >> 1], c & 1);
+                    if (CAREFUL && !all)
+                        careful_product<DB>(acc, down, L, c, z, h, [&](int r) { return sees_key(r0 + r); });
+                    else
+                        product<DB>(acc, down, L, c, z);
                 }
             }
         }
+        mine = mine == 2 ? 0 : mine + 1;
     }
-    if (!CAREFUL && __syncthreads_or(j < S.lk && (not_finite<DB>(gk) || not_finite<DB>(gv))))
+    if (!CAREFUL && __syncthreads_or(j < S.lk && not_finite<DB>(acc)))
         return false;
     if (CAREFUL)
         __syncthreads();
+    // planes of the far sums: grad_k's, grad_v's
+    const int plane = second ? 0 : DB * 16 * 64;
     if constexpr (FAR) {
-        float *to = far_part<DB>(A, chunk, hk, j0 / 32) + l;
+        float *to = far_part<DB>(A, chunk, hk, j0 / 32) + plane + l;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                to[(d * 16 + e) * 64] = gk[d][e];
-                to[((DB + d) * 16 + e) * 64] = gv[d][e];
-            }
+            for (int e = 0; e < 16; ++e)
+                to[(d * 16 + e) * 64] = acc[d][e];
         return true;
     }
     if (jw < S.lk && jw < A.sinks && max(jw + A.window - S.off, 0) < S.lq) { // add the sums that the sinks have from far queries
         const int at = S.q0 / A.chunk + b;
         for (int c = max(jw + A.window - S.off, 0) / A.chunk; c <= (S.lq - 1) / A.chunk; ++c) {
-            const float *from = far_part<DB>(A, at + c, hk, jw / 32) + l;
+            const float *from = far_part<DB>(A, at + c, hk, jw / 32) + plane + l;
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    gk[d][e] += from[(d * 16 + e) * 64];
-                    gv[d][e] += from[((DB + d) * 16 + e) * 64];
-                }
+                for (int e = 0; e < 16; ++e)
+                    acc[d][e] += from[(d * 16 + e) * 64];
         }
     }
-    LDS_AS uint8_t *mine = lds + w * 32 * kRow<DB>;
-    store_rows<DB>(gk, A.scale, mine, A.gk.p + (int64_t)(S.k0 + jw) * A.gk.ts + hk * A.gk.hs, A.gk.ts, S.lk - jw, A.D, l);
-    store_rows<DB>(gv, 1.0f, mine, A.gv.p + (int64_t)(S.k0 + jw) * A.gv.ts + hk * A.gv.hs, A.gv.ts, S.lk - jw, A.D, l);
+    const Out &to = second ? A.gk : A.gv;
+    store_rows<DB>(acc, second ? A.scale : 1.0f, lds + w * 32 * kRow<DB>,
+                   to.p + (int64_t)(S.k0 + jw) * to.ts + hk * to.hs, to.ts, S.lk - jw, A.D, l);
     return true;
 }
 
-template <int DB> constexpr int kStageKV = 2 * BK * kRow<DB> + 8 * BK;
-
-template <int DB, int NW>
-__global__ void __launch_bounds__(64 * NW) bwd_kv_kernel(Args A)
+template <int DB, int NP>
+__global__ void __launch_bounds__(128 * NP, 2) bwd_kv_kernel(Args A)
 {
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * kStageKV<DB>];
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[kBytesKV<DB, NP>];
     LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
     int rank, hk, g, b, j0;
     Span S;
     if (!item_of(blockIdx.x, A.tiles, A.Hk, 1, rank, hk, g) ||
-        !span_of(A, A.ks, A.Tk, rank, 32 * NW, true, S, b, j0))
+        !span_of(A, A.ks, A.Tk, rank, 32 * NP, true, S, b, j0))
         return;
     if (A.D != 32 * DB)
-        zero_lds<2 * kStageKV<DB>>(lds, 64 * NW);
+        zero_lds<3 * kStageKV<DB>>(lds, 128 * NP);
     const int i0 = max(j0 - S.off, 0);
-    const int i1 = min(min(j0 + 32 * NW, S.lk) - 2 + A.window - S.off, S.lq - 1);
-    if (!backward_kv<DB, NW, false, false>(A, lds, S, j0, i0, i1, hk, b, 0))
-        backward_kv<DB, NW, false, true>(A, lds, S, j0, i0, i1, hk, b, 0);
+    const int i1 = min(min(j0 + 32 * NP, S.lk) - 2 + A.window - S.off, S.lq - 1);
+    if (!backward_kv<DB, NP, false, false>(A, lds, S, j0, i0, i1, hk, b, 0))
+        backward_kv<DB, NP, false, true>(A, lds, S, j0, i0, i1, hk, b, 0);
 }
 
 template <int DB>
-__global__ void __launch_bounds__(64) bwd_far_kernel(Args A)
+__global__ void __launch_bounds__(128, 2) bwd_far_kernel(Args A)
 {
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * kStageKV<DB>];
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[kBytesKV<DB, 1>];
     LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
     int b, i0;
     Span S;
@@ -505,7 +548,7 @@ __global__ void __launch_bounds__(64) bwd_far_kernel(Args A)
     if (j0 >= S.lk || i0 > i1)
         return;
     if (A.D != 32 * DB)
-        zero_lds<2 * kStageKV<DB>>(lds, 64);
+        zero_lds<3 * kStageKV<DB>>(lds, 128);
     if (!backward_kv<DB, 1, true, false>(A, lds, S, j0, i0, i1, hk, b, blockIdx.x))
         backward_kv<DB, 1, true, true>(A, lds, S, j0, i0, i1, hk, b, blockIdx.x);
 }
@@ -695,17 +738,17 @@ mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_
         if (Tq > 0 && A.sinks > 0) {
             const dim3 grid((unsigned)mxa::tiles_of(Tq, A.chunk, sequences, packed), (unsigned)A.Hk, (unsigned)((A.sinks + 31) / 32));
             switch (DB) {
-            case 2: hipLaunchKernelGGL((mxa::bwd_far_kernel<2>), grid, dim3(64), 0, stream, A); break;
-            case 3: hipLaunchKernelGGL((mxa::bwd_far_kernel<3>), grid, dim3(64), 0, stream, A); break;
-            default: hipLaunchKernelGGL((mxa::bwd_far_kernel<4>), grid, dim3(64), 0, stream, A); break;
+            case 2: hipLaunchKernelGGL((mxa::bwd_far_kernel<2>), grid, dim3(128), 0, stream, A); break;
+            case 3: hipLaunchKernelGGL((mxa::bwd_far_kernel<3>), grid, dim3(128), 0, stream, A); break;
+            default: hipLaunchKernelGGL((mxa::bwd_far_kernel<4>), grid, dim3(128), 0, stream, A); break;
             }
         }
         A.tiles = (int)mxa::tiles_of(Tk, 128, sequences, packed);
         const dim3 grid((unsigned)mxa::items(A.tiles, A.Hk, 1));
         switch (DB) {
-        case 2: hipLaunchKernelGGL((mxa::bwd_kv_kernel<2, 4>), grid, dim3(256), 0, stream, A); break;
-        case 3: hipLaunchKernelGGL((mxa::bwd_kv_kernel<3, 4>), grid, dim3(256), 0, stream, A); break;
-        default: hipLaunchKernelGGL((mxa::bwd_kv_kernel<4, 4>), grid, dim3(256), 0, stream, A); break;
+        case 2: hipLaunchKernelGGL((mxa::bwd_kv_kernel<2, 4>), grid, dim3(512), 0, stream, A); break;
+        case 3: hipLaunchKernelGGL((mxa::bwd_kv_kernel<3, 4>), grid, dim3(512), 0, stream, A); break;
+        default: hipLaunchKernelGGL((mxa::bwd_kv_kernel<4, 4>), grid, dim3(512), 0, stream, A); break;
         }
     }
     return launched();
