@@ -259,6 +259,17 @@ __device__ __forceinline__ void load_rows(b8 (&x)[2 * DB], const uint16_t *head,
     }
 }
 
+// Waits for loads to registers here.  Left to their first use, inside the loop over
+// tiles, the wait would stand there in every turn, and for the tile in flight too:
+// the compiler does not see the LDS DMA that comes after them.
+template <int N> __device__ __forceinline__ void settle(b8 (&x)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        asm volatile("" : "+v"(x[i]));
+}
+__device__ __forceinline__ void settle(float &x) { asm volatile("" : "+v"(x)); }
+
 template <int BYTES> __device__ __forceinline__ void zero_lds(LDS_AS uint8_t *lds, int threads)
 {
     for (int i = threadIdx.x * 16; i < BYTES; i += threads * 16)

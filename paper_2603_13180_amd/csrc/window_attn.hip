@@ -126,6 +126,14 @@ template <int DB> struct Scores {
 #pragma unroll
             for (int b = 0; b < 2; ++b)
                 s[b] = mfma(row_frag<DB>(tile, L, ks, b), x[ks], s[b]);
+        // eight fragments are on their way ahead of the products
+        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * DB - 4; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x8, 8, 0);
     }
 };
 
@@ -152,6 +160,7 @@ __device__ __forceinline__ bool forward(const Args &A, LDS_AS uint8_t *lds, cons
     const int p = min(iw + n, S.lq - 1) + S.off;
     b8 q[2 * DB];
     load_rows<DB>(q, A.q.p + S.q0 * A.q.ts + hq * A.q.hs, A.q.ts, iw, S.lq - 1, A.D, l);
+    settle(q);
     f16v o[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -275,7 +284,9 @@ __device__ __forceinline__ bool backward_q(const Args &A, LDS_AS uint8_t *lds, c
         go[ks] = q[ks];
     load_rows<DB>(q, A.q.p + S.q0 * A.q.ts + hq * A.q.hs, A.q.ts, iw, S.lq - 1, A.D, l);
     const int64_t row = (int64_t)hq * A.Tq + S.q0 + min(iw + n, S.lq - 1);
-    const float lse2 = A.lse[row] * LOG2E;
+    float lse2 = A.lse[row] * LOG2E;
+    settle(q);
+    settle(lse2);
     if (h == 0 && iw + n < S.lq) {
         A.lse2[row] = lse2;
         A.delta[row] = delta;
@@ -391,6 +402,7 @@ __device__ __forceinline__ bool backward_kv(const Args &A, LDS_AS uint8_t *lds, 
     b8 x[2 * DB];
     const In &kv = second ? A.v : A.k;
     load_rows<DB>(x, kv.p + S.k0 * kv.ts + hk * kv.hs, kv.ts, jw, S.lk - 1, A.D, l);
+    settle(x);
     f16v acc[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d)
