@@ -65,6 +65,17 @@ __device__ __forceinline__ void lds_load16(const void *p, uint32_t lds_base)
 }
 
 __device__ __forceinline__ uint32_t lds_address(const LDS_AS uint8_t *p) { return (uint32_t)(uintptr_t)p; }
+__device__ __forceinline__ LDS_AS uint8_t *lds_pointer(uint32_t a) { return (LDS_AS uint8_t *)(uintptr_t)a; }
+
+// The thread's number.  A kernel's second, careful pass asks apart: what the compiler
+// could keep for it from the first would take registers from the first's loop.
+template <bool APART> __device__ __forceinline__ int thread_number()
+{
+    int t = threadIdx.x;
+    if (APART)
+        asm volatile("" : "+v"(t));
+    return t;
+}
 
 // One kind of heads: element (t, h, e) at p[t ts + h hs + e].
 struct In {
@@ -76,41 +87,99 @@ struct Out {
     int64_t ts, hs;
 };
 
-// Rows r0 .. r0 + ROWS - 1 (those past `last` as `last`) of a head into LDS, by
-// wave w of NW.  Chunks past D keep what the LDS held.
-template <int DB, int ROWS, int NW>
-__device__ __forceinline__ void load_tile(const uint16_t *head, int64_t ts, int r0, int last, int D,
-                                          uint32_t lds, int w, int l)
-{
-    constexpr int RPL = 64 / kChunks<DB>, LOADS = ROWS / RPL;
-    static_assert(LOADS % NW == 0, "whole loads for every wave");
-    const int c = l % kChunks<DB>;
+// Loads tiles of ROWS rows of a head into LDS, by NW waves.  FULL: the heads have all
+// of their 32 DB elements; else chunks past D keep what the LDS held.
+template <int DB, int ROWS, int NW, bool FULL> struct Loader {
+    static constexpr int RPL = 64 / kChunks<DB>, N = ROWS / RPL / NW; // rows of a load, loads of a wave
+    static_assert(ROWS % (RPL * NW) == 0, "whole loads for every wave");
+    int64_t ts;
+    uint32_t off[N]; // the lane's bytes from the tile's first row
+    int first, D;    // the wave's first row
+
+    __device__ __forceinline__ Loader(int64_t stride, int d, int w, int l) : ts(stride), first(w * N * RPL), D(d)
+    {
 #pragma unroll
-    for (int i = 0; i < LOADS / NW; ++i) {
-        const int n = w * (LOADS / NW) + i, r = n * RPL + l / kChunks<DB>;
-        const int ch = c ^ swz<DB>(r);
-        if (ch * 8 < D)
-            lds_load16(head + (int64_t)min(r0 + r, last) * ts + ch * 8, lds + n * 1024);
+        for (int i = 0; i < N; ++i)
+            off[i] = (uint32_t)row(i, l) * (uint32_t)ts * 2 + chunk(i, l) * 16;
+    }
+    __device__ __forceinline__ int row(int i, int l) const { return first + i * RPL + l / kChunks<DB>; }
+    __device__ __forceinline__ uint32_t chunk(int i, int l) const { return (l % kChunks<DB>) ^ swz<DB>(row(i, l)); }
+
+    // rows r0 .. (those past `last` as `last`)
+    __device__ __forceinline__ void load(const uint16_t *head, int r0, int last, uint32_t lds, int l) const
+    {
+        const uint16_t *base = head + (int64_t)r0 * ts;
+        const uint32_t to = lds + w_bytes();
+        if (__builtin_expect(ts >= 1 << 24, 0)) { // 32-bit offsets do not hold a tile
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (FULL || (int)chunk(i, l) * 8 < D)
+                    lds_load16(head + (int64_t)min(r0 + row(i, l), last) * ts + chunk(i, l) * 8, to + i * 1024);
+        } else if (r0 + ROWS - 1 > last) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (FULL || (int)chunk(i, l) * 8 < D)
+                    mxg::lds_load16(base, (uint32_t)min(row(i, l), last - r0) * (uint32_t)ts * 2 + chunk(i, l) * 16, to + i * 1024);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (FULL || (int)chunk(i, l) * 8 < D)
+                    mxg::lds_load16(base, off[i], to + i * 1024);
+        }
+    }
+    __device__ __forceinline__ uint32_t w_bytes() const { return first / RPL * 1024; }
+};
+
+// A run of tiles by what a wave's rows see of them: 0 before `some` and from `none`
+// on, 2 (all) from `all` to `less` - 1, 1 (some) else.
+// `sinks` tiles in front of the run are seen in part.
+struct Seen {
+    int sinks, some, all, less, none;
+    __device__ __forceinline__ int operator()(int t) const
+    {
+        return t >= all && t < less ? 2 : t < sinks || (t >= some && t < none) ? 1 : 0;
+    }
+};
+
+// Tiles 0 .. n - 1 through three LDS stages, loads two tiles ahead, one barrier a
+// tile.  LOADS: a wave's loads of a tile.
+template <int LOADS, typename Load, typename Work> __device__ __forceinline__ void tile_loop(int n, Load load, Work work)
+{
+    if (n > 0)
+        load(0, 0);
+    if (n > 1)
+        load(1, 1);
+    int mine = 0, next = 2; // the stage of tile it, and of tile it + 2
+    for (int it = 0; it < n; ++it) {
+        if (it + 1 < n)
+            wait_vmcnt<LOADS>();
+        else
+            wait_vmcnt<0>();
+        barrier();
+        if (it + 2 < n)
+            load(it + 2, next);
+        work(it, mine);
+        mine = mine == 2 ? 0 : mine + 1;
+        next = next == 2 ? 0 : next + 1;
     }
 }
 
-// A lane's offsets into a tile.
+// A lane's offsets into a tile.  Of an offset, the bits that say which 16 bytes (ks)
+// or which 32 columns (d) of its row are its own: they are XORed in when it is used,
+// behind a sum that differs from tile to tile, so that no register holds them.
 template <int DB> struct Lane {
-    uint32_t row;        // chunk h of row n
-    uint32_t tr[2][DB];  // the transposing read of rows 8 u + 4 h .. + 3, columns 32 d ..
+    uint32_t row;   // chunk h of row n
+    uint32_t tr[2]; // the transposing read of rows 8 u + 4 h .. + 3, columns 0 .. 31
 
     __device__ __forceinline__ explicit Lane(int l)
     {
         const int n = l & 31, h = l >> 5, i = l & 15;
         row = n * kRow<DB> + (h ^ swz<DB>(n)) * 16;
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                const int r = 8 * u + 4 * h + (i >> 2);
-                const int c = 4 * d + 2 * ((l >> 4) & 1) + ((i & 3) >> 1);
-                tr[u][d] = r * kRow<DB> + (c ^ swz<DB>(r)) * 16 + (i & 1) * 8;
-            }
+        for (int u = 0; u < 2; ++u) {
+            const int r = 8 * u + 4 * h + (i >> 2), c = 2 * ((l >> 4) & 1) + ((i & 3) >> 1);
+            tr[u] = r * kRow<DB> + (c ^ swz<DB>(r)) * 16 + (i & 1) * 8;
+        }
     }
 };
 
@@ -118,7 +187,7 @@ template <int DB> struct Lane {
 template <int DB>
 __device__ __forceinline__ b8 row_frag(const LDS_AS uint8_t *tile, const Lane<DB> &L, int ks, int b)
 {
-    return *reinterpret_cast<const LDS_AS b8 *>(tile + b * 32 * kRow<DB> + (L.row ^ (ks * 32)));
+    return *reinterpret_cast<const LDS_AS b8 *>(lds_pointer((lds_address(tile) + L.row) ^ (ks * 32)) + b * 32 * kRow<DB>);
 }
 
 // elements 32 d + n of rows 16 s + 8 u + 4 h + j
@@ -126,9 +195,12 @@ template <int DB>
 __device__ __forceinline__ b8 col_frag(const LDS_AS uint8_t *tile, const Lane<DB> &L, int s, int d)
 {
     typedef short s4 __attribute__((ext_vector_type(4)));
-    const s4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s4 *)(tile + s * 16 * kRow<DB> + L.tr[0][d]));
-    const s4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s4 *)(tile + s * 16 * kRow<DB> + L.tr[1][d]));
-    return __builtin_bit_cast(b8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    s4 x[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+        x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_AS s4 *>(
+            lds_pointer((lds_address(tile) + L.tr[u]) ^ (d * 64)) + s * 16 * kRow<DB>));
+    return __builtin_bit_cast(b8, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
 __device__ __forceinline__ f16v mfma(b8 a, b8 b, f16v c)
@@ -164,43 +236,70 @@ __device__ __forceinline__ float halves_sum(float x)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// acc += (rows 16 s .. of the tile)^T x
-template <int DB>
-__device__ __forceinline__ void product(f16v (&acc)[DB], const LDS_AS uint8_t *tile, const Lane<DB> &L, int s, b8 x)
+// acc += tile^T x, the tile of 32 NB rows, x in C's layout and rounded to bf16
+template <int DB, int NB>
+__device__ __forceinline__ void products(f16v (&acc)[DB], const LDS_AS uint8_t *tile, const Lane<DB> &L, const f16v (&x)[NB])
 {
 #pragma unroll
-    for (int d = 0; d < DB; ++d)
-        acc[d] = mfma(col_frag<DB>(tile, L, s, d), x, acc[d]);
+    for (int s = 0; s < 2 * NB; ++s) {
+        const b8 y = pack8(x[s >> 1], s & 1);
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+            acc[d] = mfma(col_frag<DB>(tile, L, s, d), y, acc[d]);
+    }
+}
+
+// s = the tile's 64 rows times x
+template <int DB>
+__device__ __forceinline__ void scores(f16v (&s)[2], const LDS_AS uint8_t *tile, const Lane<DB> &L, const b8 (&x)[2 * DB])
+{
+    s[0] = s[1] = zero16();
+#pragma unroll
+    for (int ks = 0; ks < 2 * DB; ++ks)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+            s[b] = mfma(row_frag<DB>(tile, L, ks, b), x[ks], s[b]);
+    // eight fragments are on their way ahead of the products
+    __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+    for (int i = 0; i < 4 * DB - 8; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x8, 8, 0);
 }
 
 // The same of a tile some of whose rows are masked and may hold infinities or
 // NaN: 0 times those is NaN, so every row is a product of its own, kept where
 // seen(row) of the lane's column.  Only for tiles where the plain product gave
 // something that is not finite.
-template <int DB, typename Seen>
-__device__ __forceinline__ void careful_product(f16v (&acc)[DB], const LDS_AS uint8_t *tile, const Lane<DB> &L, int s, b8 x,
-                                                int h, Seen seen)
+template <int DB, int NB, typename Seen>
+__device__ __forceinline__ void careful_products(f16v (&acc)[DB], const LDS_AS uint8_t *tile, const Lane<DB> &L,
+                                                 const f16v (&x)[NB], int h, Seen seen)
 {
     typedef short s8 __attribute__((ext_vector_type(8)));
-    const s8 xi = __builtin_bit_cast(s8, x);
+#pragma unroll
+    for (int s = 0; s < 2 * NB; ++s) {
+        const s8 xi = __builtin_bit_cast(s8, pack8(x[s >> 1], s & 1));
 #pragma unroll 1
-    for (int r = 0; r < 16; ++r) {
-        const bool mine = ((r >> 2) & 1) == h, see = seen(16 * s + r);
-        const int e = 4 * (r >> 3) + (r & 3);
-        s8 xr;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            xr[i] = mine && i == e ? xi[i] : (short)0;
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-            s8 a = __builtin_bit_cast(s8, col_frag<DB>(tile, L, s, d));
+        for (int r = 0; r < 16; ++r) {
+            const bool mine = ((r >> 2) & 1) == h, see = seen(16 * s + r);
+            const int e = 4 * (r >> 3) + (r & 3);
+            s8 xr;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                a[i] = mine && i == e ? a[i] : (short)0;
-            const f16v t = mfma(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, xr), acc[d]);
+                xr[i] = mine && i == e ? xi[i] : (short)0;
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                acc[d][i] = see ? t[i] : acc[d][i];
+            for (int d = 0; d < DB; ++d) {
+                s8 a = __builtin_bit_cast(s8, col_frag<DB>(tile, L, s, d));
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    a[i] = mine && i == e ? a[i] : (short)0;
+                const f16v t = mfma(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, xr), acc[d]);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    acc[d][i] = see ? t[i] : acc[d][i];
+            }
         }
     }
 }

@@ -281,8 +281,9 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
     using O = Shape<RB>;
     constexpr int TILE = O::KEYS * kRow<DB>, GROUP = O::STAGES * 2 * TILE;
     const Cache &C = A.C;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, h = l >> 5;
-    const int kw = w / RB, in_group = threadIdx.x - kw * RB * 64;
+    const int thread = thread_number<CAREFUL>();
+    const int w = __builtin_amdgcn_readfirstlane(thread >> 6), l = thread & 63, n = l & 31, h = l >> 5;
+    const int kw = w / RB, in_group = thread - kw * RB * 64;
     const Lane<DB> L(l);
     const int rw = r0 + 32 * (w % RB), r = min(rw + n, S.R - 1), i = r / A.G, hq = hk * A.G + r % A.G;
     const bool mine = rw + n < S.R;
@@ -391,14 +392,10 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
                 s[x][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e], A.c, -m));
                 sum += s[x][e];
             }
-#pragma unroll
-        for (int x = 0; x < 2 * O::NB; ++x) {
-            const b8 y = pack8(s[x >> 1], x & 1);
-            if (CAREFUL && !full)
-                careful_product<DB>(o, vt, L, x, y, h, seen);
-            else
-                product<DB>(o, vt, L, x, y);
-        }
+        if (CAREFUL && !full)
+            careful_products<DB, O::NB>(o, vt, L, s, h, seen);
+        else
+            products<DB, O::NB>(o, vt, L, s);
     }
     if (!CAREFUL && __syncthreads_or(mine && not_finite<DB>(o)))
         return false;

@@ -107,57 +107,57 @@ __device__ __forceinline__ bool sees(const Args &A, int p, int j)
     return j <= p && (p - j < A.window || j < A.sinks);
 }
 
-// What queries at p0 .. p1 see of keys j0 .. j0 + n - 1: 0 none, 1 some, 2 all.
-__device__ __forceinline__ int seen(const Args &A, int p0, int p1, int j0, int n)
-{
-    if (j0 > p1 || (j0 + n - 1 <= p0 - A.window && j0 >= A.sinks))
-        return 0;
-    return j0 + n - 1 <= p0 && p1 - j0 < A.window ? 2 : 1;
-}
-
-template <int DB> struct Scores {
-    f16v s[2];
-    // the tile's rows times x
-    __device__ __forceinline__ Scores(const LDS_AS uint8_t *tile, const Lane<DB> &L, const b8 (&x)[2 * DB])
+// The same of the keys j0 + c, for constants c.  The sums are hidden from the
+// compiler, which would keep one for every c in a register.
+struct Mask {
+    int most, least, sinks;
+    __device__ __forceinline__ Mask(const Args &A, int p, int j0) : most(p - j0), least(p - j0 - A.window), sinks(A.sinks - j0)
     {
-        s[0] = s[1] = zero16();
-#pragma unroll
-        for (int ks = 0; ks < 2 * DB; ++ks)
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-                s[b] = mfma(row_frag<DB>(tile, L, ks, b), x[ks], s[b]);
-        // eight fragments are on their way ahead of the products
-        __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-#pragma unroll
-        for (int i = 0; i < 2 * DB - 4; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-        }
-        __builtin_amdgcn_sched_group_barrier(0x8, 8, 0);
+        asm volatile("" : "+v"(most), "+v"(least), "+v"(sinks));
     }
+    __device__ __forceinline__ bool operator()(int c) const { return c <= most && (c > least || c < sinks); }
 };
+
+// floor(x / BK) for any x
+__device__ __forceinline__ int tile_floor(int x) { return x >> 6; }
+static_assert(BK == 64, "tile_floor");
+
+// What queries at p0 .. p1 (p1 < p0: none) see of the tiles, by their number in the list.
+__device__ __forceinline__ Seen seen_of(const Args &A, const Tiles &T, int p0, int p1)
+{
+    const int shift = T.first - T.sinks;
+    Seen S;
+    S.some = max(tile_floor(p0 - A.window + 1) - shift, T.sinks);
+    S.none = p1 < p0 ? 0 : tile_floor(p1) + 1 - shift;
+    S.sinks = min(max(tile_floor(A.sinks + BK - 1) - shift, T.sinks), S.none);
+    S.all = max(tile_floor(p1 - A.window) + 1 - shift, T.sinks);
+    S.less = p1 < p0 ? 0 : tile_floor(p0 + 1) - shift;
+    return S;
+}
 
 // ---------------------------------------------------------------- forward --
 
-template <int DB, int NW, bool CAREFUL>
+template <int DB, int NW, bool FULL, bool CAREFUL>
 __device__ __forceinline__ bool forward(const Args &A, LDS_AS uint8_t *lds, const Span &S, int i0, int hk, int hq)
 {
     constexpr int TILE = BK * kRow<DB>;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, h = l >> 5;
+    const int thread = thread_number<CAREFUL>();
+    const int w = __builtin_amdgcn_readfirstlane(thread >> 6), l = thread & 63, n = l & 31, h = l >> 5;
     const uint32_t base = lds_address(lds);
     const Lane<DB> L(l);
     const uint16_t *kh = A.k.p + S.k0 * A.k.ts + hk * A.k.hs, *vh = A.v.p + S.k0 * A.v.ts + hk * A.v.hs;
     const Tiles tiles(A, i0 + S.off, min(i0 + 32 * NW, S.lq) - 1 + S.off);
-    auto load = [&](int it) {
-        const uint32_t to = base + (it & 1) * 2 * TILE;
-        load_tile<DB, BK, NW>(kh, A.k.ts, tiles[it], S.lk - 1, A.D, to, w, l);
-        load_tile<DB, BK, NW>(vh, A.v.ts, tiles[it], S.lk - 1, A.D, to + TILE, w, l);
+    using Load = Loader<DB, BK, NW, FULL>;
+    const Load kl(A.k.ts, A.D, w, l), vl(A.v.ts, A.D, w, l);
+    auto load = [&](int it, int stage) {
+        const uint32_t to = base + stage * 2 * TILE;
+        kl.load(kh, tiles[it], S.lk - 1, to, l);
+        vl.load(vh, tiles[it], S.lk - 1, to + TILE, l);
     };
-    if (tiles.n > 0)
-        load(0);
     const int iw = i0 + 32 * w;                             // the wave's first query
     const int p0 = iw + S.off, p1 = min(iw + 31, S.lq - 1) + S.off;
     const int p = min(iw + n, S.lq - 1) + S.off;
+    const Seen what = seen_of(A, tiles, p0, p1);
     b8 q[2 * DB];
     load_rows<DB>(q, A.q.p + S.q0 * A.q.ts + hq * A.q.hs, A.q.ts, iw, S.lq - 1, A.D, l);
     settle(q);
@@ -166,29 +166,27 @@ __device__ __forceinline__ bool forward(const Args &A, LDS_AS uint8_t *lds, cons
     for (int d = 0; d < DB; ++d)
         o[d] = zero16();
     float m = -FLT_MAX, sum = 0.0f; // m: of scores in powers of two; sum: the lane's half of the keys
-    for (int it = 0; it < tiles.n; ++it) {
-        wait_vmcnt<0>();
-        barrier();
-        if (it + 1 < tiles.n)
-            load(it + 1);
-        const int j0 = tiles[it];
-        const int see = iw < S.lq ? seen(A, p0, p1, j0, BK) : 0;
+    auto work = [&](int it, int stage) {
+        const int see = what(it), j0 = tiles[it];
         if (see == 0)
-            continue;
-        const LDS_AS uint8_t *kt = lds + (it & 1) * 2 * TILE, *vt = kt + TILE;
-        Scores<DB> x(kt, L, q);
-        if (see == 1)
+            return;
+        const LDS_AS uint8_t *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
+        f16v x[2]; // scores, then P
+        scores<DB>(x, kt, L, q);
+        if (see == 1) {
+            const Mask mask(A, p, j0 + 4 * h);
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    x.s[b][e] = sees(A, p, j0 + 32 * b + c_row(e, h)) ? x.s[b][e] : -INFINITY;
+                    x[b][e] = mask(32 * b + c_row(e, 0)) ? x[b][e] : -INFINITY;
+        }
         float mt = -INFINITY;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-                mt = fmaxf(mt, x.s[b][e]);
+                mt = fmaxf(mt, x[b][e]);
         mt = halves_max(mt) * A.c;
         // The maximum is followed only where it grows by more than 2^8: what
         // exponentials and sums gain from that stays far inside float and bf16.
@@ -204,18 +202,15 @@ __device__ __forceinline__ bool forward(const Args &A, LDS_AS uint8_t *lds, cons
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                x.s[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x.s[b][e], A.c, -m));
-                sum += x.s[b][e];
+                x[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], A.c, -m));
+                sum += x[b][e];
             }
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const b8 y = pack8(x.s[s >> 1], s & 1);
-            if (CAREFUL && see == 1)
-                careful_product<DB>(o, vt, L, s, y, h, [&](int r) { return sees(A, p, j0 + r); });
-            else
-                product<DB>(o, vt, L, s, y);
-        }
-    }
+        if (CAREFUL && see == 1)
+            careful_products<DB, 2>(o, vt, L, x, h, [&](int r) { return sees(A, p, j0 + r); });
+        else
+            products<DB, 2>(o, vt, L, x);
+    };
+    tile_loop<2 * Load::N>(tiles.n, load, work);
     if (!CAREFUL && __syncthreads_or(iw + n < S.lq && not_finite<DB>(o)))
         return false;
     if (CAREFUL)
@@ -231,41 +226,42 @@ __device__ __forceinline__ bool forward(const Args &A, LDS_AS uint8_t *lds, cons
     return true;
 }
 
-template <int DB, int NW>
+template <int DB, int NW, bool FULL>
 __global__ void __launch_bounds__(64 * NW, 2) fwd_kernel(Args A)
 {
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * BK * kRow<DB>];
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[6 * BK * kRow<DB>];
     LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
     int rank, hk, g, b, i0;
     Span S;
     if (!item_of(blockIdx.x, A.tiles, A.Hk, A.G, rank, hk, g) ||
         !span_of(A, A.qs, A.Tq, A.tiles - 1 - rank, 32 * NW, false, S, b, i0))
         return;
-    if (A.D != 32 * DB)
-        zero_lds<4 * BK * kRow<DB>>(lds, 64 * NW);
-    if (!forward<DB, NW, false>(A, lds, S, i0, hk, hk * A.G + g))
-        forward<DB, NW, true>(A, lds, S, i0, hk, hk * A.G + g);
+    if (!FULL)
+        zero_lds<6 * BK * kRow<DB>>(lds, 64 * NW);
+    if (!forward<DB, NW, FULL, false>(A, lds, S, i0, hk, hk * A.G + g))
+        forward<DB, NW, FULL, true>(A, lds, S, i0, hk, hk * A.G + g);
 }
 
 // --------------------------------------------------------------- backward --
 
 // grad_q, and for the other kernels lse log2(e) and delta.
-template <int DB, int NW, bool CAREFUL>
+template <int DB, int NW, bool FULL, bool CAREFUL>
 __device__ __forceinline__ bool backward_q(const Args &A, LDS_AS uint8_t *lds, const Span &S, int i0, int hk, int hq)
 {
     constexpr int TILE = BK * kRow<DB>;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, h = l >> 5;
+    const int thread = thread_number<CAREFUL>();
+    const int w = __builtin_amdgcn_readfirstlane(thread >> 6), l = thread & 63, n = l & 31, h = l >> 5;
     const uint32_t base = lds_address(lds);
     const Lane<DB> L(l);
     const uint16_t *kh = A.k.p + S.k0 * A.k.ts + hk * A.k.hs, *vh = A.v.p + S.k0 * A.v.ts + hk * A.v.hs;
     const Tiles tiles(A, i0 + S.off, min(i0 + 32 * NW, S.lq) - 1 + S.off);
-    auto load = [&](int it) {
-        const uint32_t to = base + (it & 1) * 2 * TILE;
-        load_tile<DB, BK, NW>(kh, A.k.ts, tiles[it], S.lk - 1, A.D, to, w, l);
-        load_tile<DB, BK, NW>(vh, A.v.ts, tiles[it], S.lk - 1, A.D, to + TILE, w, l);
+    using Load = Loader<DB, BK, NW, FULL>;
+    const Load kl(A.k.ts, A.D, w, l), vl(A.v.ts, A.D, w, l);
+    auto load = [&](int it, int stage) {
+        const uint32_t to = base + stage * 2 * TILE;
+        kl.load(kh, tiles[it], S.lk - 1, to, l);
+        vl.load(vh, tiles[it], S.lk - 1, to + TILE, l);
     };
-    if (tiles.n > 0)
-        load(0);
     const int iw = i0 + 32 * w;
     const int p0 = iw + S.off, p1 = min(iw + 31, S.lq - 1) + S.off;
     const int p = min(iw + n, S.lq - 1) + S.off;
@@ -291,43 +287,40 @@ __device__ __forceinline__ bool backward_q(const Args &A, LDS_AS uint8_t *lds, c
         A.lse2[row] = lse2;
         A.delta[row] = delta;
     }
+    const Seen what = seen_of(A, tiles, p0, p1);
     f16v o[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d)
         o[d] = zero16();
-    for (int it = 0; it < tiles.n; ++it) {
-        wait_vmcnt<0>();
-        barrier();
-        if (it + 1 < tiles.n)
-            load(it + 1);
-        const int j0 = tiles[it];
-        const int see = iw < S.lq ? seen(A, p0, p1, j0, BK) : 0;
+    auto work = [&](int it, int stage) {
+        const int see = what(it), j0 = tiles[it];
         if (see == 0)
-            continue;
-        const LDS_AS uint8_t *kt = lds + (it & 1) * 2 * TILE, *vt = kt + TILE;
-        Scores<DB> x(kt, L, q), y(vt, L, go);
+            return;
+        const LDS_AS uint8_t *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
+        f16v x[2], y[2]; // x: scores, then dS
+        scores<DB>(x, kt, L, q);
+        scores<DB>(y, vt, L, go);
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(x.s[b][e], A.c, -lse2));
-                x.s[b][e] = pr * (y.s[b][e] - delta);
+                const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][e], A.c, -lse2));
+                x[b][e] = pr * (y[b][e] - delta);
             }
-        if (see == 1)
+        if (see == 1) {
+            const Mask mask(A, p, j0 + 4 * h);
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    x.s[b][e] = sees(A, p, j0 + 32 * b + c_row(e, h)) ? x.s[b][e] : 0.0f;
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const b8 z = pack8(x.s[s >> 1], s & 1);
-            if (CAREFUL && see == 1)
-                careful_product<DB>(o, kt, L, s, z, h, [&](int r) { return sees(A, p, j0 + r); });
-            else
-                product<DB>(o, kt, L, s, z);
+                    x[b][e] = mask(32 * b + c_row(e, 0)) ? x[b][e] : 0.0f;
         }
-    }
+        if (CAREFUL && see == 1)
+            careful_products<DB, 2>(o, kt, L, x, h, [&](int r) { return sees(A, p, j0 + r); });
+        else
+            products<DB, 2>(o, kt, L, x);
+    };
+    tile_loop<2 * Load::N>(tiles.n, load, work);
     if (!CAREFUL && __syncthreads_or(iw + n < S.lq && not_finite<DB>(o)))
         return false;
     if (CAREFUL)
@@ -337,20 +330,20 @@ __device__ __forceinline__ bool backward_q(const Args &A, LDS_AS uint8_t *lds, c
     return true;
 }
 
-template <int DB, int NW>
+template <int DB, int NW, bool FULL>
 __global__ void __launch_bounds__(64 * NW, 2) bwd_q_kernel(Args A)
 {
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * BK * kRow<DB>];
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[6 * BK * kRow<DB>];
     LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
     int rank, hk, g, b, i0;
     Span S;
     if (!item_of(blockIdx.x, A.tiles, A.Hk, A.G, rank, hk, g) ||
         !span_of(A, A.qs, A.Tq, A.tiles - 1 - rank, 32 * NW, false, S, b, i0))
         return;
-    if (A.D != 32 * DB)
-        zero_lds<4 * BK * kRow<DB>>(lds, 64 * NW);
-    if (!backward_q<DB, NW, false>(A, lds, S, i0, hk, hk * A.G + g))
-        backward_q<DB, NW, true>(A, lds, S, i0, hk, hk * A.G + g);
+    if (!FULL)
+        zero_lds<6 * BK * kRow<DB>>(lds, 64 * NW);
+    if (!backward_q<DB, NW, FULL, false>(A, lds, S, i0, hk, hk * A.G + g))
+        backward_q<DB, NW, FULL, true>(A, lds, S, i0, hk, hk * A.G + g);
 }
 
 // The sinks' sums over queries that lie the window or more behind: chunk `at`
@@ -369,13 +362,12 @@ template <int DB> __device__ __forceinline__ float *far_part(const Args &A, int 
 // A wave has registers for one of the two sums at two waves a SIMD.  So of a pair
 // the first wave forms the scores, P and grad_v += grad_out^T P, and the second, a
 // tile of queries later, grad_out . v, dS from the P that the first left in LDS,
-// and grad_k += Q^T dS: two products each, one a SIMD's exponentials beside the
-// other's products, one barrier a tile.  P goes over as the upper 24 bits of its
+// and grad_k += Q^T dS: two products each, one barrier a tile.  P goes over as the upper 24 bits of its
 // float, within 2^-15, so dS is rounded to bf16 from what is nearly float (P in bf16
 // would double that rounding, whole floats do not fit).
 template <int DB> constexpr int kStageKV = 2 * BK * kRow<DB> + 8 * BK;
 template <int DB, int NP> constexpr int kBytesKV = 3 * kStageKV<DB> + NP * 2 * BK * 96;
-template <int DB, int NP, bool FAR, bool CAREFUL>
+template <int DB, int NP, bool FULL, bool FAR, bool CAREFUL>
 __device__ __forceinline__ bool backward_kv(const Args &A, LDS_AS uint8_t *lds, const Span &S, int j0, int i0, int i1, int hk,
                                             int b, int chunk)
 {
@@ -385,19 +377,23 @@ __device__ __forceinline__ bool backward_kv(const Args &A, LDS_AS uint8_t *lds, 
     const uint32_t base = lds_address(lds);
     const Lane<DB> L(l);
     const int steps = i1 < i0 ? 0 : (i1 - i0) / BK + 1, total = steps * A.G;
-    auto load = [&](int it, int stage) {
-        const int hq = hk * A.G + it / steps, r0 = i0 + it % steps * BK;
+    using Load = Loader<DB, BK, NW, FULL>;
+    const Load ql(A.q.ts, A.D, w, l), gl(A.go.ts, A.D, w, l);
+    int lr = i0, lq = hk * A.G; // of the tile to load next: first query, head
+    auto load = [&](int stage) { // the next one
         const uint32_t to = base + stage * STAGE;
-        load_tile<DB, BK, NW>(A.q.p + S.q0 * A.q.ts + hq * A.q.hs, A.q.ts, r0, i1, A.D, to, w, l);
-        load_tile<DB, BK, NW>(A.go.p + S.q0 * A.go.ts + hq * A.go.hs, A.go.ts, r0, i1, A.D, to + TILE, w, l);
-        const int64_t row = (int64_t)hq * A.Tq + S.q0 + min(r0 + l, i1);
-        if (w == 0)
-            mxg::lds_load4(A.lse2 + row, to + 2 * TILE);
-        if (w == NW - 1)
-            mxg::lds_load4(A.delta + row, to + 2 * TILE + 4 * BK);
+        ql.load(A.q.p + S.q0 * A.q.ts + lq * A.q.hs, lr, i1, to, l);
+        gl.load(A.go.p + S.q0 * A.go.ts + lq * A.go.hs, lr, i1, to + TILE, l);
+        // the rows' lse and delta
+        const int64_t row = (int64_t)lq * A.Tq + S.q0 + min(lr + l, i1);
+        if (w < 2)
+            mxg::lds_load4((w ? A.delta : A.lse2) + row, to + 2 * TILE + w * 4 * BK);
+        lr += BK;
+        if (lr > i1) {
+            lr = i0;
+            ++lq;
+        }
     };
-    if (total > 0)
-        load(0, 0);
     const int jw = j0 + 32 * pair, j = jw + n;
     b8 x[2 * DB];
     const In &kv = second ? A.v : A.k;
@@ -412,88 +408,102 @@ __device__ __forceinline__ bool backward_kv(const Args &A, LDS_AS uint8_t *lds, 
         return i <= i1 && (FAR ? back >= A.window && j < A.sinks : back >= 0 && back < A.window);
     };
     LDS_AS uint8_t *ps = lds + 3 * STAGE + pair * 2 * BK * 96 + l * 16;
-    int mine = second ? 2 : 0, next = 1; // the wave's stage; the one to load next
+    // What of the wave's keys the tiles of a head's queries see.
+    auto tiles_to = [&](int i) { return tile_floor(i - i0 + BK - 1); }; // tiles that start before query i
+    Seen what{0, 0, 0, 0, jw < S.lk ? steps : 0};
+    if (!FAR && jw < S.lk) {
+        what.some = tiles_to(jw - S.off - BK + 1);
+        what.none = tiles_to(jw + 31 - S.off + A.window);
+        what.all = tiles_to(jw + 31 - S.off);
+        what.less = tile_floor(min(i1, jw + A.window - 1 - S.off) - BK + 1 - i0) + 1;
+    }
+    auto work = [&](int u, int stage, int odd) { // tile u of a head; odd: that of all heads' tiles
+        const int see = what(u), r0 = i0 + u * BK;
+        if (see == 0)
+            return;
+        const LDS_AS uint8_t *qt = lds + stage * STAGE, *gt = qt + TILE;
+        LDS_AS uint8_t *pt = ps + odd * BK * 96;
+        f16v s[2]; // scores or grad_out . v, then P or dS
+        scores<DB>(s, second ? gt : qt, L, x);
+        const LDS_AS float *st = reinterpret_cast<const LDS_AS float *>(qt + 2 * TILE) + second * BK + 4 * h;
+        if (second) { // dS: cells 0 .. 3 hold P's upper halves, 4 and 5 the bytes below
+            u32x4 low[2];
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+                low[c] = *reinterpret_cast<const LDS_AS u32x4 *>(pt + (4 + c) * 1024);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const u32x4 up = *reinterpret_cast<const LDS_AS u32x4 *>(pt + c * 1024);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    constexpr uint32_t BYTES[4] = {0x0504000Cu, 0x0706010Cu, 0x0504020Cu, 0x0706030Cu};
+                    const int e = 8 * (c & 1) + i;
+                    const float pr =
+                        __uint_as_float(__builtin_amdgcn_perm(up[i / 2], low[c >> 1][2 * (c & 1) + i / 4], BYTES[i & 3]));
+                    s[c >> 1][e] = pr * (s[c >> 1][e] - st[32 * (c >> 1) + 8 * (e >> 2) + (e & 3)]);
+                }
+            }
+        } else { // P
+#pragma unroll
+            for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    s[qb][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qb][e], A.c, -st[32 * qb + 8 * (e >> 2) + (e & 3)]));
+        }
+        if (see == 1) { // queries first + c, for constants c (hidden sums as in Mask)
+            const int first = r0 + 4 * h;
+            int least = FAR ? (j < A.sinks ? j + A.window - S.off - first : 64) : j - S.off - first;
+            int most = FAR ? i1 - first : min(i1 - first, least + A.window - 1);
+            asm volatile("" : "+v"(least), "+v"(most));
+#pragma unroll
+            for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int c = 32 * qb + c_row(e, 0);
+                    s[qb][e] = c >= least && c <= most ? s[qb][e] : 0.0f;
+                }
+        }
+        if (!second) {
+            u32x4 low[2];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                u32x4 up;
+                uint32_t y[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    y[i] = __float_as_uint(s[c >> 1][8 * (c & 1) + i]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    up[i] = __builtin_amdgcn_perm(y[2 * i + 1], y[2 * i], 0x07060302u);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    low[c >> 1][2 * (c & 1) + i] = __builtin_amdgcn_perm(y[4 * i + 1], y[4 * i], 0x0C0C0501u) |
+                                                   __builtin_amdgcn_perm(y[4 * i + 3], y[4 * i + 2], 0x05010C0Cu);
+                *reinterpret_cast<LDS_AS u32x4 *>(pt + c * 1024) = up;
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+                *reinterpret_cast<LDS_AS u32x4 *>(pt + (4 + c) * 1024) = low[c];
+        }
+        const LDS_AS uint8_t *down = second ? qt : gt;
+        if (CAREFUL && see == 1)
+            careful_products<DB, 2>(acc, down, L, s, h, [&](int i) { return sees_key(r0 + i); });
+        else
+            products<DB, 2>(acc, down, L, s);
+    };
+    if (total > 0)
+        load(0);
+    int stage = second ? 2 : 0, next = 1, u = second ? -1 : 0; // the wave's stage and tile; the stage to load next
     for (int it = 0; it <= total; ++it) {
         wait_vmcnt<0>();
         barrier();
         if (it + 1 < total)
-            load(it + 1, next);
+            load(next);
+        if (it - second >= 0 && it - second < total)
+            work(u, stage, (it - second) & 1);
+        u = u + 1 == steps ? 0 : u + 1;
+        stage = stage == 2 ? 0 : stage + 1;
         next = next == 2 ? 0 : next + 1;
-        const int t = it - second;
-        if (t >= 0 && t < total && jw < S.lk) {
-            const int r0 = i0 + t % steps * BK, p0 = r0 + S.off, p1 = min(r0 + BK - 1, i1) + S.off;
-            const bool none = !FAR && (p1 < jw || p0 - (jw + 31) >= A.window);
-            const bool all = !FAR && p0 >= jw + 31 && p1 - jw < A.window && r0 + BK - 1 <= i1;
-            if (!none) {
-                const LDS_AS uint8_t *qt = lds + mine * STAGE, *gt = qt + TILE;
-                const LDS_AS float *st = reinterpret_cast<const LDS_AS float *>(qt + 2 * TILE) + second * BK + 4 * h;
-                LDS_AS uint8_t *pt = ps + (t & 1) * BK * 96;
-                Scores<DB> s(second ? gt : qt, L, x);
-                if (second) { // dS: cells 0 .. 3 hold P's upper halves, 4 and 5 the bytes below
-                    u32x4 low[2];
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-                        low[c] = *reinterpret_cast<const LDS_AS u32x4 *>(pt + (4 + c) * 1024);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const u32x4 up = *reinterpret_cast<const LDS_AS u32x4 *>(pt + c * 1024);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            constexpr uint32_t BYTES[4] = {0x0504000Cu, 0x0706010Cu, 0x0504020Cu, 0x0706030Cu};
-                            const int e = 8 * (c & 1) + i;
-                            const float pr = __uint_as_float(
-                                __builtin_amdgcn_perm(up[i / 2], low[c >> 1][2 * (c & 1) + i / 4], BYTES[i & 3]));
-                            s.s[c >> 1][e] = pr * (s.s[c >> 1][e] - st[32 * (c >> 1) + 8 * (e >> 2) + (e & 3)]);
-                        }
-                    }
-                } else { // P
-#pragma unroll
-                    for (int qb = 0; qb < 2; ++qb)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            s.s[qb][e] = __builtin_amdgcn_exp2f(
-                                __builtin_fmaf(s.s[qb][e], A.c, -st[32 * qb + 8 * (e >> 2) + (e & 3)]));
-                }
-                if (!all)
-#pragma unroll
-                    for (int qb = 0; qb < 2; ++qb)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            s.s[qb][e] = sees_key(r0 + 32 * qb + c_row(e, h)) ? s.s[qb][e] : 0.0f;
-                if (!second) {
-                    u32x4 low[2];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        u32x4 up;
-                        uint32_t y[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            y[i] = __float_as_uint(s.s[c >> 1][8 * (c & 1) + i]);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            up[i] = __builtin_amdgcn_perm(y[2 * i + 1], y[2 * i], 0x07060302u);
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            low[c >> 1][2 * (c & 1) + i] = __builtin_amdgcn_perm(y[4 * i + 1], y[4 * i], 0x0C0C0501u) |
-                                                           __builtin_amdgcn_perm(y[4 * i + 3], y[4 * i + 2], 0x05010C0Cu);
-                        *reinterpret_cast<LDS_AS u32x4 *>(pt + c * 1024) = up;
-                    }
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-                        *reinterpret_cast<LDS_AS u32x4 *>(pt + (4 + c) * 1024) = low[c];
-                }
-                const LDS_AS uint8_t *down = second ? qt : gt;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const b8 z = pack8(s.s[c >> 1], c & 1);
-                    if (CAREFUL && !all)
-                        careful_product<DB>(acc, down, L, c, z, h, [&](int r) { return sees_key(r0 + r); });
-                    else
-                        product<DB>(acc, down, L, c, z);
-                }
-            }
-        }
-        mine = mine == 2 ? 0 : mine + 1;
     }
     if (!CAREFUL && __syncthreads_or(j < S.lk && not_finite<DB>(acc)))
         return false;
@@ -527,7 +537,7 @@ __device__ __forceinline__ bool backward_kv(const Args &A, LDS_AS uint8_t *lds, 
     return true;
 }
 
-template <int DB, int NP>
+template <int DB, int NP, bool FULL>
 __global__ void __launch_bounds__(128 * NP, 2) bwd_kv_kernel(Args A)
 {
     __shared__ __attribute__((aligned(1024))) uint8_t smem[kBytesKV<DB, NP>];
@@ -537,15 +547,15 @@ __global__ void __launch_bounds__(128 * NP, 2) bwd_kv_kernel(Args A)
     if (!item_of(blockIdx.x, A.tiles, A.Hk, 1, rank, hk, g) ||
         !span_of(A, A.ks, A.Tk, rank, 32 * NP, true, S, b, j0))
         return;
-    if (A.D != 32 * DB)
+    if (!FULL)
         zero_lds<3 * kStageKV<DB>>(lds, 128 * NP);
     const int i0 = max(j0 - S.off, 0);
     const int i1 = min(min(j0 + 32 * NP, S.lk) - 2 + A.window - S.off, S.lq - 1);
-    if (!backward_kv<DB, NP, false, false>(A, lds, S, j0, i0, i1, hk, b, 0))
-        backward_kv<DB, NP, false, true>(A, lds, S, j0, i0, i1, hk, b, 0);
+    if (!backward_kv<DB, NP, FULL, false, false>(A, lds, S, j0, i0, i1, hk, b, 0))
+        backward_kv<DB, NP, FULL, false, true>(A, lds, S, j0, i0, i1, hk, b, 0);
 }
 
-template <int DB>
+template <int DB, bool FULL>
 __global__ void __launch_bounds__(128, 2) bwd_far_kernel(Args A)
 {
     __shared__ __attribute__((aligned(1024))) uint8_t smem[kBytesKV<DB, 1>];
@@ -559,22 +569,39 @@ __global__ void __launch_bounds__(128, 2) bwd_far_kernel(Args A)
     i0 = max(i0, j0 + A.window - S.off);
     if (j0 >= S.lk || i0 > i1)
         return;
-    if (A.D != 32 * DB)
+    if (!FULL)
         zero_lds<3 * kStageKV<DB>>(lds, 128);
-    if (!backward_kv<DB, 1, true, false>(A, lds, S, j0, i0, i1, hk, b, blockIdx.x))
-        backward_kv<DB, 1, true, true>(A, lds, S, j0, i0, i1, hk, b, blockIdx.x);
+    if (!backward_kv<DB, 1, FULL, true, false>(A, lds, S, j0, i0, i1, hk, b, blockIdx.x))
+        backward_kv<DB, 1, FULL, true, true>(A, lds, S, j0, i0, i1, hk, b, blockIdx.x);
 }
 
 // ------------------------------------------------------------------- host --
 
-template <int DB, int NW> void launch_fwd(Args &A, hipStream_t st)
+enum Kind { FWD, BWD_Q, BWD_KV, BWD_FAR };
+
+template <Kind K, int DB, bool FULL> void launch_full(const Args &A, dim3 grid, hipStream_t st)
 {
-    hipLaunchKernelGGL((fwd_kernel<DB, NW>), dim3((unsigned)items(A.tiles, A.Hk, A.G)), dim3(64 * NW), 0, st, A);
+    if constexpr (K == FWD)
+        hipLaunchKernelGGL((fwd_kernel<DB, 8, FULL>), grid, dim3(512), 0, st, A);
+    else if constexpr (K == BWD_Q)
+        hipLaunchKernelGGL((bwd_q_kernel<DB, 8, FULL>), grid, dim3(512), 0, st, A);
+    else if constexpr (K == BWD_KV)
+        hipLaunchKernelGGL((bwd_kv_kernel<DB, 4, FULL>), grid, dim3(512), 0, st, A);
+    else
+        hipLaunchKernelGGL((bwd_far_kernel<DB, FULL>), grid, dim3(128), 0, st, A);
 }
 
-template <int DB, int NW> void launch_bwd_q(Args &A, hipStream_t st)
+template <Kind K> void launch(const Args &A, dim3 grid, hipStream_t st)
 {
-    hipLaunchKernelGGL((bwd_q_kernel<DB, NW>), dim3((unsigned)items(A.tiles, A.Hk, A.G)), dim3(64 * NW), 0, st, A);
+    switch (A.D) {
+    case 64: launch_full<K, 2, true>(A, grid, st); break;
+    case 96: launch_full<K, 3, true>(A, grid, st); break;
+    case 128: launch_full<K, 4, true>(A, grid, st); break;
+    default:
+        A.D < 64   ? launch_full<K, 2, false>(A, grid, st)
+        : A.D < 96 ? launch_full<K, 3, false>(A, grid, st)
+                   : launch_full<K, 4, false>(A, grid, st);
+    }
 }
 
 // tiles of R rows that T rows of B sequences may have, numbered as span_of does
@@ -688,11 +715,7 @@ mx_status window_attn_fwd(const mx_heads *q, const mx_heads *k, const mx_heads *
     A.out = out_of(out);
     A.lse_out = lse;
     A.tiles = (int)mxa::tiles_of(Tq, 256, sequences, q_start != nullptr);
-    switch (mxa::blocks_of(D)) {
-    case 2: mxa::launch_fwd<2, 8>(A, stream); break;
-    case 3: mxa::launch_fwd<3, 8>(A, stream); break;
-    default: mxa::launch_fwd<4, 8>(A, stream); break;
-    }
+    mxa::launch<mxa::FWD>(A, dim3((unsigned)mxa::items(A.tiles, A.Hk, A.G)), stream);
     return launched();
 }
 
@@ -727,7 +750,6 @@ mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_
         return fail(MX_EINVAL, "lse must be given, 4-byte aligned, and a 256-byte aligned workspace of %zu bytes", need);
     mxa::Args A = arguments(q, k, v, Tq, Tk, D, q_start, k_start, sequences, window, sinks, scale);
     const bool packed = q_start != nullptr;
-    const int DB = (int)mxa::blocks_of(D);
     if (Tq > 0) {
         A.go = in_of(grad_out);
         A.o = in_of(out);
@@ -738,30 +760,17 @@ mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_
         A.chunk = (int)mxa::chunk_of(Tq);
         A.out = out_of(grad_q);
         A.tiles = (int)mxa::tiles_of(Tq, 256, sequences, packed);
-        switch (DB) {
-        case 2: mxa::launch_bwd_q<2, 8>(A, stream); break;
-        case 3: mxa::launch_bwd_q<3, 8>(A, stream); break;
-        default: mxa::launch_bwd_q<4, 8>(A, stream); break;
-        }
+        mxa::launch<mxa::BWD_Q>(A, dim3((unsigned)mxa::items(A.tiles, A.Hk, A.G)), stream);
     }
     if (Tk > 0) {
         A.gk = out_of(grad_k);
         A.gv = out_of(grad_v);
         if (Tq > 0 && A.sinks > 0) {
             const dim3 grid((unsigned)mxa::tiles_of(Tq, A.chunk, sequences, packed), (unsigned)A.Hk, (unsigned)((A.sinks + 31) / 32));
-            switch (DB) {
-            case 2: hipLaunchKernelGGL((mxa::bwd_far_kernel<2>), grid, dim3(128), 0, stream, A); break;
-            case 3: hipLaunchKernelGGL((mxa::bwd_far_kernel<3>), grid, dim3(128), 0, stream, A); break;
-            default: hipLaunchKernelGGL((mxa::bwd_far_kernel<4>), grid, dim3(128), 0, stream, A); break;
-            }
+            mxa::launch<mxa::BWD_FAR>(A, grid, stream);
         }
         A.tiles = (int)mxa::tiles_of(Tk, 128, sequences, packed);
-        const dim3 grid((unsigned)mxa::items(A.tiles, A.Hk, 1));
-        switch (DB) {
-        case 2: hipLaunchKernelGGL((mxa::bwd_kv_kernel<2, 4>), grid, dim3(512), 0, stream, A); break;
-        case 3: hipLaunchKernelGGL((mxa::bwd_kv_kernel<3, 4>), grid, dim3(512), 0, stream, A); break;
-        default: hipLaunchKernelGGL((mxa::bwd_kv_kernel<4, 4>), grid, dim3(512), 0, stream, A); break;
-        }
+        mxa::launch<mxa::BWD_KV>(A, dim3((unsigned)mxa::items(A.tiles, A.Hk, 1)), stream);
     }
     return launched();
 }
