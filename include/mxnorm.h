@@ -529,11 +529,11 @@ mx_status window_attn_fwd(const mx_heads *q, const mx_heads *k, const mx_heads *
  * they were.  grad_q, grad_k and grad_v may be parts of one buffer, and must not
  * overlap an input.
  * `workspace`: caller-owned device memory of window_attn_bwd_workspace_bytes()
- * bytes (of the heads, D, sequences and sinks of the call), 256-byte aligned,
+ * bytes (with the arguments of the call), 256-byte aligned,
  * overwritten; calls that overlap in time need one each.
  */
-size_t window_attn_bwd_workspace_bytes(int64_t Tq, int64_t q_heads, int64_t k_heads, int64_t D,
-                                       int64_t sequences, int64_t sinks);
+size_t window_attn_bwd_workspace_bytes(int64_t Tq, int64_t Tk, int64_t q_heads, int64_t k_heads,
+                                       int64_t D, int64_t sequences, int64_t window, int64_t sinks);
 mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_heads *k, const mx_heads *v,
                           const mx_heads *out, const float *lse, int64_t Tq, int64_t Tk, int64_t D,
                           const int32_t *q_start, const int32_t *k_start, int64_t sequences, int64_t window,

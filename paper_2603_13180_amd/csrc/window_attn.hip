@@ -19,10 +19,11 @@ struct Args {
     const float *lse;     // backward: [Hq, Tq]
     float *lse_out;       // forward: or NULL
     float *lse2, *delta;  // backward: lse log2(e), grad_o . o, [Hq, Tq]
-    float *part;          // backward: the sinks' sums over queries far behind them
+    float *far;           // backward: the sinks' sums over queries far behind them, by chunk and share
+    float *near;          // with shares of near queries: their sums
     const int *qs, *ks;   // [B + 1], or NULL: one sequence
     int Tq, Tk, B, Hk, G, D;
-    int tiles, window, sinks, chunk;
+    int tiles, window, sinks, chunk, far_shares, shares;
     float c, scale;       // scale log2(e), scale
 };
 
@@ -346,18 +347,39 @@ __global__ void __launch_bounds__(64 * NW, 2) bwd_q_kernel(Args A)
         backward_q<DB, NW, FULL, true>(A, lds, S, i0, hk, hk * A.G + g);
 }
 
-// The sinks' sums over queries that lie the window or more behind: chunk `at`
-// (numbered as tiles are) of block kb of 32 keys, one plane each for grad_k and
-// grad_v, in the order in which a wave holds them.
-template <int DB> __device__ __forceinline__ float *far_part(const Args &A, int at, int hk, int kb)
+// Sums of 32 keys as the waves hold them: a plane each for grad_k and grad_v.
+template <int DB> constexpr int kPlane = DB * 16 * 64;
+
+// Of block kb of the sinks, over share s of the queries of chunk `at` (numbered as
+// tiles are) that lie the window or more behind.
+template <int DB> __device__ __forceinline__ float *far_part(const Args &A, int at, int hk, int kb, int s)
 {
     const int blocks = (A.sinks + 31) / 32;
-    return A.part + (((int64_t)at * A.Hk + hk) * blocks + kb) * (2 * DB * 16 * 64);
+    return A.far + ((((int64_t)at * A.Hk + hk) * blocks + kb) * A.far_shares + s) * (2 * kPlane<DB>);
 }
 
-// grad_k and grad_v of 32 keys for each of NP pairs of waves, from queries i0 .. i1
-// of every head of the group.  FAR: those that see them as sinks, not through the
-// window.
+// Of key block `at` (numbered as tiles of 32), over share s of its near queries.
+template <int DB> __device__ __forceinline__ float *near_part(const Args &A, int at, int hk, int s)
+{
+    return A.near + (((int64_t)at * A.Hk + hk) * A.shares + s) * (2 * kPlane<DB>);
+}
+
+// The chunks with far queries of sink block jw: first and last, and the number of chunk 0.
+struct Chunks {
+    int first, last, at;
+    __device__ __forceinline__ Chunks(const Args &A, const Span &S, int b, int jw)
+    {
+        const int i = max(jw + A.window - S.off, 0);
+        const bool any = jw < A.sinks && i < S.lq;
+        first = any ? i / A.chunk : 0;
+        last = any ? (S.lq - 1) / A.chunk : -1;
+        at = S.q0 / A.chunk + (A.qs ? b : 0);
+    }
+};
+
+// grad_k and grad_v of 32 keys for each of NP pairs of waves, from share `share` of
+// `shares` of the tiles of queries i0 .. i1 of the group's heads, one head behind the
+// other.  FAR: those that see them as sinks, not through the window.
 //
 // A wave has registers for one of the two sums at two waves a SIMD.  So of a pair
 // the first wave forms the scores, P and grad_v += grad_out^T P, and the second, a
@@ -369,17 +391,20 @@ template <int DB> constexpr int kStageKV = 2 * BK * kRow<DB> + 8 * BK;
 template <int DB, int NP> constexpr int kBytesKV = 3 * kStageKV<DB> + NP * 2 * BK * 96;
 template <int DB, int NP, bool FULL, bool FAR, bool CAREFUL>
 __device__ __forceinline__ bool backward_kv(const Args &A, LDS_AS uint8_t *lds, const Span &S, int j0, int i0, int i1, int hk,
-                                            int b, int chunk)
+                                            int b, int chunk, int share, int shares)
 {
     constexpr int TILE = BK * kRow<DB>, STAGE = kStageKV<DB>, NW = 2 * NP;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, h = l >> 5;
+    const int thread = thread_number<CAREFUL>();
+    const int w = __builtin_amdgcn_readfirstlane(thread >> 6), l = thread & 63, n = l & 31, h = l >> 5;
     const int pair = w % NP, second = w / NP;
     const uint32_t base = lds_address(lds);
     const Lane<DB> L(l);
-    const int steps = i1 < i0 ? 0 : (i1 - i0) / BK + 1, total = steps * A.G;
+    const int steps = i1 < i0 ? 0 : (i1 - i0) / BK + 1;
+    const int from = (int)((int64_t)steps * A.G * share / shares), total = (int)((int64_t)steps * A.G * (share + 1) / shares) - from;
+    const int u0 = steps ? from % steps : 0;
     using Load = Loader<DB, BK, NW, FULL>;
     const Load ql(A.q.ts, A.D, w, l), gl(A.go.ts, A.D, w, l);
-    int lr = i0, lq = hk * A.G; // of the tile to load next: first query, head
+    int lr = i0 + u0 * BK, lq = hk * A.G + (steps ? from / steps : 0); // of the tile to load next: first query, head
     auto load = [&](int stage) { // the next one
         const uint32_t to = base + stage * STAGE;
         ql.load(A.q.p + S.q0 * A.q.ts + lq * A.q.hs, lr, i1, to, l);
@@ -493,7 +518,7 @@ __device__ __forceinline__ bool backward_kv(const Args &A, LDS_AS uint8_t *lds, 
     };
     if (total > 0)
         load(0);
-    int stage = second ? 2 : 0, next = 1, u = second ? -1 : 0; // the wave's stage and tile; the stage to load next
+    int stage = second ? 2 : 0, next = 1, u = u0 - second; // the wave's stage and tile; the stage to load next
     for (int it = 0; it <= total; ++it) {
         wait_vmcnt<0>();
         barrier();
@@ -509,10 +534,12 @@ __device__ __forceinline__ bool backward_kv(const Args &A, LDS_AS uint8_t *lds, 
         return false;
     if (CAREFUL)
         __syncthreads();
-    // planes of the far sums: grad_k's, grad_v's
-    const int plane = second ? 0 : DB * 16 * 64;
-    if constexpr (FAR) {
-        float *to = far_part<DB>(A, chunk, hk, j0 / 32) + plane + l;
+    const int plane = second ? 0 : kPlane<DB>;
+    if (FAR || shares > 1) {
+        if (jw >= S.lk)
+            return true;
+        float *to = (FAR ? far_part<DB>(A, chunk, hk, j0 / 32, share)
+                         : near_part<DB>(A, (A.ks ? S.k0 / 32 + b : 0) + jw / 32, hk, share)) + plane + l;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -520,16 +547,17 @@ __device__ __forceinline__ bool backward_kv(const Args &A, LDS_AS uint8_t *lds, 
                 to[(d * 16 + e) * 64] = acc[d][e];
         return true;
     }
-    if (jw < S.lk && jw < A.sinks && max(jw + A.window - S.off, 0) < S.lq) { // add the sums that the sinks have from far queries
-        const int at = S.q0 / A.chunk + b;
-        for (int c = max(jw + A.window - S.off, 0) / A.chunk; c <= (S.lq - 1) / A.chunk; ++c) {
-            const float *from = far_part<DB>(A, at + c, hk, jw / 32) + plane + l;
+    if (jw < S.lk) { // add the sums that sinks have from far queries
+        const Chunks C(A, S, b, jw);
+        for (int c = C.first; c <= C.last; ++c)
+            for (int f = 0; f < A.far_shares; ++f) {
+                const float *from = far_part<DB>(A, C.at + c, hk, jw / 32, f) + plane + l;
 #pragma unroll
-            for (int d = 0; d < DB; ++d)
+                for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    acc[d][e] += from[(d * 16 + e) * 64];
-        }
+                    for (int e = 0; e < 16; ++e)
+                        acc[d][e] += from[(d * 16 + e) * 64];
+            }
     }
     const Out &to = second ? A.gk : A.gv;
     store_rows<DB>(acc, second ? A.scale : 1.0f, lds + w * 32 * kRow<DB>,
@@ -542,17 +570,56 @@ __global__ void __launch_bounds__(128 * NP, 2) bwd_kv_kernel(Args A)
 {
     __shared__ __attribute__((aligned(1024))) uint8_t smem[kBytesKV<DB, NP>];
     LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
-    int rank, hk, g, b, j0;
+    int rank, hk, share, b, j0;
     Span S;
-    if (!item_of(blockIdx.x, A.tiles, A.Hk, 1, rank, hk, g) ||
+    if (!item_of(blockIdx.x, A.tiles, A.Hk, A.shares, rank, hk, share) ||
         !span_of(A, A.ks, A.Tk, rank, 32 * NP, true, S, b, j0))
         return;
     if (!FULL)
         zero_lds<3 * kStageKV<DB>>(lds, 128 * NP);
     const int i0 = max(j0 - S.off, 0);
     const int i1 = min(min(j0 + 32 * NP, S.lk) - 2 + A.window - S.off, S.lq - 1);
-    if (!backward_kv<DB, NP, FULL, false, false>(A, lds, S, j0, i0, i1, hk, b, 0))
-        backward_kv<DB, NP, FULL, false, true>(A, lds, S, j0, i0, i1, hk, b, 0);
+    if (!backward_kv<DB, NP, FULL, false, false>(A, lds, S, j0, i0, i1, hk, b, 0, share, A.shares))
+        backward_kv<DB, NP, FULL, false, true>(A, lds, S, j0, i0, i1, hk, b, 0, share, A.shares);
+}
+
+// The shares of 32 keys' sums added in order, near queries' and then far ones', and
+// rounded: wave d of a plane's DB takes its elements 32 d ..
+template <int DB> __global__ void __launch_bounds__(128 * DB) bwd_sum_kernel(Args A)
+{
+    const int w = threadIdx.x >> 6, l = threadIdx.x & 63, n = l & 31, h = l >> 5, d = w % DB;
+    const bool key = w < DB; // grad_k
+    const int hk = blockIdx.y;
+    int b, jw;
+    Span S;
+    if (!span_of(A, A.ks, A.Tk, blockIdx.x, 32, true, S, b, jw))
+        return;
+    const int at = (key ? 0 : kPlane<DB>) + d * 1024 + l;
+    float acc[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        acc[e] = 0.0f;
+#pragma unroll 4
+    for (int s = 0; s < A.shares; ++s)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            acc[e] += near_part<DB>(A, blockIdx.x, hk, s)[at + e * 64];
+    const Chunks C(A, S, b, jw);
+    for (int c = C.first; c <= C.last; ++c)
+        for (int f = 0; f < A.far_shares; ++f)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                acc[e] += far_part<DB>(A, C.at + c, hk, jw / 32, f)[at + e * 64];
+    if (jw + n >= S.lk)
+        return;
+    const Out &to = key ? A.gk : A.gv;
+    const float by = key ? A.scale : 1.0f;
+    uint16_t *row = to.p + (int64_t)(S.k0 + jw + n) * to.ts + hk * to.hs + 32 * d + 4 * h;
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+        if (32 * d + 8 * g + 4 * h < A.D)
+            *reinterpret_cast<u32x2 *>(row + 8 * g) = u32x2{pack_bf16(acc[4 * g] * by, acc[4 * g + 1] * by),
+                                                            pack_bf16(acc[4 * g + 2] * by, acc[4 * g + 3] * by)};
 }
 
 template <int DB, bool FULL>
@@ -562,7 +629,7 @@ __global__ void __launch_bounds__(128, 2) bwd_far_kernel(Args A)
     LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
     int b, i0;
     Span S;
-    const int hk = blockIdx.y, j0 = 32 * blockIdx.z;
+    const int hk = blockIdx.y / A.far_shares, share = blockIdx.y % A.far_shares, j0 = 32 * blockIdx.z;
     if (!span_of(A, A.qs, A.Tq, blockIdx.x, A.chunk, false, S, b, i0))
         return;
     const int i1 = min(i0 + A.chunk, S.lq) - 1;
@@ -571,24 +638,30 @@ __global__ void __launch_bounds__(128, 2) bwd_far_kernel(Args A)
         return;
     if (!FULL)
         zero_lds<3 * kStageKV<DB>>(lds, 128);
-    if (!backward_kv<DB, 1, FULL, true, false>(A, lds, S, j0, i0, i1, hk, b, blockIdx.x))
-        backward_kv<DB, 1, FULL, true, true>(A, lds, S, j0, i0, i1, hk, b, blockIdx.x);
+    if (!backward_kv<DB, 1, FULL, true, false>(A, lds, S, j0, i0, i1, hk, b, blockIdx.x, share, A.far_shares))
+        backward_kv<DB, 1, FULL, true, true>(A, lds, S, j0, i0, i1, hk, b, blockIdx.x, share, A.far_shares);
 }
 
 // ------------------------------------------------------------------- host --
 
-enum Kind { FWD, BWD_Q, BWD_KV, BWD_FAR };
+enum Kind { FWD, FWD_SMALL, BWD_Q, BWD_Q_SMALL, BWD_KV, BWD_FAR, BWD_SUM };
 
 template <Kind K, int DB, bool FULL> void launch_full(const Args &A, dim3 grid, hipStream_t st)
 {
     if constexpr (K == FWD)
         hipLaunchKernelGGL((fwd_kernel<DB, 8, FULL>), grid, dim3(512), 0, st, A);
+    else if constexpr (K == FWD_SMALL)
+        hipLaunchKernelGGL((fwd_kernel<DB, 4, FULL>), grid, dim3(256), 0, st, A);
     else if constexpr (K == BWD_Q)
         hipLaunchKernelGGL((bwd_q_kernel<DB, 8, FULL>), grid, dim3(512), 0, st, A);
+    else if constexpr (K == BWD_Q_SMALL)
+        hipLaunchKernelGGL((bwd_q_kernel<DB, 4, FULL>), grid, dim3(256), 0, st, A);
     else if constexpr (K == BWD_KV)
         hipLaunchKernelGGL((bwd_kv_kernel<DB, 4, FULL>), grid, dim3(512), 0, st, A);
-    else
+    else if constexpr (K == BWD_FAR)
         hipLaunchKernelGGL((bwd_far_kernel<DB, FULL>), grid, dim3(128), 0, st, A);
+    else
+        hipLaunchKernelGGL((bwd_sum_kernel<DB>), grid, dim3(128 * DB), 0, st, A);
 }
 
 template <Kind K> void launch(const Args &A, dim3 grid, hipStream_t st)
@@ -622,6 +695,45 @@ inline int64_t chunk_of(int64_t Tq)
 inline int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
 inline int64_t row_bytes(int64_t Tq, int64_t Hq) { return round256(4 * Tq * Hq); }
 inline int64_t blocks_of(int64_t D) { return D <= 64 ? 2 : D <= 96 ? 3 : 4; }
+
+// A launch of tiles of queries: 256 a workgroup, or 128 where that leaves compute
+// units without one.
+template <Kind LARGE, Kind SMALL> void launch_queries(Args &A, hipStream_t st)
+{
+    const bool packed = A.qs != nullptr;
+    const bool small = tiles_of(A.Tq, 256, A.B, packed) * A.Hk * A.G <= 192;
+    A.tiles = (int)tiles_of(A.Tq, small ? 128 : 256, A.B, packed);
+    const dim3 grid((unsigned)items(A.tiles, A.Hk, A.G));
+    small ? launch<SMALL>(A, grid, st) : launch<LARGE>(A, grid, st);
+}
+
+// Shares of the queries that a block of 128 keys, and the sinks' far sums of a chunk,
+// are summed over.  A tile of 64 queries takes a workgroup about 1.8 us, and few
+// workgroups leave compute units idle; but shares are written, read and added (about
+// 4 us and 0.5 us a MB).
+struct BwdPlan {
+    int shares, far_shares;
+};
+
+inline BwdPlan bwd_plan(int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hk, int64_t D, int64_t B, int64_t window, int64_t sinks)
+{
+    BwdPlan P{1, 1};
+    const int64_t G = Hq / Hk, tiles = tiles_of(Tk, 128, B, true) * Hk;
+    const int64_t length = std::max<int64_t>(Tq / B, 1), seen = window > 0 ? std::min(window + 128, length) : length;
+    const double steps = (double)(G * (seen / BK + 1)), mb = (double)tiles * 4 * blocks_of(D) * 8e-3;
+    double best = 1e30;
+    for (int s = 1; s <= 8 && (s == 1 || tiles < 192); ++s) {
+        const double rounds = (double)((tiles * s + 255) / 256);
+        const double us = rounds * (steps / s * 1.8 + 4) + (s > 1 ? 4 + 0.5 * s * mb : 0);
+        if (us < 0.95 * best) {
+            best = us;
+            P.shares = s;
+        }
+    }
+    const int64_t far = tiles_of(Tq, chunk_of(Tq), B, true) * Hk * std::max<int64_t>((sinks + 31) / 32, 1);
+    P.far_shares = (int)std::max<int64_t>(std::min<int64_t>(256 / far, 8), 1);
+    return P;
+}
 
 } // namespace mxa
 
@@ -714,18 +826,22 @@ mx_status window_attn_fwd(const mx_heads *q, const mx_heads *k, const mx_heads *
     mxa::Args A = arguments(q, k, v, Tq, Tk, D, q_start, k_start, sequences, window, sinks, scale);
     A.out = out_of(out);
     A.lse_out = lse;
-    A.tiles = (int)mxa::tiles_of(Tq, 256, sequences, q_start != nullptr);
-    mxa::launch<mxa::FWD>(A, dim3((unsigned)mxa::items(A.tiles, A.Hk, A.G)), stream);
+    mxa::launch_queries<mxa::FWD, mxa::FWD_SMALL>(A, stream);
     return launched();
 }
 
-size_t window_attn_bwd_workspace_bytes(int64_t Tq, int64_t q_heads, int64_t k_heads, int64_t D, int64_t sequences, int64_t sinks)
+size_t window_attn_bwd_workspace_bytes(int64_t Tq, int64_t Tk, int64_t q_heads, int64_t k_heads, int64_t D, int64_t sequences,
+                                       int64_t window, int64_t sinks)
 {
-    if (Tq <= 0 || Tq > MX_ATTN_MAX_TOKENS || q_heads < 1 || q_heads > 4096 || k_heads < 1 || k_heads > q_heads || D < 1 ||
-        D > MX_ATTN_MAX_D || sequences < 1 || sequences > 1 << 20 || sinks < 0 || sinks > MX_ATTN_MAX_SINKS)
+    if (Tq <= 0 || Tq > MX_ATTN_MAX_TOKENS || Tk < 0 || Tk > MX_ATTN_MAX_TOKENS || q_heads < 1 || q_heads > 4096 || k_heads < 1 ||
+        k_heads > q_heads || D < 1 || D > MX_ATTN_MAX_D || sequences < 1 || sequences > 1 << 20 || window < 0 || sinks < 0 ||
+        sinks > MX_ATTN_MAX_SINKS)
         return 0;
-    const int64_t slots = mxa::tiles_of(Tq, mxa::chunk_of(Tq), sequences, true) + 1;
-    return 2 * mxa::row_bytes(Tq, q_heads) + slots * k_heads * ((sinks + 31) / 32) * mxa::blocks_of(D) * (2 * 16 * 64 * 4);
+    const mxa::BwdPlan P = mxa::bwd_plan(Tq, Tk, q_heads, k_heads, D, sequences, window, sinks);
+    const int64_t block = mxa::blocks_of(D) * (2 * 16 * 64 * 4);
+    const int64_t far = mxa::tiles_of(Tq, mxa::chunk_of(Tq), sequences, true) + 1;
+    const int64_t near = P.shares > 1 ? mxa::tiles_of(Tk, 32, sequences, true) + 1 : 0;
+    return 2 * mxa::row_bytes(Tq, q_heads) + k_heads * block * (far * ((sinks + 31) / 32) * P.far_shares + near * P.shares);
 }
 
 mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_heads *k, const mx_heads *v,
@@ -745,7 +861,7 @@ mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_
         (st = check_heads(grad_k, "grad_k", Tk, D, k->heads, true)) != MX_OK ||
         (st = check_heads(grad_v, "grad_v", Tk, D, k->heads, true)) != MX_OK)
         return st;
-    const size_t need = window_attn_bwd_workspace_bytes(Tq, q->heads, k->heads, D, sequences, sinks);
+    const size_t need = window_attn_bwd_workspace_bytes(Tq, Tk, q->heads, k->heads, D, sequences, window, sinks);
     if (Tq > 0 && (!lse || !aligned(lse, 4) || !workspace || !aligned(workspace, 256) || workspace_bytes < need))
         return fail(MX_EINVAL, "lse must be given, 4-byte aligned, and a 256-byte aligned workspace of %zu bytes", need);
     mxa::Args A = arguments(q, k, v, Tq, Tk, D, q_start, k_start, sequences, window, sinks, scale);
@@ -756,21 +872,28 @@ mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_
         A.lse = lse;
         A.lse2 = static_cast<float *>(workspace);
         A.delta = A.lse2 + mxa::row_bytes(Tq, q->heads) / 4;
-        A.part = A.delta + mxa::row_bytes(Tq, q->heads) / 4;
         A.chunk = (int)mxa::chunk_of(Tq);
+        const mxa::BwdPlan P = mxa::bwd_plan(Tq, Tk, q->heads, k->heads, D, sequences, window, sinks);
+        A.shares = P.shares;
+        A.far_shares = P.far_shares;
+        A.far = A.delta + mxa::row_bytes(Tq, q->heads) / 4;
+        A.near = A.far + (mxa::tiles_of(Tq, A.chunk, sequences, true) + 1) * k->heads * ((sinks + 31) / 32) * P.far_shares *
+                             mxa::blocks_of(D) * (2 * 16 * 64);
         A.out = out_of(grad_q);
-        A.tiles = (int)mxa::tiles_of(Tq, 256, sequences, packed);
-        mxa::launch<mxa::BWD_Q>(A, dim3((unsigned)mxa::items(A.tiles, A.Hk, A.G)), stream);
+        mxa::launch_queries<mxa::BWD_Q, mxa::BWD_Q_SMALL>(A, stream);
+    } else {
+        A.chunk = A.shares = A.far_shares = 1;
     }
     if (Tk > 0) {
         A.gk = out_of(grad_k);
         A.gv = out_of(grad_v);
-        if (Tq > 0 && A.sinks > 0) {
-            const dim3 grid((unsigned)mxa::tiles_of(Tq, A.chunk, sequences, packed), (unsigned)A.Hk, (unsigned)((A.sinks + 31) / 32));
-            mxa::launch<mxa::BWD_FAR>(A, grid, stream);
-        }
+        if (Tq > 0 && A.sinks > 0)
+            mxa::launch<mxa::BWD_FAR>(A, dim3((unsigned)mxa::tiles_of(Tq, A.chunk, sequences, packed), (unsigned)(A.Hk * A.far_shares),
+                                              (unsigned)((A.sinks + 31) / 32)), stream);
         A.tiles = (int)mxa::tiles_of(Tk, 128, sequences, packed);
-        mxa::launch<mxa::BWD_KV>(A, dim3((unsigned)mxa::items(A.tiles, A.Hk, 1)), stream);
+        mxa::launch<mxa::BWD_KV>(A, dim3((unsigned)mxa::items(A.tiles, A.Hk, A.shares)), stream);
+        if (A.shares > 1)
+            mxa::launch<mxa::BWD_SUM>(A, dim3((unsigned)mxa::tiles_of(Tk, 32, sequences, packed), (unsigned)A.Hk), stream);
     }
     return launched();
 }

@@ -82,7 +82,7 @@ def load():
         "qk_norm_rope_bwd": (I, [P, P, P, P, P, P, I64, I64, I64, P, P, I, F, P, P, P, P, P,
                                  ctypes.c_size_t, P]),
         "window_attn_fwd": (I, [P, P, P, I64, I64, I64, P, P, I64, I64, I64, F, P, P, P]),
-        "window_attn_bwd_workspace_bytes": (ctypes.c_size_t, [I64, I64, I64, I64, I64, I64]),
+        "window_attn_bwd_workspace_bytes": (ctypes.c_size_t, [I64] * 8),
         "window_attn_bwd": (I, [P, P, P, P, P, P, I64, I64, I64, P, P, I64, I64, I64, F, P, P, P, P,
                                 ctypes.c_size_t, P]),
         "kv_cache_append": (I, [P, P, P, I64, I64, I64, P, I64, P, P, I64, P, P]),
@@ -718,8 +718,8 @@ def qk_norm_rope_bwd(grad_q_out, grad_k_out, q, k, q_gamma, k_gamma, pos, inv_fr
 
 def _starts(t, name, device, n=None):
     """An int32 vector of n elements, if given; None stays None."""
-    if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or t.device != device or not t.is_contiguous()
-                          or (n is not None and t.shape[0] != n)):
+    if t is not None and (t.dtype is not torch.int32 or t.dim() != 1 or t.device != device or not t.is_contiguous()
+                          or (n is not None and len(t) != n)):
         raise ValueError("%s must be a contiguous int32 tensor%s on q's device" % (name, "" if n is None else " [%d]" % n))
     return t
 
@@ -774,7 +774,7 @@ def window_attn_bwd(grad_out, q, k, v, out, lse, window=0, sinks=0, scale=None, 
     grad_k, gk = _new_heads(k) if grad_k is None else (grad_k, _heads(grad_k, "grad_k", k))
     grad_v, gv = _new_heads(v) if grad_v is None else (grad_v, _heads(grad_v, "grad_v", v))
     lib = load()
-    ws_bytes = lib.window_attn_bwd_workspace_bytes(T, Hq, k.shape[1], D, B, sinks)
+    ws_bytes = lib.window_attn_bwd_workspace_bytes(T, S, Hq, k.shape[1], D, B, window, sinks)
     ws = q.new_empty((ws_bytes,), dtype=torch.uint8) if ws_bytes else None
     ref = ctypes.byref
     _call(lib.window_attn_bwd, device, ref(dg), ref(dq), ref(dk), ref(dv), ref(do), _ptr(lse), T, S, D,
@@ -789,33 +789,38 @@ class _Cache(ctypes.Structure):
                 + [("type", ctypes.c_int)])
 
 
-def _paged(t, name, dtype, shape, device):
-    """The page stride of pages whose slots are contiguous."""
-    if t.dtype != dtype or t.shape != shape or t.device != device or not t[:1].is_contiguous():
+def _paged(t, name, dtype, shape, device, page):
+    """The page stride of pages whose slots are contiguous; page: their strides."""
+    strides = t.stride()
+    if t.dtype != dtype or t.shape != shape or t.device != device or (strides[1:] != page and not t[:1].is_contiguous()):
         raise ValueError("%s must be %s %s on q's device, every page contiguous" % (name, dtype, list(shape)))
-    return t.stride(0)
+    return strides[0]
 
 
 def _cache(k_cache, v_cache, k_scales, v_scales, table, length, start, T, D, device):
     """(mx_kv_cache, table width, sequences) of a call."""
-    if k_cache.dim() != 4 or k_cache.dtype not in (torch.bfloat16, torch.uint8):
+    dtype = k_cache.dtype
+    mx = dtype is torch.uint8
+    if k_cache.dim() != 4 or not (mx or dtype is torch.bfloat16):
         raise TypeError("k_cache must be [pages, heads, slots, D], torch.bfloat16, or torch.uint8 for E4M3 codes")
     if not k_cache.is_cuda:
         raise RuntimeError("k_cache must be on the GPU: libmxnorm has no CPU path")
     shape = k_cache.shape
     pages, heads, slots, Dc = shape
-    stride = _paged(k_cache, "k_cache", k_cache.dtype, shape, device)
-    if Dc != D or _paged(v_cache, "v_cache", k_cache.dtype, shape, device) != stride:
+    page = (slots * Dc, Dc, 1)
+    stride = _paged(k_cache, "k_cache", dtype, shape, device, page)
+    if Dc != D or _paged(v_cache, "v_cache", dtype, shape, device, page) != stride:
         raise ValueError("k_cache and v_cache must have the head size of the call and the same pages")
-    mx, scale_stride = k_cache.dtype == torch.uint8, 0
     if mx != (k_scales is not None) or mx != (v_scales is not None):
         raise ValueError("k_scales and v_scales belong to E4M3 codes")
+    scale_stride = 0
     if mx:
-        scales = (pages, heads, slots, D // 32)
-        scale_stride = _paged(k_scales, "k_scales", torch.uint8, scales, device)
-        if _paged(v_scales, "v_scales", torch.uint8, scales, device) != scale_stride:
+        n = D // 32
+        scales, page = (pages, heads, slots, n), (slots * n, n, 1)
+        scale_stride = _paged(k_scales, "k_scales", dtype, scales, device, page)
+        if _paged(v_scales, "v_scales", dtype, scales, device, page) != scale_stride:
             raise ValueError("k_scales and v_scales must have the same pages")
-    if table.dim() != 2 or table.dtype != torch.int32 or table.device != device or not table.is_contiguous():
+    if table.dim() != 2 or table.dtype is not torch.int32 or table.device != device or not table.is_contiguous():
         raise ValueError("table must be a contiguous int32 [sequences, pages] tensor on q's device")
     B, width = table.shape
     _starts(length, "length", device, B)
