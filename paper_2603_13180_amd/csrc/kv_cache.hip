@@ -220,8 +220,8 @@ template <int DB, int RB, bool MX> struct Staged {
             }
             if ((PIECES % (64 * RB) == 0 || p < PIECES) && j0 + r < S.end && (there >> y & 1) && c * (MX ? 16 : 8) < C.D) {
                 const uint32_t off = (uint32_t)((r & 15) * C.D * (MX ? 1 : 2) + c * 16);
-                k[x] = *reinterpret_cast<const u32x4 *>(kp + off);
-                v[x] = *reinterpret_cast<const u32x4 *>(vp + off);
+                k[x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kp + off));
+                v[x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(vp + off));
                 if constexpr (MX) {
                     const uint32_t soff = (uint32_t)((r & 15) * (C.D / 32) + c / 2);
                     sk[x] = ksp[soff];
@@ -274,6 +274,11 @@ template <int DB, int RB, bool MX> struct Staged {
     }
 };
 
+// A workgroup's LDS: the groups' tiles, or their sums when they are joined; the queries.
+template <int DB, int RB>
+constexpr int kQueriesAt = std::max(Shape<RB>::KW * Shape<RB>::STAGES * 2 * Shape<RB>::KEYS * kRow<DB>,
+                                    Shape<RB>::KW > 1 ? Shape<RB>::KW *RB *(DB * 1024 + 96) * 4 : 0);
+
 template <int DB, int RB, bool MX, bool CAREFUL>
 __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds, const LDS_AS int *places, const Rows &S,
                                        int hk, int split, int r0)
@@ -287,21 +292,35 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
     const Lane<DB> L(l);
     const int rw = r0 + 32 * (w % RB), r = min(rw + n, S.R - 1), i = r / A.G, hq = hk * A.G + r % A.G;
     const bool mine = rw + n < S.R;
-    b8 q[2 * DB];
+    // The rows' queries: in registers, or in LDS for the KW groups that share them (the
+    // tiles in flight take the registers).
+    constexpr bool SHARED = RB == 1;
+    LDS_AS uint8_t *const qt = lds + kQueriesAt<DB, RB>;
+    b8 q[SHARED ? 1 : 2 * DB];
     {
         const uint16_t *row = A.q.p + (int64_t)(S.t0 + i) * A.q.ts + hq * A.q.hs;
 #pragma unroll
         for (int ks = 0; ks < 2 * DB; ++ks) {
             const int e = 16 * ks + 8 * h;
             u32x4 x = {0, 0, 0, 0};
-            if (e < C.D)
+            if (e < C.D && (!SHARED || kw == 0))
                 x = *reinterpret_cast<const u32x4 *>(row + e);
-            q[ks] = __builtin_bit_cast(b8, x);
+            if constexpr (!SHARED)
+                q[ks] = __builtin_bit_cast(b8, x);
+            else if (kw == 0)
+                *reinterpret_cast<LDS_AS u32x4 *>(qt + n * kRow<DB> + ((2 * ks + h) ^ swz<DB>(n)) * 16) = x;
         }
     }
+    auto query = [&](int ks) { return SHARED ? row_frag<DB>(qt, L, ks, 0) : q[SHARED ? 0 : ks]; };
+    if (SHARED)
+        __syncthreads();
     const uint64_t all = S.n >= 64 ? ~0ull : (1ull << S.n) - 1;
-    const uint64_t bits = (A.bits ? (uint64_t)A.bits[S.t0 + i] : (2ull << i) - 1) & all;
+    uint64_t bits = (A.bits ? (uint64_t)A.bits[S.t0 + i] : (2ull << i) - 1) & all;
     const int place = S.len + __popcll(bits) - 1;
+    if (A.window < MAX_NEW) // drafted tokens that lie the window before
+        for (int u = 0; u < S.n; ++u)
+            if (place - places[u] >= A.window && places[u] >= A.sinks)
+                bits &= ~(1ull << u);
     // Tiles: the sinks', then from the first key that the window of a token at
     // length - 1 holds.  Row blocks differ in their places, not in their tiles.
     const int first = max(S.len - A.window, 0) / O::KEYS;
@@ -309,16 +328,19 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
     const int tiles = sinks + max((S.end + O::KEYS - 1) / O::KEYS - first, 0);
     const int from = (int)((int64_t)tiles * split / A.splits), to = (int)((int64_t)tiles * (split + 1) / A.splits);
     auto key_of = [&](int t) { return (t < sinks ? t : first + t - sinks) * O::KEYS; };
-    auto sees = [&](int j) {
-        int at = j;
-        if (j >= S.len) {
-            if (j >= S.end || !(bits >> (j - S.len) & 1))
-                return false;
-            at = places[j - S.len];
-        }
-        return place - at < A.window || at < A.sinks;
+    // The keys of a tile that the row sees, a bit each: of the cached ones those of the
+    // window and the sinks, of the drafted ones its bits.
+    auto below = [&](int x) { return x <= 0 ? 0ull : x >= 64 ? ~0ull : (1ull << x) - 1; };
+    auto seen_of = [&](int j0, uint32_t there) {
+        const int to_draft = S.len - j0;
+        uint64_t m = (below(to_draft) & ~below(place - A.window + 1 - j0)) | below(min(A.sinks, S.len) - j0);
+        if (to_draft < 64 && to_draft > -64)
+            m |= to_draft >= 0 ? bits << to_draft : bits >> -to_draft;
+#pragma unroll
+        for (int y = 0; y < O::KEYS / 16; ++y)
+            m &= there >> y & 1 ? ~0ull : ~(0xFFFFull << 16 * y);
+        return m;
     };
-    Staged<DB, RB, MX> next;
     f16v o[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -327,13 +349,22 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
     bool any = false;
     const int rounds = (to - from + O::KW - 1) / O::KW;
     auto tile_of = [&](int it) { return from + it * O::KW + kw; };
-    // the pages of the tile after the one in flight are on their way as well
+    // A tile goes through registers to LDS; DEPTH tiles are in flight, and the pages
+    // of the one after them are on their way as well.  (Codes are half the bytes: with
+    // one tile of them a wave, too little is in flight for the memory's latency.)
+    constexpr int DEPTH = MX && RB == 1 ? 2 : 1;
+    Staged<DB, RB, MX> staged[DEPTH];
     const int last = max(to - 1, from);
     Pages<RB> pages(S, C.shift, key_of(min(tile_of(0), last)));
-    if (tile_of(0) < to)
-        next.load(C, S, pages, hk, key_of(tile_of(0)), in_group);
-    pages = Pages<RB>(S, C.shift, key_of(min(tile_of(1), last)));
-    for (int it = 0; it < rounds; ++it) {
+    auto load = [&](Staged<DB, RB, MX> &next, int it) {
+        if (tile_of(it) < to)
+            next.load(C, S, pages, hk, key_of(tile_of(it)), in_group);
+        pages = Pages<RB>(S, C.shift, key_of(min(tile_of(it + 1), last)));
+    };
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+        load(staged[d], d);
+    auto step = [&](Staged<DB, RB, MX> &next, int it) __attribute__((always_inline)) {
         const int t = tile_of(it);
         LDS_AS uint8_t *kt = lds + kw * GROUP + (O::STAGES == 2 ? (it & 1) * 2 * TILE : 0), *vt = kt + TILE;
         const uint32_t there = next.there;
@@ -341,16 +372,14 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
             next.store(kt, in_group);
         if (RB > 1)
             __syncthreads();
-        if (tile_of(it + 1) < to) {
-            next.load(C, S, pages, hk, key_of(tile_of(it + 1)), in_group);
-            pages = Pages<RB>(S, C.shift, key_of(min(tile_of(it + 2), last)));
-        }
+        load(next, it + DEPTH);
         if (t >= to || rw >= S.R)
-            continue;
+            return;
         const int j0 = key_of(t);
         const bool full = j0 + O::KEYS <= S.len && there == (1u << O::KEYS / 16) - 1 &&
                           S.len + S.n - 1 - j0 < A.window;
-        auto seen = [&](int x) { return (there >> (x >> 4) & 1) && sees(j0 + x); };
+        const uint64_t keys = full ? ~0ull : seen_of(j0, there);
+        auto seen = [&](int x) { return (keys >> x & 1) != 0; };
         f16v s[O::NB];
 #pragma unroll
         for (int x = 0; x < O::NB; ++x)
@@ -359,17 +388,16 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
         for (int ks = 0; ks < 2 * DB; ++ks)
 #pragma unroll
             for (int x = 0; x < O::NB; ++x)
-                s[x] = mfma(row_frag<DB>(kt, L, ks, x), q[ks], s[x]);
-        if (!full)
+                s[x] = mfma(row_frag<DB>(kt, L, ks, x), query(ks), s[x]);
+        if (!full) {
+            const uint64_t half = keys >> (4 * h);
 #pragma unroll
             for (int x = 0; x < O::NB; ++x)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const bool see = seen(32 * x + c_row(e, h));
-                    s[x][e] = see ? s[x][e] : -INFINITY;
-                    any |= see;
-                }
-        any |= full;
+                for (int e = 0; e < 16; ++e)
+                    s[x][e] = (uint32_t)(half >> 32 * x) & 1u << c_row(e, 0) ? s[x][e] : -INFINITY;
+        }
+        any |= O::KEYS == 64 ? keys != 0 : (uint32_t)keys != 0;
         float mt = -INFINITY;
 #pragma unroll
         for (int x = 0; x < O::NB; ++x)
@@ -396,7 +424,12 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
             careful_products<DB, O::NB>(o, vt, L, s, h, seen);
         else
             products<DB, O::NB>(o, vt, L, s);
-    }
+    };
+    for (int it = 0; it < rounds; it += DEPTH)
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d)
+            if (d == 0 || it + d < rounds)
+                step(staged[d], it + d);
     if (!CAREFUL && __syncthreads_or(mine && not_finite<DB>(o)))
         return false;
     if (CAREFUL)
@@ -477,10 +510,7 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
 
 template <int DB, int RB, bool MX> __global__ void __launch_bounds__(64 * Shape<RB>::NW, 2) cached_kernel(CachedArgs A)
 {
-    using O = Shape<RB>;
-    constexpr int TILES = O::KW * O::STAGES * 2 * O::KEYS * kRow<DB>;
-    constexpr int JOIN = O::KW > 1 ? O::KW * RB * (DB * 1024 + 96) * 4 : 0;
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[std::max(TILES, JOIN)];
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[kQueriesAt<DB, RB> + (RB == 1 ? 32 * kRow<DB> : 0)];
     __shared__ int places[MAX_NEW];
     LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
     const Cache &C = A.C;
@@ -588,8 +618,8 @@ inline CachedPlan cached_plan(int64_t B, int64_t Hk, int64_t G, int64_t max_new,
     P.RB = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
     P.blocks = (int)((rows + 32 * P.RB - 1) / (32 * P.RB));
     const int64_t groups = std::max<int64_t>(B * Hk * P.blocks, 1), want = P.RB == 8 ? 512 : 1024;
-    // at least four tiles of 32 keys for each wave of a share
-    const int64_t most = std::max<int64_t>(keys / (P.RB == 1 ? 512 : 256), 1);
+    // at least 256 keys a share
+    const int64_t most = std::max<int64_t>(keys / 256, 1);
     P.splits = (int)std::min<int64_t>(std::min<int64_t>((want + groups - 1) / groups, most), MAX_SPLITS);
     return P;
 }
