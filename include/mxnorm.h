@@ -552,7 +552,7 @@ typedef enum {
  * used with one page), so k and v may be halves of one buffer.  MX_CACHE_E4M3: the
  * codes of mx_cast_fwd along D (RCEIL) and k_scales, v_scales uint8 at page
  * scale_page_stride + (head page_size + slot) D / 32 + block; D a multiple of 32.
- * k and v 16-byte aligned.
+ * k, v, k_scales and v_scales 16-byte aligned, scale_page_stride a multiple of 16.
  *
  * Sequence b's token at place j is in slot j % page_size of page table[b
  * table_width + j / page_size] (int32, device).  A page outside 0 .. pages - 1, or

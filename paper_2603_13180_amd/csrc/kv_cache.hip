@@ -174,16 +174,19 @@ template <int DB, int RB, bool MX> struct Staged {
     static constexpr int PIECES = O::KEYS * PER, N = (PIECES + 64 * RB - 1) / (64 * RB);
     static constexpr int RUNS = O::KEYS / 16;
     u32x4 k[N], v[N];
-    uint32_t sk[N], sv[N]; // scale bytes
-    uint32_t there;        // bit y: run y's page is there
+    u32x4 scales;   // the wave's copy of the tile's scale bytes, 16 a lane: K's rows, V's rows
+    uint32_t there; // bit y: run y's page is there
+    int rows;       // that the tile has
 
     // Keys j0 .. of the tile, those past the end and those of pages that are not
     // there as zeros.  i: the thread's number among those of its group.
     __device__ __forceinline__ void load(const Cache &C, const Rows &S, const Pages<RB> &P, int hk, int j0, int i)
     {
         const uint8_t *kb[RUNS], *vb[RUNS];
-        const uint8_t *ksb[RUNS], *vsb[RUNS];
         there = 0;
+        rows = S.end - j0;
+        if constexpr (MX) // a run's scales lie one behind the other
+            scales = u32x4{0, 0, 0, 0};
 #pragma unroll
         for (int y = 0; y < RUNS; ++y) {
             const bool is = (unsigned)P.id[y] < (unsigned)C.pages;
@@ -194,8 +197,11 @@ template <int DB, int RB, bool MX> struct Staged {
             vb[y] = C.v + at;
             if constexpr (MX) {
                 const int64_t sc = (is ? P.id[y] : 0) * C.page_scales + slot * (C.D / 32);
-                ksb[y] = C.ks + sc;
-                vsb[y] = C.vs + sc;
+                const int n = C.D / 32, l = i & 63, of = l - y * n; // K's run y, then V's behind all of K's
+                if (is && of >= 0 && of < n)
+                    scales = *reinterpret_cast<const u32x4 *>(C.ks + sc + of * 16);
+                if (is && of - RUNS * n >= 0 && of - RUNS * n < n)
+                    scales = *reinterpret_cast<const u32x4 *>(C.vs + sc + (of - RUNS * n) * 16);
             }
         }
 #pragma unroll
@@ -203,30 +209,20 @@ template <int DB, int RB, bool MX> struct Staged {
             constexpr int STEP = 64 * RB / PER; // rows that the group's threads take at once
             const int p = x * 64 * RB + i, r = p / PER, c = p % PER;
             k[x] = v[x] = u32x4{0, 0, 0, 0};
-            sk[x] = sv[x] = 127;
             int y = x * STEP / 16;
-            const uint8_t *kp = kb[y < RUNS ? y : 0], *vp = vb[y < RUNS ? y : 0], *ksp = ksb[y < RUNS ? y : 0], *vsp = vsb[y < RUNS ? y : 0];
+            const uint8_t *kp = kb[y < RUNS ? y : 0], *vp = vb[y < RUNS ? y : 0];
             if constexpr (STEP > 16) { // several runs: the thread's own
                 y = r / 16;
 #pragma unroll
                 for (int z = 0; z < RUNS; ++z) {
                     kp = y == z ? kb[z] : kp;
                     vp = y == z ? vb[z] : vp;
-                    if constexpr (MX) {
-                        ksp = y == z ? ksb[z] : ksp;
-                        vsp = y == z ? vsb[z] : vsp;
-                    }
                 }
             }
             if ((PIECES % (64 * RB) == 0 || p < PIECES) && j0 + r < S.end && (there >> y & 1) && c * (MX ? 16 : 8) < C.D) {
                 const uint32_t off = (uint32_t)((r & 15) * C.D * (MX ? 1 : 2) + c * 16);
                 k[x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kp + off));
                 v[x] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(vp + off));
-                if constexpr (MX) {
-                    const uint32_t soff = (uint32_t)((r & 15) * (C.D / 32) + c / 2);
-                    sk[x] = ksp[soff];
-                    sv[x] = vsp[soff];
-                }
             }
         }
     }
@@ -247,9 +243,15 @@ template <int DB, int RB, bool MX> struct Staged {
         hi = o[1];
     }
 
-    __device__ __forceinline__ void store(LDS_AS uint8_t *tile, int i) const
+    // `area`: the wave's, for scales.
+    __device__ __forceinline__ void store(const Cache &C, LDS_AS uint8_t *tile, LDS_AS uint8_t *area, int i) const
     {
         constexpr int TILE = O::KEYS * kRow<DB>;
+        const int n = C.D / 32;
+        if constexpr (MX) {
+            if ((i & 63) < 2 * RUNS * n)
+                *reinterpret_cast<LDS_AS u32x4 *>(area + (i & 63) * 16) = scales;
+        }
 #pragma unroll
         for (int x = 0; x < N; ++x) {
             const int p = x * 64 * RB + i, r = p / PER, c = p % PER;
@@ -259,10 +261,13 @@ template <int DB, int RB, bool MX> struct Staged {
             if constexpr (MX) {
                 u32x4 lo, hi;
                 const int a = ((2 * c) ^ swz<DB>(r)) * 16, b = ((2 * c + 1) ^ swz<DB>(r)) * 16;
-                decode(k[x], sk[x], lo, hi);
+                // what slots past the end have for scales does not count
+                const bool is = r < rows && c * 16 < C.D;
+                const uint32_t sk = is ? area[r * n + c / 2] : 127, sv = is ? area[(O::KEYS + r) * n + c / 2] : 127;
+                decode(k[x], sk, lo, hi);
                 *reinterpret_cast<LDS_AS u32x4 *>(row + a) = lo;
                 *reinterpret_cast<LDS_AS u32x4 *>(row + b) = hi;
-                decode(v[x], sv[x], lo, hi);
+                decode(v[x], sv, lo, hi);
                 *reinterpret_cast<LDS_AS u32x4 *>(row + TILE + a) = lo;
                 *reinterpret_cast<LDS_AS u32x4 *>(row + TILE + b) = hi;
             } else {
@@ -311,6 +316,7 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
                 *reinterpret_cast<LDS_AS u32x4 *>(qt + n * kRow<DB> + ((2 * ks + h) ^ swz<DB>(n)) * 16) = x;
         }
     }
+    LDS_AS uint8_t *const area = qt + (SHARED ? 32 * kRow<DB> : 0) + w * (O::KEYS * 8);
     auto query = [&](int ks) { return SHARED ? row_frag<DB>(qt, L, ks, 0) : q[SHARED ? 0 : ks]; };
     if (SHARED)
         __syncthreads();
@@ -369,7 +375,7 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
         LDS_AS uint8_t *kt = lds + kw * GROUP + (O::STAGES == 2 ? (it & 1) * 2 * TILE : 0), *vt = kt + TILE;
         const uint32_t there = next.there;
         if (t < to)
-            next.store(kt, in_group);
+            next.store(C, kt, area, in_group);
         if (RB > 1)
             __syncthreads();
         load(next, it + DEPTH);
@@ -510,7 +516,8 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
 
 template <int DB, int RB, bool MX> __global__ void __launch_bounds__(64 * Shape<RB>::NW, 2) cached_kernel(CachedArgs A)
 {
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[kQueriesAt<DB, RB> + (RB == 1 ? 32 * kRow<DB> : 0)];
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[kQueriesAt<DB, RB> + (RB == 1 ? 32 * kRow<DB> : 0) +
+                                                            (MX ? Shape<RB>::NW * Shape<RB>::KEYS * 8 : 0)];
     __shared__ int places[MAX_NEW];
     LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
     const Cache &C = A.C;
@@ -603,6 +610,47 @@ __global__ void __launch_bounds__(256) join_kernel(CachedArgs A)
         u32x2{pack_bf16(o.x * by, o.y * by), pack_bf16(o.z * by, o.w * by)};
 }
 
+// The same for few shares: 32 lanes a row, eight rows a workgroup.
+constexpr int FEW_SPLITS = 16;
+__global__ void __launch_bounds__(256) join_few_kernel(CachedArgs A)
+{
+    const Cache &C = A.C;
+    const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int Hq = A.G * C.Hk, l = threadIdx.x & 31, e = 4 * l;
+    const int64_t t = row / Hq;
+    if (t < first_of(A.start, 0, A.T) || t >= first_of(A.start, C.B, A.T))
+        return;
+    const float2 mine = l < A.splits ? A.stat[row * A.splits + l] : float2{-FLT_MAX, 0.0f};
+    float m = mine.x;
+    for (int x = 8; x; x >>= 1)
+        m = fmaxf(m, __shfl_xor(m, x, 16));
+    m = __shfl(m, 0, 32);
+    // shares without a sum have no weight, and their sums are not there
+    const float w = mine.y == 0.0f || mine.y == -1.0f ? -1.0f : __builtin_amdgcn_exp2f(mine.x - m);
+    float sum = 0.0f;
+    bool any = false;
+    float4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int s = 0; s < A.splits; ++s) {
+        const float by = __shfl(w, s, 32), y = __shfl(mine.y, s, 32);
+        any |= y != 0.0f;
+        if (by == -1.0f)
+            continue;
+        sum = __builtin_fmaf(y, by, sum);
+        if (e < C.D) {
+            const float4 v = *reinterpret_cast<const float4 *>(A.part + (row * A.splits + s) * C.D + e);
+            o.x = __builtin_fmaf(v.x, by, o.x);
+            o.y = __builtin_fmaf(v.y, by, o.y);
+            o.z = __builtin_fmaf(v.z, by, o.z);
+            o.w = __builtin_fmaf(v.w, by, o.w);
+        }
+    }
+    const float by = any ? 1.0f / sum : 0.0f;
+    if (e < C.D)
+        *reinterpret_cast<u32x2 *>(A.out.p + t * A.out.ts + (row - t * Hq) * A.out.hs + e) =
+            u32x2{pack_bf16(o.x * by, o.y * by), pack_bf16(o.z * by, o.w * by)};
+}
+
 // ------------------------------------------------------------------- host --
 
 // Blocks of 32 rows of a workgroup, workgroups a sequence and head takes for its
@@ -664,12 +712,12 @@ mx_status check_cache(const mx_kv_cache *c, int64_t D, const int32_t *table, int
     const int64_t page = c->heads * c->page_size * D;
     if (c->pages > 1 && (c->page_stride < page || c->page_stride % (mx ? 16 : 8) != 0 || c->page_stride > INT64_MAX / 8 / c->pages))
         return fail(MX_EINVAL, "page_stride must be at least heads page_size D elements, whole 16-byte pieces");
-    if (mx && c->pages > 1 && (c->scale_page_stride < page / 32 || c->scale_page_stride > INT64_MAX / 8 / c->pages))
-        return fail(MX_EINVAL, "scale_page_stride must be at least heads page_size D / 32");
+    if (mx && c->pages > 1 && (c->scale_page_stride < page / 32 || c->scale_page_stride % 16 != 0 || c->scale_page_stride > INT64_MAX / 8 / c->pages))
+        return fail(MX_EINVAL, "scale_page_stride must be at least heads page_size D / 32, whole 16-byte pieces");
     if (T == 0 || sequences == 0)
         return MX_OK;
-    if (c->pages > 0 && (!c->k || !c->v || !aligned(c->k, 16) || !aligned(c->v, 16) || (mx && (!c->k_scales || !c->v_scales))))
-        return fail(MX_EINVAL, "the cache's k and v must be non-NULL and 16-byte aligned, its scales given for codes");
+    if (c->pages > 0 && (!c->k || !c->v || !aligned(c->k, 16) || !aligned(c->v, 16) || (mx && (!c->k_scales || !c->v_scales || !aligned(c->k_scales, 16) || !aligned(c->v_scales, 16)))))
+        return fail(MX_EINVAL, "the cache's k and v, and the scales of codes, must be non-NULL and 16-byte aligned");
     if ((width > 0 && !table) || !aligned(table, 4) || !length || !aligned(length, 4) || !aligned(start, 4))
         return fail(MX_EINVAL, "table and length must be non-NULL; table, length and start 4-byte aligned");
     if (!start && T != sequences)
@@ -825,7 +873,9 @@ mx_status kv_cache_attn_fwd(const mx_kv_cache *cache, const mx_heads *q, int64_t
         default: mxa::launch_cached<4, false>(A, P.RB, (unsigned)grid, stream); break;
         }
     }
-    if (P.splits > 1)
+    if (P.splits > 1 && P.splits <= mxa::FEW_SPLITS)
+        hipLaunchKernelGGL(mxa::join_few_kernel, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, stream, A);
+    else if (P.splits > 1)
         hipLaunchKernelGGL(mxa::join_kernel, dim3((unsigned)rows), dim3(256), 0, stream, A);
     return launched();
 }
