@@ -864,6 +864,8 @@ mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_
     const size_t need = window_attn_bwd_workspace_bytes(Tq, Tk, q->heads, k->heads, D, sequences, window, sinks);
     if (Tq > 0 && (!lse || !aligned(lse, 4) || !workspace || !aligned(workspace, 256) || workspace_bytes < need))
         return fail(MX_EINVAL, "lse must be given, 4-byte aligned, and a 256-byte aligned workspace of %zu bytes", need);
+    if (Tq == 0 && Tk == 0)
+        return MX_OK;
     mxa::Args A = arguments(q, k, v, Tq, Tk, D, q_start, k_start, sequences, window, sinks, scale);
     const bool packed = q_start != nullptr;
     if (Tq > 0) {
