@@ -388,3 +388,62 @@ def test_a_prompt_then_steps_then_a_draft():
                            rows=torch.arange(1, 4 * steps, 2, dtype=torch.int32, device=DEV))
     last = torch.tensor([s - 1 for s in st[1:]], device=DEV)
     near(mxnorm.kv_cache_attn_fwd(q[last], kc, vc, table, i32([m - 1 for m in n]), **kw), whole[last])
+
+
+def test_many_sequences_by_length():
+    # long and short ones, taken in the order of their lengths; more than that order covers
+    for n in (40, 300):
+        cached = [(37 * i * i) % 2500 for i in range(n)]
+        c = Case(cached, [1] * n, 4, 2, 64)
+        check(c)
+        check(c, window=300, sinks=2)
+
+
+@pytest.mark.parametrize("mx", [False, True])
+def test_slots_past_the_end_may_hold_anything(mx):
+    # the slots behind the last token, their scales too, are NaN (the case's filling)
+    for n in (1, 17, 33):
+        c = Case([n], [1], 4, 2, 128, page=64, mx=mx)
+        check(c)
+
+
+def test_lengths_that_do_not_fit():
+    # negative, and past the table: no slot outside the cache is read
+    c = Case([40, 50], [1, 1], 4, 2, 64)
+    c.length = i32([-7, 1 << 30])
+    c.run()
+    torch.cuda.synchronize()
+    c.length, want = i32([-7, 50]), i32([0, 50])
+    o = c.run()
+    c.length = want
+    assert torch.equal(o, c.run())
+
+
+def test_starts_that_do_not_fit():
+    c = Case([40, 50], [3, 2], 4, 2, 64, tree=True)
+    for st in ([0, 1 << 30, 5], [3, 0, 5], [-4, 3, 99]):
+        c.start = i32(st)
+        c.run()
+        c.append(c.k[:5], c.v[:5], c.length, c.start)
+    torch.cuda.synchronize()
+
+
+def test_max_new_bounds_what_is_read():
+    # a sequence has more new tokens than max_new says: the rows of the others hold
+    c = Case([20, 30, 40], [2, 9, 2], 4, 2, 64)
+    want = c.run()
+    got = c.run(max_new=2)
+    assert torch.equal(got[:2], want[:2]) and torch.equal(got[11:], want[11:])
+
+
+def test_two_streams_at_once():
+    c, d = Case([3000, 100], [1, 1], 8, 2, 128), Case([2500, 4000], [1, 1], 8, 2, 128, mx=True)
+    want = c.run(), d.run()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            b = d.run()
+        a = c.run()
+        torch.cuda.synchronize()
+        assert torch.equal(a, want[0]) and torch.equal(b, want[1])

@@ -241,3 +241,82 @@ def test_tokens_far_apart():
     assert all(torch.equal(x, y) for x, y in zip(got, c.backward(*want, 0, 0)))
     del buf, q, k, v, out, o, got
     torch.cuda.empty_cache()
+
+
+@gpu
+@pytest.mark.parametrize("Hq,Hk", [(8, 2), (3, 3), (2, 1), (16, 8)])
+@pytest.mark.parametrize("D", [64, 96, 128, 120])
+def test_larger(Hq, Hk, D):
+    # several tiles of queries a head, workgroups of both sizes, shares of a key block's queries
+    check(Case([1500, 700], [1500, 700], Hq, Hk, D), 0, 0)
+    check(Case([1500, 700], [1600, 700], Hq, Hk, D), 300, 20)
+
+
+@gpu
+def test_many_heads():
+    # enough workgroups that none shares a key block's queries
+    check(Case([1100], [1100], 64, 32, 64), 500, 4)
+
+
+@gpu
+def test_two_streams_at_once():
+    c, d = Case([900], [900], 4, 2, 64), Case([800], [800], 4, 2, 64, seed=5)
+    want = []
+    for x in (c, d):
+        o, lse = x.forward(100, 2)
+        want.append([o, lse, *x.backward(o, lse, 100, 2)])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [None, None]
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            o, lse = d.forward(100, 2)
+            got[1] = [o, lse, *d.backward(o, lse, 100, 2)]
+        o, lse = c.forward(100, 2)
+        got[0] = [o, lse, *c.backward(o, lse, 100, 2)]
+    side.synchronize()
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@gpu
+def test_a_row_that_is_used_twice():
+    # queries that share their memory (a stride of 0), keys and values the same heads
+    c = Case([130], [130], 4, 2, 64)
+    q = c.q[:, :1].expand(-1, 4, -1)
+    o, lse = mxnorm.window_attn_fwd(q, c.k, c.k, 50, 2)
+    want = mxnorm.window_attn_fwd(q.contiguous(), c.k, c.k.clone(), 50, 2)
+    assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+    got = mxnorm.window_attn_bwd(c.go, q, c.k, c.k, o, lse, 50, 2)
+    want = mxnorm.window_attn_bwd(c.go, q.contiguous(), c.k, c.k.clone(), o, lse, 50, 2)
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@gpu
+def test_starts_that_do_not_fit():
+    # past the end, descending, negative: no row outside the tensors is touched
+    c = Case([100, 60], [100, 60], 2, 1, 64)
+    for st in ([0, 1 << 30, 160], [0, 200, 50], [-5, 100, 1 << 20], [160, 0, 160]):
+        starts = torch.tensor(st, dtype=torch.int32, device=DEV)
+        o, lse = c.forward(0, 3, q_start=starts)
+        c.backward(o, lse, 20, 3, q_start=starts)
+    torch.cuda.synchronize()
+    check(c, 20, 3)
+
+
+@gpu
+def test_small_heads_and_wide_strides():
+    # tokens 2^24 elements apart take the loads of whole addresses
+    T, far = 70, 1 << 24
+    buf = torch.empty(T * far + 4096, dtype=torch.bfloat16, device=DEV)
+    c = Case([T], [T], 2, 2, 64)
+    k, v = (buf.as_strided((T, 2, 64), (far, 64, 1), 128 * i) for i in range(2))
+    k.copy_(c.k), v.copy_(c.v)
+    o, lse = mxnorm.window_attn_fwd(c.q, k, v)
+    want = c.forward(0, 0)
+    assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+    got = mxnorm.window_attn_bwd(c.go, c.q, k, v, o, lse)
+    assert all(torch.equal(x, y) for x, y in zip(got, c.backward(*want, 0, 0)))
+    del buf, k, v
+    torch.cuda.empty_cache()
