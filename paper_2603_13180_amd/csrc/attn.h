@@ -141,26 +141,28 @@ struct Seen {
     }
 };
 
-// Tiles 0 .. n - 1 through three LDS stages, loads two tiles ahead, one barrier a
-// tile.  LOADS: a wave's loads of a tile.
-template <int LOADS, typename Load, typename Work> __device__ __forceinline__ void tile_loop(int n, Load load, Work work)
+// Tiles 0 .. n - 1 through STAGES LDS stages (2 or 3), loads STAGES - 1 tiles ahead,
+// one barrier a tile.  LOADS: a wave's loads of a tile.
+template <int STAGES, int LOADS, typename Load, typename Work>
+__device__ __forceinline__ void tile_loop(int n, Load load, Work work)
 {
-    if (n > 0)
-        load(0, 0);
-    if (n > 1)
-        load(1, 1);
-    int mine = 0, next = 2; // the stage of tile it, and of tile it + 2
+    constexpr int AHEAD = STAGES - 1;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+        if (i < n)
+            load(i, i);
+    int mine = 0, next = AHEAD; // the stage of tile it, and of tile it + AHEAD
     for (int it = 0; it < n; ++it) {
-        if (it + 1 < n)
+        if (AHEAD > 1 && it + 1 < n)
             wait_vmcnt<LOADS>();
         else
             wait_vmcnt<0>();
         barrier();
-        if (it + 2 < n)
-            load(it + 2, next);
+        if (it + AHEAD < n)
+            load(it + AHEAD, next);
         work(it, mine);
-        mine = mine == 2 ? 0 : mine + 1;
-        next = next == 2 ? 0 : next + 1;
+        mine = mine == AHEAD ? 0 : mine + 1;
+        next = next == AHEAD ? 0 : next + 1;
     }
 }
 

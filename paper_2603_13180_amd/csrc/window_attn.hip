@@ -136,9 +136,17 @@ __device__ __forceinline__ Seen seen_of(const Args &A, const Tiles &T, int p0, i
     return S;
 }
 
+// Waves of a workgroup, 32 queries each.  Two workgroups of four have room on a compute
+// unit, and what one waits for at its barrier the other fills (eight in one, with
+// three stages: 8192 tokens of 32 + 8 heads of 128 567 us, so 552; 5003 of 12 + 4 of
+// 80, window 1000, 41 and 34).
+constexpr int QW = 4;
+// Stages of keys and values: three, or two where that makes the room.
+template <int DB> constexpr int kStages = DB > 2 ? 2 : 3;
+
 // ---------------------------------------------------------------- forward --
 
-template <int DB, int NW, bool FULL, bool CAREFUL>
+template <int DB, bool FULL, bool CAREFUL>
 __device__ __forceinline__ bool forward(const Args &A, LDS_AS uint8_t *lds, const Span &S, int i0, int hk, int hq)
 {
     constexpr int TILE = BK * kRow<DB>;
@@ -147,8 +155,8 @@ __device__ __forceinline__ bool forward(const Args &A, LDS_AS uint8_t *lds, cons
     const uint32_t base = lds_address(lds);
     const Lane<DB> L(l);
     const uint16_t *kh = A.k.p + S.k0 * A.k.ts + hk * A.k.hs, *vh = A.v.p + S.k0 * A.v.ts + hk * A.v.hs;
-    const Tiles tiles(A, i0 + S.off, min(i0 + 32 * NW, S.lq) - 1 + S.off);
-    using Load = Loader<DB, BK, NW, FULL>;
+    const Tiles tiles(A, i0 + S.off, min(i0 + 32 * QW, S.lq) - 1 + S.off);
+    using Load = Loader<DB, BK, QW, FULL>;
     const Load kl(A.k.ts, A.D, w, l), vl(A.v.ts, A.D, w, l);
     auto load = [&](int it, int stage) {
         const uint32_t to = base + stage * 2 * TILE;
@@ -211,7 +219,7 @@ __device__ __forceinline__ bool forward(const Args &A, LDS_AS uint8_t *lds, cons
         else
             products<DB, 2>(o, vt, L, x);
     };
-    tile_loop<2 * Load::N>(tiles.n, load, work);
+    tile_loop<kStages<DB>, 2 * Load::N>(tiles.n, load, work);
     if (!CAREFUL && __syncthreads_or(iw + n < S.lq && not_finite<DB>(o)))
         return false;
     if (CAREFUL)
@@ -227,26 +235,26 @@ __device__ __forceinline__ bool forward(const Args &A, LDS_AS uint8_t *lds, cons
     return true;
 }
 
-template <int DB, int NW, bool FULL>
-__global__ void __launch_bounds__(64 * NW, 2) fwd_kernel(Args A)
+template <int DB, bool FULL>
+__global__ void __launch_bounds__(64 * QW, 2) fwd_kernel(Args A)
 {
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[6 * BK * kRow<DB>];
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages<DB> * 2 * BK * kRow<DB>];
     LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
     int rank, hk, g, b, i0;
     Span S;
     if (!item_of(blockIdx.x, A.tiles, A.Hk, A.G, rank, hk, g) ||
-        !span_of(A, A.qs, A.Tq, A.tiles - 1 - rank, 32 * NW, false, S, b, i0))
+        !span_of(A, A.qs, A.Tq, A.tiles - 1 - rank, 32 * QW, false, S, b, i0))
         return;
     if (!FULL)
-        zero_lds<6 * BK * kRow<DB>>(lds, 64 * NW);
-    if (!forward<DB, NW, FULL, false>(A, lds, S, i0, hk, hk * A.G + g))
-        forward<DB, NW, FULL, true>(A, lds, S, i0, hk, hk * A.G + g);
+        zero_lds<kStages<DB> * 2 * BK * kRow<DB>>(lds, 64 * QW);
+    if (!forward<DB, FULL, false>(A, lds, S, i0, hk, hk * A.G + g))
+        forward<DB, FULL, true>(A, lds, S, i0, hk, hk * A.G + g);
 }
 
 // --------------------------------------------------------------- backward --
 
 // grad_q, and for the other kernels lse log2(e) and delta.
-template <int DB, int NW, bool FULL, bool CAREFUL>
+template <int DB, bool FULL, bool CAREFUL>
 __device__ __forceinline__ bool backward_q(const Args &A, LDS_AS uint8_t *lds, const Span &S, int i0, int hk, int hq)
 {
     constexpr int TILE = BK * kRow<DB>;
@@ -255,8 +263,8 @@ __device__ __forceinline__ bool backward_q(const Args &A, LDS_AS uint8_t *lds, c
     const uint32_t base = lds_address(lds);
     const Lane<DB> L(l);
     const uint16_t *kh = A.k.p + S.k0 * A.k.ts + hk * A.k.hs, *vh = A.v.p + S.k0 * A.v.ts + hk * A.v.hs;
-    const Tiles tiles(A, i0 + S.off, min(i0 + 32 * NW, S.lq) - 1 + S.off);
-    using Load = Loader<DB, BK, NW, FULL>;
+    const Tiles tiles(A, i0 + S.off, min(i0 + 32 * QW, S.lq) - 1 + S.off);
+    using Load = Loader<DB, BK, QW, FULL>;
     const Load kl(A.k.ts, A.D, w, l), vl(A.v.ts, A.D, w, l);
     auto load = [&](int it, int stage) {
         const uint32_t to = base + stage * 2 * TILE;
@@ -321,7 +329,7 @@ __device__ __forceinline__ bool backward_q(const Args &A, LDS_AS uint8_t *lds, c
         else
             products<DB, 2>(o, kt, L, x);
     };
-    tile_loop<2 * Load::N>(tiles.n, load, work);
+    tile_loop<kStages<DB>, 2 * Load::N>(tiles.n, load, work);
     if (!CAREFUL && __syncthreads_or(iw + n < S.lq && not_finite<DB>(o)))
         return false;
     if (CAREFUL)
@@ -331,20 +339,20 @@ __device__ __forceinline__ bool backward_q(const Args &A, LDS_AS uint8_t *lds, c
     return true;
 }
 
-template <int DB, int NW, bool FULL>
-__global__ void __launch_bounds__(64 * NW, 2) bwd_q_kernel(Args A)
+template <int DB, bool FULL>
+__global__ void __launch_bounds__(64 * QW, 2) bwd_q_kernel(Args A)
 {
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[6 * BK * kRow<DB>];
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages<DB> * 2 * BK * kRow<DB>];
     LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
     int rank, hk, g, b, i0;
     Span S;
     if (!item_of(blockIdx.x, A.tiles, A.Hk, A.G, rank, hk, g) ||
-        !span_of(A, A.qs, A.Tq, A.tiles - 1 - rank, 32 * NW, false, S, b, i0))
+        !span_of(A, A.qs, A.Tq, A.tiles - 1 - rank, 32 * QW, false, S, b, i0))
         return;
     if (!FULL)
-        zero_lds<6 * BK * kRow<DB>>(lds, 64 * NW);
-    if (!backward_q<DB, NW, FULL, false>(A, lds, S, i0, hk, hk * A.G + g))
-        backward_q<DB, NW, FULL, true>(A, lds, S, i0, hk, hk * A.G + g);
+        zero_lds<kStages<DB> * 2 * BK * kRow<DB>>(lds, 64 * QW);
+    if (!backward_q<DB, FULL, false>(A, lds, S, i0, hk, hk * A.G + g))
+        backward_q<DB, FULL, true>(A, lds, S, i0, hk, hk * A.G + g);
 }
 
 // Sums of 32 keys as the waves hold them: a plane each for grad_k and grad_v.
@@ -644,18 +652,14 @@ __global__ void __launch_bounds__(128, 2) bwd_far_kernel(Args A)
 
 // ------------------------------------------------------------------- host --
 
-enum Kind { FWD, FWD_SMALL, BWD_Q, BWD_Q_SMALL, BWD_KV, BWD_FAR, BWD_SUM };
+enum Kind { FWD, BWD_Q, BWD_KV, BWD_FAR, BWD_SUM };
 
 template <Kind K, int DB, bool FULL> void launch_full(const Args &A, dim3 grid, hipStream_t st)
 {
     if constexpr (K == FWD)
-        hipLaunchKernelGGL((fwd_kernel<DB, 8, FULL>), grid, dim3(512), 0, st, A);
-    else if constexpr (K == FWD_SMALL)
-        hipLaunchKernelGGL((fwd_kernel<DB, 4, FULL>), grid, dim3(256), 0, st, A);
+        hipLaunchKernelGGL((fwd_kernel<DB, FULL>), grid, dim3(64 * QW), 0, st, A);
     else if constexpr (K == BWD_Q)
-        hipLaunchKernelGGL((bwd_q_kernel<DB, 8, FULL>), grid, dim3(512), 0, st, A);
-    else if constexpr (K == BWD_Q_SMALL)
-        hipLaunchKernelGGL((bwd_q_kernel<DB, 4, FULL>), grid, dim3(256), 0, st, A);
+        hipLaunchKernelGGL((bwd_q_kernel<DB, FULL>), grid, dim3(64 * QW), 0, st, A);
     else if constexpr (K == BWD_KV)
         hipLaunchKernelGGL((bwd_kv_kernel<DB, 4, FULL>), grid, dim3(512), 0, st, A);
     else if constexpr (K == BWD_FAR)
@@ -696,15 +700,11 @@ inline int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
 inline int64_t row_bytes(int64_t Tq, int64_t Hq) { return round256(4 * Tq * Hq); }
 inline int64_t blocks_of(int64_t D) { return D <= 64 ? 2 : D <= 96 ? 3 : 4; }
 
-// A launch of tiles of queries: 256 a workgroup, or 128 where that leaves compute
-// units without one.
-template <Kind LARGE, Kind SMALL> void launch_queries(Args &A, hipStream_t st)
+// A launch of tiles of queries.
+template <Kind K> void launch_queries(Args &A, hipStream_t st)
 {
-    const bool packed = A.qs != nullptr;
-    const bool small = tiles_of(A.Tq, 256, A.B, packed) * A.Hk * A.G <= 192;
-    A.tiles = (int)tiles_of(A.Tq, small ? 128 : 256, A.B, packed);
-    const dim3 grid((unsigned)items(A.tiles, A.Hk, A.G));
-    small ? launch<SMALL>(A, grid, st) : launch<LARGE>(A, grid, st);
+    A.tiles = (int)tiles_of(A.Tq, 32 * QW, A.B, A.qs != nullptr);
+    launch<K>(A, dim3((unsigned)items(A.tiles, A.Hk, A.G)), st);
 }
 
 // Shares of the queries that a block of 128 keys, and the sinks' far sums of a chunk,
@@ -826,7 +826,7 @@ mx_status window_attn_fwd(const mx_heads *q, const mx_heads *k, const mx_heads *
     mxa::Args A = arguments(q, k, v, Tq, Tk, D, q_start, k_start, sequences, window, sinks, scale);
     A.out = out_of(out);
     A.lse_out = lse;
-    mxa::launch_queries<mxa::FWD, mxa::FWD_SMALL>(A, stream);
+    mxa::launch_queries<mxa::FWD>(A, stream);
     return launched();
 }
 
@@ -882,7 +882,7 @@ mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_
         A.near = A.far + (mxa::tiles_of(Tq, A.chunk, sequences, true) + 1) * k->heads * ((sinks + 31) / 32) * P.far_shares *
                              mxa::blocks_of(D) * (2 * 16 * 64);
         A.out = out_of(grad_q);
-        mxa::launch_queries<mxa::BWD_Q, mxa::BWD_Q_SMALL>(A, stream);
+        mxa::launch_queries<mxa::BWD_Q>(A, stream);
     } else {
         A.chunk = A.shares = A.far_shares = 1;
     }
