@@ -251,11 +251,10 @@ __device__ __forceinline__ void products(f16v (&acc)[DB], const LDS_AS uint8_t *
     }
 }
 
-// s = the tile's 64 rows times x
+// s += the tile's 64 rows times x
 template <int DB>
-__device__ __forceinline__ void scores(f16v (&s)[2], const LDS_AS uint8_t *tile, const Lane<DB> &L, const b8 (&x)[2 * DB])
+__device__ __forceinline__ void add_scores(f16v (&s)[2], const LDS_AS uint8_t *tile, const Lane<DB> &L, const b8 (&x)[2 * DB])
 {
-    s[0] = s[1] = zero16();
 #pragma unroll
     for (int ks = 0; ks < 2 * DB; ++ks)
 #pragma unroll
@@ -271,7 +270,15 @@ __device__ __forceinline__ void scores(f16v (&s)[2], const LDS_AS uint8_t *tile,
     __builtin_amdgcn_sched_group_barrier(0x8, 8, 0);
 }
 
-// The same of a tile some of whose rows are masked and may hold infinities or
+// s = the tile's 64 rows times x
+template <int DB>
+__device__ __forceinline__ void scores(f16v (&s)[2], const LDS_AS uint8_t *tile, const Lane<DB> &L, const b8 (&x)[2 * DB])
+{
+    s[0] = s[1] = zero16();
+    add_scores<DB>(s, tile, L, x);
+}
+
+// acc += tile^T x of a tile some of whose rows are masked and may hold infinities or
 // NaN: 0 times those is NaN, so every row is a product of its own, kept where
 // seen(row) of the lane's column.  Only for tiles where the plain product gave
 // something that is not finite.

@@ -18,7 +18,7 @@ struct Args {
     Out out, gk, gv;      // out: the output, or grad_q
     const float *lse;     // backward: [Hq, Tq]
     float *lse_out;       // forward: or NULL
-    float *lse2, *delta;  // backward: lse log2(e), grad_o . o, [Hq, Tq]
+    float *lse_s, *delta; // backward: -lse / scale and -delta, where scores and grad_o . v start, [Hq, Tq]
     float *far;           // backward: the sinks' sums over queries far behind them, by chunk and share
     float *near;          // with shares of near queries: their sums
     const int *qs, *ks;   // [B + 1], or NULL: one sequence
@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(64 * QW, 2) fwd_kernel(Args A)
 
 // --------------------------------------------------------------- backward --
 
-// grad_q, and for the other kernels lse log2(e) and delta.
+// grad_q, and for the other kernels where a query's scores and grad_out . v start.
 template <int DB, bool FULL, bool CAREFUL>
 __device__ __forceinline__ bool backward_q(const Args &A, LDS_AS uint8_t *lds, const Span &S, int i0, int hk, int hq)
 {
@@ -293,8 +293,8 @@ __device__ __forceinline__ bool backward_q(const Args &A, LDS_AS uint8_t *lds, c
     settle(q);
     settle(lse2);
     if (h == 0 && iw + n < S.lq) {
-        A.lse2[row] = lse2;
-        A.delta[row] = delta;
+        A.lse_s[row] = -A.lse[row] / A.scale;
+        A.delta[row] = -delta;
     }
     const Seen what = seen_of(A, tiles, p0, p1);
     f16v o[DB];
@@ -417,10 +417,10 @@ __device__ __forceinline__ bool backward_kv(const Args &A, LDS_AS uint8_t *lds, 
         const uint32_t to = base + stage * STAGE;
         ql.load(A.q.p + S.q0 * A.q.ts + lq * A.q.hs, lr, i1, to, l);
         gl.load(A.go.p + S.q0 * A.go.ts + lq * A.go.hs, lr, i1, to + TILE, l);
-        // the rows' lse and delta
+        // where the rows start
         const int64_t row = (int64_t)lq * A.Tq + S.q0 + min(lr + l, i1);
         if (w < 2)
-            mxg::lds_load4((w ? A.delta : A.lse2) + row, to + 2 * TILE + w * 4 * BK);
+            mxg::lds_load4((w ? A.delta : A.lse_s) + row, to + 2 * TILE + w * 4 * BK);
         lr += BK;
         if (lr > i1) {
             lr = i0;
@@ -456,9 +456,15 @@ __device__ __forceinline__ bool backward_kv(const Args &A, LDS_AS uint8_t *lds, 
             return;
         const LDS_AS uint8_t *qt = lds + stage * STAGE, *gt = qt + TILE;
         LDS_AS uint8_t *pt = ps + odd * BK * 96;
-        f16v s[2]; // scores or grad_out . v, then P or dS
-        scores<DB>(s, second ? gt : qt, L, x);
+        // scores less lse / scale, or grad_out . v less delta; then P or dS
         const LDS_AS float *st = reinterpret_cast<const LDS_AS float *>(qt + 2 * TILE) + second * BK + 4 * h;
+        f16v s[2];
+#pragma unroll
+        for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                s[qb][e] = st[32 * qb + 8 * (e >> 2) + (e & 3)];
+        add_scores<DB>(s, second ? gt : qt, L, x);
         if (second) { // dS: cells 0 .. 3 hold P's upper halves, 4 and 5 the bytes below
             u32x4 low[2];
 #pragma unroll
@@ -473,7 +479,7 @@ __device__ __forceinline__ bool backward_kv(const Args &A, LDS_AS uint8_t *lds, 
                     const int e = 8 * (c & 1) + i;
                     const float pr =
                         __uint_as_float(__builtin_amdgcn_perm(up[i / 2], low[c >> 1][2 * (c & 1) + i / 4], BYTES[i & 3]));
-                    s[c >> 1][e] = pr * (s[c >> 1][e] - st[32 * (c >> 1) + 8 * (e >> 2) + (e & 3)]);
+                    s[c >> 1][e] *= pr;
                 }
             }
         } else { // P
@@ -481,7 +487,7 @@ __device__ __forceinline__ bool backward_kv(const Args &A, LDS_AS uint8_t *lds, 
             for (int qb = 0; qb < 2; ++qb)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    s[qb][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[qb][e], A.c, -st[32 * qb + 8 * (e >> 2) + (e & 3)]));
+                    s[qb][e] = __builtin_amdgcn_exp2f(s[qb][e] * A.c);
         }
         if (see == 1) { // queries first + c, for constants c (hidden sums as in Mask)
             const int first = r0 + 4 * h;
@@ -872,8 +878,8 @@ mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_
         A.go = in_of(grad_out);
         A.o = in_of(out);
         A.lse = lse;
-        A.lse2 = static_cast<float *>(workspace);
-        A.delta = A.lse2 + mxa::row_bytes(Tq, q->heads) / 4;
+        A.lse_s = static_cast<float *>(workspace);
+        A.delta = A.lse_s + mxa::row_bytes(Tq, q->heads) / 4;
         A.chunk = (int)mxa::chunk_of(Tq);
         const mxa::BwdPlan P = mxa::bwd_plan(Tq, Tk, q->heads, k->heads, D, sequences, window, sinks);
         A.shares = P.shares;
