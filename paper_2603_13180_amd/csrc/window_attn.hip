@@ -143,16 +143,51 @@ __device__ __forceinline__ Seen seen_of(const Args &A, const Tiles &T, int p0, i
 constexpr int QW = 4;
 // Stages of keys and values: three, or two where that makes the room.
 template <int DB> constexpr int kStages = DB > 2 ? 2 : 3;
+template <int DB> constexpr int kTiles = kStages<DB> * 2 * BK * kRow<DB>;
+
+// Where few workgroups leave compute units idle, two groups of waves (KW = 2) take the
+// tiles in turn, and the second hands its sums over at the end (in LDS: the sums, the
+// rows' maxima and sums, the rows on their way out).
+template <int DB> constexpr int kSums = QW * DB * 4096;
+template <int DB, int KW> constexpr int kRows = KW == 1 ? 0 : kSums<DB> + QW * 256;
+
+// False in the second group, whose sums are then in LDS.
+template <int DB> __device__ __forceinline__ bool hand_over(const f16v (&o)[DB], LDS_AS uint8_t *lds, int w, int kw, int l)
+{
+    static_assert(kRows<DB, 2> + QW * 32 * kRow<DB> <= 2 * kTiles<DB>, "room for all");
+    LDS_AS float *const to = reinterpret_cast<LDS_AS float *>(lds) + w * DB * 1024 + l;
+    if (kw == 1)
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                to[(d * 16 + e) * 64] = o[d][e];
+    __syncthreads();
+    return kw == 0;
+}
+
+// o = a o + b (the second group's)
+template <int DB> __device__ __forceinline__ void take_over(f16v (&o)[DB], float a, float b, const LDS_AS uint8_t *lds, int w, int l)
+{
+    const LDS_AS float *const from = reinterpret_cast<const LDS_AS float *>(lds) + w * DB * 1024 + l;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            o[d][e] = o[d][e] * a + from[(d * 16 + e) * 64] * b;
+}
 
 // ---------------------------------------------------------------- forward --
 
-template <int DB, bool FULL, bool CAREFUL>
+template <int DB, bool FULL, int KW, bool CAREFUL>
 __device__ __forceinline__ bool forward(const Args &A, LDS_AS uint8_t *lds, const Span &S, int i0, int hk, int hq)
 {
     constexpr int TILE = BK * kRow<DB>;
     const int thread = thread_number<CAREFUL>();
-    const int w = __builtin_amdgcn_readfirstlane(thread >> 6), l = thread & 63, n = l & 31, h = l >> 5;
-    const uint32_t base = lds_address(lds);
+    const int wave = __builtin_amdgcn_readfirstlane(thread >> 6), l = thread & 63, n = l & 31, h = l >> 5;
+    const int w = wave % QW, kw = wave / QW;
+    LDS_AS uint8_t *const mine = lds + kw * kTiles<DB>;
+    const uint32_t base = lds_address(mine);
     const Lane<DB> L(l);
     const uint16_t *kh = A.k.p + S.k0 * A.k.ts + hk * A.k.hs, *vh = A.v.p + S.k0 * A.v.ts + hk * A.v.hs;
     const Tiles tiles(A, i0 + S.off, min(i0 + 32 * QW, S.lq) - 1 + S.off);
@@ -160,8 +195,9 @@ __device__ __forceinline__ bool forward(const Args &A, LDS_AS uint8_t *lds, cons
     const Load kl(A.k.ts, A.D, w, l), vl(A.v.ts, A.D, w, l);
     auto load = [&](int it, int stage) {
         const uint32_t to = base + stage * 2 * TILE;
-        kl.load(kh, tiles[it], S.lk - 1, to, l);
-        vl.load(vh, tiles[it], S.lk - 1, to + TILE, l);
+        const int j0 = tiles[min(it * KW + kw, tiles.n - 1)]; // a group without a last tile loads for the count's sake
+        kl.load(kh, j0, S.lk - 1, to, l);
+        vl.load(vh, j0, S.lk - 1, to + TILE, l);
     };
     const int iw = i0 + 32 * w;                             // the wave's first query
     const int p0 = iw + S.off, p1 = min(iw + 31, S.lq - 1) + S.off;
@@ -176,10 +212,11 @@ __device__ __forceinline__ bool forward(const Args &A, LDS_AS uint8_t *lds, cons
         o[d] = zero16();
     float m = -FLT_MAX, sum = 0.0f; // m: of scores in powers of two; sum: the lane's half of the keys
     auto work = [&](int it, int stage) {
-        const int see = what(it), j0 = tiles[it];
+        const int t = it * KW + kw;
+        const int see = t < tiles.n ? what(t) : 0, j0 = tiles[t];
         if (see == 0)
             return;
-        const LDS_AS uint8_t *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
+        const LDS_AS uint8_t *kt = mine + stage * 2 * TILE, *vt = kt + TILE;
         f16v x[2]; // scores, then P
         scores<DB>(x, kt, L, q);
         if (see == 1) {
@@ -219,26 +256,40 @@ __device__ __forceinline__ bool forward(const Args &A, LDS_AS uint8_t *lds, cons
         else
             products<DB, 2>(o, vt, L, x);
     };
-    tile_loop<kStages<DB>, 2 * Load::N>(tiles.n, load, work);
+    tile_loop<kStages<DB>, 2 * Load::N>((tiles.n + KW - 1) / KW, load, work);
     if (!CAREFUL && __syncthreads_or(iw + n < S.lq && not_finite<DB>(o)))
         return false;
     if (CAREFUL)
         __syncthreads();
     sum = halves_sum(sum);
+    if constexpr (KW == 2) {
+        LDS_AS float *const stat = reinterpret_cast<LDS_AS float *>(lds + kSums<DB>) + w * 64 + n;
+        if (kw == 1 && h == 0) {
+            stat[0] = m;
+            stat[32] = sum;
+        }
+        if (!hand_over<DB>(o, lds, w, kw, l))
+            return true;
+        const float m1 = stat[0], mn = fmaxf(m, m1);
+        const float a = __builtin_amdgcn_exp2f(m - mn), a1 = __builtin_amdgcn_exp2f(m1 - mn);
+        sum = sum * a + stat[32] * a1;
+        m = mn;
+        take_over<DB>(o, a, a1, lds, w, l);
+    }
     // a row that sees no key gives 0; one that sees only scores of -inf NaN
     const float by = p < 0 ? 0.0f : 1.0f / sum;
     if (A.lse_out && h == 0 && iw + n < S.lq)
         A.lse_out[(int64_t)hq * A.Tq + S.q0 + iw + n] =
             p < 0 ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * LN2;
-    store_rows<DB>(o, by, lds + w * 32 * kRow<DB>, A.out.p + (int64_t)(S.q0 + iw) * A.out.ts + hq * A.out.hs, A.out.ts,
+    store_rows<DB>(o, by, lds + kRows<DB, KW> + w * 32 * kRow<DB>, A.out.p + (int64_t)(S.q0 + iw) * A.out.ts + hq * A.out.hs, A.out.ts,
                    S.lq - iw, A.D, l);
     return true;
 }
 
-template <int DB, bool FULL>
-__global__ void __launch_bounds__(64 * QW, 2) fwd_kernel(Args A)
+template <int DB, bool FULL, int KW>
+__global__ void __launch_bounds__(64 * QW * KW, 2) fwd_kernel(Args A)
 {
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages<DB> * 2 * BK * kRow<DB>];
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[KW * kTiles<DB>];
     LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
     int rank, hk, g, b, i0;
     Span S;
@@ -246,21 +297,23 @@ __global__ void __launch_bounds__(64 * QW, 2) fwd_kernel(Args A)
         !span_of(A, A.qs, A.Tq, A.tiles - 1 - rank, 32 * QW, false, S, b, i0))
         return;
     if (!FULL)
-        zero_lds<kStages<DB> * 2 * BK * kRow<DB>>(lds, 64 * QW);
-    if (!forward<DB, FULL, false>(A, lds, S, i0, hk, hk * A.G + g))
-        forward<DB, FULL, true>(A, lds, S, i0, hk, hk * A.G + g);
+        zero_lds<KW * kTiles<DB>>(lds, 64 * QW * KW);
+    if (!forward<DB, FULL, KW, false>(A, lds, S, i0, hk, hk * A.G + g))
+        forward<DB, FULL, KW, true>(A, lds, S, i0, hk, hk * A.G + g);
 }
 
 // --------------------------------------------------------------- backward --
 
 // grad_q, and for the other kernels where a query's scores and grad_out . v start.
-template <int DB, bool FULL, bool CAREFUL>
+template <int DB, bool FULL, int KW, bool CAREFUL>
 __device__ __forceinline__ bool backward_q(const Args &A, LDS_AS uint8_t *lds, const Span &S, int i0, int hk, int hq)
 {
     constexpr int TILE = BK * kRow<DB>;
     const int thread = thread_number<CAREFUL>();
-    const int w = __builtin_amdgcn_readfirstlane(thread >> 6), l = thread & 63, n = l & 31, h = l >> 5;
-    const uint32_t base = lds_address(lds);
+    const int wave = __builtin_amdgcn_readfirstlane(thread >> 6), l = thread & 63, n = l & 31, h = l >> 5;
+    const int w = wave % QW, kw = wave / QW;
+    LDS_AS uint8_t *const mine = lds + kw * kTiles<DB>;
+    const uint32_t base = lds_address(mine);
     const Lane<DB> L(l);
     const uint16_t *kh = A.k.p + S.k0 * A.k.ts + hk * A.k.hs, *vh = A.v.p + S.k0 * A.v.ts + hk * A.v.hs;
     const Tiles tiles(A, i0 + S.off, min(i0 + 32 * QW, S.lq) - 1 + S.off);
@@ -268,8 +321,9 @@ __device__ __forceinline__ bool backward_q(const Args &A, LDS_AS uint8_t *lds, c
     const Load kl(A.k.ts, A.D, w, l), vl(A.v.ts, A.D, w, l);
     auto load = [&](int it, int stage) {
         const uint32_t to = base + stage * 2 * TILE;
-        kl.load(kh, tiles[it], S.lk - 1, to, l);
-        vl.load(vh, tiles[it], S.lk - 1, to + TILE, l);
+        const int j0 = tiles[min(it * KW + kw, tiles.n - 1)]; // a group without a last tile loads for the count's sake
+        kl.load(kh, j0, S.lk - 1, to, l);
+        vl.load(vh, j0, S.lk - 1, to + TILE, l);
     };
     const int iw = i0 + 32 * w;
     const int p0 = iw + S.off, p1 = min(iw + 31, S.lq - 1) + S.off;
@@ -302,10 +356,11 @@ __device__ __forceinline__ bool backward_q(const Args &A, LDS_AS uint8_t *lds, c
     for (int d = 0; d < DB; ++d)
         o[d] = zero16();
     auto work = [&](int it, int stage) {
-        const int see = what(it), j0 = tiles[it];
+        const int t = it * KW + kw;
+        const int see = t < tiles.n ? what(t) : 0, j0 = tiles[t];
         if (see == 0)
             return;
-        const LDS_AS uint8_t *kt = lds + stage * 2 * TILE, *vt = kt + TILE;
+        const LDS_AS uint8_t *kt = mine + stage * 2 * TILE, *vt = kt + TILE;
         f16v x[2], y[2]; // x: scores, then dS
         scores<DB>(x, kt, L, q);
         scores<DB>(y, vt, L, go);
@@ -329,20 +384,25 @@ __device__ __forceinline__ bool backward_q(const Args &A, LDS_AS uint8_t *lds, c
         else
             products<DB, 2>(o, kt, L, x);
     };
-    tile_loop<kStages<DB>, 2 * Load::N>(tiles.n, load, work);
+    tile_loop<kStages<DB>, 2 * Load::N>((tiles.n + KW - 1) / KW, load, work);
     if (!CAREFUL && __syncthreads_or(iw + n < S.lq && not_finite<DB>(o)))
         return false;
     if (CAREFUL)
         __syncthreads();
-    store_rows<DB>(o, A.scale, lds + w * 32 * kRow<DB>, A.out.p + (int64_t)(S.q0 + iw) * A.out.ts + hq * A.out.hs, A.out.ts,
+    if constexpr (KW == 2) {
+        if (!hand_over<DB>(o, lds, w, kw, l))
+            return true;
+        take_over<DB>(o, 1.0f, 1.0f, lds, w, l);
+    }
+    store_rows<DB>(o, A.scale, lds + kRows<DB, KW> + w * 32 * kRow<DB>, A.out.p + (int64_t)(S.q0 + iw) * A.out.ts + hq * A.out.hs, A.out.ts,
                    S.lq - iw, A.D, l);
     return true;
 }
 
-template <int DB, bool FULL>
-__global__ void __launch_bounds__(64 * QW, 2) bwd_q_kernel(Args A)
+template <int DB, bool FULL, int KW>
+__global__ void __launch_bounds__(64 * QW * KW, 2) bwd_q_kernel(Args A)
 {
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages<DB> * 2 * BK * kRow<DB>];
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[KW * kTiles<DB>];
     LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
     int rank, hk, g, b, i0;
     Span S;
@@ -350,9 +410,9 @@ __global__ void __launch_bounds__(64 * QW, 2) bwd_q_kernel(Args A)
         !span_of(A, A.qs, A.Tq, A.tiles - 1 - rank, 32 * QW, false, S, b, i0))
         return;
     if (!FULL)
-        zero_lds<kStages<DB> * 2 * BK * kRow<DB>>(lds, 64 * QW);
-    if (!backward_q<DB, FULL, false>(A, lds, S, i0, hk, hk * A.G + g))
-        backward_q<DB, FULL, true>(A, lds, S, i0, hk, hk * A.G + g);
+        zero_lds<KW * kTiles<DB>>(lds, 64 * QW * KW);
+    if (!backward_q<DB, FULL, KW, false>(A, lds, S, i0, hk, hk * A.G + g))
+        backward_q<DB, FULL, KW, true>(A, lds, S, i0, hk, hk * A.G + g);
 }
 
 // Sums of 32 keys as the waves hold them: a plane each for grad_k and grad_v.
@@ -658,14 +718,18 @@ __global__ void __launch_bounds__(128, 2) bwd_far_kernel(Args A)
 
 // ------------------------------------------------------------------- host --
 
-enum Kind { FWD, BWD_Q, BWD_KV, BWD_FAR, BWD_SUM };
+enum Kind { FWD, FWD_FEW, BWD_Q, BWD_Q_FEW, BWD_KV, BWD_FAR, BWD_SUM };
 
 template <Kind K, int DB, bool FULL> void launch_full(const Args &A, dim3 grid, hipStream_t st)
 {
     if constexpr (K == FWD)
-        hipLaunchKernelGGL((fwd_kernel<DB, FULL>), grid, dim3(64 * QW), 0, st, A);
+        hipLaunchKernelGGL((fwd_kernel<DB, FULL, 1>), grid, dim3(64 * QW), 0, st, A);
+    else if constexpr (K == FWD_FEW)
+        hipLaunchKernelGGL((fwd_kernel<DB, FULL, 2>), grid, dim3(128 * QW), 0, st, A);
     else if constexpr (K == BWD_Q)
-        hipLaunchKernelGGL((bwd_q_kernel<DB, FULL>), grid, dim3(64 * QW), 0, st, A);
+        hipLaunchKernelGGL((bwd_q_kernel<DB, FULL, 1>), grid, dim3(64 * QW), 0, st, A);
+    else if constexpr (K == BWD_Q_FEW)
+        hipLaunchKernelGGL((bwd_q_kernel<DB, FULL, 2>), grid, dim3(128 * QW), 0, st, A);
     else if constexpr (K == BWD_KV)
         hipLaunchKernelGGL((bwd_kv_kernel<DB, 4, FULL>), grid, dim3(512), 0, st, A);
     else if constexpr (K == BWD_FAR)
@@ -706,11 +770,16 @@ inline int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
 inline int64_t row_bytes(int64_t Tq, int64_t Hq) { return round256(4 * Tq * Hq); }
 inline int64_t blocks_of(int64_t D) { return D <= 64 ? 2 : D <= 96 ? 3 : 4; }
 
-// A launch of tiles of queries.
-template <Kind K> void launch_queries(Args &A, hipStream_t st)
+// A launch of tiles of queries, with two groups of waves where there are fewer
+// workgroups than compute units, or not many more and the last queries of a sequence
+// without a window see twice the average (3000 tokens of 16 heads of 128: 70 us, so 57;
+// 2000 of 32 of 64 with a window of 500: 26, so 30).
+template <Kind MANY, Kind FEW> void launch_queries(Args &A, hipStream_t st)
 {
     A.tiles = (int)tiles_of(A.Tq, 32 * QW, A.B, A.qs != nullptr);
-    launch<K>(A, dim3((unsigned)items(A.tiles, A.Hk, A.G)), st);
+    const dim3 grid((unsigned)items(A.tiles, A.Hk, A.G));
+    const int64_t n = (int64_t)A.tiles * A.Hk * A.G;
+    n <= 256 || (n <= 600 && A.window == MX_ATTN_MAX_TOKENS) ? launch<FEW>(A, grid, st) : launch<MANY>(A, grid, st);
 }
 
 // Shares of the queries that a block of 128 keys, and the sinks' far sums of a chunk,
@@ -832,7 +901,7 @@ mx_status window_attn_fwd(const mx_heads *q, const mx_heads *k, const mx_heads *
     mxa::Args A = arguments(q, k, v, Tq, Tk, D, q_start, k_start, sequences, window, sinks, scale);
     A.out = out_of(out);
     A.lse_out = lse;
-    mxa::launch_queries<mxa::FWD>(A, stream);
+    mxa::launch_queries<mxa::FWD, mxa::FWD_FEW>(A, stream);
     return launched();
 }
 
@@ -888,7 +957,7 @@ mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_
         A.near = A.far + (mxa::tiles_of(Tq, A.chunk, sequences, true) + 1) * k->heads * ((sinks + 31) / 32) * P.far_shares *
                              mxa::blocks_of(D) * (2 * 16 * 64);
         A.out = out_of(grad_q);
-        mxa::launch_queries<mxa::BWD_Q>(A, stream);
+        mxa::launch_queries<mxa::BWD_Q, mxa::BWD_Q_FEW>(A, stream);
     } else {
         A.chunk = A.shares = A.far_shares = 1;
     }
