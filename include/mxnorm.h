@@ -501,8 +501,9 @@ mx_status qk_norm_rope_bwd(const mx_heads *grad_q_out, const mx_heads *grad_k_ou
  * over the keys that i sees.  A query that sees none (p < 0) gives 0 and an lse of
  * -inf.  Products and sums are float, the exponentials, relative to a running
  * maximum, rounded to bf16 for the product with v, out rounded once more.  What a
- * masked key or value holds (infinities, NaN) changes nothing; visible ones
- * follow the formula, and a row whose visible scores are all -inf gives NaN.
+ * masked key or value holds (infinities, NaN) does not reach a row (such rows' float
+ * sums may be taken in another order); visible ones follow the formula, and a row
+ * whose visible scores are all -inf gives NaN.
  * Rows of out and lse that no sequence has are left as they were.  Starts past
  * Tq or Tk count as Tq and Tk; descending ones give unspecified rows.
  * D a multiple of 8, at most MX_ATTN_MAX_D; at most MX_ATTN_MAX_SINKS sinks,
@@ -523,8 +524,8 @@ mx_status window_attn_fwd(const mx_heads *q, const mx_heads *k, const mx_heads *
  *   grad_v_j = sum_i P_ij grad_out_i,
  * the sums of grad_k and grad_v over the query heads of a key head too.  Products
  * and sums are float, in a fixed order (the same call gives the same bits), P and
- * dS rounded to bf16 for the last three products, the gradients once more.  What
- * a pair that is masked holds changes nothing.  Queries and keys without a
+ * dS rounded to bf16 for the last three products, the gradients once more.  Pairs
+ * that are masked do not count, whatever they hold, as in the forward.  Queries and keys without a
  * visible partner have a gradient of 0; rows that no sequence has are left as
  * they were.  grad_q, grad_k and grad_v may be parts of one buffer, and must not
  * overlap an input.

@@ -342,7 +342,7 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
     // Tiles: the sinks', then from the first key that the window of a token at
     // length - 1 holds.  Row blocks differ in their places, not in their tiles.
     const int first = max(S.len - A.window, 0) / O::KEYS;
-    const int sinks = min((A.sinks + O::KEYS - 1) / O::KEYS, first);
+    const int sinks = min((min(A.sinks, S.end) + O::KEYS - 1) / O::KEYS, first);
     const int tiles = sinks + max((S.end + O::KEYS - 1) / O::KEYS - first, 0);
     const int from = (int)((int64_t)tiles * split / A.splits), to = (int)((int64_t)tiles * (split + 1) / A.splits);
     auto key_of = [&](int t) { return (t < sinks ? t : first + t - sinks) * O::KEYS; };

@@ -859,7 +859,7 @@ mx_status check_common(const mx_heads *q, const mx_heads *k, const mx_heads *v, 
         return fail(MX_EUNSUPPORTED, "heads of more than %d elements, or more than %d sinks", MX_ATTN_MAX_D, MX_ATTN_MAX_SINKS);
     if (Tq > MX_ATTN_MAX_TOKENS || Tk > MX_ATTN_MAX_TOKENS || q->heads > 4096 || sequences > 1 << 20)
         return fail(MX_EUNSUPPORTED, "at most %d tokens, 4096 heads and 2^20 sequences", MX_ATTN_MAX_TOKENS);
-    if ((mxa::tiles_of(Tq, 128, sequences, true) + 1) * q->heads > 1 << 30)
+    if ((mxa::tiles_of(std::max(Tq, Tk), 128, sequences, true) + 1) * q->heads > 1 << 30)
         return fail(MX_EUNSUPPORTED, "too many tokens times heads");
     return MX_OK;
 }

@@ -73,7 +73,8 @@ COMMON = [
     (dict(B=2), EINVAL), (dict(ks=P), EINVAL), (dict(qs=P, B=0), EINVAL), (dict(qs=P + 2, B=1), EINVAL),
     (dict(qs=P, ks=P + 1, B=1), EINVAL), (dict(qs=P, Tk=11), EINVAL), (dict(qs=P, B=(1 << 20) + 1), UNSUPPORTED),
     (dict(Tq=BIG + 1), UNSUPPORTED), (dict(Tk=BIG + 1), UNSUPPORTED), (dict(q=heads(8192), k=heads(8192), v=heads(8192)), UNSUPPORTED),
-    (dict(Tq=BIG, Tk=BIG, q=heads(4096, 64), k=heads(4096), v=heads(4096)), UNSUPPORTED)]
+    (dict(Tq=BIG, Tk=BIG, q=heads(4096, 64), k=heads(4096), v=heads(4096)), UNSUPPORTED),
+    (dict(Tk=BIG, q=heads(4096, 64), k=heads(4096), v=heads(4096)), UNSUPPORTED)]
 
 
 @pytest.mark.parametrize("kw,status", COMMON + [

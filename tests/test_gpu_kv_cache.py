@@ -417,6 +417,11 @@ def test_lengths_that_do_not_fit():
     o = c.run()
     c.length = want
     assert torch.equal(o, c.run())
+    # sinks and a window far past what the table has room for
+    c.length = i32([1 << 28, 50])
+    c.run(window=5, sinks=1 << 27)
+    c.length = i32([40, 50])
+    check(c, window=5, sinks=1 << 27)
 
 
 def test_starts_that_do_not_fit():
