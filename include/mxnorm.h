@@ -507,8 +507,9 @@ mx_status qk_norm_rope_bwd(const mx_heads *grad_q_out, const mx_heads *grad_k_ou
  * Rows of out and lse that no sequence has are left as they were.  Starts past
  * Tq or Tk count as Tq and Tk; descending ones give unspecified rows.
  * D a multiple of 8, at most MX_ATTN_MAX_D; at most MX_ATTN_MAX_SINKS sinks,
- * MX_ATTN_MAX_TOKENS tokens, 4096 heads and 2^20 sequences (else
- * MX_EUNSUPPORTED); scale from 2^-100 to 2^100.  out must not overlap an input.
+ * MX_ATTN_MAX_TOKENS tokens, 4096 heads and 2^20 sequences, and fewer than 2^24
+ * tiles of 128 queries times heads (the gradients: and 2^23 of keys; a sequence may
+ * end inside one) (else MX_EUNSUPPORTED); scale from 2^-100 to 2^100.  out must not overlap an input.
  * The same call gives the same bits.  Tq == 0 is a no-op.
  */
 mx_status window_attn_fwd(const mx_heads *q, const mx_heads *k, const mx_heads *v, int64_t Tq, int64_t Tk,

@@ -36,6 +36,9 @@ inline mx_status check_heads(const mx_heads *h, const char *name, int64_t T, int
     return MX_OK;
 }
 
+// A launch's threads are counted in 32 bits.
+inline bool launchable(int64_t workgroups, int64_t threads) { return workgroups <= (int64_t)UINT32_MAX / threads; }
+
 inline mx_status launched()
 {
     const hipError_t e = hipGetLastError();

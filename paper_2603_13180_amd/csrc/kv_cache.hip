@@ -659,7 +659,6 @@ __global__ void __launch_bounds__(256) join_few_kernel(CachedArgs A)
     float sum = 0.0f;
     bool any = false;
     float4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
     for (int s = 0; s < A.splits; ++s) {
         const float by = __shfl(w, s, 32), y = __shfl(mine.y, s, 32);
         any |= y != 0.0f;
@@ -816,6 +815,8 @@ mx_status kv_cache_append(const mx_kv_cache *cache, const mx_heads *k, const mx_
     const int64_t per = cache->heads * D / 8;
     A.tpw = (int)std::min<int64_t>(std::max<int64_t>(mxa::APPEND_THREADS / per, 1), mxa::APPEND_TOKENS);
     const dim3 grid((unsigned)((T + A.tpw - 1) / A.tpw));
+    if (!mxk::launchable(grid.x, mxa::APPEND_THREADS))
+        return fail(MX_EUNSUPPORTED, "too many tokens");
     if (cache->type == MX_CACHE_E4M3)
         hipLaunchKernelGGL((mxa::append_kernel<true>), grid, dim3(mxa::APPEND_THREADS), 0, stream, A);
     else
@@ -867,8 +868,9 @@ mx_status kv_cache_attn_fwd(const mx_kv_cache *cache, const mx_heads *q, int64_t
     const mxa::CachedPlan P = mxa::cached_plan(
         sequences, Hk, G, max_new, keys_of(table_width, cache->page_size, max_new, max_length, window, sinks));
     const int64_t grid = (int64_t)P.splits * Hk * P.blocks * sequences, rows = T * q->heads;
-    if (grid > 0x7FFFFFFF || rows > 0x7FFFFFFF)
-        return fail(MX_EUNSUPPORTED, "too many sequences times heads");
+    const int64_t joins = P.splits == 1 ? 0 : P.splits <= mxa::FEW_SPLITS ? (rows + 7) / 8 : rows;
+    if (!mxk::launchable(grid, P.RB == 8 ? 512 : 256) || !mxk::launchable(joins, 256))
+        return fail(MX_EUNSUPPORTED, "too many sequences, or tokens, times heads");
     const size_t need = P.splits == 1 ? 0 : (size_t)rows * P.splits * (D + 2) * sizeof(float);
     if (need && (!workspace || !aligned(workspace, 256) || workspace_bytes < need))
         return fail(MX_EINVAL, "a 256-byte aligned workspace of %zu bytes is needed", need);
@@ -905,9 +907,9 @@ mx_status kv_cache_attn_fwd(const mx_kv_cache *cache, const mx_heads *q, int64_t
         }
     }
     if (P.splits > 1 && P.splits <= mxa::FEW_SPLITS)
-        hipLaunchKernelGGL(mxa::join_few_kernel, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, stream, A);
+        hipLaunchKernelGGL(mxa::join_few_kernel, dim3((unsigned)joins), dim3(256), 0, stream, A);
     else if (P.splits > 1)
-        hipLaunchKernelGGL(mxa::join_kernel, dim3((unsigned)rows), dim3(256), 0, stream, A);
+        hipLaunchKernelGGL(mxa::join_kernel, dim3((unsigned)joins), dim3(256), 0, stream, A);
     return launched();
 }
 

@@ -715,7 +715,7 @@ template <int DB> __global__ void __launch_bounds__(128 * DB) bwd_sum_kernel(Arg
 }
 
 template <int DB, bool FULL>
-__global__ void __launch_bounds__(128, 2) bwd_far_kernel(Args A)
+__global__ void __launch_bounds__(128) bwd_far_kernel(Args A)
 {
     __shared__ __attribute__((aligned(1024))) uint8_t smem[kBytesKV<DB, 1>];
     LDS_AS uint8_t *lds = (LDS_AS uint8_t *)smem;
@@ -839,7 +839,7 @@ using mxk::launched;
 
 mx_status check_common(const mx_heads *q, const mx_heads *k, const mx_heads *v, int64_t Tq, int64_t Tk, int64_t D,
                        const int32_t *q_start, const int32_t *k_start, int64_t sequences, int64_t window, int64_t sinks,
-                       float scale)
+                       float scale, bool backward)
 {
     if (Tq < 0 || Tk < 0)
         return fail(MX_EINVAL, "Tq and Tk must be >= 0");
@@ -859,7 +859,11 @@ mx_status check_common(const mx_heads *q, const mx_heads *k, const mx_heads *v, 
         return fail(MX_EUNSUPPORTED, "heads of more than %d elements, or more than %d sinks", MX_ATTN_MAX_D, MX_ATTN_MAX_SINKS);
     if (Tq > MX_ATTN_MAX_TOKENS || Tk > MX_ATTN_MAX_TOKENS || q->heads > 4096 || sequences > 1 << 20)
         return fail(MX_EUNSUPPORTED, "at most %d tokens, 4096 heads and 2^20 sequences", MX_ATTN_MAX_TOKENS);
-    if ((mxa::tiles_of(std::max(Tq, Tk), 128, sequences, true) + 1) * q->heads > 1 << 30)
+    // workgroups as they are launched (a key block has shares only where its blocks are few)
+    const int64_t G = q->heads / k->heads;
+    if ((mxa::tiles_of(std::max(Tq, Tk), 128, sequences, true) + 1) * q->heads > 1 << 30 ||
+        !mxk::launchable(mxa::items(mxa::tiles_of(Tq, 128, sequences, q_start != nullptr), k->heads, G), 256) ||
+        (backward && !mxk::launchable(mxa::items(mxa::tiles_of(Tk, 128, sequences, q_start != nullptr), k->heads, 1), 512)))
         return fail(MX_EUNSUPPORTED, "too many tokens times heads");
     return MX_OK;
 }
@@ -906,7 +910,7 @@ mx_status window_attn_fwd(const mx_heads *q, const mx_heads *k, const mx_heads *
                           float scale, const mx_heads *out, float *lse, hipStream_t stream)
 {
     mxk::clear_error();
-    mx_status st = check_common(q, k, v, Tq, Tk, D, q_start, k_start, sequences, window, sinks, scale);
+    mx_status st = check_common(q, k, v, Tq, Tk, D, q_start, k_start, sequences, window, sinks, scale, false);
     if (st != MX_OK || (st = check_heads(q, "q", Tq, D, q->heads, false)) != MX_OK ||
         (st = check_heads(k, "k", Tk, D, k->heads, false)) != MX_OK ||
         (st = check_heads(v, "v", Tk, D, k->heads, false)) != MX_OK ||
@@ -944,7 +948,7 @@ mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_
                           size_t workspace_bytes, hipStream_t stream)
 {
     mxk::clear_error();
-    mx_status st = check_common(q, k, v, Tq, Tk, D, q_start, k_start, sequences, window, sinks, scale);
+    mx_status st = check_common(q, k, v, Tq, Tk, D, q_start, k_start, sequences, window, sinks, scale, true);
     if (st != MX_OK || (st = check_heads(grad_out, "grad_out", Tq, D, q->heads, false)) != MX_OK ||
         (st = check_heads(q, "q", Tq, D, q->heads, false)) != MX_OK ||
         (st = check_heads(k, "k", Tk, D, k->heads, false)) != MX_OK ||

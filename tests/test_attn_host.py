@@ -129,6 +129,20 @@ def test_cached_refuses(kw, status):
     assert got == status and text
 
 
+@pytest.mark.parametrize("fn,kw", [
+    # 2^24 workgroups of 256 threads, 2^23 of 512: a launch's threads no longer fit 32 bits
+    (forward, dict(Tq=BIG, Tk=BIG, q=heads(8), out=heads(8))),
+    (forward, dict(Tq=BIG, Tk=BIG, q=heads(8), out=heads(8), k=heads(8), v=heads(8))),
+    (backward, dict(Tq=BIG, Tk=BIG, go=heads(8), q=heads(8), out=heads(8), gq=heads(8))),
+    (backward, dict(Tk=BIG, k=heads(4), v=heads(4), gk=heads(4), gv=heads(4))),
+    (append, dict(T=BIG, S=BIG, c=cache(heads=64, page_stride=64 * 16 * 64), k=heads(64), v=heads(64))),
+    (cached, dict(T=BIG, q=heads(4), B=1, width=1024)),
+    (cached, dict(T=1 << 20, B=1 << 20, start=None, c=cache(heads=16, page_stride=16 * 16 * 64), q=heads(16), out=heads(16)))])
+def test_more_workgroups_than_a_launch_counts(fn, kw):
+    got, text = fn(**kw)
+    assert got == UNSUPPORTED and text
+
+
 def test_calls_that_launch_nothing():
     none = heads(4, data=None), heads(2, data=None)
     assert forward(Tq=0, q=none[0], out=none[0])[0] == 0
