@@ -313,25 +313,14 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
     // tiles in flight take the registers).
     constexpr bool SHARED = RB == 1;
     LDS_AS uint8_t *const qt = lds + kQueriesAt<DB, RB>;
-    b8 q[SHARED ? 1 : 2 * DB];
-    {
+    u32x4 x[2 * DB]; // all on their way before the first is waited for
+    if (!SHARED || kw == 0) {
         const uint16_t *row = A.q.p + (int64_t)(S.t0 + i) * A.q.ts + hq * A.q.hs;
 #pragma unroll
-        for (int ks = 0; ks < 2 * DB; ++ks) {
-            const int e = 16 * ks + 8 * h;
-            u32x4 x = {0, 0, 0, 0};
-            if (e < C.D && (!SHARED || kw == 0))
-                x = *reinterpret_cast<const u32x4 *>(row + e);
-            if constexpr (!SHARED)
-                q[ks] = __builtin_bit_cast(b8, x);
-            else if (kw == 0)
-                *reinterpret_cast<LDS_AS u32x4 *>(qt + n * kRow<DB> + ((2 * ks + h) ^ swz<DB>(n)) * 16) = x;
-        }
+        for (int ks = 0; ks < 2 * DB; ++ks)
+            x[ks] = *reinterpret_cast<const u32x4 *>(row + min(16 * ks + 8 * h, C.D - 8));
     }
     LDS_AS uint8_t *const area = qt + (SHARED ? 32 * kRow<DB> : 0) + w * (O::KEYS * 8);
-    auto query = [&](int ks) { return SHARED ? row_frag<DB>(qt, L, ks, 0) : q[SHARED ? 0 : ks]; };
-    if (SHARED)
-        __syncthreads();
     const uint64_t all = S.n >= 64 ? ~0ull : (1ull << S.n) - 1;
     uint64_t bits = (A.bits ? (uint64_t)A.bits[S.t0 + i] : (2ull << i) - 1) & all;
     const int place = S.len + __popcll(bits) - 1;
@@ -382,6 +371,18 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d)
         load(staged[d], d);
+    b8 q[SHARED ? 1 : 2 * DB];
+#pragma unroll
+    for (int ks = 0; ks < 2 * DB; ++ks) {
+        const u32x4 own = 16 * ks + 8 * h < C.D ? x[ks] : u32x4{0, 0, 0, 0};
+        if constexpr (!SHARED)
+            q[ks] = __builtin_bit_cast(b8, own);
+        else if (kw == 0)
+            *reinterpret_cast<LDS_AS u32x4 *>(qt + n * kRow<DB> + ((2 * ks + h) ^ swz<DB>(n)) * 16) = own;
+    }
+    auto query = [&](int ks) { return SHARED ? row_frag<DB>(qt, L, ks, 0) : q[SHARED ? 0 : ks]; };
+    if (SHARED)
+        __syncthreads();
     auto step = [&](Staged<DB, RB, MX> &next, int it) __attribute__((always_inline)) {
         const int t = tile_of(it);
         LDS_AS uint8_t *kt = lds + kw * GROUP + (O::STAGES == 2 ? (it & 1) * 2 * TILE : 0), *vt = kt + TILE;

@@ -441,6 +441,61 @@ def test_max_new_bounds_what_is_read():
     assert torch.equal(got[:2], want[:2]) and torch.equal(got[11:], want[11:])
 
 
+def uneven(B, longest, new=1, **kw):
+    """A long sequence, one of half its length, empty ones and short ones; some without new tokens."""
+    cached = [longest if b == B // 3 else longest // 2 if b == B - 1 else 0 if b % 7 == 1 else 5 + 37 * b % 200 for b in range(B)]
+    return Case(cached, [0 if b % 5 == 4 and b < B - 1 else max(1, new - b % 3) for b in range(B)], D=64, **kw)
+
+
+@pytest.mark.parametrize("mx", [False, True])
+@pytest.mark.parametrize("B,longest,new,Hq,Hk", [
+    (24, 6000, 1, 4, 2), (60, 5001, 1, 8, 2), (256, 2500, 1, 2, 1), (9, 4100, 5, 16, 4), (24, 3001, 40, 8, 2), (40, 2200, 20, 8, 2)])
+def test_uneven_lengths(B, longest, new, Hq, Hk, mx):
+    c = uneven(B, longest, new, Hq=Hq, Hk=Hk, mx=mx, tree=new > 1)
+    a = check(c)
+    assert torch.equal(a, c.run())
+    check(c, window=300, sinks=20)
+    # a bound of the lengths changes the shares
+    near = c.run(max_length=longest + 900)
+    o, bound = c.want()
+    assert off(near, o, bound) <= 1
+
+
+def test_uneven_lengths_captured():
+    # lengths that change between a graph's replays
+    c = uneven(30, 4000, Hq=8, Hk=2)
+    out = torch.empty_like(c.q)
+    c.run(out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.run(out=out)
+    for turn in range(4):
+        now = [n if turn != 1 else n // 3 for n in c.cached]
+        if turn == 2:
+            now[0], now[10] = 150, 17
+        c.length.copy_(i32(now))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        # (bits: the slots that a grown length brings in hold NaN)
+        assert torch.equal(out.view(torch.int16), c.run().view(torch.int16))
+
+
+def test_uneven_starts_and_lengths_that_do_not_fit():
+    c = uneven(24, 6000, 3, Hq=4, Hk=2)
+    st, length = c.start.clone(), c.length.clone()
+    for i, x in ((3, 1 << 30), (5, -9), (24, 10), (0, 40)):
+        c.start = st.clone()
+        c.start[i] = x
+        c.run()
+    c.start = st
+    c.length[2], c.length[9] = 1 << 30, -5
+    c.run()
+    c.length = length
+    check(c)
+
+
 def test_two_streams_at_once():
     c, d = Case([3000, 100], [1, 1], 8, 2, 128), Case([2500, 4000], [1, 1], 8, 2, 128, mx=True)
     want = c.run(), d.run()
