@@ -694,7 +694,10 @@ inline CachedPlan cached_plan(int64_t B, int64_t Hk, int64_t G, int64_t max_new,
     const int64_t rows = max_new * G;
     P.RB = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
     P.blocks = (int)((rows + 32 * P.RB - 1) / (32 * P.RB));
-    const int64_t groups = std::max<int64_t>(B * Hk * P.blocks, 1), want = P.RB == 8 ? 512 : 1024;
+    // As many workgroups as run at once, two a compute unit; twice that for sequences of
+    // different lengths and few rows, so that short shares make room (61 of 5000 to 16384
+    // keys of codes 282 us, so 312; one of 131072 keys 97, so 92).
+    const int64_t groups = std::max<int64_t>(B * Hk * P.blocks, 1), want = P.RB == 8 || B == 1 ? 512 : 1024;
     // at least 256 keys a share
     const int64_t most = std::max<int64_t>(keys / 256, 1);
     P.splits = (int)std::max<int64_t>(std::min<int64_t>(std::min<int64_t>(want / groups, most), MAX_SPLITS), 1);
