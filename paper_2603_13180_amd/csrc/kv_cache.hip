@@ -13,8 +13,8 @@
 // across workgroups by a second kernel.
 //
 // What bounds it: for single tokens the cache's bytes.  One token behind 131072 (8 key
-// heads of 128, 537 MB) 86 us and 8 for the join, 6.1 TB/s (read through the caches
-// 109; 16 loads of 1 KB in flight a wave, and pages looked up a tile ahead: in the tile
+// heads of 128, 537 MB) 82 to 85 us and 7 for the join, 6.4 TB/s (read through the caches
+// 109 with twice the workgroups; 16 loads of 1 KB in flight a wave, and pages looked up a tile ahead: in the tile
 // itself they took 139); 61 tokens behind 4916 to 16384 in E4M3 (1.37 GB) 268 to 300,
 // 4.6 to 5.1 TB/s, of which the sequences' lengths cost a tenth.  For trees the products:
 // 63 tokens behind 16 sequences of up to 8192 145 to 170 us, 0.5 to 0.6 PFLOP/s.  The
@@ -694,10 +694,13 @@ inline CachedPlan cached_plan(int64_t B, int64_t Hk, int64_t G, int64_t max_new,
     const int64_t rows = max_new * G;
     P.RB = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
     P.blocks = (int)((rows + 32 * P.RB - 1) / (32 * P.RB));
-    // As many workgroups as run at once, two a compute unit; twice that for sequences of
-    // different lengths and few rows, so that short shares make room (61 of 5000 to 16384
-    // keys of codes 282 us, so 312; one of 131072 keys 97, so 92).
-    const int64_t groups = std::max<int64_t>(B * Hk * P.blocks, 1), want = P.RB == 8 || B == 1 ? 512 : 1024;
+    // As many workgroups as run at once, two a compute unit; twice that where sequences of
+    // different lengths have few rows and shares would be long, so that short ones make
+    // room (32 + 8 heads of 128, new tokens behind uneven lengths, us with 512 and with 1024
+    // workgroups: 61 behind up to 2048 60 and 67, 8 behind 8192 39 and 46, 16 behind 16384
+    // 126 and 124, 61 behind 16384 of codes 312 and 282; one behind 131072 92 and 97).
+    const int64_t groups = std::max<int64_t>(B * Hk * P.blocks, 1);
+    const int64_t want = P.RB < 8 && B > 1 && groups * keys >= 512 * 4096 ? 1024 : 512;
     // at least 256 keys a share
     const int64_t most = std::max<int64_t>(keys / 256, 1);
     P.splits = (int)std::max<int64_t>(std::min<int64_t>(std::min<int64_t>(want / groups, most), MAX_SPLITS), 1);
