@@ -13,12 +13,12 @@
 // across workgroups by a second kernel.
 //
 // What bounds it: for single tokens the cache's bytes.  One token behind 131072 (8 key
-// heads of 128, 537 MB) 82 to 85 us and 7 for the join, 6.4 TB/s (read through the caches
-// 109 with twice the workgroups; 16 loads of 1 KB in flight a wave, and pages looked up a tile ahead: in the tile
-// itself they took 139); 61 tokens behind 4916 to 16384 in E4M3 (1.37 GB) 268 to 300,
-// 4.6 to 5.1 TB/s, of which the sequences' lengths cost a tenth.  For trees the products:
-// 63 tokens behind 16 sequences of up to 8192 145 to 170 us, 0.5 to 0.6 PFLOP/s.  The
-// append moves 134 MB in 21.2 to 22.3 us, 6.0 TB/s.
+// heads of 128, 537 MB) 81 to 84 us and 6 for the join, 6.4 TB/s (16 loads of 1 KB in
+// flight a wave; with twice the workgroups 86, of those reads through the caches 109, and
+// pages looked up in the tile itself instead of one ahead 139); 61 tokens behind 4916 to
+// 16384 in E4M3 (1.37 GB) 264 to 300, 4.6 to 5.2 TB/s, of which the sequences' lengths
+// cost a tenth.  For trees the products: 63 tokens behind 16 sequences of up to 8192 145
+// to 170 us, 0.5 to 0.6 PFLOP/s.  The append moves 134 MB in 21.2 to 22.3 us, 6.0 TB/s.
 #include "attn.h"
 #include "norm_cast.h"
 
