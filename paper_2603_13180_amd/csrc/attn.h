@@ -54,7 +54,7 @@ template <int DB> constexpr int kChunks = kRow<DB> / 16;
 
 // The 16 rows of a group of lanes that read one chunk each, and the 4 rows by 64
 // bytes of a transposing read, lie in different banks.
-template <int DB> __device__ __forceinline__ int swz(int r)
+template <int DB> __host__ __device__ __forceinline__ int swz(int r)
 {
     return DB <= 2 ? ((r >> 1) & 1) << 2 | ((r >> 2) & 3) : (r & 3) << 2 | ((r >> 2) & 3);
 }
@@ -88,7 +88,8 @@ struct Out {
 };
 
 // Loads tiles of ROWS rows of a head into LDS, by NW waves.  FULL: the heads have all
-// of their 32 DB elements; else chunks past D keep what the LDS held.
+// of their 32 DB elements.  Chunks past D keep what the LDS held: behind the last head
+// there may be no memory to read.
 template <int DB, int ROWS, int NW, bool FULL> struct Loader {
     static constexpr int RPL = 64 / kChunks<DB>, N = ROWS / RPL / NW; // rows of a load, loads of a wave
     static_assert(ROWS % (RPL * NW) == 0, "whole loads for every wave");
@@ -96,14 +97,20 @@ template <int DB, int ROWS, int NW, bool FULL> struct Loader {
     uint32_t off[N]; // the lane's bytes from the tile's first row
     int first, D;    // the wave's first row
 
-    __device__ __forceinline__ Loader(int64_t stride, int d, int w, int l) : ts(stride), first(w * N * RPL), D(d)
+    __host__ __device__ __forceinline__ Loader(int64_t stride, int d, int w, int l) : ts(stride), first(w * N * RPL), D(d)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i)
             off[i] = (uint32_t)row(i, l) * (uint32_t)ts * 2 + chunk(i, l) * 16;
     }
-    __device__ __forceinline__ int row(int i, int l) const { return first + i * RPL + l / kChunks<DB>; }
-    __device__ __forceinline__ uint32_t chunk(int i, int l) const { return (l % kChunks<DB>) ^ swz<DB>(row(i, l)); }
+    __host__ __device__ __forceinline__ int row(int i, int l) const { return first + i * RPL + l / kChunks<DB>; }
+    __host__ __device__ __forceinline__ uint32_t chunk(int i, int l) const { return (l % kChunks<DB>) ^ swz<DB>(row(i, l)); }
+    // Whether the head has the chunk.  FULL: a lane's rows differ in the lower two bits of
+    // swz alone, so its chunks are all before 4 DB or none is (all, but for DB = 3).
+    __host__ __device__ __forceinline__ bool has(int i, int l) const
+    {
+        return FULL ? 4 * DB == kChunks<DB> || (int)chunk(0, l) < 4 * DB : (int)chunk(i, l) * 8 < D;
+    }
 
     // rows r0 .. (those past `last` as `last`)
     __device__ __forceinline__ void load(const uint16_t *head, int r0, int last, uint32_t lds, int l) const
@@ -113,17 +120,17 @@ template <int DB, int ROWS, int NW, bool FULL> struct Loader {
         if (__builtin_expect(ts >= 1 << 24, 0)) { // 32-bit offsets do not hold a tile
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                if (FULL || (int)chunk(i, l) * 8 < D)
+                if (has(i, l))
                     lds_load16(head + (int64_t)min(r0 + row(i, l), last) * ts + chunk(i, l) * 8, to + i * 1024);
         } else if (r0 + ROWS - 1 > last) {
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                if (FULL || (int)chunk(i, l) * 8 < D)
+                if (has(i, l))
                     mxg::lds_load16(base, (uint32_t)min(row(i, l), last - r0) * (uint32_t)ts * 2 + chunk(i, l) * 16, to + i * 1024);
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                if (FULL || (int)chunk(i, l) * 8 < D)
+                if (has(i, l))
                     mxg::lds_load16(base, off[i], to + i * 1024);
         }
     }

@@ -76,4 +76,9 @@ typedef struct MxtProduct {
 mx_status mxt_matmul_pair(const MxtProduct *f32, const MxtProduct *bf16, int elem, int mode,
                           int units, hipStream_t stream);
 
+// How often a workgroup of window_attn_fwd and window_attn_bwd with `waves` waves a tile
+// (2, 4 or 8) loads each 16-byte piece of a tile's rows of D elements, added to
+// count[rows][16]; returns the rows (64), or -1 for sizes the calls refuse.
+int mxt_attn_tile_loads(int64_t D, int waves, uint8_t *count);
+
 } // extern "C"

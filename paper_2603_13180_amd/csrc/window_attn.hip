@@ -24,7 +24,10 @@
 // to 1640: grad_q 590 (1.05 PFLOP/s of its three products), grad_k and grad_v 970 to
 // 1045 (0.83 of its four; matrix instructions alone 511, without LDS reads 767, without
 // the exponentials and the hand-over of P 800), the sinks' far queries 45.
+#include <type_traits>
+
 #include "attn.h"
+#include "testing.h"
 
 namespace mxa {
 
@@ -756,17 +759,37 @@ template <Kind K, int DB, bool FULL> void launch_full(const Args &A, dim3 grid, 
         hipLaunchKernelGGL((bwd_sum_kernel<DB>), grid, dim3(128 * DB), 0, st, A);
 }
 
+// f(DB, FULL) for heads of D elements
+template <typename F> auto by_head_size(int D, F f)
+{
+    using std::integral_constant;
+    switch (D) {
+    case 64: return f(integral_constant<int, 2>(), std::true_type());
+    case 96: return f(integral_constant<int, 3>(), std::true_type());
+    case 128: return f(integral_constant<int, 4>(), std::true_type());
+    default:
+        return D < 64   ? f(integral_constant<int, 2>(), std::false_type())
+               : D < 96 ? f(integral_constant<int, 3>(), std::false_type())
+                        : f(integral_constant<int, 4>(), std::false_type());
+    }
+}
+
 template <Kind K> void launch(const Args &A, dim3 grid, hipStream_t st)
 {
-    switch (A.D) {
-    case 64: launch_full<K, 2, true>(A, grid, st); break;
-    case 96: launch_full<K, 3, true>(A, grid, st); break;
-    case 128: launch_full<K, 4, true>(A, grid, st); break;
-    default:
-        A.D < 64   ? launch_full<K, 2, false>(A, grid, st)
-        : A.D < 96 ? launch_full<K, 3, false>(A, grid, st)
-                   : launch_full<K, 4, false>(A, grid, st);
-    }
+    by_head_size(A.D, [&](auto db, auto full) { launch_full<K, db(), full()>(A, grid, st); });
+}
+
+// How often the loads of a tile by NW waves bring each 16-byte piece of its rows.
+template <int DB, int NW, bool FULL> void count_loads(int D, uint8_t (*count)[16])
+{
+    using Load = Loader<DB, BK, NW, FULL>;
+    for (int w = 0; w < NW; ++w)
+        for (int l = 0; l < 64; ++l) {
+            const Load load(0, D, w, l);
+            for (int i = 0; i < Load::N; ++i)
+                if (load.has(i, l))
+                    ++count[load.row(i, l)][load.chunk(i, l)];
+        }
 }
 
 // tiles of R rows that T rows of B sequences may have, numbered as span_of does
@@ -995,6 +1018,19 @@ mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_
             mxa::launch<mxa::BWD_SUM>(A, dim3((unsigned)mxa::tiles_of(Tk, 32, sequences, packed), (unsigned)A.Hk), stream);
     }
     return launched();
+}
+
+int mxt_attn_tile_loads(int64_t D, int waves, uint8_t *count)
+{
+    if (D <= 0 || D % 8 != 0 || D > MX_ATTN_MAX_D || (waves != 2 && waves != 4 && waves != 8))
+        return -1;
+    uint8_t(*rows)[16] = reinterpret_cast<uint8_t(*)[16]>(count);
+    mxa::by_head_size((int)D, [&](auto db, auto full) {
+        waves == 2   ? mxa::count_loads<db(), 2, full()>((int)D, rows)
+        : waves == 4 ? mxa::count_loads<db(), 4, full()>((int)D, rows)
+                     : mxa::count_loads<db(), 8, full()>((int)D, rows);
+    });
+    return mxa::BK;
 }
 
 } // extern "C"

@@ -62,6 +62,13 @@ def matmul_as(ac, as_, bc, bs, K, elem, shape, whole=0, units=0, out=None, b_gai
     return out
 
 
+def attn_tile_loads(D, waves):
+    """How often a tile's loads bring each 16-byte piece: [64, 16]."""
+    count = torch.zeros(64, 16, dtype=torch.uint8)
+    assert _fn("mxt_attn_tile_loads", [_L, _I, _P])(D, waves, count.data_ptr()) == 64
+    return count
+
+
 class _Product(ctypes.Structure):
     _fields_ = [(n, _P) for n in ("a", "as_", "b", "bs")] + [(n, _L) for n in "MNK"] + \
         [("gain", _P), ("out", _P)]

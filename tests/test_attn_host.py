@@ -6,6 +6,7 @@ import os
 import pytest
 import torch
 
+import launch_rules
 from paper_2603_13180_amd import mxnorm
 
 pytestmark = pytest.mark.skipif(not os.path.exists(mxnorm.LIB_PATH), reason="libmxnorm.so not built")
@@ -178,3 +179,11 @@ def test_binding_refuses():
         mxnorm.kv_cache_append(t[0], t, t, t, t, t)
     with pytest.raises(RuntimeError, match="GPU"):
         mxnorm.kv_cache_attn_fwd(t, t, t, t, t)
+
+
+@pytest.mark.parametrize("waves", [2, 4, 8])
+@pytest.mark.parametrize("D", range(8, 129, 8))
+def test_a_tile_loads_its_heads_alone(D, waves):
+    # every lane's loads: each 16 bytes of a head once, nothing behind it
+    want = (torch.arange(16) * 8 < D).to(torch.uint8).expand(64, 16)
+    assert torch.equal(launch_rules.attn_tile_loads(D, waves), want)
