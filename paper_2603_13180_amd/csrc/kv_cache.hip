@@ -80,9 +80,9 @@ template <bool MX> __global__ void __launch_bounds__(APPEND_THREADS) append_kern
         const int i = t - first(b), src = A.rows ? A.rows[t] : t;
         int page = -1, slot = 0;
         if (b < C.B && i >= 0 && t < first(b + 1) && (unsigned)src < (unsigned)A.S) {
-            const int64_t at = (int64_t)C.length[b] + i;
+            const int64_t at = (int64_t)max(C.length[b], 0) + i;
             slot = (int)(at & ((1 << C.shift) - 1));
-            if (at >= 0 && at >> C.shift < C.width)
+            if (at >> C.shift < C.width)
                 page = C.table[(int64_t)b * C.width + (at >> C.shift)];
         }
         to[threadIdx.x] = (unsigned)page < (unsigned)C.pages ? page : -1;

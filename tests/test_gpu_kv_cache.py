@@ -507,3 +507,18 @@ def test_two_streams_at_once():
         a = c.run()
         torch.cuda.synchronize()
         assert torch.equal(a, want[0]) and torch.equal(b, want[1])
+
+
+@pytest.mark.parametrize("mx", [False, True])
+@pytest.mark.parametrize("length", [-1, -5, -(1 << 31)])
+def test_append_takes_a_negative_length_as_0(length, mx):
+    # below 0 by less than the new tokens, by as many, and by far more
+    c, d = [Case([0, 0, 0], [20, 3, 5], 2, 2, 64, mx=mx) for _ in range(2)]
+    k, v = torch.randn(2, 28, 2, 64, device=DEV).bfloat16()
+    c.append(k, v, i32([length, 0, length]), c.start)
+    d.append(k, v, i32([0, 0, 0]), d.start)
+    assert torch.equal(c.buf.view(torch.uint8), d.buf.view(torch.uint8))
+    assert not mx or all(torch.equal(x, y) for x, y in zip(c.scales, d.scales))
+    # and attention finds them
+    c.length = i32([length, 0, length])
+    check(c)
