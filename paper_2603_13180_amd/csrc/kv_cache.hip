@@ -324,7 +324,7 @@ __device__ __forceinline__ bool cached(const CachedArgs &A, LDS_AS uint8_t *lds,
     const uint64_t all = S.n >= 64 ? ~0ull : (1ull << S.n) - 1;
     uint64_t bits = (A.bits ? (uint64_t)A.bits[S.t0 + i] : (2ull << i) - 1) & all;
     const int place = S.len + __popcll(bits) - 1;
-    if (A.window < MAX_NEW) // drafted tokens that lie the window before
+    if (A.window <= MAX_NEW) // drafted tokens that lie the window before (places differ by 64 at most)
         for (int u = 0; u < S.n; ++u)
             if (place - places[u] >= A.window && places[u] >= A.sinks)
                 bits &= ~(1ull << u);

@@ -522,3 +522,32 @@ def test_append_takes_a_negative_length_as_0(length, mx):
     # and attention finds them
     c.length = i32([length, 0, length])
     check(c)
+
+
+@pytest.mark.parametrize("mx", [False, True])
+@pytest.mark.parametrize("length", [-1, -5, -(1 << 31)])
+def test_append_takes_a_negative_length_as_0(length, mx):
+    # below 0 by less than the new tokens, by as many, and by far more
+    c, d = [Case([0, 0, 0], [20, 3, 5], 2, 2, 64, mx=mx) for _ in range(2)]
+    k, v = torch.randn(2, 28, 2, 64, device=DEV).bfloat16()
+    c.append(k, v, i32([length, 0, length]), c.start)
+    d.append(k, v, i32([0, 0, 0]), d.start)
+    assert torch.equal(c.buf.view(torch.uint8), d.buf.view(torch.uint8))
+    assert not mx or all(torch.equal(x, y) for x, y in zip(c.scales, d.scales))
+    # and attention finds them
+    c.length = i32([length, 0, length])
+    check(c)
+
+
+@pytest.mark.parametrize("Hq,Hk", [(2, 2), (4, 2), (8, 1)])
+@pytest.mark.parametrize("window", [62, 63, 64, 65])
+def test_windows_as_long_as_a_draft(window, Hq, Hk):
+    # a token whose mask is empty has a place 64 before that of one that names all 64
+    c = Case([30], [64], Hq, Hk, 64, tree=True)
+    c.bits[0], c.bits[40], c.bits[63], c.bits[62] = 0, 0, -1, (1 << 63) - 1
+    for i in (0, 40):
+        at = 30 + i
+        c.vc[int(c.table[0, at // 16]), :, at % 16] *= 30
+    check(c, window=window)
+    check(c, window=window, sinks=29)
+    check(c, window=window, sinks=30)  # their place, 29, is a sink
