@@ -787,8 +787,8 @@ int64_t keys_of(int64_t width, int64_t page_size, int64_t max_new, int64_t max_l
     int64_t n = width * page_size;
     if (max_length > 0)
         n = std::min(n, max_length + max_new);
-    if (window > 0)
-        n = std::min(n, window + max_new + sinks);
+    if (window > 0) // either may be as large as an int64
+        n = std::min(n, std::min(window, n) + max_new + std::min(sinks, n));
     return n;
 }
 

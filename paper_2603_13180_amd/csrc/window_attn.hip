@@ -835,7 +835,7 @@ inline BwdPlan bwd_plan(int64_t Tq, int64_t Tk, int64_t Hq, int64_t Hk, int64_t 
 {
     BwdPlan P{1, 1};
     const int64_t G = Hq / Hk, tiles = tiles_of(Tk, 128, B, true) * Hk;
-    const int64_t length = std::max<int64_t>(Tq / B, 1), seen = window > 0 ? std::min(window + 128, length) : length;
+    const int64_t length = std::max<int64_t>(Tq / B, 1), seen = window > 0 ? std::min(std::min(window, length) + 128, length) : length;
     const double steps = (double)(G * (seen / BK + 1)), mb = (double)tiles * 4 * blocks_of(D) * 8e-3;
     double best = 1e30;
     for (int s = 1; s <= 8 && (s == 1 || tiles < 192); ++s) {

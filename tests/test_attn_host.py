@@ -187,3 +187,17 @@ def test_a_tile_loads_its_heads_alone(D, waves):
     # every lane's loads: each 16 bytes of a head once, nothing behind it
     want = (torch.arange(16) * 8 < D).to(torch.uint8).expand(64, 16)
     assert torch.equal(launch_rules.attn_tile_loads(D, waves), want)
+
+
+def test_windows_and_sinks_of_any_size_plan_as_no_window():
+    # as far as 64 bits go, without overflow in the choice of shares
+    lib, most = mxnorm.load(), (1 << 63) - 1
+    att, bwd = lib.kv_cache_attn_fwd_workspace_bytes, lib.window_attn_bwd_workspace_bytes
+    want = att(1, 32, 8, 128, 1, 64, 2048, 1, 0, 0, 0)
+    assert want > 0
+    for window, sinks in ((most, 0), (most, most), (most - 1, 4), (100, most), (BIG, BIG)):
+        assert att(1, 32, 8, 128, 1, 64, 2048, 1, 0, window, sinks) == want
+    want = bwd(1024, 1024, 12, 12, 64, 1, 0, 0)
+    assert want > 2 * 4 * 1024 * 12
+    for window in (BIG, most - 200, most - 100, most):
+        assert bwd(1024, 1024, 12, 12, 64, 1, window, 0) == want

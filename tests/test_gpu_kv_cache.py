@@ -551,3 +551,11 @@ def test_windows_as_long_as_a_draft(window, Hq, Hk):
     check(c, window=window)
     check(c, window=window, sinks=29)
     check(c, window=window, sinks=30)  # their place, 29, is a sink
+
+
+def test_the_largest_window_and_sinks():
+    most = (1 << 63) - 1
+    c = Case([5000, 70], [1, 1], 4, 2, 64)
+    want = c.run()
+    for window, sinks in ((most, 0), (most, most), (9, most)):
+        assert torch.equal(c.run(window, sinks), want)

@@ -320,3 +320,14 @@ def test_small_heads_and_wide_strides():
     assert all(torch.equal(x, y) for x, y in zip(got, c.backward(*want, 0, 0)))
     del buf, k, v
     torch.cuda.empty_cache()
+
+
+@gpu
+def test_the_largest_window():
+    c = Case([1100], [1100], 4, 2, 64)
+    o, lse = c.forward(0, 0)
+    want = [o, lse, *c.backward(o, lse, 0, 0)]
+    for sinks in (0, 9):
+        o, lse = c.forward((1 << 63) - 1, sinks)
+        got = [o, lse, *c.backward(o, lse, (1 << 63) - 1, sinks)]
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
