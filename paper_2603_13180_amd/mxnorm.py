@@ -790,11 +790,12 @@ class _Cache(ctypes.Structure):
 
 
 def _paged(t, name, dtype, shape, device, page):
-    """The page stride of pages whose slots are contiguous; page: their strides."""
+    """The page stride of pages whose slots are contiguous (0 of one page alone, which
+    has no use for it); page: their strides."""
     strides = t.stride()
     if t.dtype != dtype or t.shape != shape or t.device != device or (strides[1:] != page and not t[:1].is_contiguous()):
         raise ValueError("%s must be %s %s on q's device, every page contiguous" % (name, dtype, list(shape)))
-    return strides[0]
+    return strides[0] if shape[0] > 1 else 0
 
 
 def _cache(k_cache, v_cache, k_scales, v_scales, table, length, start, T, D, device):

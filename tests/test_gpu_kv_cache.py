@@ -559,3 +559,21 @@ def test_the_largest_window_and_sinks():
     want = c.run()
     for window, sinks in ((most, 0), (most, most), (9, most)):
         assert torch.equal(c.run(window, sinks), want)
+
+
+@pytest.mark.parametrize("mx", [False, True])
+def test_a_cache_of_one_page(mx):
+    # its stride is not used: k and v need not agree in it
+    c = Case([5], [3], 4, 2, 64, page=16, mx=mx)
+    want = c.run()
+    at = int(c.table[0, 0])
+    c.kc, c.vc = c.buf[at:at + 1, 0], c.buf[at, 1].clone()[None]
+    if mx:
+        wide = torch.stack((c.scales[0], c.scales[1]), 1)
+        c.scales = [wide[at:at + 1, 0], c.scales[1][at:at + 1].clone()]
+    c.table[0, 0] = 0
+    assert c.kc.stride() != c.vc.stride()
+    assert torch.equal(c.run(), want)
+    c.append(-c.k, c.v, torch.zeros_like(c.length), i32([0, 8]))
+    c.pages = 1
+    check(c)
