@@ -44,7 +44,7 @@ struct Args {
     float *near;          // with shares of near queries: their sums
     const int *qs, *ks;   // [B + 1], or NULL: one sequence
     int Tq, Tk, B, Hk, G, D;
-    int tiles, window, sinks, chunk, far_shares, shares;
+    int tiles, window, sinks, chunk, far_blocks, far_shares, shares;
     float c, scale;       // scale log2(e), scale
 };
 
@@ -439,12 +439,11 @@ __global__ void __launch_bounds__(64 * QW * KW, 2) bwd_q_kernel(Args A)
 // Sums of 32 keys as the waves hold them: a plane each for grad_k and grad_v.
 template <int DB> constexpr int kPlane = DB * 16 * 64;
 
-// Of block kb of the sinks, over share s of the queries of chunk `at` (numbered as
-// tiles are) that lie the window or more behind.
+// Of block kb of the sinks, over share s of the queries of chunk `at` (see Chunks) that
+// lie the window or more behind.
 template <int DB> __device__ __forceinline__ float *far_part(const Args &A, int at, int hk, int kb, int s)
 {
-    const int blocks = (A.sinks + 31) / 32;
-    return A.far + ((((int64_t)at * A.Hk + hk) * blocks + kb) * A.far_shares + s) * (2 * kPlane<DB>);
+    return A.far + ((((int64_t)at * A.Hk + hk) * A.far_blocks + kb) * A.far_shares + s) * (2 * kPlane<DB>);
 }
 
 // Of key block `at` (numbered as tiles of 32), over share s of its near queries.
@@ -454,6 +453,9 @@ template <int DB> __device__ __forceinline__ float *near_part(const Args &A, int
 }
 
 // The chunks with far queries of sink block jw: first and last, and the number of chunk 0.
+// Chunks are numbered as tiles are, but only sequences with far queries need room of
+// their own: those have more keys than the window, so floor(k_start / (window + 1)) tells
+// them apart, and the sums' room does not grow with the short sequences of a batch.
 struct Chunks {
     int first, last, at;
     __device__ __forceinline__ Chunks(const Args &A, const Span &S, int b, int jw)
@@ -462,7 +464,11 @@ struct Chunks {
         const bool any = jw < A.sinks && i < S.lq;
         first = any ? i / A.chunk : 0;
         last = any ? (S.lq - 1) / A.chunk : -1;
-        at = S.q0 / A.chunk + (A.qs ? b : 0);
+        at = number(A, S, b);
+    }
+    __device__ __forceinline__ static int number(const Args &A, const Span &S, int b)
+    {
+        return S.q0 / A.chunk + min(b, S.k0 / (A.window + 1));
     }
 };
 
@@ -727,14 +733,14 @@ __global__ void __launch_bounds__(128) bwd_far_kernel(Args A)
     const int hk = blockIdx.y / A.far_shares, share = blockIdx.y % A.far_shares, j0 = 32 * blockIdx.z;
     if (!span_of(A, A.qs, A.Tq, blockIdx.x, A.chunk, false, S, b, i0))
         return;
-    const int i1 = min(i0 + A.chunk, S.lq) - 1;
+    const int i1 = min(i0 + A.chunk, S.lq) - 1, at = Chunks::number(A, S, b) + i0 / A.chunk;
     i0 = max(i0, j0 + A.window - S.off);
     if (j0 >= S.lk || i0 > i1)
         return;
     if (!FULL)
         zero_lds<3 * kStageKV<DB>>(lds, 128);
-    if (!backward_kv<DB, 1, FULL, true, false>(A, lds, S, j0, i0, i1, hk, b, blockIdx.x, share, A.far_shares))
-        backward_kv<DB, 1, FULL, true, true>(A, lds, S, j0, i0, i1, hk, b, blockIdx.x, share, A.far_shares);
+    if (!backward_kv<DB, 1, FULL, true, false>(A, lds, S, j0, i0, i1, hk, b, at, share, A.far_shares))
+        backward_kv<DB, 1, FULL, true, true>(A, lds, S, j0, i0, i1, hk, b, at, share, A.far_shares);
 }
 
 // ------------------------------------------------------------------- host --
@@ -807,9 +813,27 @@ inline int64_t chunk_of(int64_t Tq)
     return c;
 }
 
+inline int64_t blocks_of(int64_t D) { return D <= 64 ? 2 : D <= 96 ? 3 : 4; }
+
+// Blocks of 32 sinks that can have queries the window or more behind them, and chunks of
+// such queries.
+inline int64_t far_blocks(int64_t Tk, int64_t window, int64_t sinks)
+{
+    return window == 0 ? 0 : (std::min(sinks, std::max<int64_t>(Tk - window, 0)) + 31) / 32;
+}
+inline int64_t far_chunks(int64_t Tq, int64_t Tk, int64_t B, int64_t window)
+{
+    return Tq / chunk_of(Tq) + std::min(B - 1, Tk / (std::min<int64_t>(window, MX_ATTN_MAX_TOKENS) + 1)) + 1;
+}
+
+// floats of the sinks' far sums
+inline int64_t far_floats(int64_t Tq, int64_t Tk, int64_t Hk, int64_t D, int64_t B, int64_t window, int64_t sinks, int64_t shares)
+{
+    return far_chunks(Tq, Tk, B, window) * Hk * far_blocks(Tk, window, sinks) * shares * blocks_of(D) * (2 * 16 * 64);
+}
+
 inline int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
 inline int64_t row_bytes(int64_t Tq, int64_t Hq) { return round256(4 * Tq * Hq); }
-inline int64_t blocks_of(int64_t D) { return D <= 64 ? 2 : D <= 96 ? 3 : 4; }
 
 // A launch of tiles of queries, with two groups of waves where there are fewer
 // workgroups than compute units, or not many more and the last queries of a sequence
@@ -959,9 +983,9 @@ size_t window_attn_bwd_workspace_bytes(int64_t Tq, int64_t Tk, int64_t q_heads, 
         return 0;
     const mxa::BwdPlan P = mxa::bwd_plan(Tq, Tk, q_heads, k_heads, D, sequences, window, sinks);
     const int64_t block = mxa::blocks_of(D) * (2 * 16 * 64 * 4);
-    const int64_t far = mxa::tiles_of(Tq, mxa::chunk_of(Tq), sequences, true) + 1;
     const int64_t near = P.shares > 1 ? mxa::tiles_of(Tk, 32, sequences, true) + 1 : 0;
-    return 2 * mxa::row_bytes(Tq, q_heads) + k_heads * block * (far * ((sinks + 31) / 32) * P.far_shares + near * P.shares);
+    return 2 * mxa::row_bytes(Tq, q_heads) + k_heads * block * near * P.shares +
+           sizeof(float) * mxa::far_floats(Tq, Tk, k_heads, D, sequences, window, sinks, P.far_shares);
 }
 
 mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_heads *k, const mx_heads *v,
@@ -999,8 +1023,8 @@ mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_
         A.shares = P.shares;
         A.far_shares = P.far_shares;
         A.far = A.delta + mxa::row_bytes(Tq, q->heads) / 4;
-        A.near = A.far + (mxa::tiles_of(Tq, A.chunk, sequences, true) + 1) * k->heads * ((sinks + 31) / 32) * P.far_shares *
-                             mxa::blocks_of(D) * (2 * 16 * 64);
+        A.far_blocks = (int)mxa::far_blocks(Tk, window, sinks);
+        A.near = A.far + mxa::far_floats(Tq, Tk, k->heads, D, sequences, window, sinks, P.far_shares);
         A.out = out_of(grad_q);
         mxa::launch_queries<mxa::BWD_Q, mxa::BWD_Q_FEW>(A, stream);
     } else {
@@ -1009,9 +1033,9 @@ mx_status window_attn_bwd(const mx_heads *grad_out, const mx_heads *q, const mx_
     if (Tk > 0) {
         A.gk = out_of(grad_k);
         A.gv = out_of(grad_v);
-        if (Tq > 0 && A.sinks > 0)
+        if (A.far_blocks > 0)
             mxa::launch<mxa::BWD_FAR>(A, dim3((unsigned)mxa::tiles_of(Tq, A.chunk, sequences, packed), (unsigned)(A.Hk * A.far_shares),
-                                              (unsigned)((A.sinks + 31) / 32)), stream);
+                                              (unsigned)A.far_blocks), stream);
         A.tiles = (int)mxa::tiles_of(Tk, 128, sequences, packed);
         mxa::launch<mxa::BWD_KV>(A, dim3((unsigned)mxa::items(A.tiles, A.Hk, A.shares)), stream);
         if (A.shares > 1)

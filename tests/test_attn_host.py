@@ -201,3 +201,16 @@ def test_windows_and_sinks_of_any_size_plan_as_no_window():
     assert want > 2 * 4 * 1024 * 12
     for window in (BIG, most - 200, most - 100, most):
         assert bwd(1024, 1024, 12, 12, 64, 1, window, 0) == want
+
+
+def test_far_sums_take_room_for_sequences_longer_than_the_window():
+    bwd = mxnorm.load().window_attn_bwd_workspace_bytes
+    args = (8192, 8192, 32, 8, 128, 512)
+    # no query lies a window of all keys behind a sink
+    for window in (8192, 8191 + 2, 0, (1 << 63) - 1):
+        assert bwd(*args, window, 256) == bwd(*args, window, 0)
+    # 32 chunks of 256 queries, and at most 8192 // 1001 sequences of more than 1000 keys
+    block = 8 * 4 * 2 * 16 * 64 * 4
+    assert 0 < bwd(*args, 1000, 4) - bwd(*args, 1000, 0) <= block * (32 + 8192 // 1001 + 1)
+    # of 256 sinks 8192 - 8160 have such queries
+    assert bwd(*args, 8160, 256) - bwd(*args, 8160, 0) <= block * (32 + 1 + 1)

@@ -1,5 +1,7 @@
 """Attention with a window and sinks, and its gradients, on the GPU against a
 plain implementation in 64 bits (attn_reference.py, which derives the bounds)."""
+import ctypes
+
 import pytest
 import torch
 
@@ -331,3 +333,45 @@ def test_the_largest_window():
         o, lse = c.forward((1 << 63) - 1, sinks)
         got = [o, lse, *c.backward(o, lse, (1 << 63) - 1, sinks)]
         assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+def backward_with_guards(c, window, sinks, **kw):
+    """The gradients by a call whose workspace lies between guards, which have to hold."""
+    lib, ref = mxnorm.load(), ctypes.byref
+    o, lse = c.forward(window, sinks, **kw)
+    dq, dk, dv, T, S, D, B, scale = mxnorm._attn_arguments(c.q, c.k, c.v, kw["q_start"], kw.get("k_start"), None)
+    need = lib.window_attn_bwd_workspace_bytes(T, S, dq.heads, dk.heads, D, B, window, sinks)
+    buf = torch.full((need + (2 << 20),), 0xA5, dtype=torch.uint8, device=DEV)
+    ws = buf[1 << 20:][:need]
+    grads = [torch.empty_like(t) for t in (c.q, c.k, c.v)]
+    mxnorm._call(lib.window_attn_bwd, c.q.device, ref(mxnorm._heads(c.go, "grad_out")), ref(dq), ref(dk), ref(dv),
+                 ref(mxnorm._heads(o, "out")), lse.data_ptr(), T, S, D, kw["q_start"].data_ptr(),
+                 kw["k_start"].data_ptr() if "k_start" in kw else None, B, window, sinks, scale,
+                 *[ref(mxnorm._heads(g, "grad")) for g in grads], ws.data_ptr(), need)
+    assert (buf[:1 << 20] == 0xA5).all() and (buf[(1 << 20) + need:] == 0xA5).all()
+    return grads
+
+
+@gpu
+@pytest.mark.parametrize("Hq,Hk,D", [(4, 2, 64), (2, 1, 96), (3, 3, 128)])
+@pytest.mark.parametrize("window,sinks", [(10, 4), (40, 70), (1, 1), (300, 256)])
+def test_far_sums_of_many_sequences(window, sinks, Hq, Hk, D):
+    # short and long sequences in turn, empty ones, keys without queries and kept ones;
+    # those longer than the window alone have room for far sums
+    queries = [(7 * b * b + 3 * b) % 53 if b % 9 else 400 * (b % 2) for b in range(70)]
+    keys = [n + (0 if b % 4 else 11 * b % 60) for b, n in enumerate(queries)]
+    for q, k in ((queries, queries), (queries, keys)):
+        c = Case(q, k, Hq, Hk, D)
+        check(c, window, sinks)
+        want, bound = c.want(window, sinks)
+        for name, got in zip(("gq", "gk", "gv"), backward_with_guards(c, window, sinks, **c.starts())):
+            assert off(got, want[name], bound[name]) <= 1
+
+
+@gpu
+def test_far_sums_of_starts_that_do_not_fit():
+    c = Case([300, 60, 200], [300, 60, 200], 2, 1, 64)
+    for st in ([0, 1 << 30, 160, 560], [0, 200, 50, 560], [-5, 100, 1 << 20, 3], [560, 0, 560, 0]):
+        starts = torch.tensor(st, dtype=torch.int32, device=DEV)
+        for window, sinks in ((20, 40), (1, 1), (500, 256)):
+            backward_with_guards(c, window, sinks, q_start=starts)
