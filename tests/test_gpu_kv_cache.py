@@ -577,3 +577,66 @@ def test_a_cache_of_one_page(mx):
     c.append(-c.k, c.v, torch.zeros_like(c.length), i32([0, 8]))
     c.pages = 1
     check(c)
+
+
+@pytest.mark.parametrize("mx", [False, True])
+@pytest.mark.parametrize("new", [[3, 2, 4], [40, 2, 30]])
+def test_calls_that_do_not_fit_write_their_own_rows(new, mx):
+    """Starts, lengths, rows and pages that do not fit: the memory around the cache, the
+    scales and the output holds, and so do the pages that no table row names."""
+    c = Case([400, 0, 3], new, 4, 2, 64, mx=mx, tree=True)
+    P, T = c.pages, c.T
+
+    def guarded(t, fill):
+        big = torch.full((t.shape[0] + 8,) + t.shape[1:], fill, dtype=t.dtype, device=DEV)
+        big[4:-4] = t
+        return big, big[4:-4]
+
+    buf, inner = guarded(c.buf, 7)
+    c.kc, c.vc = inner[:, 0], inner[:, 1]
+    scales = [guarded(s, 7) for s in c.scales] if mx else []
+    c.scales = [s for _, s in scales] if mx else [None, None]
+    outs, out = guarded(c.q, 7)
+    named = torch.tensor(sorted(set(c.table.flatten().tolist()) - {-1}), device=DEV)
+    spare = torch.tensor([p for p in range(P) if p not in named.tolist()], device=DEV)
+    assert len(spare) == 2
+    before = [t[4 + spare].clone() for t in [buf] + [s for s, _ in scales]]
+    far = (1 << 31) - 1
+    st, length, table, bits = c.start.clone(), c.length.clone(), c.table.clone(), c.bits.clone()
+    rows = torch.arange(T, dtype=torch.int32, device=DEV)
+    wild = rows.clone()
+    wild[::3], wild[1::3] = far, -far - 1
+    for starts in (st, i32([0, 1 << 30, 5, T]), i32([3, 0, 5, far]), i32([-far - 1, 3, 99, -1]), i32([T, T, 0, 0])):
+        for lengths in (length, i32([-5, far, -far - 1]), i32([1 << 28, 401, 390])):
+            for pages in (table, torch.where(table % 2 == 0, table, far), torch.where(table % 3 == 0, table, -far - 1)):
+                c.start, c.length, c.table = starts, lengths, pages
+                for kw in (dict(), dict(window=9, sinks=5), dict(window=300, sinks=far, max_length=1)):
+                    c.run(out=out, **kw)
+                c.append(c.k[:T], c.v[:T], lengths, starts)
+                c.append(c.k[:T], c.v[:T], lengths, starts, wild)
+    torch.cuda.synchronize()
+    for t in [buf, outs] + [s for s, _ in scales]:
+        assert (t[:4] == 7).all() and (t[-4:] == 7).all()
+    for t, b in zip([buf] + [s for s, _ in scales], before):
+        assert torch.equal(t[4 + spare].view(torch.uint8), b.view(torch.uint8))
+    # and calls that fit are right after them
+    c.start, c.length, c.table = st, length, table
+    c.append(c.k[:T], c.v[:T], length, st)
+    whole = i32([sum(c.cached[:b]) + sum(c.new[:b]) for b in range(4)])
+    c.append(c.k, c.v, torch.zeros_like(length), whole)
+    check(c)
+
+
+@pytest.mark.parametrize("byte", [0, 1, 5, 100])
+def test_values_of_small_scales(byte):
+    # codes of 2 .. 448 times 2^(byte - 127), none below bf16's normal numbers
+    c = Case([40], [1], 2, 1, 64, mx=True)
+    g = torch.Generator().manual_seed(byte)
+    c.vc[:] = torch.randint(0x40, 0x7F, c.vc.shape, generator=g, dtype=torch.uint8).to(DEV)
+    c.scales[1].fill_(byte)
+    want, _ = c.want()
+    big = 448 * 2.0 ** (byte - 127)
+    # P's rounding is at most HALF of the largest value, the output's too; P itself and
+    # the sums of 41 terms are off by less than 2^-12 of it
+    assert ((c.run().double() - want).abs() <= (2 * HALF + 2.0 ** -12) * big).all()
+    assert (want > 2 * 2.0 ** (byte - 127)).all()

@@ -1,6 +1,7 @@
 """Attention with a window and sinks, and its gradients, on the GPU against a
 plain implementation in 64 bits (attn_reference.py, which derives the bounds)."""
 import ctypes
+import math
 
 import pytest
 import torch
@@ -375,3 +376,29 @@ def test_far_sums_of_starts_that_do_not_fit():
         starts = torch.tensor(st, dtype=torch.int32, device=DEV)
         for window, sinks in ((20, 40), (1, 1), (500, 256)):
             backward_with_guards(c, window, sinks, q_start=starts)
+
+
+@gpu
+@pytest.mark.parametrize("D", [64, 80, 128])
+def test_starts_that_do_not_fit_write_their_own_rows(D):
+    # the memory around the output, the lse and the gradients holds
+    c = Case([100, 60, 200], [100, 60, 200], 4, 2, D)
+    far = (1 << 31) - 1
+
+    def guarded(*shape, dtype=torch.bfloat16):
+        n, edge = math.prod(shape), 4096
+        big = torch.full((n + 2 * edge,), 7.0, dtype=dtype, device=DEV)
+        return big, big[edge:-edge].view(shape)
+
+    bufs = [guarded(*c.q.shape), guarded(4, c.T, dtype=torch.float32)] + [guarded(*t.shape) for t in (c.q, c.k, c.v)]
+    (_, o), (_, lse), (_, gq), (_, gk), (_, gv) = bufs
+    for st in ([0, 1 << 30, 160, 360], [0, 200, 50, far], [-far - 1, 100, 1 << 20, -1], [360, 0, 360, 0], [300, 310, 311, 312]):
+        for kst in (st, [0, 360, 360, 360], [far, 0, -5, 200]):
+            kw = {n: torch.tensor(x, dtype=torch.int32, device=DEV) for n, x in (("q_start", st), ("k_start", kst))}
+            for window, sinks in ((0, 0), (20, 40), (1, 1)):
+                c.forward(window, sinks, out=o, lse=lse, **kw)
+                c.backward(o, lse, window, sinks, grad_q=gq, grad_k=gk, grad_v=gv, **kw)
+    torch.cuda.synchronize()
+    for big, _ in bufs:
+        assert (big[:4096] == 7).all() and (big[-4096:] == 7).all()
+    check(c, 20, 3)
