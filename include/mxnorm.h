@@ -525,7 +525,8 @@ mx_status window_attn_fwd(const mx_heads *q, const mx_heads *k, const mx_heads *
  *   grad_v_j = sum_i P_ij grad_out_i,
  * the sums of grad_k and grad_v over the query heads of a key head too.  Products
  * and sums are float, in a fixed order (the same call gives the same bits), P and
- * dS rounded to bf16 for the last three products, the gradients once more.  Pairs
+ * dS rounded to bf16 for the last three products, the gradients once more; for grad_k,
+ * dS is formed from P cut to 24 bits (within 2^-15 of it).  Pairs
  * that are masked do not count, whatever they hold, as in the forward.  Queries and keys without a
  * visible partner have a gradient of 0; rows that no sequence has are left as
  * they were.  grad_q, grad_k and grad_v may be parts of one buffer, and must not
@@ -578,8 +579,9 @@ typedef struct {
  * rows[t] (int32 [T], device), so that of drafted tokens those kept are written
  * again, one behind the other.  MX_CACHE_E4M3: cast as mx_cast_fwd casts, with its
  * codes for blocks that hold infinities or NaN.  Tokens that no sequence has, and
- * rows outside 0 .. S - 1, are not written.  length is not changed.  Two tokens at
- * one place (pages shared by sequences) leave either.  D a multiple of 8 (32), at
+ * rows outside 0 .. S - 1, are not written.  length is not changed.  Of two tokens at
+ * one place (pages shared by sequences) any part of either may be left, a code with the
+ * other's scale among them: only equal ones may meet there.  D a multiple of 8 (32), at
  * most MX_ATTN_MAX_D; T == 0 is a no-op.
  */
 mx_status kv_cache_append(const mx_kv_cache *cache, const mx_heads *k, const mx_heads *v, int64_t T, int64_t S,
@@ -598,7 +600,8 @@ mx_status kv_cache_append(const mx_kv_cache *cache, const mx_heads *k, const mx_
  * drafted ones its bits name, it sees those whose place is less than `window`
  * before its own or below `sinks` (window 0: all).
  * A token that sees none gives 0.  Arithmetic, masked places and rows that no
- * sequence has as in window_attn_fwd; keys and values of codes are exact.  Where
+ * sequence has as in window_attn_fwd; keys and values of codes are exact (below 2^-126
+ * rounded to bf16's subnormals).  Where
  * few sequences and heads would leave compute units idle, shares of a sequence's
  * keys are summed apart and joined in order: how many depends on the arguments, so
  * a token's last bits may depend on its batch; the same call gives the same bits.

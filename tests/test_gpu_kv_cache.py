@@ -640,3 +640,40 @@ def test_values_of_small_scales(byte):
     # the sums of 41 terms are off by less than 2^-12 of it
     assert ((c.run().double() - want).abs() <= (2 * HALF + 2.0 ** -12) * big).all()
     assert (want > 2 * 2.0 ** (byte - 127)).all()
+
+
+@pytest.mark.parametrize("mx", [False, True])
+def test_sequences_that_write_the_same_token_at_one_place(mx):
+    # a page that two sequences share, and the same rows named twice
+    c = Case([0, 0], [12, 12], 4, 2, 64, mx=mx)
+    c.table[1] = c.table[0]
+    k, v = torch.randn(2, 12, 2, 64, device=DEV).bfloat16()
+    rows = torch.arange(12, dtype=torch.int32, device=DEV).repeat(2)
+    c.append(k, v, c.length, c.start, rows)
+    at = int(c.table[0, 0])
+    for which, x in ((0, k), (1, v)):
+        got = (c.kc, c.vc)[which][at, :, :12].transpose(0, 1)
+        if mx:
+            codes, scales = mxnorm.mx_cast_fwd(x.flatten(0, 1))
+            assert torch.equal(got, codes.view_as(got))
+            assert torch.equal(c.scales[which][at, :, :12].transpose(0, 1), scales.view(12, 2, 2))
+        else:
+            assert torch.equal(got, x)
+    c.q[12:] = c.q[:12]
+    o = check(c)
+    assert torch.equal(o[:12], o[12:])
+
+
+@pytest.mark.parametrize("Hq,Hk,new", [(4096, 1, 1), (512, 2, 64)])
+def test_many_heads(Hq, Hk, new):
+    check(Case([40, 3], [new, 1], Hq, Hk, 64), window=30, sinks=2)
+
+
+def test_an_empty_cache():
+    # no pages: no token sees a key
+    q = torch.randn(2, 4, 64, device=DEV).bfloat16()
+    kc = torch.empty(0, 2, 16, 64, dtype=torch.bfloat16, device=DEV)
+    k = torch.randn(2, 2, 64, device=DEV).bfloat16()
+    table = i32([[0, 1], [2, 3]])
+    mxnorm.kv_cache_append(k, k, kc, kc, table, i32([5, 0]))
+    assert (mxnorm.kv_cache_attn_fwd(q, kc, kc, table, i32([5, 0])) == 0).all()

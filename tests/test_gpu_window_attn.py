@@ -402,3 +402,39 @@ def test_starts_that_do_not_fit_write_their_own_rows(D):
     for big, _ in bufs:
         assert (big[:4096] == 7).all() and (big[-4096:] == 7).all()
     check(c, 20, 3)
+
+
+@gpu
+@pytest.mark.parametrize("Hq,Hk", [(512, 1), (200, 200)])
+def test_very_many_heads(Hq, Hk):
+    check(Case([70, 9], [70, 9], Hq, Hk, 64), 20, 2)
+
+
+@gpu
+def test_no_keys_at_all():
+    c = Case([5], [0], 4, 2, 64)
+    for kw in (dict(), dict(q_start=torch.tensor([0, 2, 5], dtype=torch.int32, device=DEV),
+                            k_start=torch.zeros(3, dtype=torch.int32, device=DEV))):
+        o, lse = c.forward(0, 0, **kw)
+        assert (o == 0).all() and (lse == -torch.inf).all()
+        gq, gk, gv = c.backward(o, lse, 0, 0, **kw)
+        assert (gq == 0).all() and gk.numel() == gv.numel() == 0
+    # and no queries: the keys' gradients are 0
+    c = Case([0], [7], 4, 2, 64)
+    for kw in (dict(), dict(window=3, sinks=2)):
+        o, lse = mxnorm.window_attn_fwd(c.q, c.k, c.v, **kw)
+        _, gk, gv = mxnorm.window_attn_bwd(c.go, c.q, c.k, c.v, o, lse, **kw)
+        assert (gk == 0).all() and (gv == 0).all()
+
+
+@gpu
+def test_a_hundred_thousand_sequences():
+    # each of one token: its value
+    n = 100000
+    c = Case([n], [n], 2, 1, 8)
+    starts = torch.arange(n + 1, dtype=torch.int32, device=DEV)
+    o, lse = c.forward(9, 3, q_start=starts)
+    assert torch.equal(o, c.v.expand(-1, 2, -1))
+    gq, gk, gv = c.backward(o, lse, 9, 3, q_start=starts)
+    # P is 1, so grad_v is the sum of two heads' gradients, rounded once
+    assert torch.equal(gv, c.go.float().sum(1, keepdim=True).bfloat16())
