@@ -677,3 +677,24 @@ def test_an_empty_cache():
     table = i32([[0, 1], [2, 3]])
     mxnorm.kv_cache_append(k, k, kc, kc, table, i32([5, 0]))
     assert (mxnorm.kv_cache_attn_fwd(q, kc, kc, table, i32([5, 0])) == 0).all()
+
+
+@pytest.mark.parametrize("new,Hq", [(1, 4), (1, 64), (30, 4), (30, 8), (60, 16)])
+def test_masked_codes_may_hold_anything(new, Hq):
+    # codes and scales that are NaN, behind the window but above the sinks; rows of every kind of workgroup
+    for long in (200, 6000):
+        c = Case([long], [new], Hq, 2, 64, mx=True, tree=new > 1)
+        want, bound = c.want(50, 2)
+        for j in list(range(2, 20)) + list(range(long - 60, long - 50)):
+            at = int(c.table[0, j // 16]), slice(None), j % 16
+            if j % 2:
+                c.kc[at] = c.vc[at] = 0x7F
+            else:
+                c.scales[0][at] = c.scales[1][at] = 255
+        assert off(c.run(50, 2), want, bound) <= 1
+        # and with as many shares as a cache without a window has
+        c = Case([long], [new], Hq, 2, 64, mx=True, tree=new > 1)
+        at = int(c.table[0, 5])
+        c.vc[at], c.kc[at], c.scales[0][at] = 0xFF, 0x7F, 255
+        c.table[0, 5] = -1
+        check(c)

@@ -438,3 +438,29 @@ def test_a_hundred_thousand_sequences():
     gq, gk, gv = c.backward(o, lse, 9, 3, q_start=starts)
     # P is 1, so grad_v is the sum of two heads' gradients, rounded once
     assert torch.equal(gv, c.go.float().sum(1, keepdim=True).bfloat16())
+
+
+@gpu
+@pytest.mark.parametrize("bad", [float("nan"), -float("inf")])
+@pytest.mark.parametrize("Hq,Hk,D", [(64, 32, 96), (64, 32, 80), (6, 2, 96), (64, 32, 64)])
+def test_masked_places_of_many_heads(bad, Hq, Hk, D):
+    # token 300 is visible to tokens 300 .. 339 alone; more workgroups than share tiles or queries, and fewer
+    T, W, S = 700, 40, 2
+    near = torch.zeros(T, dtype=torch.bool, device=DEV)
+    near[300:340] = True
+    clean, c = Case([T], [T], Hq, Hk, D), Case([T], [T], Hq, Hk, D)
+    want, bound = clean.want(W, S)
+    c.k[300], c.v[300] = bad, bad
+    o, lse = c.forward(W, S)
+    assert off(o[~near], want["o"][~near], bound["o"][~near]) <= 1
+    assert off(lse[:, ~near], want["lse"][:, ~near], bound["lse"][:, ~near]) <= 1
+    o, lse = clean.forward(W, S)
+    gq, _, _ = c.backward(o, lse, W, S)
+    assert off(gq[~near], want["gq"][~near], bound["gq"][~near]) <= 1
+    # a query, its gradient, output and lse: the keys that it does not see, as sinks or in its window
+    c = Case([T], [T], Hq, Hk, D)
+    c.q[500], c.go[500], o[500], lse[:, 500] = bad, bad, bad, bad
+    _, gk, gv = c.backward(o, lse, W, S)
+    unseen = torch.tensor([j for j in range(S, T) if not 460 < j <= 500], device=DEV)
+    for n, t in (("gk", gk), ("gv", gv)):
+        assert off(t[unseen], want[n][unseen], bound[n][unseen]) <= 1
