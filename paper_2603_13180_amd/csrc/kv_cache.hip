@@ -18,7 +18,8 @@
 // pages looked up in the tile itself instead of one ahead 139); 61 tokens behind 4916 to
 // 16384 in E4M3 (1.37 GB) 264 to 300, 4.6 to 5.2 TB/s, of which the sequences' lengths
 // cost a tenth.  For trees the products: 63 tokens behind 16 sequences of up to 8192 145
-// to 170 us, 0.5 to 0.6 PFLOP/s.  The append moves 134 MB in 21.2 to 22.3 us, 6.0 TB/s.
+// to 170 us, 0.5 to 0.6 PFLOP/s (the whole call over codes 166, over bf16 152).  The append
+// moves 134 MB in 21.2 to 22.3 us, 6.0 TB/s; 102 MB into codes, the whole call, in 20.7.
 #include "attn.h"
 #include "norm_cast.h"
 
@@ -698,7 +699,7 @@ inline CachedPlan cached_plan(int64_t B, int64_t Hk, int64_t G, int64_t max_new,
     // different lengths have few rows and shares would be long, so that short ones make
     // room (32 + 8 heads of 128, new tokens behind uneven lengths, us with 512 and with 1024
     // workgroups: 61 behind up to 2048 60 and 67, 8 behind 8192 39 and 46, 16 behind 16384
-    // 126 and 124, 61 behind 16384 of codes 312 and 282; one behind 131072 92 and 97).
+    // 121 and 120, 61 behind 16384 of codes 303 and 261; one behind 131072 89 and 94).
     const int64_t groups = std::max<int64_t>(B * Hk * P.blocks, 1);
     const int64_t want = P.RB < 8 && B > 1 && groups * keys >= 512 * 4096 ? 1024 : 512;
     // at least 256 keys a share

@@ -21,8 +21,8 @@
 // more rows a wave, which would halve that, need more than the 256 registers of two
 // waves a SIMD.  Two halves of a workgroup in opposite phases, products beside
 // exponentials by two barriers a tile, took 595.  Backward with a window of 4096 1600
-// to 1640: grad_q 590 (1.05 PFLOP/s of its three products), grad_k and grad_v 970 to
-// 1045 (0.83 of its four; matrix instructions alone 511, without LDS reads 767, without
+// to 1680: grad_q 590 to 610 (1.05 PFLOP/s of its three products), grad_k and grad_v 970
+// to 1045 (0.83 of its four; matrix instructions alone 511, without LDS reads 767, without
 // the exponentials and the hand-over of P 800), the sinks' far queries 45.
 #include <type_traits>
 
