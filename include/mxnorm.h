@@ -490,7 +490,7 @@ mx_status qk_norm_rope_bwd(const mx_heads *grad_q_out, const mx_heads *grad_k_ou
  * token [Tq, Hq, D]; k, v: Hk heads [Tk, Hk, D], Hq a multiple of Hk; query head
  * h reads key head h Hk / Hq (mx_heads: views of a projection's output, or
  * qk_norm_rope_fwd's).
- * q_start, k_start: device int32 [sequences + 1]; sequence b has the queries
+ * q_start, k_start: device int32 [sequences + 1], sequences >= 1; sequence b has the queries
  * q_start[b] .. q_start[b + 1] - 1 and the keys k_start[b] .. likewise, lq and lk
  * of them, in ascending order; k_start NULL: q_start's (Tk = Tq).  Both NULL: one
  * sequence of Tq and Tk (sequences = 1).  A sequence's queries are its last
